@@ -161,7 +161,8 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// d > 2048: one warp per token, 256-column passes.
+// d > 2048 or no divisor of 2048: one warp per token, 256-column passes.  All
+// lanes stay in the loop (slots lie in lanes whose columns may be past d).
 template <typename Te>
 __global__ void __launch_bounds__(kThreads)
     combine_wide_kernel(const Te* __restrict__ y, const Te* __restrict__ ysh,
@@ -185,17 +186,20 @@ __global__ void __launch_bounds__(kThreads)
     if (my_row >= cap_rows) set_err(err, kErrIndex);
     if (my_row < 0 || my_row >= cap_rows) my_row = -1;
   }
-  for (int c = lane * 8; c < d; c += 256) {
+  for (int c0 = 0; c0 < d; c0 += 256) {
+    const int c = c0 + lane * 8;
+    const bool in = c < d;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < kt; ++j) {
       const int r = __shfl_sync(0xffffffffu, my_row, j);
       const float a = __shfl_sync(0xffffffffu, my_a, j);
-      if (r < 0) continue;
+      if (r < 0 || !in) continue;
       float v[8];
       load8(y + static_cast<int64_t>(r) * d + c, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[i] = __fmaf_rn(a, v[i], acc[i]);
     }
+    if (!in) continue;
     if (ysh != nullptr) {
       float v[8];
       load8(ysh + static_cast<int64_t>(t) * d + c, v);
