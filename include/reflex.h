@@ -405,6 +405,104 @@ int reflex_route_noalloc(int32_t dtype, const void* hidden,
                          int32_t* ids_out, float* alpha_out,
                          int32_t* dev_status, void* stream);
 
+/*
+ * ---- 8-bit products -------------------------------------------------------
+ * Values are held as e4m3 codes (OCP 8-bit floating point, largest 448) with
+ * one fp32 scale for each block of 128 consecutive columns of a row
+ * (activations) or for each 128 x 128 block (weights); the last block of a
+ * row or column may be shorter.  A code c of scale s stands for c * s.
+ */
+
+/*
+ * reflex_quantize_fp8 — rows [rows, cols] to codes and scales.  With a = the
+ * largest magnitude of a block, at least 2^-100 (a NaN counts as largest):
+ *   scale = a / 448,  code = e4m3(x * (448 * (1 / a)))
+ * in fp32, each operation rounded to nearest even.  An infinity or a NaN makes
+ * every value that its block stands for NaN.
+ *   dtype       REFLEX_DTYPE_F32 or REFLEX_DTYPE_BF16 (of x).
+ *   x           [rows, cols], row stride ldx >= cols elements, any alignment
+ *               of the elements' own size.
+ *   block_rows  1 (a scale per row and 128 columns) or 128 (per 128 x 128).
+ *   codes       [rows, cols] bytes, row stride ldc >= cols.
+ *   scales      [ceil(rows / block_rows), ceil(cols / 128)] fp32, row stride
+ *               lds >= ceil(cols / 128).
+ * rows == 0 or cols == 0 writes nothing.
+ */
+int reflex_quantize_fp8(int32_t dtype, const void* x, int64_t rows, int64_t cols,
+                        int64_t ldx, int32_t block_rows, uint8_t* codes, int64_t ldc,
+                        float* scales, int64_t lds, void* stream);
+
+/*
+ * reflex_matmul_fp8 — out = A B^T over codes:
+ *   out[m, n] = sum_b sa[m, b] sb[n / 128, b] sum_{k in block b} A[m, k] B[n, k]
+ * with fp32 sums; each block of K is summed by the tensor cores and scaled
+ * once.
+ *   a         [M, K] codes, row stride lda (a multiple of 16, >= K);
+ *             a_scales [M, ceil(K / 128)], row stride ldas.
+ *   b         [N, K] codes, row stride ldb (a multiple of 16, >= K);
+ *             b_scales [ceil(N / 128), ceil(K / 128)], row stride ldbs.
+ *   out_dtype REFLEX_DTYPE_F32 or REFLEX_DTYPE_BF16; out [M, N], row stride
+ *             ldo >= N elements.
+ *   dev_status nullable device error word, cleared by this call.
+ * a and b start on 16-byte boundaries.  M == 0 computes nothing.  Any N, K
+ * >= 1; the same bits for a row whatever M and the other rows are, as long as
+ * the number of CTAs that share a tile's K stays the same (it is chosen from M,
+ * N and K).
+ */
+int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int64_t ldas,
+                      const uint8_t* b, int64_t ldb, const float* b_scales, int64_t ldbs,
+                      int32_t M, int32_t N, int32_t K, int32_t out_dtype, void* out,
+                      int64_t ldo, int32_t* dev_status, void* stream);
+
+/*
+ * reflex_linear_fp8 — a dense layer in 8 bits: x [M, K] (fp32 or bf16, row
+ * stride ldx) is quantised in rows as by reflex_quantize_fp8 and multiplied
+ * with the codes w [N, K] and w_scales as by reflex_matmul_fp8.
+ *   workspace  >= reflex_linear_fp8_workspace_size(M, K) bytes, 256-B aligned;
+ *              its first word is the call's error word (reflex_moe_status).
+ * A workspace sized for M rows serves every smaller batch.
+ */
+size_t reflex_linear_fp8_workspace_size(int32_t M, int32_t K);
+int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* w,
+                      int64_t ldw, const float* w_scales, int64_t ldws, int32_t M,
+                      int32_t N, int32_t K, int32_t out_dtype, void* out, int64_t ldo,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * reflex_experts_fp8 — the routed SwiGLU experts of Eq. 2 in 8 bits, for a
+ * routing that the caller holds (the ids, alpha of a route record):
+ *   out_t = sum_{j < k_t} alpha[t, j] E_{ids[t, j]}(h_t)   (+ h_t)
+ * with h_t quantised in rows, the activation silu(g) u of each pair quantised
+ * again in rows of 128 columns, and the pairs' outputs rounded to bf16 before
+ * the weighted fp32 sum.
+ *   hidden         [T, d] bf16.
+ *   ids, alpha     [T, k_max]: slots j < k[t] are read; an id outside [0, E)
+ *                  there sets REFLEX_EINVAL in the error word and its pair
+ *                  is left out.
+ *   k              [T] int32 counts in [1, min(k_max, E)] (else REFLEX_EKRANGE
+ *                  in the error word and the count is clamped).
+ *   w_gate_up      [E, 2 inter, d] codes: gate rows, then up rows;
+ *   gate_up_scales [E, 2, ceil(inter / 128), ceil(d / 128)]: the blocks of the
+ *                  gate rows and of the up rows are counted by themselves.
+ *   w_down         [E, d, inter] codes; down_scales [E, ceil(d / 128),
+ *                  ceil(inter / 128)].
+ *   flags          REFLEX_FLAG_RESIDUAL or 0.
+ *   workspace      >= reflex_experts_fp8_workspace_size(...) bytes (0 for
+ *                  shapes that are not supported), 256-B aligned; reads as
+ *                  reflex_moe_forward's with reflex_moe_status.
+ *   out            [T, d] bf16.
+ * hidden, out and the codes start on 16-byte boundaries.  Shape rules: d % 64
+ * == 0, inter % 64 == 0, 1 <= E <= 1024, 1 <= k_max <= 32, T >= 0.
+ */
+size_t reflex_experts_fp8_workspace_size(int32_t T, int32_t d, int32_t E, int32_t inter,
+                                         int32_t k_max);
+int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alpha,
+                       const int32_t* k, const uint8_t* w_gate_up,
+                       const float* gate_up_scales, const uint8_t* w_down,
+                       const float* down_scales, int32_t T, int32_t d, int32_t E,
+                       int32_t inter, int32_t k_max, uint32_t flags, void* workspace,
+                       size_t ws_bytes, void* out, void* stream);
+
 /* Synchronises `stream` and returns the status recorded in the workspace's
  * device error word by the last forward (REFLEX_OK if clean). */
 int reflex_moe_status(const void* workspace, void* stream);

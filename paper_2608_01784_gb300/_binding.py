@@ -50,7 +50,9 @@ EXPORTED = (
     "reflex_moe_forward", "reflex_moe_status", "reflex_read_status",
     "reflex_selftest_wait_timeout", "reflex_status_string",
     "reflex_abi_version", "reflex_route_noalloc", "reflex_update_state",
-    "reflex_step",
+    "reflex_step", "reflex_quantize_fp8", "reflex_matmul_fp8",
+    "reflex_linear_fp8_workspace_size", "reflex_linear_fp8",
+    "reflex_experts_fp8_workspace_size", "reflex_experts_fp8",
 )
 
 
@@ -130,6 +132,22 @@ def load():
     lib.reflex_route_noalloc.restype = ctypes.c_int
     lib.reflex_route_noalloc.argtypes = [i32, P, P, P, i32, i32, i32, i32,
                                          ctypes.c_uint32, P, P, P, P]
+    i64, sz = ctypes.c_int64, ctypes.c_size_t
+    lib.reflex_quantize_fp8.restype = ctypes.c_int
+    lib.reflex_quantize_fp8.argtypes = [i32, P, i64, i64, i64, i32, P, i64, P, i64, P]
+    lib.reflex_matmul_fp8.restype = ctypes.c_int
+    lib.reflex_matmul_fp8.argtypes = [P, i64, P, i64, P, i64, P, i64, i32, i32, i32, i32, P,
+                                      i64, P, P]
+    lib.reflex_linear_fp8_workspace_size.restype = sz
+    lib.reflex_linear_fp8_workspace_size.argtypes = [i32, i32]
+    lib.reflex_linear_fp8.restype = ctypes.c_int
+    lib.reflex_linear_fp8.argtypes = [i32, P, i64, P, i64, P, i64, i32, i32, i32, i32, P, i64,
+                                      P, sz, P]
+    lib.reflex_experts_fp8_workspace_size.restype = sz
+    lib.reflex_experts_fp8_workspace_size.argtypes = [i32] * 5
+    lib.reflex_experts_fp8.restype = ctypes.c_int
+    lib.reflex_experts_fp8.argtypes = [P, P, P, P, P, P, P, P, i32, i32, i32, i32, i32,
+                                       ctypes.c_uint32, P, sz, P, P]
     if lib.reflex_abi_version() != ABI_VERSION:
         raise ImportError(f"{_LIB_PATH} has ABI version {lib.reflex_abi_version()}, "
                           f"this binding needs {ABI_VERSION}: rebuild it")
@@ -274,3 +292,54 @@ def reflex_route_noalloc(dtype: int, hidden, w_router, k, T: int, d: int,
     return int(load().reflex_route_noalloc(
         dtype, _ptr(hidden), _ptr(w_router), _ptr(k), T, d, E, k_max, flags,
         _ptr(ids_out), _ptr(alpha_out), _ptr(dev_status), _stream(stream)))
+
+
+def reflex_quantize_fp8(dtype: int, x, rows: int, cols: int, ldx: int, block_rows: int, codes,
+                        ldc: int, scales, lds: int, stream=None, check: bool = True) -> int:
+    rc = load().reflex_quantize_fp8(dtype, _ptr(x), rows, cols, ldx, block_rows, _ptr(codes), ldc,
+                                    _ptr(scales), lds, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_quantize_fp8")
+    return rc
+
+
+def reflex_matmul_fp8(a, lda: int, a_scales, ldas: int, b, ldb: int, b_scales, ldbs: int, M: int,
+                      N: int, K: int, out_dtype: int, out, ldo: int, dev_status=None,
+                      stream=None, check: bool = True) -> int:
+    rc = load().reflex_matmul_fp8(_ptr(a), lda, _ptr(a_scales), ldas, _ptr(b), ldb, _ptr(b_scales),
+                                  ldbs, M, N, K, out_dtype, _ptr(out), ldo, _ptr(dev_status),
+                                  _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_matmul_fp8")
+    return rc
+
+
+def reflex_linear_fp8_workspace_size(M: int, K: int) -> int:
+    return int(load().reflex_linear_fp8_workspace_size(M, K))
+
+
+def reflex_linear_fp8(dtype: int, x, ldx: int, w, ldw: int, w_scales, ldws: int, M: int, N: int,
+                      K: int, out_dtype: int, out, ldo: int, workspace, ws_bytes: int,
+                      stream=None, check: bool = True) -> int:
+    rc = load().reflex_linear_fp8(dtype, _ptr(x), ldx, _ptr(w), ldw, _ptr(w_scales), ldws, M, N, K,
+                                  out_dtype, _ptr(out), ldo, _ptr(workspace), ws_bytes,
+                                  _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_linear_fp8")
+    return rc
+
+
+def reflex_experts_fp8_workspace_size(T: int, d: int, E: int, inter: int, k_max: int) -> int:
+    return int(load().reflex_experts_fp8_workspace_size(T, d, E, inter, k_max))
+
+
+def reflex_experts_fp8(hidden, ids, alpha, k, w_gate_up, gate_up_scales, w_down, down_scales,
+                       T: int, d: int, E: int, inter: int, k_max: int, flags: int, workspace,
+                       ws_bytes: int, out, stream=None, check: bool = True) -> int:
+    rc = load().reflex_experts_fp8(_ptr(hidden), _ptr(ids), _ptr(alpha), _ptr(k), _ptr(w_gate_up),
+                                   _ptr(gate_up_scales), _ptr(w_down), _ptr(down_scales), T, d, E,
+                                   inter, k_max, flags, _ptr(workspace), ws_bytes, _ptr(out),
+                                   _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_experts_fp8")
+    return rc

@@ -8,6 +8,8 @@ import numpy as np
 import torch
 
 from . import _binding as B
+from .fp8 import (ExpertsFp8, LinearFp8, matmul_fp8, quantize_experts,  # noqa: F401
+                  quantize_fp8)
 
 
 def _dev(a: np.ndarray, device, dtype=None) -> torch.Tensor:

@@ -1,0 +1,720 @@
+// fp8_gemm.cu — products of e4m3 codes with one fp32 scale for each block of
+// 128, on the 5th-generation tensor cores, dense or grouped by expert.
+//
+//   D[r, c] = sum_kb sa[r, kb] * sb[c / 128, kb] * sum_{k in kb} A[r, k] B[c, k]
+//   matmul: out = D (bf16 or fp32);
+//   SwiGLU: act = silu(D gate) * (D up), quantised again: codes and a scale
+//           for each 128 columns of act, the next product's A.
+//
+// The tensor cores sum one block of K (128) at a time: four
+// tcgen05.mma.kind::f8f6f4 of K = 32 into a fresh TMEM accumulator.  Its
+// products by the two scales are added to fp32 accumulators in registers,
+// because neither scale is constant along K and neither need be a power of
+// two.  Two TMEM accumulators of 256 columns (all 512) alternate, so that the
+// MMAs of the next block run while the last one is read.
+//
+// Tiles: 128 rows of A x 256 rows of B (SwiGLU: 128 gate rows and the matching
+// 128 up rows, hence whole groups of act columns in one CTA).  Per block of K
+// a CTA reads 16 + 32 KB of codes and the MMAs take 512 cycles; reading the
+// accumulator back (128 KB) and 16384 packed fp32 FMAs fit beside them on
+// eight warps.
+//   warp 0      TMA producer: ring of four 48 KB stages, 128-byte swizzle;
+//   warp 1      allocates TMEM, issues the MMAs from one thread;
+//   warps 4-11  two warpgroups, each thread one row and 64 + 64 columns (64
+//               of either 128-row half of B): 128 accumulators in registers.
+// Split tiles (few tiles, long K): the CTAs of a cluster take a part of K
+// each and add their accumulators through distributed shared memory, 32 rows
+// at a time in rank order, so the sums do not depend on timing.
+//
+// Every wait is bounded (2 s); on expiry the CTA records the timeout in the
+// error word, drains its loads and MMAs, frees TMEM and exits.
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+#include "tcgen05.cuh"
+
+namespace rx {
+namespace {
+
+constexpr int BM = 128;
+constexpr int BN = 256;
+constexpr int kStages = 4;
+constexpr int kABytes = BM * 128;
+constexpr int kBBytes = BN * 128;
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kPatchBytes = 32 * 1024;  // 4 KB a warp, or 32 rows x 256 fp32
+constexpr int kIndexInts = 320;
+constexpr int kBarBytes = 256;
+constexpr int kSmemBytes =
+    kStages * kStageBytes + kPatchBytes + kBarBytes + kIndexInts * 4 + 1024;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
+// 384 x 168 registers at launch = 128 x 56 + 256 x 224 after the split
+constexpr int kThreads = 384;
+constexpr int kFirstPromoter = 4;
+constexpr int kPromoters = 8;
+constexpr int kGroupM = 32;  // m-tiles whose rows stay in L2 across the n-tiles
+constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr uint64_t kDrainNs = 1000000000ull;
+
+enum { kSwiGLU = 0, kMatmul = 1 };
+
+struct Params {
+  int nkb;
+  int n_out;
+  int n_tiles;
+  GroupRows g;
+  int max_mtiles;
+  int a_box;
+  const uint8_t* a_scales;
+  int64_t a_scale_row_bytes;
+  const float* b_scales;
+  int64_t b_scale_group;
+  int64_t b_scale_ld;
+  void* out;
+  int64_t ldo;
+  int out_f32;
+  int out_vec;  // rows of out start on 16-byte boundaries
+  int64_t scale_offset;  // SwiGLU: the scales' place in a packed row
+  int splits;
+  uint32_t* err;
+};
+
+// kind::f8f6f4: e4m3 A and B (types 0), fp32 accumulator, both K-major.
+constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(BN >> 3) << 17) |
+                            (static_cast<uint32_t>(BM >> 4) << 24);
+__device__ __forceinline__ void mma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+      "l"(da), "l"(db), "r"(kIdesc), "r"(accumulate)
+      : "memory");
+}
+// The registers of a tcgen05.ld may be used once this has returned.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]),
+                 "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+
+// Two fp32 in one 64-bit register: one FMA instruction for both.
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
+  return v;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  uint32_t lo, hi;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
+  return make_float2(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ void fma2(uint64_t& acc, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ void scaled_add(uint64_t* acc, const uint32_t (&r)[32], uint64_t s2) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) fma2(acc[i], pack2(r[2 * i], r[2 * i + 1]), s2);
+}
+
+// ---- clusters ---------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t saddr, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t peer_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_bar)
+               : "memory");
+}
+__device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// mbar_wait for arrivals from the other CTAs of the cluster.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity,
+                                                  const volatile int* abort) {
+  const uint64_t t0 = global_ns();
+  while (true) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if (*abort || global_ns() - t0 > kWaitNs) return false;
+  }
+}
+
+// ---- tiles ------------------------------------------------------------------
+struct Tile {
+  int e, n, row0, rows;
+};
+
+// Tile counts per expert in shared memory where they fit; row offsets in L2.
+__device__ __forceinline__ const int32_t* load_prefix(const Params& p, int32_t* cache) {
+  if (p.g.offsets == nullptr || p.g.E + 1 > kIndexInts) return p.g.mt_prefix;
+  for (int i = threadIdx.x; i <= p.g.E; i += kThreads) cache[i] = p.g.mt_prefix[i];
+  return cache;  // the caller synchronises
+}
+__device__ __forceinline__ int tile_count(const Params& p, const int32_t* pref) {
+  int mt = p.max_mtiles;
+  if (p.g.offsets != nullptr) mt = max(0, min(pref[p.g.E], p.max_mtiles));
+  return mt * p.n_tiles;
+}
+// Dense: n-tile by n-tile over kGroupM m-tiles at a time.  Grouped: expert,
+// n-tile, m-tile, so CTAs at work at the same time share weights in L2.
+// False: the workspace is inconsistent (in unsigned arithmetic whatever wraps
+// fails one of the comparisons).
+__device__ __forceinline__ bool decode_tile(const Params& p, const int32_t* pref, int t,
+                                            Tile& o) {
+  if (p.g.offsets == nullptr) {
+    const int per = kGroupM * p.n_tiles;
+    const int m0 = t / per * kGroupM, r = t % per;
+    const int gm = min(kGroupM, p.max_mtiles - m0);
+    o.e = 0;
+    o.n = r / gm;
+    o.row0 = (m0 + r % gm) * BM;
+    o.rows = min(BM, p.g.dense_rows - o.row0);
+    return true;
+  }
+  int lo = 0, hi = p.g.E;  // n_tiles * prefix[lo] <= t < n_tiles * prefix[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.n_tiles * pref[mid] <= t) lo = mid; else hi = mid;
+  }
+  const uint32_t first = pref[lo], last = pref[lo + 1];
+  const uint32_t row_lo = p.g.offsets[lo], row_hi = p.g.offsets[lo + 1];
+  const uint32_t mt_e = last - first, most = p.max_mtiles;
+  if (mt_e - 1u >= most) return false;
+  const uint32_t l = t - p.n_tiles * first, n = l / mt_e;
+  const uint32_t row0 = row_lo + (l - n * mt_e) * BM;
+  o.e = lo;
+  o.n = n;
+  o.row0 = row0;
+  o.rows = min(static_cast<uint32_t>(BM), row_hi - row0);
+  return n < static_cast<uint32_t>(p.n_tiles) && row_lo <= row0 && row0 < row_hi &&
+         row_hi <= static_cast<uint32_t>(p.g.cap_rows);
+}
+
+// silu(g) u
+__device__ __forceinline__ float swiglu(float g, float u) {
+  return g / (1.0f + __expf(-g)) * u;
+}
+
+template <int MODE, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+    fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a,
+                    const __grid_constant__ CUtensorMap map_b, const Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sa = smem;
+  uint8_t* sb = smem + kStages * kABytes;
+  uint8_t* patch = smem + kStages * kStageBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(patch + kPatchBytes);
+  uint64_t* full = bars;                 // [kStages]
+  uint64_t* empty = bars + kStages;      // [kStages]
+  uint64_t* tfull = bars + 2 * kStages;  // [2] a TMEM accumulator is complete
+  uint64_t* tempty = tfull + 2;          // [2] it has been read
+  uint64_t* xbar = tempty + 2;           // [4] SwiGLU: row maxima of a quarter's two warps
+  uint64_t* red_full = xbar + 4;         // split: every CTA's rows are in its patch
+  uint64_t* red_empty = red_full + 1;    // split: every CTA has read them
+  uint64_t* drain = red_empty + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int32_t* cache = reinterpret_cast<int32_t*>(patch + kPatchBytes + kBarBytes);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const int S = SPLIT ? p.splits : 1;
+  const int rank = SPLIT ? static_cast<int>(cluster_rank()) : 0;
+  const int t_first = blockIdx.x / S, t_step = gridDim.x / S;
+  const int kb0 = p.nkb * rank / S, kb1 = p.nkb * (rank + 1) / S;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], kPromoters);
+    }
+    for (int q = 0; q < 4; ++q) mbar_init(&xbar[q], 2);
+    mbar_init(red_full, 2 * S);
+    mbar_init(red_empty, kPromoters * S);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+  }
+  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), 2 * BN);
+  tc_fence_before();
+  if (SPLIT) cluster_sync();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int32_t* pref = load_prefix(p, cache);
+  __syncthreads();
+  const int ntiles = tile_count(p, pref);
+
+  if (warp < kFirstPromoter) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0 && lane == 0) {
+      // ---------------- TMA producer ----------------
+      int stage = 0;
+      uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
+      bool ok = true;
+      for (int t = t_first; t < ntiles && ok; t += t_step) {
+        Tile tl;
+        if (!decode_tile(p, pref, t, tl)) {
+          set_err(p.err, kErrIndex);
+          *abort_flag = 1;
+          break;
+        }
+        // rows of a box past the tile's last row are of no use: leave them out
+        const int boxes = (tl.rows + p.a_box - 1) / p.a_box;
+        const int c1 = MODE == kSwiGLU ? tl.n * 128 : tl.n * BN;
+        const int c2 = MODE == kSwiGLU ? 2 * tl.e : tl.e;
+        const bool second = MODE == kSwiGLU || c1 + 128 < p.n_out;
+        const uint32_t bytes = boxes * p.a_box * 128 + (second ? 2 : 1) * (kBBytes / 2);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
+            ok = false;
+            break;
+          }
+          const uint32_t fb = smem_addr(&full[stage]);
+          mbar_expect_tx(fb, bytes);
+          const uint32_t a_dst = smem_addr(sa + stage * kABytes);
+          const uint32_t b_dst = smem_addr(sb + stage * kBBytes);
+          tma_load_3d(b_dst, &map_b, kb * 128, c1, c2, fb);
+          if (second)
+            tma_load_3d(b_dst + kBBytes / 2, &map_b, kb * 128,
+                        MODE == kSwiGLU ? c1 : c1 + 128, MODE == kSwiGLU ? c2 + 1 : c2, fb);
+          for (int i = 0; i < boxes; ++i)
+            tma_load_2d(a_dst + i * p.a_box * 128, &map_a, kb * 128, tl.row0 + i * p.a_box, fb);
+          issued_mask |= 1u << stage;
+          issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) {
+        set_err(p.err, kErrTimeout);
+        *abort_flag = 1;
+      }
+      if (*abort_flag) {
+        // every issued load must land before the CTA may exit
+        for (int s = 0; s < kStages; ++s)
+          if (issued_mask & (1u << s))
+            mbar_wait(&full[s], (issued_phase >> s) & 1u, nullptr, kDrainNs);
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ---------------- MMA issuer ----------------
+      int stage = 0;
+      uint32_t phase = 0;
+      uint32_t it = 0;
+      bool ok = true, issued_any = false;
+      for (int t = t_first; t < ntiles && ok; t += t_step) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          const int b = it & 1;
+          if (!mbar_wait(&tempty[b], ((it >> 1) & 1u) ^ 1u, abort_flag, kWaitNs) ||
+              !mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a0 = smem_addr(sa + stage * kABytes);
+          const uint32_t b0 = smem_addr(sb + stage * kBBytes);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            mma_e4m3(tmem_base + b * BN, desc_sw128(a0 + k * 32), desc_sw128(b0 + k * 32),
+                     k > 0 ? 1u : 0u);
+          issued_any = true;
+          mma_commit(smem_addr(&empty[stage]));
+          mma_commit(smem_addr(&tfull[b]));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) {
+        if (!*abort_flag) set_err(p.err, kErrTimeout);
+        *abort_flag = 1;
+      }
+      if (*abort_flag && issued_any) {
+        // MMAs in flight must finish before TMEM is freed
+        mma_commit(smem_addr(drain));
+        mbar_wait(drain, 0, nullptr, kDrainNs);
+      }
+    }
+  } else {
+    // ---------------- scales, sums and stores ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    const int quarter = warp & 3;          // TMEM lanes 32 * quarter ..
+    const int wg = (warp - kFirstPromoter) >> 2;  // columns 64 wg .. of both halves
+    const int pw = warp - kFirstPromoter;
+    const int row = quarter * 32 + lane;
+    uint8_t* my_patch = patch + pw * 4096;
+    float* s_max = reinterpret_cast<float*>(patch);  // SwiGLU: [2][2][128] row maxima
+    uint32_t it = 0, red_phase = 0;
+    uint32_t xt = 0;  // SwiGLU tiles that this quarter has had rows in
+    bool ok = true;
+    for (int t = t_first; t < ntiles && ok; t += t_step) {
+      Tile tl;
+      if (!decode_tile(p, pref, t, tl)) break;
+      const bool live = quarter * 32 < tl.rows;
+      const bool store = row < tl.rows;
+      const float* sb0 = MODE == kSwiGLU
+                             ? p.b_scales + (2 * tl.e) * p.b_scale_group + tl.n * p.b_scale_ld
+                             : p.b_scales + tl.e * p.b_scale_group + 2 * tl.n * p.b_scale_ld;
+      const float* sb1 = sb0;
+      if (MODE == kSwiGLU) sb1 += p.b_scale_group;
+      else if (tl.n * BN + 128 < p.n_out) sb1 += p.b_scale_ld;
+      const float* sa_row = reinterpret_cast<const float*>(
+          p.a_scales + static_cast<int64_t>(tl.row0 + (store ? row : 0)) * p.a_scale_row_bytes);
+      uint64_t acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = 0;
+      float na = sa_row[kb0], n0 = sb0[kb0], n1 = sb1[kb0];
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int b = it & 1;
+        const float s0 = na * n0, s1 = na * n1;
+        if (kb + 1 < kb1) {
+          na = sa_row[kb + 1];
+          n0 = sb0[kb + 1];
+          n1 = sb1[kb + 1];
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(&tfull[b], (it >> 1) & 1u, abort_flag, kWaitNs))) {
+          ok = false;
+          break;
+        }
+        if (live) {
+          tc_fence_after();
+          const uint32_t ta = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                              static_cast<uint32_t>(b * BN + wg * 64);
+          const uint64_t p0 = pack2(__float_as_uint(s0), __float_as_uint(s0));
+          const uint64_t p1 = pack2(__float_as_uint(s1), __float_as_uint(s1));
+          uint32_t r0[32], r1[32];
+          tmem_ld32(ta, r0);
+          tmem_ld_wait_for(r0);
+          tmem_ld32(ta + 32, r1);
+          scaled_add(acc, r0, p0);
+          tmem_ld_wait_for(r1);
+          tmem_ld32(ta + 128, r0);
+          scaled_add(acc + 16, r1, p0);
+          tmem_ld_wait_for(r0);
+          tmem_ld32(ta + 160, r1);
+          scaled_add(acc + 32, r0, p1);
+          tmem_ld_wait_for(r1);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(smem_addr(&tempty[b]));
+          scaled_add(acc + 48, r1, p1);
+        } else if (lane == 0) {
+          mbar_arrive1(smem_addr(&tempty[b]));
+        }
+      }
+      if (!ok) break;
+
+      if (SPLIT) {
+        // the cluster's accumulators, 32 rows at a time: rows i = rank, rank +
+        // S, .. are this CTA's to add up and store, a warp a row
+        float* red = reinterpret_cast<float*>(patch);
+        for (int q = 0; q * 32 < tl.rows && ok; ++q, red_phase ^= 1u) {
+          if (quarter == q) {
+            ok = __all_sync(0xffffffffu, mbar_wait_cluster(red_empty, red_phase ^ 1u, abort_flag));
+            if (!ok) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const float2 v0 = unpack2(acc[h * 32 + 2 * j]), v1 = unpack2(acc[h * 32 + 2 * j + 1]);
+                const int chunk = (h * 32 + wg * 16 + j) ^ (lane & 7);
+                *reinterpret_cast<float4*>(red + lane * BN + chunk * 4) =
+                    make_float4(v0.x, v0.y, v1.x, v1.y);
+              }
+            __syncwarp();
+            if (lane < S) mbar_arrive_peer(peer_addr(smem_addr(red_full), lane));
+          }
+          ok = __all_sync(0xffffffffu, mbar_wait_cluster(red_full, red_phase, abort_flag));
+          if (!ok) break;
+          for (int i = rank + S * pw; i < 32 && q * 32 + i < tl.rows; i += S * kPromoters) {
+            float v[2][4] = {};
+            const uint32_t at = smem_addr(red + i * BN);
+            for (int s = 0; s < S; ++s) {
+              const uint32_t from = peer_addr(at, s);
+              const float4 x = ld_peer4(from + ((lane ^ (i & 7)) << 4));
+              const float4 y = ld_peer4(from + (((32 + lane) ^ (i & 7)) << 4));
+              v[0][0] += x.x; v[0][1] += x.y; v[0][2] += x.z; v[0][3] += x.w;
+              v[1][0] += y.x; v[1][1] += y.y; v[1][2] += y.z; v[1][3] += y.w;
+            }
+            const int64_t r = tl.row0 + q * 32 + i;
+            if (MODE == kSwiGLU) {
+              const int col = tl.n * 128 + lane * 4;
+              float a[4];
+              uint32_t m = 0;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                a[j] = col + j < p.n_out ? swiglu(v[0][j], v[1][j]) : 0.f;
+                m = max(m, __float_as_uint(a[j]) & 0x7fffffffu);
+              }
+              const float am = fp8_amax(__reduce_max_sync(0xffffffffu, m));
+              const float inv = fp8_inverse(am);
+              uint8_t* o = static_cast<uint8_t*>(p.out) + r * p.ldo;
+              if (col < p.n_out)  // n_out is a multiple of 64
+                *reinterpret_cast<uint32_t*>(o + col) =
+                    e4m3x4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+              if (lane == 0)
+                reinterpret_cast<float*>(o + p.scale_offset)[tl.n] = __fdiv_rn(am, kE4m3Max);
+            } else {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int col = tl.n * BN + h * 128 + lane * 4;
+                const bool whole = p.out_vec && col + 4 <= p.n_out;
+                if (p.out_f32) {
+                  float* o = static_cast<float*>(p.out) + r * p.ldo + col;
+                  if (whole) {
+                    *reinterpret_cast<float4*>(o) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+                  } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      if (col + j < p.n_out) o[j] = v[h][j];
+                  }
+                } else {
+                  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + r * p.ldo + col;
+                  if (whole) {
+                    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v[h][0], v[h][1]),
+                                           __floats2bfloat162_rn(v[h][2], v[h][3])};
+                    *reinterpret_cast<uint2*>(o) = *reinterpret_cast<uint2*>(w);
+                  } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      if (col + j < p.n_out) o[j] = __float2bfloat16_rn(v[h][j]);
+                  }
+                }
+              }
+            }
+          }
+          __syncwarp();
+          if (lane < S) mbar_arrive_peer(peer_addr(smem_addr(red_empty), lane));
+        }
+        continue;
+      }
+
+      if (!live) continue;
+      if (MODE == kSwiGLU) {
+        // act in place of the gate sums; the row's maximum over both warps
+        uint32_t m = 0;
+        const int col0 = tl.n * 128 + wg * 64;
+        const bool in = col0 < p.n_out;  // n_out is a multiple of 64
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float2 g = unpack2(acc[i]), u = unpack2(acc[32 + i]);
+          const float a0 = swiglu(g.x, u.x), a1 = swiglu(g.y, u.y);
+          m = max(m, max(__float_as_uint(a0) & 0x7fffffffu, __float_as_uint(a1) & 0x7fffffffu));
+          acc[i] = pack2(__float_as_uint(a0), __float_as_uint(a1));
+        }
+        if (!in) m = 0;
+        // two buffers: a warp that is a tile ahead has seen the other's
+        // arrival for this tile, which follows its reads of the tile before
+        float* mine = s_max + (xt & 1) * 256;
+        mine[wg * 128 + row] = __uint_as_float(m);
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(&xbar[quarter]));
+        ok = __all_sync(0xffffffffu, mbar_wait(&xbar[quarter], xt & 1, abort_flag, kWaitNs));
+        ++xt;
+        if (!ok) break;
+        m = max(m, __float_as_uint(mine[(wg ^ 1) * 128 + row]));
+        const float am = fp8_amax(m), inv = fp8_inverse(am);
+        if (store) {
+          uint8_t* o = static_cast<uint8_t*>(p.out) + static_cast<int64_t>(tl.row0 + row) * p.ldo;
+          if (in) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 x = unpack2(acc[8 * v + 2 * j]), y = unpack2(acc[8 * v + 2 * j + 1]);
+                w[j] = e4m3x4(x.x * inv, x.y * inv, y.x * inv, y.y * inv);
+              }
+              *reinterpret_cast<uint4*>(o + col0 + 16 * v) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+          if (wg == 0)
+            reinterpret_cast<float*>(o + p.scale_offset)[tl.n] = __fdiv_rn(am, kE4m3Max);
+        }
+      } else {
+        // through a 32-row patch of 128-byte rows (16-byte chunks swizzled by
+        // the row), so that a store instruction writes four whole lines
+        const int es = p.out_f32 ? 4 : 2;
+        const int64_t row_base = tl.row0 + quarter * 32;
+        const int rows = min(32, tl.rows - quarter * 32);
+        for (int part = 0; part < es; ++part) {
+          // part: (half, and which 32 of its 64 columns in fp32)
+          const int h = p.out_f32 ? part >> 1 : part;
+          const int sub = p.out_f32 ? (part & 1) * 32 : 0;
+          __syncwarp();
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            if (hh != h) continue;
+            if (p.out_f32) {
+#pragma unroll
+              for (int ss = 0; ss < 2; ++ss) {
+                if (ss * 32 != sub) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const float2 v0 = unpack2(acc[hh * 32 + ss * 16 + 2 * j]);
+                  const float2 v1 = unpack2(acc[hh * 32 + ss * 16 + 2 * j + 1]);
+                  *reinterpret_cast<float4*>(my_patch + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                      make_float4(v0.x, v0.y, v1.x, v1.y);
+                }
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float2 v = unpack2(acc[hh * 32 + 4 * j + i]);
+                  __nv_bfloat162 b2 = __floats2bfloat162_rn(v.x, v.y);
+                  w[i] = *reinterpret_cast<uint32_t*>(&b2);
+                }
+                *reinterpret_cast<uint4*>(my_patch + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                    make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            }
+          }
+          __syncwarp();
+          const int chunk = lane & 7;
+          const int col = tl.n * BN + h * 128 + wg * 64 + sub + chunk * (16 / es);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            const uint4 v =
+                *reinterpret_cast<const uint4*>(my_patch + r * 128 + ((chunk ^ (r & 7)) << 4));
+            if (r >= rows) continue;
+            uint8_t* o = static_cast<uint8_t*>(p.out) + ((row_base + r) * p.ldo + col) * es;
+            if (p.out_vec && col + 16 / es <= p.n_out) {
+              *reinterpret_cast<uint4*>(o) = v;
+            } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+              if (p.out_f32) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (col + j < p.n_out) reinterpret_cast<uint32_t*>(o)[j] = w[j];
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (col + j < p.n_out)
+                    reinterpret_cast<uint16_t*>(o)[j] =
+                        static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+              }
+            }
+          }
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      if (!*abort_flag) set_err(p.err, kErrTimeout);
+      *abort_flag = 1;
+    }
+  }
+
+  tc_fence_before();
+  __syncwarp();
+  if (SPLIT) cluster_sync();  // no CTA leaves while its rows are read
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem_base, 2 * BN);
+  }
+}
+
+template <int MODE, bool SPLIT>
+cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
+  auto kernel = fp8_gemm_kernel<MODE, SPLIT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kSmemBytes);
+  if (e != cudaSuccess) return e;
+  Params p{};
+  p.nkb = (a.K + 127) / 128;
+  p.n_out = a.n_out;
+  p.n_tiles = MODE == kSwiGLU ? (a.n_out + 127) / 128 : (a.n_out + BN - 1) / BN;
+  p.g = a.g;
+  p.max_mtiles = a.g.offsets != nullptr ? a.g.E + (a.g.cap_rows + BM - 1) / BM
+                                        : (a.g.dense_rows + BM - 1) / BM;
+  p.a_box = a.a_box;
+  p.a_scales = a.a_scales;
+  p.a_scale_row_bytes = a.a_scale_row_bytes;
+  p.b_scales = a.b_scales;
+  p.b_scale_group = a.b_scale_group;
+  p.b_scale_ld = a.b_scale_ld;
+  p.out = a.out;
+  p.ldo = a.ldo;
+  p.out_f32 = a.out_f32;
+  p.out_vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
+              a.ldo * (a.out_f32 ? 4 : 2) % 16 == 0;
+  p.scale_offset = fp8_scale_offset(a.n_out);
+  p.splits = a.splits;
+  p.err = a.err;
+  const int64_t most = static_cast<int64_t>(p.max_mtiles) * p.n_tiles;
+  int64_t grid = std::min<int64_t>(a.num_sms / a.splits, most) * a.splits;
+  if (grid < a.splits) grid = a.splits;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {static_cast<unsigned>(a.splits), 1, 1};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = SPLIT ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, *a.map_a, *a.map_b, p);
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_swiglu(const Fp8GemmArgs& a, cudaStream_t stream) {
+  return a.splits > 1 ? launch_impl<kSwiGLU, true>(a, stream)
+                      : launch_impl<kSwiGLU, false>(a, stream);
+}
+cudaError_t launch_fp8_matmul(const Fp8GemmArgs& a, cudaStream_t stream) {
+  return a.splits > 1 ? launch_impl<kMatmul, true>(a, stream)
+                      : launch_impl<kMatmul, false>(a, stream);
+}
+
+}  // namespace rx

@@ -1,0 +1,200 @@
+// fp8_quantize.cu — e4m3 codes with one fp32 scale for each block of 128.
+//
+// Rows (activations): the 128 columns of a group share a scale; blocks
+// (weights): 128 rows x 128 columns do.  With a = the largest magnitude of
+// the group, at least 2^-100,
+//   scale = a / 448,   code = e4m3(x * (448 * (1 / a)))      (448: the largest e4m3)
+// in fp32 IEEE operations, rounded to nearest even, so that the codes are the
+// same bits wherever these operations are written out.  The product with the
+// reciprocal instead of a division costs at most one rounding of x; the floor
+// of a keeps the reciprocal finite and gives a group of zeros zero codes.  An
+// infinity or a NaN makes every value that its group stands for NaN (the
+// scale is infinite or NaN), as it would in the unquantised product.
+//
+// Bound: HBM (2 or 4 bytes in, 1 out per element).  16 lanes hold a group in
+// registers (8 consecutive elements each, one 16-byte vector in bf16), so one
+// pass over the data serves the maximum and the conversion.
+#include "common.cuh"
+#include "fp8.cuh"
+#include "internal.h"
+
+namespace rx {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnits = 4;  // pairs of groups that a warp has in flight
+
+// 8 elements from column c on; those at or past cols are 0.
+template <typename Te>
+__device__ __forceinline__ void load_elems(const Te* row, int64_t c, int64_t cols, bool vec,
+                                           float (&f)[8]) {
+  if (vec && c + 8 <= cols) {
+    load8(row + c, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = c + i < cols ? to_f32(row[c + i]) : 0.f;
+  }
+}
+
+// Magnitudes compare as unsigned integers; a NaN's are the largest.
+__device__ __forceinline__ uint32_t amax_bits(const float (&f)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+  return m;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t* row, int64_t c, int64_t cols, bool vec,
+                                            const float (&f)[8], float inv) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = e4m3x4(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
+  if (vec && c + 8 <= cols) {
+    *reinterpret_cast<uint2*>(row + c) = make_uint2(w[0], w[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < cols) row[c + i] = static_cast<uint8_t>(w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+template <typename Te>
+__global__ void __launch_bounds__(kThreads)
+    quantize_rows_kernel(const Te* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
+                         uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scales,
+                         int64_t scale_row_bytes, int vec_x, int vec_c, ZeroWords zero,
+                         const int32_t* __restrict__ k, int64_t n_k, int k_most,
+                         uint32_t* err) {
+  grid_dep_wait();
+  grid_dep_launch();
+  if (blockIdx.x == 0 && (zero.n > 0 || k != nullptr)) {
+    clear_words(zero);
+    if (k != nullptr) {  // the counts of the call that these rows belong to
+      __syncthreads();
+      bool bad = false;
+      for (int64_t i = threadIdx.x; i < n_k; i += kThreads) bad |= k[i] < 1 || k[i] > k_most;
+      if (bad) set_err(err, kErrKRange);
+    }
+  }
+  const int lane = threadIdx.x & 31;
+  const int64_t per_row = (cols + 255) / 256, units = rows * per_row;
+  const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+  const int64_t w0 = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  for (int64_t u0 = w0 * kUnits; u0 < units; u0 += warps * kUnits) {
+    float f[kUnits][8];
+    int64_t r[kUnits], c[kUnits];
+    r[0] = u0 / per_row;
+    c[0] = u0 - r[0] * per_row;
+#pragma unroll
+    for (int i = 1; i < kUnits; ++i) {
+      const bool wrap = c[i - 1] + 1 == per_row;
+      r[i] = r[i - 1] + (wrap ? 1 : 0);
+      c[i] = wrap ? 0 : c[i - 1] + 1;
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      c[i] = c[i] * 256 + lane * 8;
+      if (r[i] < rows) {
+        load_elems(x + r[i] * ldx, c[i], cols, vec_x != 0, f[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      if (r[i] >= rows) break;
+      uint32_t m = amax_bits(f[i]);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const float a = fp8_amax(m);
+      store_codes(codes + r[i] * ldc, c[i], cols, vec_c != 0, f[i], fp8_inverse(a));
+      if ((lane & 15) == 0 && c[i] < cols)
+        *reinterpret_cast<float*>(scales + r[i] * scale_row_bytes + (c[i] >> 7) * 4) =
+            __fdiv_rn(a, kE4m3Max);
+    }
+  }
+}
+
+// One CTA per 128 x 128 block (weights, laid out once): the block is read
+// twice, the second time from L2.
+template <typename Te>
+__global__ void __launch_bounds__(kThreads)
+    quantize_blocks_kernel(const Te* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
+                           uint8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scales,
+                           int64_t lds, int vec_x, int vec_c) {
+  __shared__ uint32_t s_max[kThreads / 32];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t kb = (cols + 127) / 128;
+  const int64_t br = blockIdx.x / kb, bc = blockIdx.x % kb;
+  const int64_t c = bc * 128 + (threadIdx.x & 15) * 8;
+  const int64_t r0 = br * 128 + (threadIdx.x >> 4), r1 = min(rows, br * 128 + 128);
+  uint32_t m = 0;
+  for (int64_t r = r0; r < r1; r += kThreads / 16) {
+    float f[8];
+    load_elems(x + r * ldx, c, cols, vec_x != 0, f);
+    m = max(m, amax_bits(f));
+  }
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) m = max(m, s_max[i]);
+  const float a = fp8_amax(m), inv = fp8_inverse(a);
+  for (int64_t r = r0; r < r1; r += kThreads / 16) {
+    float f[8];
+    load_elems(x + r * ldx, c, cols, vec_x != 0, f);
+    store_codes(codes + r * ldc, c, cols, vec_c != 0, f, inv);
+  }
+  if (threadIdx.x == 0) scales[br * lds + bc] = __fdiv_rn(a, kE4m3Max);
+}
+
+template <typename Te>
+bool aligned_rows(const Te* x, int64_t ld) {
+  constexpr int64_t kVec = sizeof(Te) == 1 ? 8 : 16;
+  return reinterpret_cast<uintptr_t>(x) % kVec == 0 &&
+         ld * static_cast<int64_t>(sizeof(Te)) % kVec == 0;
+}
+
+template <typename Te>
+cudaError_t rows_typed(const Te* x, const Fp8Rows& q, int num_sms, cudaStream_t stream) {
+  const int64_t units = q.rows * ((q.cols + 255) / 256);
+  int64_t grid = (units + 8 * kUnits - 1) / (8 * kUnits);
+  // short inputs spread over the SMs, one unit a warp, no matter the unroll
+  if (grid < num_sms) grid = std::min<int64_t>(num_sms, (units + 7) / 8);
+  grid = std::max<int64_t>(1, std::min<int64_t>(grid, 8 * num_sms));
+  return launch_pdl(quantize_rows_kernel<Te>, dim3(static_cast<unsigned>(grid)), dim3(kThreads),
+                    0, stream, x, q.rows, q.cols, q.ldx, q.codes, q.ldc, q.scales,
+                    q.scale_row_bytes, static_cast<int>(aligned_rows(x, q.ldx)),
+                    static_cast<int>(aligned_rows(q.codes, q.ldc)), q.zero, q.k, q.n_k, q.k_most,
+                    q.err);
+}
+
+template <typename Te>
+cudaError_t blocks_typed(const Te* x, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes,
+                         int64_t ldc, float* scales, int64_t lds, cudaStream_t stream) {
+  const int64_t blocks = ((rows + 127) / 128) * ((cols + 127) / 128);
+  return launch_pdl(quantize_blocks_kernel<Te>, dim3(static_cast<unsigned>(blocks)),
+                    dim3(kThreads), 0, stream, x, rows, cols, ldx, codes, ldc, scales, lds,
+                    static_cast<int>(aligned_rows(x, ldx)),
+                    static_cast<int>(aligned_rows(codes, ldc)));
+}
+
+}  // namespace
+
+cudaError_t launch_quantize_rows(int dtype, const void* x, const Fp8Rows& q, int num_sms,
+                                 cudaStream_t stream) {
+  if (dtype == 0) return rows_typed(static_cast<const float*>(x), q, num_sms, stream);
+  return rows_typed(static_cast<const __nv_bfloat16*>(x), q, num_sms, stream);
+}
+
+cudaError_t launch_quantize_blocks(int dtype, const void* x, int64_t rows, int64_t cols,
+                                   int64_t ldx, uint8_t* codes, int64_t ldc, float* scales,
+                                   int64_t lds, cudaStream_t stream) {
+  if (dtype == 0)
+    return blocks_typed(static_cast<const float*>(x), rows, cols, ldx, codes, ldc, scales, lds,
+                        stream);
+  return blocks_typed(static_cast<const __nv_bfloat16*>(x), rows, cols, ldx, codes, ldc, scales,
+                      lds, stream);
+}
+
+}  // namespace rx

@@ -304,6 +304,11 @@ cudaError_t launch_alloc(const AllocCall& c, int32_t T, cudaStream_t s, bool alo
 
 }  // namespace
 
+namespace rx {
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() { return encode_fn(); }
+int device_sms() { return num_sms_current(); }
+}  // namespace rx
+
 extern "C" {
 
 int reflex_abi_version(void) { return 114; }

@@ -1,0 +1,202 @@
+"""Torch-facing convenience over the 8-bit entry points: quantisation, the
+dense layer and the routed experts.  Codes are torch.float8_e4m3fn tensors,
+scales fp32; a scale covers 128 columns of a row (activations) or a 128 x 128
+block (weights).  Every step runs in libreflex.so's kernels.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _binding as B
+
+_DTYPES = {torch.float32: B.REFLEX_DTYPE_F32, torch.bfloat16: B.REFLEX_DTYPE_BF16}
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t: torch.Tensor, what: str, dtypes) -> torch.Tensor:
+    """A device matrix whose rows are contiguous (any row stride)."""
+    _want(t.is_cuda and t.dim() == 2 and t.dtype in dtypes, f"{what}: a CUDA matrix of " +
+          " or ".join(str(d) for d in dtypes))
+    _want(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
+    _want(t.shape[0] <= 1 or t.stride(0) >= t.shape[1], f"{what}: rows must not overlap")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return max(int(t.stride(0)) if t.shape[0] > 1 else 0, int(t.shape[1]))
+
+
+def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | None = None,
+                 scales: torch.Tensor | None = None, stream=None):
+    """reflex_quantize_fp8 of x [rows, cols] (fp32 or bf16) -> (codes [rows,
+    cols] float8_e4m3fn, scales [ceil(rows / block_rows), ceil(cols / 128)]).
+    New codes have rows on 16-byte boundaries, as the products take them."""
+    _rows(x, "x", _DTYPES)
+    rows, cols = int(x.shape[0]), int(x.shape[1])
+    _want(block_rows in (1, 128), "block_rows is 1 or 128")
+    if codes is None:
+        ld = -(-cols // 16) * 16
+        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=x.device)[:, :cols]
+    if scales is None:
+        scales = torch.empty((-(-rows // block_rows), _blocks(cols)), dtype=torch.float32,
+                             device=x.device)
+    _rows(codes, "codes", (torch.float8_e4m3fn,))
+    _rows(scales, "scales", (torch.float32,))
+    _want(tuple(codes.shape) == (rows, cols), "codes: another shape than x")
+    _want(tuple(scales.shape) == (-(-rows // block_rows), _blocks(cols)), "scales: shape")
+    _want(codes.device == x.device and scales.device == x.device, "tensors on several devices")
+    B.reflex_quantize_fp8(_DTYPES[x.dtype], x, rows, cols, _ld(x), block_rows, codes, _ld(codes),
+                          scales, _ld(scales), stream)
+    return codes, scales
+
+
+def _code_rows(codes: torch.Tensor, what: str):
+    _rows(codes, what, (torch.float8_e4m3fn,))
+    _want(_code_ld(codes) % 16 == 0 and codes.data_ptr() % 16 == 0,
+          f"{what}: rows start on 16-byte boundaries (as quantize_fp8 lays them out)")
+
+
+def _code_ld(codes: torch.Tensor) -> int:
+    """Row stride; of a single row, its length in whole 16-byte vectors."""
+    return int(codes.stride(0)) if codes.shape[0] > 1 else -(-int(codes.shape[1]) // 16) * 16
+
+
+def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+               out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
+               status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """reflex_matmul_fp8: A B^T of codes a [M, K] (scales per row and 128
+    columns) and b [N, K] (scales per 128 x 128 block) -> [M, N]."""
+    _code_rows(a, "a")
+    _code_rows(b, "b")
+    M, K, N = int(a.shape[0]), int(a.shape[1]), int(b.shape[0])
+    _want(int(b.shape[1]) == K, "a and b disagree on K")
+    _rows(a_scales, "a_scales", (torch.float32,))
+    _rows(b_scales, "b_scales", (torch.float32,))
+    _want(tuple(a_scales.shape) == (M, _blocks(K)), "a_scales: shape")
+    _want(tuple(b_scales.shape) == (_blocks(N), _blocks(K)), "b_scales: shape")
+    out = _output(out, M, N, out_dtype, a.device)
+    B.reflex_matmul_fp8(a, _code_ld(a), a_scales, _ld(a_scales), b, _code_ld(b), b_scales,
+                        _ld(b_scales), M, N, K, _DTYPES[out.dtype], out, _ld(out), status, stream)
+    return out
+
+
+def _output(out, M: int, N: int, dtype, device) -> torch.Tensor:
+    _want(dtype in _DTYPES, "outputs are fp32 or bf16")
+    if out is None:
+        return torch.empty((M, N), dtype=dtype, device=device)
+    _rows(out, "out", _DTYPES)
+    _want(tuple(out.shape) == (M, N) and out.device == device, "out: shape or device")
+    return out
+
+
+class LinearFp8:
+    """A dense layer x W^T in 8 bits with its workspace sized for `max_rows`
+    rows: codes [N, K] and scales [ceil(N / 128), ceil(K / 128)] of the weights
+    (quantize_fp8 with block_rows 128)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, *, max_rows: int,
+                 out_dtype: torch.dtype = torch.bfloat16):
+        _code_rows(codes, "codes")
+        _rows(scales, "scales", (torch.float32,))
+        self.codes, self.scales = codes, scales
+        self.N, self.K = int(codes.shape[0]), int(codes.shape[1])
+        _want(tuple(scales.shape) == (_blocks(self.N), _blocks(self.K)), "scales: shape")
+        _want(out_dtype in _DTYPES, "outputs are fp32 or bf16")
+        self.max_rows, self.out_dtype = max_rows, out_dtype
+        self.ws_bytes = B.reflex_linear_fp8_workspace_size(max_rows, self.K)
+        _want(self.ws_bytes > 0, "unsupported shape")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=codes.device)
+        self._w_ld, self._s_ld = _code_ld(codes), _ld(scales)
+
+    def forward(self, x: torch.Tensor, out: torch.Tensor | None = None, stream=None,
+                check: bool = True) -> torch.Tensor:
+        """x [M, K] fp32 or bf16 -> [M, N] of the layer's output type (or out's)."""
+        _rows(x, "x", _DTYPES)
+        M = int(x.shape[0])
+        _want(int(x.shape[1]) == self.K, "x: another number of columns than the weights")
+        _want(x.device == self.codes.device, "x is on another device than the weights")
+        _want(M <= self.max_rows, "more rows than the workspace was sized for")
+        out = _output(out, M, self.N, self.out_dtype, x.device)
+        B.reflex_linear_fp8(_DTYPES[x.dtype], x, _ld(x), self.codes, self._w_ld, self.scales,
+                            self._s_ld, M, self.N, self.K, _DTYPES[out.dtype], out, _ld(out),
+                            self.ws, self.ws_bytes, stream, check)
+        return out
+
+    def status(self, stream=None) -> int:
+        return B.reflex_moe_status(self.ws, stream)
+
+
+def quantize_experts(w_gate_up: torch.Tensor, w_down: torch.Tensor, stream=None) -> dict:
+    """The experts' weights w_gate_up [E, 2 inter, d] and w_down [E, d, inter]
+    (fp32 or bf16) in 128 x 128 blocks, for ExpertsFp8.  Gate rows and up rows
+    are blocked by themselves."""
+    e, two, d = (int(n) for n in w_gate_up.shape)
+    inter = two // 2
+    _want(two == 2 * inter and tuple(w_down.shape) == (e, d, inter), "weights: shapes")
+    gu = torch.empty((e, 2 * inter, d), dtype=torch.float8_e4m3fn, device=w_gate_up.device)
+    dn = torch.empty((e, d, inter), dtype=torch.float8_e4m3fn, device=w_down.device)
+    gus = torch.empty((e, 2, _blocks(inter), _blocks(d)), device=w_gate_up.device)
+    dns = torch.empty((e, _blocks(d), _blocks(inter)), device=w_down.device)
+    for i in range(e):
+        for h in range(2):
+            part = slice(h * inter, (h + 1) * inter)
+            quantize_fp8(w_gate_up[i, part], 128, gu[i, part], gus[i, h], stream)
+        quantize_fp8(w_down[i], 128, dn[i], dns[i], stream)
+    return dict(w_gate_up=gu, w_gate_up_scales=gus, w_down=dn, w_down_scales=dns)
+
+
+class ExpertsFp8:
+    """The routed SwiGLU experts of one layer in 8 bits (weights as
+    quantize_experts gives them), for a routing that the caller holds; the
+    workspace is sized for `max_tokens` tokens at `k_max`."""
+
+    def __init__(self, weights: dict, *, d: int, E: int, inter: int, k_max: int,
+                 max_tokens: int):
+        shapes = dict(w_gate_up=(E, 2 * inter, d), w_down=(E, d, inter),
+                      w_gate_up_scales=(E, 2, _blocks(inter), _blocks(d)),
+                      w_down_scales=(E, _blocks(d), _blocks(inter)))
+        for name, shape in shapes.items():
+            t = weights[name]
+            dt = torch.float32 if name.endswith("scales") else torch.float8_e4m3fn
+            _want(t.is_cuda and t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous(),
+                  f"{name}: a contiguous CUDA tensor {shape} of {dt}")
+        self.w, self.d, self.E, self.inter = weights, d, E, inter
+        self.k_max, self.max_tokens = k_max, max_tokens
+        self.ws_bytes = B.reflex_experts_fp8_workspace_size(max_tokens, d, E, inter, k_max)
+        _want(self.ws_bytes > 0, "unsupported MoE layer shape")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=weights["w_down"].device)
+
+    def forward(self, hidden: torch.Tensor, ids: torch.Tensor, alpha: torch.Tensor,
+                k: torch.Tensor, out: torch.Tensor | None = None, residual: bool = False,
+                stream=None, check: bool = True) -> torch.Tensor:
+        """hidden [T, d] bf16, ids int32 / alpha fp32 [T, k_max], k int32 [T]
+        -> [T, d] bf16 (hidden + experts with residual)."""
+        T = int(hidden.shape[0])
+        _want(T <= self.max_tokens, "more tokens than the workspace was sized for")
+        if out is None:
+            out = torch.empty((T, self.d), dtype=torch.bfloat16, device=hidden.device)
+        for t, dt, shape, what in ((hidden, torch.bfloat16, (T, self.d), "hidden"),
+                                   (ids, torch.int32, (T, self.k_max), "ids"),
+                                   (alpha, torch.float32, (T, self.k_max), "alpha"),
+                                   (k, torch.int32, (T,), "k"),
+                                   (out, torch.bfloat16, (T, self.d), "out")):
+            _want(t.is_cuda and t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous()
+                  and t.device == self.ws.device,
+                  f"{what}: a contiguous {shape} tensor of {dt} on the weights' device")
+        B.reflex_experts_fp8(hidden, ids, alpha, k, self.w["w_gate_up"],
+                             self.w["w_gate_up_scales"], self.w["w_down"],
+                             self.w["w_down_scales"], T, self.d, self.E, self.inter, self.k_max,
+                             B.REFLEX_FLAG_RESIDUAL if residual else 0, self.ws, self.ws_bytes,
+                             out, stream, check)
+        return out
+
+    def status(self, stream=None) -> int:
+        return B.reflex_moe_status(self.ws, stream)
