@@ -503,6 +503,51 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
                        int32_t inter, int32_t k_max, uint32_t flags, void* workspace,
                        size_t ws_bytes, void* out, void* stream);
 
+/*
+ * reflex_sample — one token for each row of logits from given uniforms, with
+ * its probability (the confidence that reflex_allocate and
+ * reflex_update_state read).  Per row, with T, top_k, top_p, min_p its
+ * settings and m its largest logit:
+ *   1. weights w_i, about 2^31 exp((z_i - m) / T), integers:
+ *      t = max((z_i - m) * c, -40), c = min(1.442695021629333 / T, FLT_MAX);
+ *      n = t rounded to an integer (ties to even); f = t - n;
+ *      p = 1 + f (c1 + f (c2 + f (c3 + f (c4 + f c5)))); w_i = floor(p 2^(n+31))
+ *      in fp32, every operation rounded by itself, c1 .. c5 = 0.6931471824645996,
+ *      0.2402234971523285, 0.055503811687231064, 0.00966636836528778,
+ *      0.0013381302123889327 (to fp32);
+ *   2. ranks by logit, higher first, lower index first on ties (-0 equals +0);
+ *      top-k keeps the first top_k; top-p keeps of these the ones whose
+ *      predecessors weigh less than top_p times all that top-k kept; min-p
+ *      keeps those with w_i >= min_p 2^31;
+ *   3. the token is the first, by index, at which the running weight of the
+ *      kept tokens exceeds u times all of it (products and comparisons with
+ *      top_p and u in fp64, where the sums are exact).
+ * T == 0 takes the largest logit (lowest index on ties).  Sums of integers
+ * have no order, so a row's token is the same whatever the batch.
+ *   dtype        REFLEX_DTYPE_F32 or REFLEX_DTYPE_BF16 (of logits).
+ *   logits       [rows, vocab], row stride ld >= vocab elements.  -inf and NaN
+ *                are never sampled; with +inf, those tokens alone are, alike.
+ *   temperature  [rows] fp32, >= 0 and finite; NULL: 1.
+ *   top_k        [rows] int32, off at <= 0; NULL: off.
+ *   top_p        [rows] fp32, > 0, off at >= 1; NULL: off.
+ *   min_p        [rows] fp32, <= 1, off at <= 0; NULL: off.
+ *   u            [rows] fp32, clamped to [0, 1 - 2^-24].
+ *   masked       [rows] u8, nullable: rows with 0 are left out.
+ *   tokens_out   [rows] int32.
+ *   conf_out     [rows] fp32: exp(z_token - m) / sum_i exp(z_i - m), the softmax
+ *                of the whole row at temperature 1, whatever the filters.
+ *   dev_status   [1] int32 nullable device error word; bits are OR-ed in (not
+ *                cleared): REFLEX_EINVAL for a row whose settings are outside
+ *                the ranges above or NaN.
+ * Such a row, a row that is left out and a row without a logit above -inf get
+ * token -1 and confidence 0.  vocab up to 2^18 (else REFLEX_EUNSUPPORTED);
+ * rows == 0 does nothing.
+ */
+int reflex_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, int32_t vocab,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, const float* u, const uint8_t* masked,
+                  int32_t* tokens_out, float* conf_out, int32_t* dev_status, void* stream);
+
 /* Synchronises `stream` and returns the status recorded in the workspace's
  * device error word by the last forward (REFLEX_OK if clean). */
 int reflex_moe_status(const void* workspace, void* stream);

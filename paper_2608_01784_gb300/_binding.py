@@ -52,7 +52,7 @@ EXPORTED = (
     "reflex_abi_version", "reflex_route_noalloc", "reflex_update_state",
     "reflex_step", "reflex_quantize_fp8", "reflex_matmul_fp8",
     "reflex_linear_fp8_workspace_size", "reflex_linear_fp8",
-    "reflex_experts_fp8_workspace_size", "reflex_experts_fp8",
+    "reflex_experts_fp8_workspace_size", "reflex_experts_fp8", "reflex_sample",
 )
 
 
@@ -148,6 +148,8 @@ def load():
     lib.reflex_experts_fp8.restype = ctypes.c_int
     lib.reflex_experts_fp8.argtypes = [P, P, P, P, P, P, P, P, i32, i32, i32, i32, i32,
                                        ctypes.c_uint32, P, sz, P, P]
+    lib.reflex_sample.restype = ctypes.c_int
+    lib.reflex_sample.argtypes = [i32, P, i64, i32, i32, P, P, P, P, P, P, P, P, P, P]
     if lib.reflex_abi_version() != ABI_VERSION:
         raise ImportError(f"{_LIB_PATH} has ABI version {lib.reflex_abi_version()}, "
                           f"this binding needs {ABI_VERSION}: rebuild it")
@@ -342,4 +344,15 @@ def reflex_experts_fp8(hidden, ids, alpha, k, w_gate_up, gate_up_scales, w_down,
                                    _stream(stream))
     if check and rc != REFLEX_OK:
         raise ReflexError(rc, "reflex_experts_fp8")
+    return rc
+
+
+def reflex_sample(dtype: int, logits, ld: int, rows: int, vocab: int, temperature, top_k, top_p,
+                  min_p, u, masked, tokens_out, conf_out, dev_status=None, stream=None,
+                  check: bool = True) -> int:
+    rc = load().reflex_sample(dtype, _ptr(logits), ld, rows, vocab, _ptr(temperature), _ptr(top_k),
+                              _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(masked), _ptr(tokens_out),
+                              _ptr(conf_out), _ptr(dev_status), _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_sample")
     return rc

@@ -294,3 +294,33 @@ class MoEStack:
 
     def status(self) -> int:
         return self.moe.status()
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor | None = None,
+           top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None,
+           min_p: torch.Tensor | None = None, masked: torch.Tensor | None = None,
+           tokens: torch.Tensor | None = None, conf: torch.Tensor | None = None,
+           status: torch.Tensor | None = None, stream=None):
+    """reflex_sample of logits [rows, vocab] (fp32 or bf16) with uniforms u
+    [rows] -> (tokens int32 [rows], conf fp32 [rows]).  Every setting is one
+    value per row; rows with masked == 0 get token -1 and confidence 0."""
+    kinds = {torch.float32: B.REFLEX_DTYPE_F32, torch.bfloat16: B.REFLEX_DTYPE_BF16}
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in kinds:
+        raise ValueError("logits: a CUDA matrix of fp32 or bf16")
+    rows, vocab = int(logits.shape[0]), int(logits.shape[1])
+    if (vocab > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
+        raise ValueError("logits: rows must be contiguous and must not overlap")
+    tokens = (torch.empty(rows, dtype=torch.int32, device=logits.device)
+              if tokens is None else tokens)
+    conf = torch.empty(rows, dtype=torch.float32, device=logits.device) if conf is None else conf
+    for t, dt, what in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"),
+                        (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+                        (min_p, torch.float32, "min_p"), (masked, torch.uint8, "masked"),
+                        (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf")):
+        if t is not None and (t.dtype != dt or t.numel() != rows or not t.is_contiguous()
+                              or t.device != logits.device):
+            raise ValueError(f"{what}: {rows} values of {dt} on the logits' device")
+    ld = int(logits.stride(0)) if rows > 1 else vocab
+    B.reflex_sample(kinds[logits.dtype], logits, ld, rows, vocab, temperature, top_k, top_p, min_p,
+                    u, masked, tokens, conf, status, stream)
+    return tokens, conf

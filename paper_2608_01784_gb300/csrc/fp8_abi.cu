@@ -1,6 +1,6 @@
-// fp8_abi.cu — C entry points of the 8-bit path: argument checks, workspace
-// carving, tensor maps and the launch sequences of one quantisation, one
-// product and one layer of routed experts.
+// fp8_abi.cu — C entry points of the 8-bit path and of sampling: argument
+// checks, workspace carving, tensor maps and the launch sequences of one
+// quantisation, one product and one layer of routed experts.
 #include <cudaTypedefs.h>
 
 #include "common.cuh"
@@ -324,6 +324,23 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   const void* resid = (flags & REFLEX_FLAG_RESIDUAL) ? hidden : nullptr;
   RX_CUDA(rx::launch_combine(REFLEX_DTYPE_BF16, ws + L.y, nullptr, resid, I32(L.row_of), alpha, k,
                              T, d, k_max, cap, out, err, sms, s));
+  return REFLEX_OK;
+}
+
+int reflex_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, int32_t vocab,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, const float* u, const uint8_t* masked, int32_t* tokens_out,
+                  float* conf_out, int32_t* dev_status, void* stream) {
+  if (!dtype_ok(dtype) || rows < 0 || vocab < 1 || ld < vocab) return REFLEX_EINVAL;
+  if (vocab > rx::sample_max_vocab() || rows > (1 << 27)) return REFLEX_EUNSUPPORTED;
+  if (rows == 0) return REFLEX_OK;
+  if (logits == nullptr || u == nullptr || tokens_out == nullptr || conf_out == nullptr ||
+      !aligned(logits, dtype == REFLEX_DTYPE_F32 ? 4 : 2))
+    return REFLEX_EINVAL;
+  const rx::SampleArgs a{logits, ld, rows,   vocab,      temperature, top_k, top_p,
+                         min_p,  u,  masked, tokens_out, conf_out,
+                         reinterpret_cast<uint32_t*>(dev_status)};
+  RX_CUDA(rx::launch_sample(dtype, a, rx::device_sms(), static_cast<cudaStream_t>(stream)));
   return REFLEX_OK;
 }
 

@@ -261,4 +261,22 @@ cudaError_t launch_combine(int dtype, const void* y, const void* y_shared,
                            int cap_rows, void* out, uint32_t* err, int num_sms,
                            cudaStream_t stream);
 
+// ---- sampling (sample.cu) ---------------------------------------------------
+struct SampleArgs {
+  const void* logits;  // [rows, vocab], row stride ld
+  int64_t ld;
+  int rows, vocab;
+  const float* temperature;  // nullable, like the next three and masked
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  const uint8_t* masked;
+  int32_t* tokens;
+  float* conf;
+  uint32_t* err;
+};
+int sample_max_vocab();
+cudaError_t launch_sample(int dtype, const SampleArgs& p, int num_sms, cudaStream_t stream);
+
 }  // namespace rx
