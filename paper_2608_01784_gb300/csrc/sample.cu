@@ -14,16 +14,23 @@
 // from about 2^-31 of it down; sums of 2^18 of them fit 64 bits and are exact
 // in a double, in which the comparisons with p * mass and u * mass are made.
 //
-// A row is held in shared memory by a cluster of 1 to 8 CTAs: it crosses HBM
-// once, and what the filters need beyond one pass over the weights are cheap
-// passes of comparisons.  The last kept token of top-k and of top-p (by logit,
-// then index) is found from a histogram of the weights by eighths of an octave
-// and, inside the bin that it falls in, by the logits' bits, 128 bins a pass.
-// Then one warp walks the 1024 tokens that u falls in.
+// A row is held in shared memory by a cluster of 1 to 8 CTAs, so it crosses HBM
+// once.  Without top-k and top-p one pass forms the weights.  With them, a
+// first pass counts the tokens by 32nds of an octave of weight; the counts (for
+// top-p, times the middle weight of each bin) name the few bins that the last
+// kept token, by logit, then index, can lie in.  A second pass collects those
+// bins' tokens in a list (with everything above them where that is little; else
+// it adds up the weights above) and, for top-p, all weights.  The cut is then
+// found in the list, exactly, from histograms of the logits' bits, 128 bins at a
+// time.  A row whose list overflows or misses the cut (many equal logits, top-p
+// of a large top-k) takes the same search over all of its tokens.  Then one warp
+// walks the 1024 tokens that u falls in.
 //
-// Bound: the fp32 pipes (about 20 operations a token in packed pairs) close
-// above HBM.
+// Bound: instruction issue, about 15 instructions a token for weights (fp32 in
+// packed pairs), 8 for counts, against the 12 cycles that HBM gives an SM for 128
+// bf16 tokens.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -35,29 +42,40 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kStep = 256;         // tokens of a warp's step: 8 consecutive ones a lane
 constexpr int kSegSteps = 4;       // steps of a segment
+constexpr int kFine = 1024;        // bins of 1/32 octave down to 2^-32
 constexpr int kBins = 128;
-constexpr int kCoarse = 96;        // level 0: eighths of an octave down to 2^-12, and the rest
+constexpr int kList = 2048;        // tokens of a CTA's list
 constexpr int kMaxSegs = 64;       // per CTA
 constexpr int kMaxVocab = 1 << 18;
 
-struct Hist {  // of one pass; masses in two halves of 16 bits, at most 2^16 tokens each
+struct Hist {  // masses in two halves of 16 bits, at most 2^16 tokens each
   uint32_t count[kBins], lo[kBins], hi[kBins];
 };
 
 struct Shared {
-  Hist hist[2];
+  uint32_t fine[kFine];  // tokens by weight
+  Hist hist;
+  uint16_t list[kList];  // tokens in reach of the cut, by their place in the slice
   unsigned long long seg_mass[kMaxSegs];
   uint32_t seg_ties[kMaxSegs];
-  unsigned long long mass;  // of the CTA's tokens
-  uint32_t tail;            // its tokens in the last coarse bin
+  // what the whole cluster reads, each written once before a cluster barrier
   float max, expsum;
-  int first;                // greedy: its first token of the largest logit
-  // results of a search
-  unsigned long long above_mass, bin_mass;
+  int first;                      // greedy: the first token of the largest logit
+  uint32_t n_list;
+  unsigned long long reach_mass;  // above the list
+  unsigned long long mass;        // of all tokens
+  unsigned long long whole_mass;  // the same, of the search over the whole row
+  // the CTA's own
+  unsigned long long warp_m[2][kWarps];
+  unsigned long long above_mass, bin_mass;  // results of a search
   uint32_t above_count, bin_count, klo, khi;
   float warp_f[kWarps];
-  unsigned long long warp_m[kWarps];
+  uint32_t warp_c[kWarps];
+  int bin[4];
+  uint32_t at[4];
 };
+static_assert(kFine == 4 * kThreads, "a thread has four bins");
+static_assert(sizeof(Shared) <= 10816, "three CTAs of 64 KB slices an SM");
 
 struct Args {
   const void* logits;
@@ -178,8 +196,12 @@ __device__ __forceinline__ Pair weigh(float z0, float z1, float neg_m, float c) 
 __device__ __forceinline__ uint32_t weight_of(float z, float neg_m, float c) {
   return weigh(z, z, neg_m, c).w0;
 }
-__device__ __forceinline__ int coarse_bin(float t) {
-  return t > -12.0f ? static_cast<int>(t * -8.0f) : kCoarse;
+__device__ __forceinline__ void add_wide(unsigned long long& sum, uint32_t w) {
+  asm("mad.wide.u32 %0, %1, 1, %0;" : "+l"(sum) : "r"(w));
+}
+// -32 t to the nearest integer; kFine and more: not counted (t < -32, NaN).
+__device__ __forceinline__ uint32_t fine_bin(float t) {
+  return __float_as_uint(__fmaf_rn(t, -32.0f, kMagic)) - 0x4b400000u;
 }
 
 // ---- logits as ordered integers ---------------------------------------------
@@ -207,61 +229,60 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums the cluster's histograms (and, at level 0, the rest of the mass and
-// count in bin kCoarse) and finds the first bin at which the running count
-// reaches want_count (by_count) or the running mass want_mass.  Warp 0 of
-// each CTA; the result goes to s.above_*, s.bin_*; returns the bin, or -1.
-__device__ int find_bin(Shared& s, const Hist& h, int C, bool level0, unsigned long long total,
-                        bool by_count, unsigned long long want_count, double want_mass,
-                        unsigned long long mass0, unsigned long long count0) {
+// Sum over the lanes below.
+template <typename T>
+__device__ __forceinline__ T warp_before(T v) {
   const int lane = threadIdx.x & 31;
-  unsigned long long cnt[4], mass[4], my_c = 0, my_m = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = lane * 4 + i;
-    cnt[i] = mass[i] = 0;
-    for (int r = 0; r < C; ++r) {
-      cnt[i] += ld_peer_u32(&h.count[b], r);
-      mass[i] += ld_peer_u32(&h.lo[b], r) +
-                 (static_cast<unsigned long long>(ld_peer_u32(&h.hi[b], r)) << 16);
-    }
-    my_c += cnt[i];
-    my_m += mass[i];
-  }
-  if (level0) {
-    // what the coarse bins leave lies in the last one
-    const unsigned long long rest = total - warp_sum(my_m);
-    if (lane * 4 == kCoarse) {
-      unsigned long long tail = 0;
-      for (int r = 0; r < C; ++r) tail += ld_peer_u32(&s.tail, r);
-      cnt[0] = tail;
-      mass[0] = rest;
-      my_c += tail;
-      my_m += rest;
-    }
-  }
-  unsigned long long c = my_c, m = my_m;
+  T x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long pc = __shfl_up_sync(0xffffffffu, c, o);
-    const unsigned long long pm = __shfl_up_sync(0xffffffffu, m, o);
-    if (lane >= o) {
-      c += pc;
-      m += pm;
+    const T y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x - v;
+}
+
+__device__ __forceinline__ uint4 ld_peer4(const void* p, int rank) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(peer(p, rank))
+               : "memory");
+  return v;
+}
+
+// Sums the cluster's histograms and finds the first bin at which the running
+// count (from count0) reaches `want`, or the running mass (from mass0) does.
+// Warp 0; the result goes to s.above_*, s.bin_*; returns the bin, or -1.
+__device__ int find_bin(Shared& s, int C, bool by_count, unsigned long long want,
+                        unsigned long long mass0, uint32_t count0) {
+  const int lane = threadIdx.x & 31;
+  uint32_t cnt[4] = {};
+  unsigned long long mass[4] = {};
+  for (int r = 0; r < C; ++r) {
+    const uint4 n = ld_peer4(&s.hist.count[lane * 4], r), l = ld_peer4(&s.hist.lo[lane * 4], r),
+                h = ld_peer4(&s.hist.hi[lane * 4], r);
+    const uint32_t nn[4] = {n.x, n.y, n.z, n.w}, ll[4] = {l.x, l.y, l.z, l.w},
+                   hh[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      cnt[i] += nn[i];
+      mass[i] += ll[i] + (static_cast<unsigned long long>(hh[i]) << 16);
     }
   }
-  c += count0 - my_c;
-  m += mass0 - my_m;
+  uint32_t c = count0 + warp_before(cnt[0] + cnt[1] + cnt[2] + cnt[3]);
+  unsigned long long m = mass0 + warp_before(mass[0] + mass[1] + mass[2] + mass[3]);
   int hit = -1;
+  uint32_t bin_c = 0;
+  unsigned long long bin_m = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool reached = by_count ? c + cnt[i] >= want_count
-                                  : static_cast<double>(m + mass[i]) >= want_mass;
-    if (hit < 0 && cnt[i] > 0 && reached) {
+    if (hit >= 0) continue;
+    if (cnt[i] > 0 && (by_count ? c + cnt[i] >= want : m + mass[i] >= want)) {
       hit = lane * 4 + i;
-      my_c = cnt[i];
-      my_m = mass[i];
-    } else if (hit < 0) {
+      bin_c = cnt[i];
+      bin_m = mass[i];
+    } else {
       c += cnt[i];
       m += mass[i];
     }
@@ -270,10 +291,10 @@ __device__ int find_bin(Shared& s, const Hist& h, int C, bool level0, unsigned l
   if (any == 0) return -1;
   const int from = __ffs(any) - 1;
   if (lane == from) {
-    s.above_count = static_cast<uint32_t>(c);
+    s.above_count = c;
     s.above_mass = m;
-    s.bin_count = static_cast<uint32_t>(my_c);
-    s.bin_mass = my_m;
+    s.bin_count = bin_c;
+    s.bin_mass = bin_m;
   }
   return __shfl_sync(0xffffffffu, hit, from);
 }
@@ -296,6 +317,34 @@ __device__ uint32_t first_key(uint32_t lo, uint32_t hi, F pred) {
   }
   return static_cast<uint32_t>(a);
 }
+
+__device__ __forceinline__ void cp_async16(void* smem, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(smem)), "l"(gmem)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// The largest of m and 8 logits; NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max8(float m, const float* z) {
+  float f[8];
+  load8(z, f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = max_nan(m, f[j]);
+  return m;
+}
+__device__ __forceinline__ float max8(float m, const __nv_bfloat16* z) {
+  const uint4 v = *reinterpret_cast<const uint4*>(z);
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+  const __nv_bfloat162 x = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  return max_nan(m, max_nan(__low2float(x), __high2float(x)));
+}
+
+enum { kListAll, kListReach, kWhole };   // where the cut is searched
 
 struct Cut {  // kept: logits above `value`, and the first `ties` of those equal to it
   float value;
@@ -350,59 +399,54 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   Te* mine = z_s + warp * steps * kStep + lane * 8;
   const int my_pos = pos0 + warp * steps * kStep + lane * 8;
   const float minus_inf = __int_as_float(0xff800000);
-  float m = minus_inf;
-  auto keep = [&](int i, const uint4 (&raw)[8 / kVec]) {
-#pragma unroll
-    for (int v = 0; v < 8 / kVec; ++v)
-      *reinterpret_cast<uint4*>(mine + i * kStep + v * kVec) = raw[v];
-    float z[8];
-    load8(reinterpret_cast<const Te*>(raw), z);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = fmaxf(m, z[j]);  // a NaN is no maximum
-  };
-  const int first_pos = pos0 + warp * steps * kStep;
-  const int whole =  // steps of the warp that lie in the row
-      first_pos < lo ? 0 : max(0, min(steps, (hi - first_pos) / kStep));
-#pragma unroll 4
-  for (int i = 0; i < whole; ++i) {
-    uint4 raw[8 / kVec];
-#pragma unroll
-    for (int v = 0; v < 8 / kVec; ++v)
-      raw[v] = __ldcs(reinterpret_cast<const uint4*>(base + my_pos + i * kStep + v * kVec));
-    keep(i, raw);
-  }
-  for (int i = whole; i < steps; ++i) {
-    uint4 raw[8 / kVec];
+  for (int i = 0; i < steps; ++i) {
 #pragma unroll
     for (int v = 0; v < 8 / kVec; ++v) {
       const int q = my_pos + i * kStep + v * kVec;
+      Te* to = mine + i * kStep + v * kVec;
       if (q >= lo && q + kVec <= hi) {
-        raw[v] = __ldcs(reinterpret_cast<const uint4*>(base + q));
+        cp_async16(to, base + q);
       } else {
-        Te* e = reinterpret_cast<Te*>(&raw[v]);
 #pragma unroll
         for (int j = 0; j < kVec; ++j)
-          e[j] = q + j >= lo && q + j < hi ? base[q + j] : from_f32<Te>(minus_inf);
+          to[j] = q + j >= lo && q + j < hi ? base[q + j] : from_f32<Te>(minus_inf);
       }
     }
-    keep(i, raw);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) s.warp_f[warp] = m;
-  for (int i = threadIdx.x; i < static_cast<int>(sizeof(s.hist) / 4); i += kThreads)
-    reinterpret_cast<uint32_t*>(s.hist)[i] = 0u;
+  for (int i = threadIdx.x; i < kFine; i += kThreads) s.fine[i] = 0u;
   if (threadIdx.x == 0) {
-    s.tail = 0;
+    s.n_list = 0;
     s.first = 0x7fffffff;
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s.warp_f[w]);
-    s.max = m;
+  cp_async_wait();  // a lane reads what it copied
+  float lane_max = minus_inf, m = minus_inf;
+#pragma unroll 4
+  for (int i = 0; i < steps; ++i) lane_max = max8(lane_max, mine + i * kStep);
+  auto block_max = [&] {
+    float x = lane_max;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+    if (lane == 0) s.warp_f[warp] = x;
+    __syncthreads();
+    x = s.warp_f[0];
+    for (int w = 1; w < kWarps; ++w) x = max_nan(x, s.warp_f[w]);
+    return x;
+  };
+  m = block_max();
+  if (m != m) {  // NaN counts as -inf
+    lane_max = minus_inf;
+    for (int i = 0; i < steps; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = to_f32(mine[i * kStep + j]);
+        if (z != z) mine[i * kStep + j] = from_f32<Te>(minus_inf);
+        lane_max = fmaxf(lane_max, z);
+      }
+    __syncthreads();
+    m = block_max();
   }
+  if (threadIdx.x == 0) s.max = m;
   cluster_sync();
-  m = minus_inf;
   for (int r = 0; r < C; ++r) m = fmaxf(m, __uint_as_float(ld_peer_u32(&s.max, r)));
   if (!(m > minus_inf)) {  // nothing to sample from
     cluster_sync();
@@ -419,101 +463,117 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
         const float z = to_f32(mine[i * kStep + j]);
         mine[i * kStep + j] = from_f32<Te>(z == m ? 0.0f : minus_inf);
       }
+    if (lane_max == m) lane_max = 0.0f;
     m = 0.0f;
   }
   const float neg_m = -m;
   const float c = fminf(__fdiv_rn(kLog2e, temp), 3.4028234e38f);
-  const bool same_t = c == kLog2e;
   const bool by_k = !greedy && top_k > 0, by_p = !greedy && top_p < 1.0f;
-  const bool cut_any = by_k || by_p, by_min = !greedy && min_p > 0.0f;
+  const bool cut_any = by_k || by_p;
+  const uint32_t w_min =
+      !greedy && min_p > 0.0f
+          ? static_cast<uint32_t>(ceil(static_cast<double>(min_p) * 2147483648.0)) : 0u;
 
-  // ---- one pass over the weights ----------------------------------------------
+  // ---- one pass over the row ----------------------------------------------------
   const int segs = (steps + kSegSteps - 1) / kSegSteps;  // of each warp
+  const bool same_t = c == kLog2e;  // T = 1: the weights give the softmax
   float esum = 0.0f;
-  {
-    unsigned long long mass = 0;
-    uint32_t tail = 0;
-    int first = 0x7fffffff;
+  uint64_t esum2 = 0;  // two partial sums
+  auto add_exp = [&](uint64_t d) {
+    float e0, e1;
+    upk(mul2(d, pk(kLog2e, kLog2e)), e0, e1);
+    esum2 = add2(esum2, pk(ex2(e0), ex2(e1)));
+  };
+  auto plain_pass = [&](auto same_c) {
+    constexpr bool kSame = decltype(same_c)::value;
     for (int g = 0; g < segs; ++g) {
       unsigned long long seg = 0;
       const int i1 = min(steps, (g + 1) * kSegSteps);
+#pragma unroll 1
       for (int i = g * kSegSteps; i < i1; ++i) {
         float z[8];
         load8(mine + i * kStep, z);
-        if (greedy) {
-#pragma unroll
-          for (int j = 7; j >= 0; --j)
-            if (z[j] == m) first = min(first, my_pos + i * kStep + j);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            esum += ex2(fmaxf(__fmul_rn(__fadd_rn(z[j], neg_m), kLog2e), -126.0f));
-          continue;
-        }
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
           const Pair w = weigh(z[j], z[j + 1], neg_m, c);
-          seg += w.w0;
-          seg += w.w1;
-          if (same_t) {
-            esum += w.v0 + w.v1;
-          } else {
-            float d0, d1;
-            upk(mul2(w.d, pk(kLog2e, kLog2e)), d0, d1);
-            esum += ex2(fmaxf(d0, -126.0f)) + ex2(fmaxf(d1, -126.0f));
-          }
-          if (cut_any) {
+          add_wide(seg, w.w0 >= w_min ? w.w0 : 0u);
+          add_wide(seg, w.w1 >= w_min ? w.w1 : 0u);
+          if (kSame) esum2 = add2(esum2, pk(w.v0, w.v1));
+          else add_exp(w.d);
+        }
+      }
+      seg = warp_sum(seg);
+      if (lane == 0) {
+        s.seg_mass[warp * segs + g] = seg;
+        s.seg_ties[warp * segs + g] = 0;
+      }
+    }
+  };
+  auto count_pass = [&](auto same_c) {
+    constexpr bool kSame = decltype(same_c)::value;
+#pragma unroll 2
+    for (int i = 0; i < steps; ++i) {
+      float z[8];
+      load8(mine + i * kStep, z);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float t = h ? w.t1 : w.t0;
-              const uint32_t ww = h ? w.w1 : w.w0;
-              if (t > -12.0f) {
-                const int b = coarse_bin(t);
-                atomicAdd(&s.hist[0].count[b], 1u);
-                atomicAdd(&s.hist[0].lo[b], ww & 0xffffu);
-                atomicAdd(&s.hist[0].hi[b], ww >> 16);
-              } else if (t > -32.0f) {
-                ++tail;
-              }
-            }
-          }
+      for (int j = 0; j < 8; j += 2) {
+        const uint64_t d = add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m));
+        const uint64_t t = mul2(d, pk(c, c));
+        if (kSame) {
+          float e0, e1;
+          upk(t, e0, e1);
+          esum2 = add2(esum2, pk(ex2(e0), ex2(e1)));
+        } else {
+          add_exp(d);
         }
-      }
-      if (!greedy) {
-        seg = warp_sum(seg);
-        mass += seg;
-        if (lane == 0) {
-          s.seg_mass[warp * segs + g] = seg;
-          s.seg_ties[warp * segs + g] = 0;
-        }
+        float b0, b1;  // fine_bin of both
+        upk(fma2(t, pk(-32.0f, -32.0f), pk(kMagic, kMagic)), b0, b1);
+        const uint32_t n0 = __float_as_uint(b0) - 0x4b400000u, n1 = __float_as_uint(b1) - 0x4b400000u;
+        if (n0 < kFine) atomicAdd(&s.fine[n0], 1u);
+        if (n1 < kFine) atomicAdd(&s.fine[n1], 1u);
       }
     }
-    if (same_t && !greedy) esum *= 1.0f / kTwo31;
-    esum = warp_sum(esum);
-    if (lane == 0) {
-      s.warp_f[warp] = esum;
-      s.warp_m[warp] = mass;
+  };
+  if (greedy) {
+#pragma unroll 2
+    for (int i = 0; i < steps; ++i) {
+      float z[8];
+      load8(mine + i * kStep, z);
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) add_exp(add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m)));
     }
-    if (cut_any && tail) atomicAdd(&s.tail, tail);
-    if (greedy && first != 0x7fffffff) atomicMin(&s.first, first);
+    if (lane_max == m) {  // the lane's first token of the largest logit
+      int first = 0x7fffffff;
+      for (int i = steps - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = 7; j >= 0; --j)
+          if (to_f32(mine[i * kStep + j]) == m) first = my_pos + i * kStep + j;
+      atomicMin(&s.first, first);
+    }
+  } else if (cut_any) {
+    if (same_t) count_pass(std::true_type());
+    else count_pass(std::false_type());
+  } else {
+    if (same_t) plain_pass(std::true_type());
+    else plain_pass(std::false_type());
   }
+  {
+    float e0, e1;
+    upk(esum2, e0, e1);
+    esum = warp_sum(e0 + e1);
+    if (same_t && !cut_any && !greedy) esum *= 1.0f / kTwo31;
+  }
+  __syncthreads();  // block_max has read warp_f
+  if (lane == 0) s.warp_f[warp] = esum;
   __syncthreads();
   if (threadIdx.x == 0) {
     float e = 0.0f;
-    unsigned long long t = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      e += s.warp_f[w];
-      t += s.warp_m[w];
-    }
+    for (int w = 0; w < kWarps; ++w) e += s.warp_f[w];
     s.expsum = e;
-    s.mass = t;
   }
   cluster_sync();
   esum = 0.0f;
-  unsigned long long total = 0;
-  for (int r = 0; r < C; ++r) {
-    esum += __uint_as_float(ld_peer_u32(&s.expsum, r));
-    total += ld_peer_u64(&s.mass, r);
-  }
+  for (int r = 0; r < C; ++r) esum += __uint_as_float(ld_peer_u32(&s.expsum, r));
   if (greedy) {
     int first = 0x7fffffff;
     for (int r = 0; r < C; ++r) first = min(first, static_cast<int>(ld_peer_u32(&s.first, r)));
@@ -526,243 +586,455 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   }
 
   // ---- the last kept token of top-k and top-p ---------------------------------
-  Cut cut{minus_inf, 0u, total};
-  const unsigned long long want_count = static_cast<unsigned long long>(top_k);
-  for (int which = 0; which < 2; ++which) {
-    const bool count_rule = which == 0;
-    if (count_rule ? !by_k : !by_p) continue;
-    const double want_mass =
-        count_rule ? 0.0 : static_cast<double>(top_p) * static_cast<double>(cut.mass);
-    // level 0 is kept for the second search; deeper levels use the other one
-    __syncthreads();
-    if (warp == 0) {
-      const int b = find_bin(s, s.hist[0], C, true, total, count_rule, want_count, want_mass, 0, 0);
-      uint32_t klo = 1, khi = 0;  // none
-      if (b >= 0) {
-        // the bin's logits: keys from the first whose bin is at most b to the
-        // last whose bin is not below b (bins fall as logits rise)
-        const uint32_t kmax = key_of<Te>(m), kmin = key_of<Te>(minus_inf);
-        auto bin_at = [&](uint32_t k) {
-          const float t = fmaxf(__fmul_rn(__fadd_rn(key_value<Te>(k), neg_m), c), -40.0f);
-          return t > -32.0f ? coarse_bin(t) : kCoarse + 1;
-        };
-        klo = first_key(kmin, kmax, [&](uint32_t k) { return bin_at(k) <= b; });
-        khi = first_key(klo, kmax, [&](uint32_t k) { return bin_at(k) < b; }) - 1;
-      }
-      if (lane == 0) {
-        s.klo = klo;
-        s.khi = khi;
-      }
-    }
-    __syncthreads();
-    uint32_t klo = s.klo, khi = s.khi;
-    if (klo > khi) continue;  // fewer tokens than asked for: nothing is cut
-    while (klo < khi) {
-      const uint32_t width = khi - klo;  // one less than the keys
-      const int sh = max(0, 25 - __clz(width));
-      Hist& h = s.hist[1];
-      // the cluster has read this histogram's last contents
-      cluster_sync();
-      for (int i = threadIdx.x; i < static_cast<int>(sizeof(Hist) / 4); i += kThreads)
-        reinterpret_cast<uint32_t*>(&h)[i] = 0u;
-      __syncthreads();
-      const float flo = key_value<Te>(klo), fhi = key_value<Te>(khi);
-      for (int i = 0; i < steps; ++i) {
-        float z[8];
-        load8(mine + i * kStep, z);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (z[j] >= flo && z[j] <= fhi) {  // false for a NaN
-            const uint32_t k = key_of<Te>(z[j]);
-            if (k - klo > width) continue;  // a zero next to a bound at the other zero
-            const uint32_t b = (khi - k) >> sh, ww = weight_of(z[j], neg_m, c);
-            atomicAdd(&h.count[b], 1u);
-            atomicAdd(&h.lo[b], ww & 0xffffu);
-            atomicAdd(&h.hi[b], ww >> 16);
-          }
-      }
-      cluster_sync();
+  Cut cut{minus_inf, 0u, 0};
+  int plan = kListAll;
+  if (cut_any) {
+    const uint32_t kmax = key_of<Te>(m), kmin = key_of<Te>(minus_inf);
+    const uint32_t want_count = static_cast<uint32_t>(max(top_k, 0));
+    uint32_t reach_lo = 0, reach_hi = 0, reach_count = 0;  // keys, and the tokens above
+    auto keys_of_bins = [&](uint32_t b_hi, uint32_t b_lo) {
+      // bins fall as logits rise; one warp finds either end
+      auto bin_at = [&](uint32_t k) {
+        return fine_bin(__fmul_rn(__fadd_rn(key_value<Te>(k), neg_m), c));
+      };
       if (warp == 0) {
-        const int b = find_bin(s, h, C, false, 0, count_rule, want_count, want_mass, s.above_mass,
-                               s.above_count);
-        if (lane == 0) {
-          const uint32_t top = khi - (static_cast<uint32_t>(b < 0 ? 0 : b) << sh);
-          s.khi = top;
-          s.klo = b < 0 ? top : top - min(top - klo, (1u << sh) - 1u);
+        const uint32_t k = first_key(kmin, kmax, [&](uint32_t k) { return bin_at(k) <= b_lo; });
+        if (lane == 0) s.klo = k;
+      } else if (warp == 1) {
+        const uint32_t k =
+            b_hi == 0 ? kmax + 1
+                      : first_key(kmin, kmax, [&](uint32_t k) { return bin_at(k) < b_hi; });
+        if (lane == 0) s.khi = k - 1;
+      }
+      __syncthreads();
+      reach_lo = s.klo;
+      reach_hi = s.khi;
+    };
+
+    {  // ---- the bins that the cut can lie in --------------------------------------
+      uint32_t n[4] = {};
+      for (int r = 0; r < C; ++r) {
+        const uint4 v = ld_peer4(&s.fine[threadIdx.x * 4], r);
+        n[0] += v.x; n[1] += v.y; n[2] += v.z; n[3] += v.w;
+      }
+      float w[4];  // the bins' middle weights, relative
+      w[0] = exp2f(static_cast<float>(threadIdx.x) * (-4.0f / 32));
+#pragma unroll
+      for (int i = 1; i < 4; ++i) w[i] = w[i - 1] * 0.97857206208770013f;  // 2^(-1/32)
+      const uint32_t own_n = n[0] + n[1] + n[2] + n[3];
+      const float own_m = n[0] * w[0] + n[1] * w[1] + n[2] * w[2] + n[3] * w[3];
+      uint32_t cnt = warp_before(own_n);
+      float est = warp_before(own_m);
+      if (lane == 31) {
+        s.warp_c[warp] = cnt + own_n;
+        s.warp_f[warp] = est + own_m;
+      }
+      if (threadIdx.x < 4) {
+        s.bin[threadIdx.x] = kFine;
+        s.at[threadIdx.x] = 0;
+      }
+      __syncthreads();
+      float whole = 0.0f;
+      for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) {
+          cnt += s.warp_c[i];
+          est += s.warp_f[i];
+        }
+        whole += s.warp_f[i];
+      }
+      // top-p: a bin's weights are within 1.1% of the middle one, so that the
+      // first pair of bins cannot miss; the second does not where the tokens
+      // spread over their bins
+      const float want = top_p * whole;
+      uint32_t c0 = cnt;
+      float e0 = est;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c0 += n[i];
+        e0 += n[i] * w[i];
+        if (n[i] == 0) continue;
+        const int b = threadIdx.x * 4 + i;
+        if (by_k) {
+          if (c0 >= want_count && c0 - n[i] < want_count) s.bin[0] = s.bin[1] = b;
+        } else {
+          // (a little less: the threads' running sums round differently)
+          const float d0 = (e0 - n[i] * w[i]) * 0.9999f;
+          if (e0 * 1.012f >= want && d0 * 1.012f < want) atomicMin(&s.bin[0], b);
+          if (e0 * 0.988f >= want && d0 * 0.988f < want) atomicMin(&s.bin[1], b);
+          if (e0 * 1.003f >= want && d0 * 1.003f < want) atomicMin(&s.bin[2], b);
+          if (e0 * 0.997f >= want && d0 * 0.997f < want) atomicMin(&s.bin[3], b);
         }
       }
       __syncthreads();
-      klo = s.klo;
-      khi = s.khi;
+      c0 = cnt;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int b = threadIdx.x * 4 + i;
+        if (b == s.bin[0]) s.at[0] = c0;
+        if (b == s.bin[2]) s.at[2] = c0;
+        c0 += n[i];
+        if (b == s.bin[1]) s.at[1] = c0;
+        if (b == s.bin[3]) s.at[3] = c0;
+      }
       __syncthreads();
+      const uint32_t room = static_cast<uint32_t>(kList * C) / 4 * 3;
+      int b_hi = s.bin[0], b_lo = s.bin[1];
+      uint32_t above = s.at[0], upto = s.at[1];
+      if (b_lo < kFine && upto <= kList) {
+        b_hi = 0;
+        above = 0;
+      } else {
+        plan = kListReach;
+        if (upto - above > room) {
+          b_hi = s.bin[2];
+          b_lo = s.bin[3];
+          above = s.at[2];
+          upto = s.at[3];
+        }
+        if (b_lo >= kFine || b_hi > b_lo || upto - above > room || (by_k && by_p)) plan = kWhole;
+      }
+      if (plan != kWhole) {
+        reach_count = above;
+        keys_of_bins(b_hi, b_lo);
+      }
     }
-    const float value = key_value<Te>(klo);
-    const unsigned long long w = s.bin_mass / s.bin_count, above = s.above_mass;
-    unsigned long long r;
-    if (count_rule) {
-      r = want_count - s.above_count;
-    } else {
-      // the smallest r >= 1 with above + r w >= want
-      r = w ? static_cast<unsigned long long>((want_mass - static_cast<double>(above)) /
-                                              static_cast<double>(w)) : 1;
-      r = r > 2 ? r - 2 : 1;
-      while (r < s.bin_count && static_cast<double>(above + r * w) < want_mass) ++r;
+
+    // weights of all tokens, of those above `from` that min-p keeps by segments,
+    // and of the others above; visit(i, z) for every step
+    auto weigh_pass = [&](float from, auto visit, unsigned long long* all_out,
+                          unsigned long long* above_out) {
+      unsigned long long all = 0, above = 0;
+      for (int g = 0; g < segs; ++g) {
+        unsigned long long seg = 0;
+        const int i1 = min(steps, (g + 1) * kSegSteps);
+#pragma unroll 1
+        for (int i = g * kSegSteps; i < i1; ++i) {
+          float z[8];
+          load8(mine + i * kStep, z);
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            const Pair w = weigh(z[j], z[j + 1], neg_m, c);
+            const uint32_t w0 = z[j] > from ? w.w0 : 0u, w1 = z[j + 1] > from ? w.w1 : 0u;
+            add_wide(all, w.w0);
+            add_wide(all, w.w1);
+            if (w_min) {  // segments: what min-p keeps; above: the rest
+              add_wide(seg, w0 >= w_min ? w0 : 0u);
+              add_wide(seg, w1 >= w_min ? w1 : 0u);
+              add_wide(above, w0 >= w_min ? 0u : w0);
+              add_wide(above, w1 >= w_min ? 0u : w1);
+            } else {
+              add_wide(seg, w0);
+              add_wide(seg, w1);
+            }
+          }
+          visit(i, z);
+        }
+        above += seg;
+        seg = warp_sum(seg);
+        if (lane == 0) {
+          s.seg_mass[warp * segs + g] = seg;
+          s.seg_ties[warp * segs + g] = 0;
+        }
+      }
+      all = warp_sum(all);
+      above = warp_sum(above);
+      if (lane == 0) {
+        s.warp_m[0][warp] = all;
+        s.warp_m[1][warp] = above;
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        all = above = 0;
+        for (int w = 0; w < kWarps; ++w) {
+          all += s.warp_m[0][w];
+          above += s.warp_m[1][w];
+        }
+        *all_out = all;
+        if (above_out) *above_out = above;
+      }
+    };
+
+    unsigned long long total = 0, above_mass = 0;
+    if (plan != kWhole) {
+      // ---- the tokens in reach of the cut, and the weights above them ---------
+      const float flo = key_value<Te>(reach_lo), fhi = key_value<Te>(reach_hi);
+      auto put = [&](int i, const float (&z)[8]) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          hits |= static_cast<uint32_t>(z[j] >= flo && z[j] <= fhi) << j;
+        if (hits) {
+          uint32_t at = atomicAdd(&s.n_list, static_cast<uint32_t>(__popc(hits)));
+          const int place = warp * steps * kStep + i * kStep + lane * 8;
+          for (; hits; hits &= hits - 1, ++at)
+            if (at < kList) s.list[at] = static_cast<uint16_t>(place + __ffs(hits) - 1);
+        }
+      };
+      if (plan == kListAll && by_k) {  // no weight but the listed ones counts
+#pragma unroll 2
+        for (int i = 0; i < steps; ++i) {
+          if (max8(minus_inf, mine + i * kStep) < flo) continue;
+          float z[8];
+          load8(mine + i * kStep, z);
+          put(i, z);
+        }
+        for (int g = lane; g < segs; g += 32) {
+          s.seg_mass[warp * segs + g] = 0;
+          s.seg_ties[warp * segs + g] = 0;
+        }
+      } else {
+        weigh_pass(fhi, put, &s.mass, &s.reach_mass);
+      }
+      cluster_sync();
+      const bool weighed = plan == kListReach || !by_k;
+      for (int r = 0; r < C; ++r) {
+        if (ld_peer_u32(&s.n_list, r) > kList) plan = kWhole;
+        if (weighed) {
+          total += ld_peer_u64(&s.mass, r);
+          above_mass += ld_peer_u64(&s.reach_mass, r);
+        }
+      }
     }
-    cut.value = value;
-    cut.ties = static_cast<uint32_t>(r < s.bin_count ? r : s.bin_count);
-    cut.mass = above + cut.ties * w;
+
+    // The search; false: the cut is not in the list.
+    auto search = [&]() {
+      cut.mass = total;
+      for (int which = 0; which < 2; ++which) {
+        const bool count_rule = which == 0;
+        if (count_rule ? !by_k : !by_p) continue;
+        // sums are below 2^53: reaching p * mass is reaching it rounded up
+        const unsigned long long want =
+            count_rule ? want_count
+                       : static_cast<unsigned long long>(
+                             ceil(static_cast<double>(top_p) * static_cast<double>(cut.mass)));
+        if (!count_rule && above_mass >= want) return false;
+        uint32_t klo = reach_lo, khi = reach_hi;
+        if (threadIdx.x == 0) {
+          s.above_count = reach_count;
+          s.above_mass = above_mass;
+        }
+        bool counted = false;
+        while (klo < khi || !counted) {
+          const uint32_t width = khi - klo;  // one less than the keys
+          const int sh = max(0, 25 - __clz(width));
+          // the cluster has read this histogram's last contents
+          cluster_sync();
+          for (int i = threadIdx.x; i < static_cast<int>(sizeof(Hist) / 4); i += kThreads)
+            reinterpret_cast<uint32_t*>(&s.hist)[i] = 0u;
+          __syncthreads();
+          auto count_in = [&](float z) {
+            const uint32_t k = key_of<Te>(z);
+            if (k - klo > width) return;
+            const uint32_t b = (khi - k) >> sh, w = weight_of(z, neg_m, c);
+            atomicAdd(&s.hist.count[b], 1u);
+            atomicAdd(&s.hist.lo[b], w & 0xffffu);
+            atomicAdd(&s.hist.hi[b], w >> 16);
+          };
+          if (plan == kWhole) {
+            const float flo = key_value<Te>(klo), fhi = key_value<Te>(khi);
+            for (int i = 0; i < steps; ++i) {
+              float z[8];
+              load8(mine + i * kStep, z);
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (z[j] >= flo && z[j] <= fhi) count_in(z[j]);
+            }
+          } else {
+            const int n = static_cast<int>(s.n_list);
+            for (int i = threadIdx.x; i < n; i += kThreads) count_in(to_f32(z_s[s.list[i]]));
+          }
+          cluster_sync();
+          counted = true;
+          if (warp == 0) {
+            const int b = find_bin(s, C, count_rule, want, s.above_mass, s.above_count);
+            if (lane == 0) {
+              const uint32_t top = khi - (static_cast<uint32_t>(b < 0 ? 0 : b) << sh);
+              s.khi = top;
+              s.klo = b < 0 ? top : top - min(top - klo, (1u << sh) - 1u);
+              if (b < 0) s.bin_count = 0;
+            }
+          }
+          __syncthreads();
+          klo = s.klo;
+          khi = s.khi;
+          if (s.bin_count == 0) break;
+          __syncthreads();
+        }
+        if (s.bin_count == 0) {  // not reached: in the whole row, nothing is cut
+          __syncthreads();
+          if (plan != kWhole) return false;
+          continue;
+        }
+        const unsigned long long w = s.bin_mass / s.bin_count, above = s.above_mass;
+        const uint32_t ties = s.bin_count, above_count = s.above_count;
+        __syncthreads();
+        // the smallest r with r tokens of the cut's logit reaching what is asked for
+        const unsigned long long r =
+            count_rule ? want - above_count : (w ? (want - above + w - 1) / w : 1);
+        cut.value = key_value<Te>(klo);
+        cut.ties = static_cast<uint32_t>(r < ties ? r : ties);
+        cut.mass = above + cut.ties * w;
+      }
+      return true;
+    };
+    if (plan == kWhole || !search()) {
+      // ---- the same over every token ----------------------------------------------
+      plan = kWhole;
+      if (by_p) {
+        weigh_pass(m, [](int, const float (&)[8]) {}, &s.whole_mass, nullptr);
+        cluster_sync();
+        total = 0;
+        for (int r = 0; r < C; ++r) total += ld_peer_u64(&s.whole_mass, r);
+      }
+      above_mass = 0;
+      reach_count = 0;
+      __syncthreads();
+      keys_of_bins(0, kFine - 1);
+      cut = Cut{minus_inf, 0u, 0};
+      search();
+    }
   }
 
   // ---- the kept mass of each segment ------------------------------------------
-  const uint32_t w_min = by_min ? static_cast<uint32_t>(ceil(static_cast<double>(min_p) *
-                                                             2147483648.0)) : 0u;
   const bool cut_used = cut.value > minus_inf;
   uint32_t w_tie = 0;
   if (cut_used) {
     w_tie = weight_of(cut.value, neg_m, c);
     if (w_tie < w_min) w_tie = 0;
   }
-  if (cut_used || by_min) {
+  if (cut_any) {
     __syncthreads();
-    for (int g = 0; g < segs; ++g) {
-      unsigned long long seg = 0;
-      uint32_t ties = 0;
-      const int i1 = min(steps, (g + 1) * kSegSteps);
-      for (int i = g * kSegSteps; i < i1; ++i) {
-        float z[8];
-        load8(mine + i * kStep, z);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (z[j] > cut.value) {
-            const uint32_t w = weight_of(z[j], neg_m, c);
-            seg += w >= w_min ? w : 0u;
-          }
-          ties += cut_used && z[j] == cut.value;
+    if (plan != kWhole) {
+      const int n = static_cast<int>(s.n_list);
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const int place = s.list[i], at = place / (steps * kStep);
+        const int q = at * segs + (place - at * steps * kStep) / (kSegSteps * kStep);
+        const float z = to_f32(z_s[place]);
+        if (z > cut.value) {
+          const uint32_t w = weight_of(z, neg_m, c);
+          if (w >= w_min) atomicAdd(&s.seg_mass[q], static_cast<unsigned long long>(w));
+        } else if (z == cut.value) {
+          atomicAdd(&s.seg_ties[q], 1u);
         }
       }
-      seg = warp_sum(seg);
-      ties = __reduce_add_sync(0xffffffffu, ties);
-      if (lane == 0) {
-        s.seg_mass[warp * segs + g] = seg;
-        s.seg_ties[warp * segs + g] = ties;
+    } else {
+      for (int g = 0; g < segs; ++g) {
+        unsigned long long seg = 0;
+        uint32_t ties = 0;
+        const int i1 = min(steps, (g + 1) * kSegSteps);
+#pragma unroll 1
+        for (int i = g * kSegSteps; i < i1; ++i) {
+          float z[8];
+          load8(mine + i * kStep, z);
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            const Pair p = weigh(z[j], z[j + 1], neg_m, c);
+            add_wide(seg, z[j] > cut.value && p.w0 >= w_min ? p.w0 : 0u);
+            add_wide(seg, z[j + 1] > cut.value && p.w1 >= w_min ? p.w1 : 0u);
+            ties += (cut_used && z[j] == cut.value) + (cut_used && z[j + 1] == cut.value);
+          }
+        }
+        seg = warp_sum(seg);
+        ties = __reduce_add_sync(0xffffffffu, ties);
+        if (lane == 0) {
+          s.seg_mass[warp * segs + g] = seg;
+          s.seg_ties[warp * segs + g] = ties;
+        }
       }
     }
   }
   cluster_sync();
 
   // ---- the segment that u falls in, then the token -----------------------------
-  const int per_cta = kWarps * segs, all = per_cta * C;
   if (warp == 0) {
-    unsigned long long kept = 0;
-    // kept mass of segment q given the ties before it
+    const int per_cta = kWarps * segs, all = per_cta * C;
+    const int per_lane = (all + 31) / 32;  // segments, in order; at most 32
     auto seg_at = [&](int q, uint32_t& ties) {
-      const int r = q / per_cta, l = q % per_cta;
+      ties = 0;
+      if (q >= all) return 0ull;
+      const int r = q / per_cta, l = q - r * per_cta;
       ties = ld_peer_u32(&s.seg_ties[l], r);
       return ld_peer_u64(&s.seg_mass[l], r);
     };
-    for (int round = 0; round < 2; ++round) {
-      // round 0: the kept mass; round 1: the segment
-      const double target = static_cast<double>(u) * static_cast<double>(kept);
-      unsigned long long run = 0;
-      uint32_t run_ties = 0;
-      int found = -1;
-      for (int q0 = 0; q0 < all && found < 0; q0 += 32) {
-        uint32_t ties = 0;
-        unsigned long long mass = q0 + lane < all ? seg_at(q0 + lane, ties) : 0;
-        uint32_t before = ties;
+    // kept mass given the tokens equal to the cut before
+    auto with_ties = [&](unsigned long long above, uint32_t before, uint32_t ties) {
+      const uint32_t left = cut.ties > before ? cut.ties - before : 0u;
+      return above + static_cast<unsigned long long>(min(left, ties)) * w_tie;
+    };
+    unsigned long long above = 0;
+    uint32_t ties = 0;
+    for (int i = 0; i < per_lane; ++i) {
+      uint32_t n;
+      above += seg_at(lane * per_lane + i, n);
+      ties += n;
+    }
+    uint32_t before = warp_before(ties);
+    unsigned long long kept = with_ties(above, before, ties);
+    unsigned long long upto = warp_before(kept) + kept;
+    // sums are integers below 2^53: exceeding u * mass is exceeding it rounded down
+    const unsigned long long target = static_cast<unsigned long long>(
+        static_cast<double>(u) * static_cast<double>(__shfl_sync(0xffffffffu, upto, 31)));
+    // u < 1: some lane's running mass exceeds the target
+    int f = __ffs(__ballot_sync(0xffffffffu, upto > target) | 1u << 31) - 1;
+    unsigned long long run = __shfl_sync(0xffffffffu, upto - kept, f);
+    uint32_t run_ties = __shfl_sync(0xffffffffu, before, f);
+    // the lane's segments, one a lane
+    above = seg_at(lane < per_lane ? f * per_lane + lane : all, ties);
+    before = run_ties + warp_before(ties);
+    kept = with_ties(above, before, ties);
+    upto = run + warp_before(kept) + kept;
+    const int q = f * per_lane;
+    f = __ffs(__ballot_sync(0xffffffffu, upto > target) | 1u << 31) - 1;
+    run = __shfl_sync(0xffffffffu, upto - kept, f);
+    run_ties = __shfl_sync(0xffffffffu, before, f);
+    const int found = min(q + f, all - 1);
+    if (found / per_cta == rank) {
+      const int l = found % per_cta, w0 = l / segs, g = l % segs;
+      const int i1 = min(steps, (g + 1) * kSegSteps);
+      for (int i = g * kSegSteps; i < i1; ++i) {
+        const int off = (w0 * steps + i) * kStep + lane * 8;
+        float z[8];
+        load8(z_s + off, z);
+        uint32_t w[8];
+        ties = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t v = __shfl_up_sync(0xffffffffu, before, o);
-          if (lane >= o) before += v;
+        for (int j = 0; j < 8; j += 2) {
+          const Pair p = weigh(z[j], z[j + 1], neg_m, c);
+          w[j] = z[j] > cut.value && p.w0 >= w_min ? p.w0 : 0u;
+          w[j + 1] = z[j + 1] > cut.value && p.w1 >= w_min ? p.w1 : 0u;
+          ties += (cut_used && z[j] == cut.value) + (cut_used && z[j + 1] == cut.value);
         }
-        const uint32_t tie_sum = __shfl_sync(0xffffffffu, before, 31);
-        before += run_ties - ties;
-        const uint32_t left = cut.ties > before ? cut.ties - before : 0u;
-        mass += static_cast<unsigned long long>(min(left, ties)) * w_tie;
-        unsigned long long incl = mass;
+        before = run_ties + warp_before(ties);
+        run_ties = __shfl_sync(0xffffffffu, before + ties, 31);
+        kept = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const unsigned long long v = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += v;
+        for (int j = 0; j < 8; ++j) {
+          if (cut_used && z[j] == cut.value) w[j] = before++ < cut.ties ? w_tie : 0u;
+          kept += w[j];
         }
-        const unsigned long long sum = __shfl_sync(0xffffffffu, incl, 31);
-        if (round == 1) {
-          const uint32_t hit =
-              __ballot_sync(0xffffffffu, static_cast<double>(run + incl) > target);
-          if (hit) {
-            const int f = __ffs(hit) - 1;
-            found = q0 + f;
-            run += __shfl_sync(0xffffffffu, incl - mass, f);
-            run_ties = __shfl_sync(0xffffffffu, before, f);
-            break;
-          }
-        }
-        run += sum;
-        run_ties += tie_sum;
-      }
-      if (round == 0) {
-        kept = run;
-      } else if (found >= 0 && found / per_cta == rank) {
-        const int l = found % per_cta, w0 = l / segs, g = l % segs;
-        const int i1 = min(steps, (g + 1) * kSegSteps);
-        for (int i = g * kSegSteps; i < i1; ++i) {
-          const int off = (w0 * steps + i) * kStep + lane * 8;
-          float z[8];
-          load8(z_s + off, z);
-          uint32_t w[8], ties = 0;
-          bool tie[8];
-          unsigned long long mass = 0;
+        upto = run + warp_before(kept) + kept;
+        const uint32_t hit = __ballot_sync(0xffffffffu, upto > target);
+        if (hit) {
+          if (lane == __ffs(hit) - 1) {
+            unsigned long long at = upto - kept;
+            int pick = 7;
+            float zt = z[7];
+            bool done = false;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint32_t x = weight_of(z[j], neg_m, c);
-            w[j] = z[j] > cut.value && x >= w_min ? x : 0u;
-            tie[j] = cut_used && z[j] == cut.value;
-            ties += tie[j];
-          }
-          uint32_t before = ties;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane >= o) before += v;
-          }
-          const uint32_t tie_sum = __shfl_sync(0xffffffffu, before, 31);
-          before += run_ties - ties;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (tie[j]) w[j] = before++ < cut.ties ? w_tie : 0u;
-            mass += w[j];
-          }
-          unsigned long long incl = mass;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-          }
-          const uint32_t hit =
-              __ballot_sync(0xffffffffu, static_cast<double>(run + incl) > target);
-          if (hit) {
-            if (lane == __ffs(hit) - 1) {
-              unsigned long long at = run + incl - mass;
-              int pick = 0;
-              float zt = 0.0f;
-              bool done = false;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                at += w[j];
-                if (!done && static_cast<double>(at) > target) {
-                  done = true;
-                  pick = j;
-                  zt = z[j];
-                }
+            for (int j = 0; j < 8; ++j) {
+              at += w[j];
+              if (!done && at > target) {
+                done = true;
+                pick = j;
+                zt = z[j];
               }
-              a.tokens[row] = pos0 + off + pick - shift;
-              a.conf[row] = ex2(fmaxf((zt + neg_m) * kLog2e, -126.0f)) / esum;
             }
-            break;
+            a.tokens[row] = pos0 + off + pick - shift;
+            a.conf[row] = ex2((zt + neg_m) * kLog2e) / esum;
           }
-          run += __shfl_sync(0xffffffffu, incl, 31);
-          run_ties += tie_sum;
+          break;
         }
+        run = __shfl_sync(0xffffffffu, upto, 31);
       }
     }
   }
@@ -774,14 +1046,18 @@ cudaError_t launch_typed(Args a, int rows, int num_sms, cudaStream_t stream) {
   auto kernel = sample_kernel<Te>;
   constexpr size_t kHead = (sizeof(Shared) + 15) / 16 * 16;
   constexpr int kGrain = kWarps * kStep;
-  auto slice_of = [&](int C) {  // 16 / sizeof(Te) - 1 positions may precede the row
-    const int per = (a.vocab + 16 / static_cast<int>(sizeof(Te)) - 1 + C - 1) / C;
+  // positions that may precede a row in its first 16 bytes
+  const bool whole = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
+                     (rows == 1 || a.ld * static_cast<int64_t>(sizeof(Te)) % 16 == 0);
+  const int lead = whole ? 0 : 16 / static_cast<int>(sizeof(Te)) - 1;
+  auto slice_of = [&](int C) {
+    const int per = (a.vocab + lead + C - 1) / C;
     return (per + kGrain - 1) / kGrain * kGrain;
   };
-  // CTAs a row: slices of at most 70 KB, three to an SM; more for few rows,
+  // CTAs a row: slices of at most 64 KB, three to an SM; more for few rows,
   // as long as each has a whole step for every warp
   int C = 1;
-  while (C < 8 && slice_of(C) * sizeof(Te) > 70 * 1024) C *= 2;
+  while (C < 8 && slice_of(C) * sizeof(Te) > 64 * 1024) C *= 2;
   while (C < 8 && static_cast<int64_t>(rows) * C * 2 <= num_sms && slice_of(C) > kGrain) C *= 2;
   a.slice = slice_of(C);
   const size_t smem = kHead + a.slice * sizeof(Te);
