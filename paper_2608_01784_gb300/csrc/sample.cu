@@ -14,8 +14,12 @@
 // from about 2^-31 of it down; sums of 2^18 of them fit 64 bits and are exact
 // in a double, in which the comparisons with p * mass and u * mass are made.
 //
-// A row is held in shared memory by a cluster of 1 to 8 CTAs, so it crosses HBM
-// once.  Without top-k and top-p one pass forms the weights.  With them, a
+// Two shapes of one kernel.  Few rows, or short ones: a row is held in the shared
+// memory of a cluster of 1 to 8 CTAs.  Many long rows: one CTA of 512 threads
+// walks a row a few times, the first time from HBM, then from L2 (two CTAs an
+// SM; a third of the cluster's barriers and none of its waits).
+//
+// Without top-k and top-p one pass forms the weights.  With them, a
 // first pass counts the tokens by 32nds of an octave of weight; the counts (for
 // top-p, times the middle weight of each bin) name the few bins that the last
 // kept token, by logit, then index, can lie in.  A second pass collects those
@@ -38,26 +42,47 @@
 namespace rx {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kStep = 256;         // tokens of a warp's step: 8 consecutive ones a lane
 constexpr int kSegSteps = 4;       // steps of a segment
 constexpr int kFine = 1024;        // bins of 1/32 octave down to 2^-32
 constexpr int kBins = 128;
-constexpr int kList = 2048;        // tokens of a CTA's list
-constexpr int kMaxSegs = 64;       // per CTA
 constexpr int kMaxVocab = 1 << 18;
 
-struct Hist {  // masses in two halves of 16 bits, at most 2^16 tokens each
-  uint32_t count[kBins], lo[kBins], hi[kBins];
+// kStream: a CTA walks a row in global memory; else a cluster holds it.
+template <bool kStream>
+struct Shape {
+  static constexpr int kThreads = kStream ? 512 : 256;
+  static constexpr int kWarps = kThreads / 32;
+  static constexpr int kCtas = kStream ? 2 : 3;         // an SM
+  static constexpr int kList = kStream ? 10240 : 2048;  // tokens of a CTA's list
+  static constexpr int kMaxSegs = kStream ? 288 : 64;   // per CTA
 };
 
+struct Hist {  // masses in pieces of 11, 11 and 10 bits, at most 2^18 tokens each
+  uint32_t count[kBins], m0[kBins], m1[kBins], m2[kBins];
+};
+
+// Tokens in reach of the cut: places in the slice, and the logits where the
+// slice is not in shared memory.
+template <bool kStream>
+struct List {
+  uint16_t place[Shape<false>::kList];
+};
+template <>
+struct List<true> {
+  uint32_t place[Shape<true>::kList];
+  float z[Shape<true>::kList];
+};
+
+template <bool kStream>
 struct Shared {
+  using S = Shape<kStream>;
   uint32_t fine[kFine];  // tokens by weight
   Hist hist;
-  uint16_t list[kList];  // tokens in reach of the cut, by their place in the slice
-  unsigned long long seg_mass[kMaxSegs];
-  uint32_t seg_ties[kMaxSegs];
+  List<kStream> list;
+  unsigned long long seg_mass[S::kMaxSegs];  // weights of a segment's kept tokens ..
+  uint32_t seg_lo[S::kMaxSegs], seg_hi[S::kMaxSegs];  // .. and of those from the list, in halves
+  uint32_t seg_ties[S::kMaxSegs];
   // what the whole cluster reads, each written once before a cluster barrier
   float max, expsum;
   int first;                      // greedy: the first token of the largest logit
@@ -66,16 +91,16 @@ struct Shared {
   unsigned long long mass;        // of all tokens
   unsigned long long whole_mass;  // the same, of the search over the whole row
   // the CTA's own
-  unsigned long long warp_m[2][kWarps];
+  unsigned long long warp_m[2][S::kWarps];
   unsigned long long above_mass, bin_mass;  // results of a search
   uint32_t above_count, bin_count, klo, khi;
-  float warp_f[kWarps];
-  uint32_t warp_c[kWarps];
+  float warp_f[S::kWarps];
+  uint32_t warp_c[S::kWarps];
   int bin[4];
   uint32_t at[4];
 };
-static_assert(kFine == 4 * kThreads, "a thread has four bins");
-static_assert(sizeof(Shared) <= 10816, "three CTAs of 64 KB slices an SM");
+static_assert(sizeof(Shared<false>) <= 12 * 1024, "three CTAs of 56 KB slices an SM");
+static_assert(sizeof(Shared<true>) <= 112 * 1024, "two CTAs an SM");
 
 struct Args {
   const void* logits;
@@ -104,23 +129,48 @@ __device__ __forceinline__ int cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return static_cast<int>(r);
 }
-__device__ __forceinline__ void cluster_sync() {
+__device__ __forceinline__ void cluster_arrive() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ uint32_t peer(const void* p, int rank) {
   uint32_t a;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
   return a;
 }
-__device__ __forceinline__ uint32_t ld_peer_u32(const void* p, int rank) {
+// A word of another CTA's Shared (kStream: there is no other).
+template <bool kStream>
+__device__ __forceinline__ uint32_t peer_u32(const uint32_t* p, int rank) {
+  if (kStream) return *p;
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
   return v;
 }
-__device__ __forceinline__ unsigned long long ld_peer_u64(const void* p, int rank) {
+template <bool kStream>
+__device__ __forceinline__ float peer_f32(const float* p, int rank) {
+  return __uint_as_float(peer_u32<kStream>(reinterpret_cast<const uint32_t*>(p), rank));
+}
+template <bool kStream>
+__device__ __forceinline__ unsigned long long peer_u64(const unsigned long long* p, int rank) {
+  if (kStream) return *p;
   unsigned long long v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
+template <bool kStream>
+__device__ __forceinline__ uint4 peer_u32x4(const uint32_t* p, int rank) {
+  if (kStream) return *reinterpret_cast<const uint4*>(p);
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(peer(p, rank))
+               : "memory");
   return v;
 }
 
@@ -242,32 +292,27 @@ __device__ __forceinline__ T warp_before(T v) {
   return x - v;
 }
 
-__device__ __forceinline__ uint4 ld_peer4(const void* p, int rank) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(peer(p, rank))
-               : "memory");
-  return v;
-}
-
 // Sums the cluster's histograms and finds the first bin at which the running
 // count (from count0) reaches `want`, or the running mass (from mass0) does.
 // Warp 0; the result goes to s.above_*, s.bin_*; returns the bin, or -1.
-__device__ int find_bin(Shared& s, int C, bool by_count, unsigned long long want,
+template <bool kStream>
+__device__ int find_bin(Shared<kStream>& s, int C, bool by_count, unsigned long long want,
                         unsigned long long mass0, uint32_t count0) {
   const int lane = threadIdx.x & 31;
   uint32_t cnt[4] = {};
   unsigned long long mass[4] = {};
   for (int r = 0; r < C; ++r) {
-    const uint4 n = ld_peer4(&s.hist.count[lane * 4], r), l = ld_peer4(&s.hist.lo[lane * 4], r),
-                h = ld_peer4(&s.hist.hi[lane * 4], r);
-    const uint32_t nn[4] = {n.x, n.y, n.z, n.w}, ll[4] = {l.x, l.y, l.z, l.w},
-                   hh[4] = {h.x, h.y, h.z, h.w};
+    const uint4 n = peer_u32x4<kStream>(&s.hist.count[lane * 4], r),
+                x = peer_u32x4<kStream>(&s.hist.m0[lane * 4], r),
+                y = peer_u32x4<kStream>(&s.hist.m1[lane * 4], r),
+                z = peer_u32x4<kStream>(&s.hist.m2[lane * 4], r);
+    const uint32_t nn[4] = {n.x, n.y, n.z, n.w}, xx[4] = {x.x, x.y, x.z, x.w},
+                   yy[4] = {y.x, y.y, y.z, y.w}, zz[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       cnt[i] += nn[i];
-      mass[i] += ll[i] + (static_cast<unsigned long long>(hh[i]) << 16);
+      mass[i] += xx[i] + (static_cast<unsigned long long>(yy[i]) << 11) +
+                 (static_cast<unsigned long long>(zz[i]) << 22);
     }
   }
   uint32_t c = count0 + warp_before(cnt[0] + cnt[1] + cnt[2] + cnt[3]);
@@ -330,18 +375,31 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-__device__ __forceinline__ float max8(float m, const float* z) {
-  float f[8];
-  load8(z, f);
+__device__ __forceinline__ float max8(float m, const uint4 (&raw)[2]) {  // fp32
+  const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w,
+                         raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) m = max_nan(m, f[j]);
+  for (int j = 0; j < 8; ++j) m = max_nan(m, __uint_as_float(w[j]));
   return m;
 }
-__device__ __forceinline__ float max8(float m, const __nv_bfloat16* z) {
-  const uint4 v = *reinterpret_cast<const uint4*>(z);
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+__device__ __forceinline__ float max8(float m, const uint4 (&raw)[1]) {  // bf16
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(raw);
   const __nv_bfloat162 x = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
   return max_nan(m, max_nan(__low2float(x), __high2float(x)));
+}
+__device__ __forceinline__ void widen(const uint4 (&raw)[2], float (&z)[8]) {
+  const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w,
+                         raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void widen(const uint4 (&raw)[1], float (&z)[8]) {
+  const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    z[2 * j] = __uint_as_float(w[j] << 16);
+    z[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  }
 }
 
 enum { kListAll, kListReach, kWhole };   // where the cut is searched
@@ -352,18 +410,19 @@ struct Cut {  // kept: logits above `value`, and the first `ties` of those equal
   unsigned long long mass;  // of what is kept
 };
 
-template <typename Te>
-__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  Shared& s = *reinterpret_cast<Shared*>(smem);
-  Te* z_s = reinterpret_cast<Te*>(smem + (sizeof(Shared) + 15) / 16 * 16);
-  constexpr int kVec = 16 / sizeof(Te);
-  const int C = cluster_size(), rank = cluster_rank();
-  const int64_t row = blockIdx.x / C;
+// One row, by the cluster or by the CTA.
+template <typename Te, bool kStream>
+__device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te* z_s, int C,
+                                           int rank, int64_t row) {
+  constexpr int kThreads = Shape<kStream>::kThreads, kWarps = Shape<kStream>::kWarps;
+  constexpr int kList = Shape<kStream>::kList;
+  constexpr int kVec = 16 / sizeof(Te), kRaw = 8 / kVec;  // a lane's step: kRaw vectors
+  auto sync_all = [] {
+    if (kStream) __syncthreads();
+    else cluster_sync();
+  };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool leader = rank == 0 && threadIdx.x == 0;
-  grid_dep_wait();
-  grid_dep_launch();
 
   // the row's settings; a row that is left out or refused costs no loads
   float temp = a.temperature ? a.temperature[row] : 1.0f;
@@ -386,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   const bool greedy = temp == 0.0f;
   if (greedy) temp = 1.0f;
 
-  // ---- the CTA's tokens into shared memory, their largest logit -------------
+  // ---- the CTA's tokens, and their largest logit ------------------------------
   // Positions are counted from the 16-byte boundary at or below the row's
   // start, so every vector of positions is one aligned load; positions outside
   // the row hold -inf.
@@ -396,20 +455,88 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   const Te* base = start - shift;
   const int pos0 = rank * a.slice;
   const int steps = a.slice / (kWarps * kStep);  // of each warp
-  Te* mine = z_s + warp * steps * kStep + lane * 8;
-  const int my_pos = pos0 + warp * steps * kStep + lane * 8;
+  const int own = warp * steps * kStep + lane * 8;  // place of the lane's first token
+  const int my_pos = pos0 + own;
   const float minus_inf = __int_as_float(0xff800000);
-  for (int i = 0; i < steps; ++i) {
+  bool fix = false, fix_inf = false;  // streamed rows with a NaN or +inf
+  // 8 tokens from a place on, as they are
+  auto fetch = [&](int place, uint4 (&raw)[kRaw]) {
 #pragma unroll
-    for (int v = 0; v < 8 / kVec; ++v) {
-      const int q = my_pos + i * kStep + v * kVec;
-      Te* to = mine + i * kStep + v * kVec;
+    for (int v = 0; v < kRaw; ++v) {
+      if (!kStream) {
+        raw[v] = *reinterpret_cast<const uint4*>(z_s + place + v * kVec);
+        continue;
+      }
+      const int q = place + v * kVec;
       if (q >= lo && q + kVec <= hi) {
-        cp_async16(to, base + q);
+        raw[v] = __ldg(reinterpret_cast<const uint4*>(base + q));
       } else {
+        Te* e = reinterpret_cast<Te*>(&raw[v]);
 #pragma unroll
         for (int j = 0; j < kVec; ++j)
-          to[j] = q + j >= lo && q + j < hi ? base[q + j] : from_f32<Te>(minus_inf);
+          e[j] = q + j >= lo && q + j < hi ? base[q + j] : from_f32<Te>(minus_inf);
+      }
+    }
+  };
+  // as fp32, without a NaN and with finite logits above -inf
+  auto open = [&](const uint4 (&raw)[kRaw], float (&z)[8]) {
+    widen(raw, z);
+    if (kStream && fix) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        z[j] = z[j] == z[j] ? z[j] : minus_inf;
+        if (fix_inf) z[j] = z[j] == -minus_inf ? 0.0f : minus_inf;
+      }
+    }
+  };
+  auto load = [&](int place, float (&z)[8]) {
+    uint4 raw[kRaw];
+    fetch(place, raw);
+    open(raw, z);
+  };
+  // the warp's steps whose vectors all lie in the row (streamed: plain loads)
+  const int in0 = pos0 + warp * steps * kStep < lo ? 1 : 0;
+  const int in1 = min(steps, (hi - (pos0 + warp * steps * kStep)) / kStep);
+  const uint4* my_vec = reinterpret_cast<const uint4*>(base + my_pos);
+  constexpr int kStepVecs = kStep / kVec;
+  // visit(i, z, raw) for the steps from i0 to i1 - 1, `kAhead` loads in flight
+  constexpr int kAhead = kStream ? (sizeof(Te) == 2 ? 4 : 2) : 1;
+  auto each_step = [&](int i0, int i1, auto visit) {
+    for (int i = i0; i < i1; i += kAhead) {
+      uint4 raw[kAhead][kRaw];
+      if (kStream && i >= in0 && i + kAhead <= in1) {
+        const uint4* at = my_vec + i * kStepVecs;
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d)
+#pragma unroll
+          for (int v = 0; v < kRaw; ++v) raw[d][v] = __ldg(at + d * kStepVecs + v);
+      } else {
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d)
+          if (d == 0 || i + d < i1) fetch(own + (i + d) * kStep, raw[d]);
+      }
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) {
+        if (d > 0 && i + d >= i1) break;
+        float z[8];
+        open(raw[d], z);
+        visit(i + d, z, raw[d]);
+      }
+    }
+  };
+  if (!kStream) {
+    for (int i = 0; i < steps; ++i) {
+#pragma unroll
+      for (int v = 0; v < kRaw; ++v) {
+        const int q = my_pos + i * kStep + v * kVec;
+        Te* to = z_s + own + i * kStep + v * kVec;
+        if (q >= lo && q + kVec <= hi) {
+          cp_async16(to, base + q);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j)
+            to[j] = q + j >= lo && q + j < hi ? base[q + j] : from_f32<Te>(minus_inf);
+        }
       }
     }
   }
@@ -418,10 +545,40 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     s.n_list = 0;
     s.first = 0x7fffffff;
   }
-  cp_async_wait();  // a lane reads what it copied
   float lane_max = minus_inf, m = minus_inf;
+  int max_step = 0;  // the lane's first step with its largest logit
+  if (!kStream) {
+    cp_async_wait();  // a lane reads what it copied
 #pragma unroll 4
-  for (int i = 0; i < steps; ++i) lane_max = max8(lane_max, mine + i * kStep);
+    for (int i = 0; i < steps; ++i) {
+      uint4 raw[kRaw];
+      fetch(own + i * kStep, raw);
+      const float x = max8(lane_max, raw);
+      if (x > lane_max) max_step = i;
+      lane_max = x;
+    }
+  } else {
+    constexpr int kMaxAhead = 8 / kRaw;
+    for (int i = 0; i < steps; i += kMaxAhead) {
+      uint4 raw[kMaxAhead][kRaw];
+      if (i >= in0 && i + kMaxAhead <= in1) {
+        const uint4* at = my_vec + i * kStepVecs;
+#pragma unroll
+        for (int d = 0; d < kMaxAhead; ++d)
+#pragma unroll
+          for (int v = 0; v < kRaw; ++v) raw[d][v] = __ldg(at + d * kStepVecs + v);
+      } else {
+#pragma unroll
+        for (int d = 0; d < kMaxAhead; ++d) fetch(own + min(i + d, steps - 1) * kStep, raw[d]);
+      }
+#pragma unroll
+      for (int d = 0; d < kMaxAhead; ++d) {
+        const float x = max8(lane_max, raw[d]);
+        if (x > lane_max) max_step = i + d;
+        lane_max = x;
+      }
+    }
+  }
   auto block_max = [&] {
     float x = lane_max;
 #pragma unroll
@@ -434,22 +591,29 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   };
   m = block_max();
   if (m != m) {  // NaN counts as -inf
+    fix = kStream;
     lane_max = minus_inf;
-    for (int i = 0; i < steps; ++i)
+    for (int i = 0; i < steps; ++i) {
+      float z[8];
+      load(own + i * kStep, z);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float z = to_f32(mine[i * kStep + j]);
-        if (z != z) mine[i * kStep + j] = from_f32<Te>(minus_inf);
-        lane_max = fmaxf(lane_max, z);
+        if (!kStream && z[j] != z[j])
+          z_s[own + i * kStep + j] = from_f32<Te>(minus_inf);
+        if (z[j] > lane_max) {
+          lane_max = z[j];
+          max_step = i;
+        }
       }
+    }
     __syncthreads();
     m = block_max();
   }
   if (threadIdx.x == 0) s.max = m;
-  cluster_sync();
-  for (int r = 0; r < C; ++r) m = fmaxf(m, __uint_as_float(ld_peer_u32(&s.max, r)));
+  sync_all();
+  for (int r = 0; r < C; ++r) m = fmaxf(m, peer_f32<kStream>(&s.max, r));
   if (!(m > minus_inf)) {  // nothing to sample from
-    cluster_sync();
+    sync_all();
     if (leader) {
       a.tokens[row] = -1;
       a.conf[row] = 0.0f;
@@ -457,12 +621,15 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     return;
   }
   if (m > 3.4028234e38f) {  // +inf: those tokens alone, alike
-    for (int i = 0; i < steps; ++i)
+    if (!kStream) {
+      for (int i = 0; i < steps; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float z = to_f32(mine[i * kStep + j]);
-        mine[i * kStep + j] = from_f32<Te>(z == m ? 0.0f : minus_inf);
-      }
+        for (int j = 0; j < 8; ++j) {
+          Te* at = z_s + own + i * kStep + j;
+          *at = from_f32<Te>(to_f32(*at) == m ? 0.0f : minus_inf);
+        }
+    }
+    fix = fix_inf = kStream;
     if (lane_max == m) lane_max = 0.0f;
     m = 0.0f;
   }
@@ -476,6 +643,12 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
 
   // ---- one pass over the row ----------------------------------------------------
   const int segs = (steps + kSegSteps - 1) / kSegSteps;  // of each warp
+  auto set_seg = [&](int g, unsigned long long w, uint32_t ties) {  // of the warp
+    const int q = warp * segs + g;
+    s.seg_mass[q] = w;
+    s.seg_lo[q] = s.seg_hi[q] = 0;
+    s.seg_ties[q] = ties;
+  };
   const bool same_t = c == kLog2e;  // T = 1: the weights give the softmax
   float esum = 0.0f;
   uint64_t esum2 = 0;  // two partial sums
@@ -484,37 +657,70 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     upk(mul2(d, pk(kLog2e, kLog2e)), e0, e1);
     esum2 = add2(esum2, pk(ex2(e0), ex2(e1)));
   };
-  auto plain_pass = [&](auto same_c) {
-    constexpr bool kSame = decltype(same_c)::value;
+  auto plain_pass = [&](auto same_c, auto min_c) {
+    constexpr bool kSame = decltype(same_c)::value, kMin = decltype(min_c)::value;
     for (int g = 0; g < segs; ++g) {
       unsigned long long seg = 0;
-      const int i1 = min(steps, (g + 1) * kSegSteps);
-#pragma unroll 1
-      for (int i = g * kSegSteps; i < i1; ++i) {
-        float z[8];
-        load8(mine + i * kStep, z);
+      each_step(g * kSegSteps, min(steps, (g + 1) * kSegSteps), [&](int, const float (&z)[8], const uint4 (&)[kRaw]) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
           const Pair w = weigh(z[j], z[j + 1], neg_m, c);
-          add_wide(seg, w.w0 >= w_min ? w.w0 : 0u);
-          add_wide(seg, w.w1 >= w_min ? w.w1 : 0u);
+          add_wide(seg, !kMin || w.w0 >= w_min ? w.w0 : 0u);
+          add_wide(seg, !kMin || w.w1 >= w_min ? w.w1 : 0u);
           if (kSame) esum2 = add2(esum2, pk(w.v0, w.v1));
           else add_exp(w.d);
         }
-      }
+      });
       seg = warp_sum(seg);
-      if (lane == 0) {
-        s.seg_mass[warp * segs + g] = seg;
-        s.seg_ties[warp * segs + g] = 0;
+      if (lane == 0) set_seg(g, seg, 0);
+    }
+  };
+  // Tokens of a step with logits from flo to fhi (`top`: of any) into the list.
+  auto enlist = [&](bool top, float flo, float fhi, int i, const float (&z)[8],
+                    const uint4 (&raw)[kRaw]) {
+    uint32_t hits = 0;
+    if (sizeof(Te) == 2 && !fix_inf) {  // two at a time; most steps have none
+      const __nv_bfloat162 flo2 = __float2bfloat162_rn(flo), fhi2 = __float2bfloat162_rn(fhi);
+      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(raw);
+      uint32_t in[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        in[j] = __hge2_mask(h[j], flo2);
+        if (!top) in[j] &= __hle2_mask(h[j], fhi2);
+      }
+      if (in[0] | in[1] | in[2] | in[3]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          hits |= (in[j] & 1u) << (2 * j) | (in[j] >> 31) << (2 * j + 1);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        hits |= static_cast<uint32_t>(z[j] >= flo && (top || z[j] <= fhi)) << j;
+    }
+    if (hits) {
+      uint32_t at = atomicAdd(&s.n_list, static_cast<uint32_t>(__popc(hits)));
+      const int place = own + i * kStep;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (!(hits >> j & 1)) continue;
+        if (at < kList) {
+          s.list.place[at] = place + j;
+          if constexpr (kStream) s.list.z[at] = z[j];
+        }
+        ++at;
       }
     }
   };
-  auto count_pass = [&](auto same_c) {
+  const uint32_t kmax = key_of<Te>(m), kmin = key_of<Te>(minus_inf);
+  auto bin_of_key = [&](uint32_t k) {  // falls as the key rises
+    return fine_bin(__fmul_rn(__fadd_rn(key_value<Te>(k), neg_m), c));
+  };
+  bool listed_already = false;  // in the first pass (streamed, top-k of few)
+  // The counts by bins, and the softmax's sum.
+  auto count_pass = [&](auto same_c, int i0, int i1) {
     constexpr bool kSame = decltype(same_c)::value;
-#pragma unroll 2
-    for (int i = 0; i < steps; ++i) {
-      float z[8];
-      load8(mine + i * kStep, z);
+    each_step(i0, i1, [&](int, const float (&z)[8], const uint4 (&)[kRaw]) {
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
         const uint64_t d = add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m));
@@ -532,30 +738,73 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
         if (n0 < kFine) atomicAdd(&s.fine[n0], 1u);
         if (n1 < kFine) atomicAdd(&s.fine[n1], 1u);
       }
-    }
+    });
   };
   if (greedy) {
-#pragma unroll 2
-    for (int i = 0; i < steps; ++i) {
-      float z[8];
-      load8(mine + i * kStep, z);
+    each_step(0, steps, [&](int, const float (&z)[8], const uint4 (&)[kRaw]) {
 #pragma unroll
       for (int j = 0; j < 8; j += 2) add_exp(add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m)));
-    }
+    });
     if (lane_max == m) {  // the lane's first token of the largest logit
-      int first = 0x7fffffff;
-      for (int i = steps - 1; i >= 0; --i)
+      float z[8];
+      load(own + max_step * kStep, z);
+      int first = 7;
 #pragma unroll
-        for (int j = 7; j >= 0; --j)
-          if (to_f32(mine[i * kStep + j]) == m) first = my_pos + i * kStep + j;
-      atomicMin(&s.first, first);
+      for (int j = 6; j >= 0; --j)
+        if (z[j] == m) first = j;
+      atomicMin(&s.first, my_pos + max_step * kStep + first);
     }
   } else if (cut_any) {
-    if (same_t) count_pass(std::true_type());
-    else count_pass(std::false_type());
+    auto counts = [&](int i0, int i1) {
+      if (same_t) count_pass(std::true_type(), i0, i1);
+      else count_pass(std::false_type(), i0, i1);
+    };
+    if (kStream && by_k && steps >= 4 * kAhead && top_k < a.vocab / 16) {
+      // Top-k of few: the counts of a sample (the first steps of every warp)
+      // name the bins that hold three times as many tokens; these make the
+      // list, and the other steps are not counted (2048 rows of 131072, top-k
+      // 50: 313 us with counts, 249 us without).  Should the list be too short
+      // all the same, or too long, the whole row is searched.
+      counts(0, kAhead);
+      __syncthreads();
+      if (warp == 0) {
+        constexpr int kPer = kFine / 32;
+        uint32_t n = 0;
+        for (int i = 0; i < kPer; ++i) n += s.fine[lane * kPer + i];
+        uint32_t upto = warp_before(n);
+        const uint32_t want = 3u * top_k * kAhead / steps + 48;
+        uint32_t b = kFine - 1;
+        for (int i = kPer - 1; i >= 0; --i) {  // the first bin at which `want` is reached
+          if (upto + n >= want) b = lane * kPer + i;
+          n -= s.fine[lane * kPer + i];
+        }
+        b = __reduce_min_sync(0xffffffffu, b);
+        const uint32_t k = first_key(kmin, kmax, [&](uint32_t k) { return bin_of_key(k) <= b; });
+        if (lane == 0) s.klo = k;
+      }
+      __syncthreads();
+      const float flo = key_value<Te>(s.klo);
+      each_step(kAhead, steps, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) add_exp(add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m)));
+        enlist(true, flo, m, i, z, raw);
+      });
+      each_step(0, kAhead, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
+        enlist(true, flo, m, i, z, raw);
+      });
+      for (int g = lane; g < segs; g += 32) set_seg(g, 0, 0);
+      listed_already = true;
+    } else {
+      counts(0, steps);
+    }
   } else {
-    if (same_t) plain_pass(std::true_type());
-    else plain_pass(std::false_type());
+    if (w_min) {
+      if (same_t) plain_pass(std::true_type(), std::true_type());
+      else plain_pass(std::false_type(), std::true_type());
+    } else {
+      if (same_t) plain_pass(std::true_type(), std::false_type());
+      else plain_pass(std::false_type(), std::false_type());
+    }
   }
   {
     float e0, e1;
@@ -571,13 +820,13 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     for (int w = 0; w < kWarps; ++w) e += s.warp_f[w];
     s.expsum = e;
   }
-  cluster_sync();
+  sync_all();
   esum = 0.0f;
-  for (int r = 0; r < C; ++r) esum += __uint_as_float(ld_peer_u32(&s.expsum, r));
+  for (int r = 0; r < C; ++r) esum += peer_f32<kStream>(&s.expsum, r);
   if (greedy) {
     int first = 0x7fffffff;
-    for (int r = 0; r < C; ++r) first = min(first, static_cast<int>(ld_peer_u32(&s.first, r)));
-    cluster_sync();
+    for (int r = 0; r < C; ++r) first = min(first, static_cast<int>(peer_u32<kStream>(reinterpret_cast<const uint32_t*>(&s.first), r)));
+    sync_all();
     if (leader) {
       a.tokens[row] = first - shift;
       a.conf[row] = 1.0f / esum;
@@ -589,21 +838,17 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
   Cut cut{minus_inf, 0u, 0};
   int plan = kListAll;
   if (cut_any) {
-    const uint32_t kmax = key_of<Te>(m), kmin = key_of<Te>(minus_inf);
     const uint32_t want_count = static_cast<uint32_t>(max(top_k, 0));
     uint32_t reach_lo = 0, reach_hi = 0, reach_count = 0;  // keys, and the tokens above
     auto keys_of_bins = [&](uint32_t b_hi, uint32_t b_lo) {
       // bins fall as logits rise; one warp finds either end
-      auto bin_at = [&](uint32_t k) {
-        return fine_bin(__fmul_rn(__fadd_rn(key_value<Te>(k), neg_m), c));
-      };
       if (warp == 0) {
-        const uint32_t k = first_key(kmin, kmax, [&](uint32_t k) { return bin_at(k) <= b_lo; });
+        const uint32_t k = first_key(kmin, kmax, [&](uint32_t k) { return bin_of_key(k) <= b_lo; });
         if (lane == 0) s.klo = k;
       } else if (warp == 1) {
         const uint32_t k =
             b_hi == 0 ? kmax + 1
-                      : first_key(kmin, kmax, [&](uint32_t k) { return bin_at(k) < b_hi; });
+                      : first_key(kmin, kmax, [&](uint32_t k) { return bin_of_key(k) < b_hi; });
         if (lane == 0) s.khi = k - 1;
       }
       __syncthreads();
@@ -611,18 +856,34 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       reach_hi = s.khi;
     };
 
-    {  // ---- the bins that the cut can lie in --------------------------------------
-      uint32_t n[4] = {};
+    if (listed_already) {
+      reach_lo = s.klo;
+      reach_hi = kmax;
+      if (s.n_list > kList || s.n_list < want_count) plan = kWhole;
+      __syncthreads();
+    } else {  // ---- the bins that the cut can lie in -----------------------------
+      constexpr int kPer = kFine / kThreads;  // bins of a thread
+      const int bin0 = threadIdx.x * kPer;
+      uint32_t n[kPer] = {};
       for (int r = 0; r < C; ++r) {
-        const uint4 v = ld_peer4(&s.fine[threadIdx.x * 4], r);
-        n[0] += v.x; n[1] += v.y; n[2] += v.z; n[3] += v.w;
-      }
-      float w[4];  // the bins' middle weights, relative
-      w[0] = exp2f(static_cast<float>(threadIdx.x) * (-4.0f / 32));
+        if constexpr (kPer == 4) {
+          const uint4 v = peer_u32x4<kStream>(&s.fine[bin0], r);
+          n[0] += v.x; n[1] += v.y; n[2] += v.z; n[3] += v.w;
+        } else {
 #pragma unroll
-      for (int i = 1; i < 4; ++i) w[i] = w[i - 1] * 0.97857206208770013f;  // 2^(-1/32)
-      const uint32_t own_n = n[0] + n[1] + n[2] + n[3];
-      const float own_m = n[0] * w[0] + n[1] * w[1] + n[2] * w[2] + n[3] * w[3];
+          for (int i = 0; i < kPer; ++i) n[i] = s.fine[bin0 + i];
+        }
+      }
+      float w[kPer];  // the bins' middle weights, relative
+      w[0] = exp2f(static_cast<float>(threadIdx.x) * (-kPer / 32.0f));
+      uint32_t own_n = n[0];
+      float own_m = n[0] * w[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) {
+        w[i] = w[i - 1] * 0.97857206208770013f;  // 2^(-1/32)
+        own_n += n[i];
+        own_m += n[i] * w[i];
+      }
       uint32_t cnt = warp_before(own_n);
       float est = warp_before(own_m);
       if (lane == 31) {
@@ -649,11 +910,11 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       uint32_t c0 = cnt;
       float e0 = est;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kPer; ++i) {
         c0 += n[i];
         e0 += n[i] * w[i];
         if (n[i] == 0) continue;
-        const int b = threadIdx.x * 4 + i;
+        const int b = bin0 + i;
         if (by_k) {
           if (c0 >= want_count && c0 - n[i] < want_count) s.bin[0] = s.bin[1] = b;
         } else {
@@ -668,8 +929,8 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       __syncthreads();
       c0 = cnt;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int b = threadIdx.x * 4 + i;
+      for (int i = 0; i < kPer; ++i) {
+        const int b = bin0 + i;
         if (b == s.bin[0]) s.at[0] = c0;
         if (b == s.bin[2]) s.at[2] = c0;
         c0 += n[i];
@@ -701,23 +962,21 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
 
     // weights of all tokens, of those above `from` that min-p keeps by segments,
     // and of the others above; visit(i, z) for every step
-    auto weigh_pass = [&](float from, auto visit, unsigned long long* all_out,
+    auto weigh_pass = [&](auto min_c, float from, auto visit, unsigned long long* all_out,
                           unsigned long long* above_out) {
+      constexpr bool kMin = decltype(min_c)::value;
       unsigned long long all = 0, above = 0;
       for (int g = 0; g < segs; ++g) {
         unsigned long long seg = 0;
-        const int i1 = min(steps, (g + 1) * kSegSteps);
-#pragma unroll 1
-        for (int i = g * kSegSteps; i < i1; ++i) {
-          float z[8];
-          load8(mine + i * kStep, z);
+        each_step(g * kSegSteps, min(steps, (g + 1) * kSegSteps), [&](int i, const float (&z)[8],
+                                                                  const uint4 (&raw)[kRaw]) {
 #pragma unroll
           for (int j = 0; j < 8; j += 2) {
             const Pair w = weigh(z[j], z[j + 1], neg_m, c);
             const uint32_t w0 = z[j] > from ? w.w0 : 0u, w1 = z[j + 1] > from ? w.w1 : 0u;
             add_wide(all, w.w0);
             add_wide(all, w.w1);
-            if (w_min) {  // segments: what min-p keeps; above: the rest
+            if (kMin) {  // segments: what min-p keeps; above: the rest
               add_wide(seg, w0 >= w_min ? w0 : 0u);
               add_wide(seg, w1 >= w_min ? w1 : 0u);
               add_wide(above, w0 >= w_min ? 0u : w0);
@@ -727,14 +986,11 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
               add_wide(seg, w1);
             }
           }
-          visit(i, z);
-        }
+          visit(i, z, raw);
+        });
         above += seg;
         seg = warp_sum(seg);
-        if (lane == 0) {
-          s.seg_mass[warp * segs + g] = seg;
-          s.seg_ties[warp * segs + g] = 0;
-        }
+        if (lane == 0) set_seg(g, seg, 0);
       }
       all = warp_sum(all);
       above = warp_sum(above);
@@ -755,48 +1011,35 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     };
 
     unsigned long long total = 0, above_mass = 0;
-    if (plan != kWhole) {
+    if (plan != kWhole && !listed_already) {
       // ---- the tokens in reach of the cut, and the weights above them ---------
       const float flo = key_value<Te>(reach_lo), fhi = key_value<Te>(reach_hi);
-      auto put = [&](int i, const float (&z)[8]) {
-        uint32_t hits = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          hits |= static_cast<uint32_t>(z[j] >= flo && z[j] <= fhi) << j;
-        if (hits) {
-          uint32_t at = atomicAdd(&s.n_list, static_cast<uint32_t>(__popc(hits)));
-          const int place = warp * steps * kStep + i * kStep + lane * 8;
-          for (; hits; hits &= hits - 1, ++at)
-            if (at < kList) s.list[at] = static_cast<uint16_t>(place + __ffs(hits) - 1);
-        }
+      auto put = [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
+        enlist(plan == kListAll, flo, fhi, i, z, raw);
       };
       if (plan == kListAll && by_k) {  // no weight but the listed ones counts
-#pragma unroll 2
-        for (int i = 0; i < steps; ++i) {
-          if (max8(minus_inf, mine + i * kStep) < flo) continue;
-          float z[8];
-          load8(mine + i * kStep, z);
-          put(i, z);
-        }
-        for (int g = lane; g < segs; g += 32) {
-          s.seg_mass[warp * segs + g] = 0;
-          s.seg_ties[warp * segs + g] = 0;
-        }
+        if (lane_max >= flo) each_step(0, steps, put);
+        for (int g = lane; g < segs; g += 32) set_seg(g, 0, 0);
       } else {
-        weigh_pass(fhi, put, &s.mass, &s.reach_mass);
+        if (w_min) weigh_pass(std::true_type(), fhi, put, &s.mass, &s.reach_mass);
+        else weigh_pass(std::false_type(), fhi, put, &s.mass, &s.reach_mass);
       }
-      cluster_sync();
+      sync_all();
       const bool weighed = plan == kListReach || !by_k;
       for (int r = 0; r < C; ++r) {
-        if (ld_peer_u32(&s.n_list, r) > kList) plan = kWhole;
+        if (peer_u32<kStream>(&s.n_list, r) > kList) plan = kWhole;
         if (weighed) {
-          total += ld_peer_u64(&s.mass, r);
-          above_mass += ld_peer_u64(&s.reach_mass, r);
+          total += peer_u64<kStream>(&s.mass, r);
+          above_mass += peer_u64<kStream>(&s.reach_mass, r);
         }
       }
     }
 
     // The search; false: the cut is not in the list.
+    auto listed = [&](int i) {
+      if constexpr (kStream) return s.list.z[i];
+      else return to_f32(z_s[s.list.place[i]]);
+    };
     auto search = [&]() {
       cut.mass = total;
       for (int which = 0; which < 2; ++which) {
@@ -818,7 +1061,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
           const uint32_t width = khi - klo;  // one less than the keys
           const int sh = max(0, 25 - __clz(width));
           // the cluster has read this histogram's last contents
-          cluster_sync();
+          sync_all();
           for (int i = threadIdx.x; i < static_cast<int>(sizeof(Hist) / 4); i += kThreads)
             reinterpret_cast<uint32_t*>(&s.hist)[i] = 0u;
           __syncthreads();
@@ -827,26 +1070,25 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
             if (k - klo > width) return;
             const uint32_t b = (khi - k) >> sh, w = weight_of(z, neg_m, c);
             atomicAdd(&s.hist.count[b], 1u);
-            atomicAdd(&s.hist.lo[b], w & 0xffffu);
-            atomicAdd(&s.hist.hi[b], w >> 16);
+            atomicAdd(&s.hist.m0[b], w & 0x7ffu);
+            atomicAdd(&s.hist.m1[b], w >> 11 & 0x7ffu);
+            atomicAdd(&s.hist.m2[b], w >> 22);
           };
           if (plan == kWhole) {
             const float flo = key_value<Te>(klo), fhi = key_value<Te>(khi);
-            for (int i = 0; i < steps; ++i) {
-              float z[8];
-              load8(mine + i * kStep, z);
+            each_step(0, steps, [&](int, const float (&z)[8], const uint4 (&)[kRaw]) {
 #pragma unroll
               for (int j = 0; j < 8; ++j)
                 if (z[j] >= flo && z[j] <= fhi) count_in(z[j]);
-            }
+            });
           } else {
             const int n = static_cast<int>(s.n_list);
-            for (int i = threadIdx.x; i < n; i += kThreads) count_in(to_f32(z_s[s.list[i]]));
+            for (int i = threadIdx.x; i < n; i += kThreads) count_in(listed(i));
           }
-          cluster_sync();
+          sync_all();
           counted = true;
           if (warp == 0) {
-            const int b = find_bin(s, C, count_rule, want, s.above_mass, s.above_count);
+            const int b = find_bin<kStream>(s, C, count_rule, want, s.above_mass, s.above_count);
             if (lane == 0) {
               const uint32_t top = khi - (static_cast<uint32_t>(b < 0 ? 0 : b) << sh);
               s.khi = top;
@@ -881,10 +1123,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       // ---- the same over every token ----------------------------------------------
       plan = kWhole;
       if (by_p) {
-        weigh_pass(m, [](int, const float (&)[8]) {}, &s.whole_mass, nullptr);
-        cluster_sync();
+        weigh_pass(std::false_type(), m, [](int, const float (&)[8], const uint4 (&)[kRaw]) {}, &s.whole_mass, nullptr);
+        sync_all();
         total = 0;
-        for (int r = 0; r < C; ++r) total += ld_peer_u64(&s.whole_mass, r);
+        for (int r = 0; r < C; ++r) total += peer_u64<kStream>(&s.whole_mass, r);
       }
       above_mass = 0;
       reach_count = 0;
@@ -907,12 +1149,17 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     if (plan != kWhole) {
       const int n = static_cast<int>(s.n_list);
       for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int place = s.list[i], at = place / (steps * kStep);
+        const int place = s.list.place[i], at = place / (steps * kStep);
         const int q = at * segs + (place - at * steps * kStep) / (kSegSteps * kStep);
-        const float z = to_f32(z_s[place]);
+        float z;
+        if constexpr (kStream) z = s.list.z[i];
+        else z = to_f32(z_s[place]);
         if (z > cut.value) {
           const uint32_t w = weight_of(z, neg_m, c);
-          if (w >= w_min) atomicAdd(&s.seg_mass[q], static_cast<unsigned long long>(w));
+          if (w >= w_min) {
+            atomicAdd(&s.seg_lo[q], w & 0xffffu);
+            atomicAdd(&s.seg_hi[q], w >> 16);
+          }
         } else if (z == cut.value) {
           atomicAdd(&s.seg_ties[q], 1u);
         }
@@ -921,11 +1168,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       for (int g = 0; g < segs; ++g) {
         unsigned long long seg = 0;
         uint32_t ties = 0;
-        const int i1 = min(steps, (g + 1) * kSegSteps);
-#pragma unroll 1
-        for (int i = g * kSegSteps; i < i1; ++i) {
-          float z[8];
-          load8(mine + i * kStep, z);
+        each_step(g * kSegSteps, min(steps, (g + 1) * kSegSteps), [&](int, const float (&z)[8], const uint4 (&)[kRaw]) {
 #pragma unroll
           for (int j = 0; j < 8; j += 2) {
             const Pair p = weigh(z[j], z[j + 1], neg_m, c);
@@ -933,17 +1176,14 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
             add_wide(seg, z[j + 1] > cut.value && p.w1 >= w_min ? p.w1 : 0u);
             ties += (cut_used && z[j] == cut.value) + (cut_used && z[j + 1] == cut.value);
           }
-        }
+        });
         seg = warp_sum(seg);
         ties = __reduce_add_sync(0xffffffffu, ties);
-        if (lane == 0) {
-          s.seg_mass[warp * segs + g] = seg;
-          s.seg_ties[warp * segs + g] = ties;
-        }
+        if (lane == 0) set_seg(g, seg, ties);
       }
     }
   }
-  cluster_sync();
+  if (cut_any) sync_all();
 
   // ---- the segment that u falls in, then the token -----------------------------
   if (warp == 0) {
@@ -953,8 +1193,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       ties = 0;
       if (q >= all) return 0ull;
       const int r = q / per_cta, l = q - r * per_cta;
-      ties = ld_peer_u32(&s.seg_ties[l], r);
-      return ld_peer_u64(&s.seg_mass[l], r);
+      ties = peer_u32<kStream>(&s.seg_ties[l], r);
+      return peer_u64<kStream>(&s.seg_mass[l], r) + peer_u32<kStream>(&s.seg_lo[l], r) +
+             (static_cast<unsigned long long>(peer_u32<kStream>(&s.seg_hi[l], r)) << 16);
     };
     // kept mass given the tokens equal to the cut before
     auto with_ties = [&](unsigned long long above, uint32_t before, uint32_t ties) {
@@ -988,13 +1229,19 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
     run = __shfl_sync(0xffffffffu, upto - kept, f);
     run_ties = __shfl_sync(0xffffffffu, before, f);
     const int found = min(q + f, all - 1);
+    if (!kStream) cluster_arrive();  // the rest reads this CTA's memory alone
     if (found / per_cta == rank) {
       const int l = found % per_cta, w0 = l / segs, g = l % segs;
-      const int i1 = min(steps, (g + 1) * kSegSteps);
-      for (int i = g * kSegSteps; i < i1; ++i) {
-        const int off = (w0 * steps + i) * kStep + lane * 8;
+      uint4 raw[kSegSteps][kRaw];
+#pragma unroll
+      for (int i = 0; i < kSegSteps; ++i)
+        fetch((w0 * steps + min(g * kSegSteps + i, steps - 1)) * kStep + lane * 8, raw[i]);
+#pragma unroll
+      for (int i = 0; i < kSegSteps; ++i) {
+        if (g * kSegSteps + i >= steps) break;
+        const int off = (w0 * steps + g * kSegSteps + i) * kStep + lane * 8;
         float z[8];
-        load8(z_s + off, z);
+        open(raw[i], z);
         uint32_t w[8];
         ties = 0;
 #pragma unroll
@@ -1038,29 +1285,32 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Args a) {
       }
     }
   }
-  cluster_sync();  // no CTA leaves while its sums are read
+  if (!kStream) {
+    if (warp != 0) cluster_arrive();
+    cluster_wait();  // no CTA leaves while its sums are read
+  }
 }
 
-template <typename Te>
-cudaError_t launch_typed(Args a, int rows, int num_sms, cudaStream_t stream) {
-  auto kernel = sample_kernel<Te>;
-  constexpr size_t kHead = (sizeof(Shared) + 15) / 16 * 16;
-  constexpr int kGrain = kWarps * kStep;
-  // positions that may precede a row in its first 16 bytes
-  const bool whole = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
-                     (rows == 1 || a.ld * static_cast<int64_t>(sizeof(Te)) % 16 == 0);
-  const int lead = whole ? 0 : 16 / static_cast<int>(sizeof(Te)) - 1;
-  auto slice_of = [&](int C) {
-    const int per = (a.vocab + lead + C - 1) / C;
-    return (per + kGrain - 1) / kGrain * kGrain;
-  };
-  // CTAs a row: slices of at most 64 KB, three to an SM; more for few rows,
-  // as long as each has a whole step for every warp
-  int C = 1;
-  while (C < 8 && slice_of(C) * sizeof(Te) > 64 * 1024) C *= 2;
-  while (C < 8 && static_cast<int64_t>(rows) * C * 2 <= num_sms && slice_of(C) > kGrain) C *= 2;
-  a.slice = slice_of(C);
-  const size_t smem = kHead + a.slice * sizeof(Te);
+template <typename Te, bool kStream>
+__global__ void __launch_bounds__(Shape<kStream>::kThreads, Shape<kStream>::kCtas)
+    sample_kernel(const Args a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared<kStream>& s = *reinterpret_cast<Shared<kStream>*>(smem);
+  Te* z_s = reinterpret_cast<Te*>(smem + (sizeof(s) + 15) / 16 * 16);  // a cluster's slice
+  grid_dep_wait();
+  grid_dep_launch();
+  if constexpr (!kStream) {
+    const int C = cluster_size();
+    sample_row<Te, false>(a, s, z_s, C, cluster_rank(), blockIdx.x / C);
+  } else {
+    sample_row<Te, true>(a, s, z_s, 1, 0, blockIdx.x);
+  }
+}
+
+template <typename Te, bool kStream>
+cudaError_t launch_shape(const Args& a, int rows, int C, cudaStream_t stream) {
+  auto kernel = sample_kernel<Te, kStream>;
+  const size_t smem = (sizeof(Shared<kStream>) + 15) / 16 * 16 + (kStream ? 0 : a.slice * sizeof(Te));
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(smem));
   if (e != cudaSuccess) return e;
@@ -1071,12 +1321,41 @@ cudaError_t launch_typed(Args a, int rows, int num_sms, cudaStream_t stream) {
   attr[1].val.clusterDim = {static_cast<unsigned>(C), 1, 1};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(rows) * C);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Shape<kStream>::kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = C > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename Te>
+cudaError_t launch_typed(Args a, int rows, int num_sms, cudaStream_t stream) {
+  // positions that may precede a row in its first 16 bytes
+  const bool whole = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
+                     (rows == 1 || a.ld * static_cast<int64_t>(sizeof(Te)) % 16 == 0);
+  const int lead = whole ? 0 : 16 / static_cast<int>(sizeof(Te)) - 1;
+  auto slice_of = [&](int C, int grain) {
+    const int per = (a.vocab + lead + C - 1) / C;
+    return (per + grain - 1) / grain * grain;
+  };
+  constexpr int kGrain = Shape<false>::kWarps * kStep;
+  // CTAs a row: slices of at most 56 KB (three CTAs an SM), or what eight CTAs
+  // give; more for few rows, as long as each has a step for every warp
+  int C = 1;
+  while (C < 8 && slice_of(C, kGrain) * sizeof(Te) > 56 * 1024) ++C;
+  // A row that no CTA holds is streamed as soon as the rows fill half of the SMs
+  // (rows of 131072 bf16 logits, cluster / stream in us, plain, top-k 50, top-p
+  // 0.9: 32 rows 17, 25, 37 / 23, 29, 66; 76 rows 25, 45, 70 / 23, 29, 66; 304
+  // rows 64, 112, 176 / 33, 42, 93).
+  if (C > 1 && 2 * static_cast<int64_t>(rows) >= num_sms) {
+    a.slice = slice_of(1, Shape<true>::kWarps * kStep);
+    return launch_shape<Te, true>(a, rows, 1, stream);
+  }
+  while (C < 8 && static_cast<int64_t>(rows) * C * 2 <= num_sms && slice_of(C, kGrain) > kGrain)
+    C = std::min(8, C * 2);
+  a.slice = slice_of(C, kGrain);
+  return launch_shape<Te, false>(a, rows, C, stream);
 }
 
 }  // namespace

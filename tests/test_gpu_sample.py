@@ -221,6 +221,42 @@ def test_a_row_is_the_same_in_any_batch(dtype):
         assert int(one[0]) == int(many[r])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab,extra", [(60000, 8), (60001, 0), (33333, 3)])
+def test_many_long_rows(dtype, vocab, extra):
+    """Enough rows that a CTA walks each in global memory: every kind of row and filter."""
+    rows = 90
+    flat = torch.full((rows, vocab + extra), 1e9, dtype=dtype, device="cuda")
+    z = flat[:, :vocab]
+    z.copy_(logits_of(vocab, rows, vocab, dtype))
+    inf = float("inf")
+    z[3] = -inf
+    z[4] = float("nan")
+    z[5, ::3] = float("nan")
+    z[6, vocab - 1] = inf
+    z[6, 9] = inf
+    z[6, 10] = float("nan")
+    z[7] = 0.25
+    z[8] = torch.finfo(dtype).min
+    z[9, : vocab - 5] = -inf
+    z[10] = (torch.arange(vocab, device="cuda") % 7).to(dtype)
+    z[11] = (torch.linspace(0, 20, vocab, device="cuda")).to(dtype)
+    z[12, 100] = 60.0
+    g = np.random.default_rng(vocab)
+    u = uniforms(vocab, rows)
+    masked = (g.random(rows) < 0.7).astype(np.uint8)
+    T = g.choice([0.0, 0.5, 1.0, 1.4], rows).astype(F)
+    k = g.choice([0, 1, 60, 2500, 20000, 59999], rows)
+    p = g.choice([0.2, 0.9, 0.97, 0.9999, 1.0], rows).astype(F)
+    min_p = g.choice([0.0, 0.0, 0.03, 0.5], rows).astype(F)
+    check(z, u)
+    check(z, u, T=T, masked=masked)
+    check(z, u, k=k)
+    check(z, u, p=p, T=T)
+    check(z, u, min_p=min_p, p=p)
+    check(z, u, T=T, k=k, p=p, min_p=min_p)
+
+
 @pytest.mark.parametrize("T,p", [(1.0, 1.0), (0.7, 1.0), (1.3, 0.8)])
 def test_frequencies(T, p):
     """Evenly spaced uniforms give each token its share to within one draw."""
