@@ -13,7 +13,9 @@
 //
 // Bound: HBM (2 or 4 bytes in, 1 out per element).  16 lanes hold a group in
 // registers (8 consecutive elements each, one 16-byte vector in bf16), so one
-// pass over the data serves the maximum and the conversion.
+// pass over the data serves the maximum and the conversion.  32768 x 2048 bf16:
+// 35 us, 86 % of the measured copy rate; 83 us with the division in every lane and
+// one pair of groups in flight.  32 x 2048: 3.4 us, one launch.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
@@ -59,12 +61,72 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int64_t c, int64_t col
   }
 }
 
+// 8 elements as loaded, their largest magnitude as fp32 bits, and their values.
+template <typename Te>
+struct Raw8;
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* row, int c, int cols, bool vec) {
+    if (vec && c + 8 <= cols) {
+      a = __ldcs(reinterpret_cast<const float4*>(row + c));
+      b = __ldcs(reinterpret_cast<const float4*>(row + c) + 1);
+    } else {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = c + i < cols ? row[c + i] : 0.f;
+      a = make_float4(f[0], f[1], f[2], f[3]);
+      b = make_float4(f[4], f[5], f[6], f[7]);
+    }
+  }
+  __device__ __forceinline__ uint32_t amax() const {
+    const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    return amax_bits(f);
+  }
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* row, int c, int cols, bool vec) {
+    if (vec && c + 8 <= cols) {
+      v = __ldcs(reinterpret_cast<const uint4*>(row + c));
+    } else {
+      uint32_t e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        e[i] = c + i < cols ? reinterpret_cast<const uint16_t*>(row)[c + i] : 0u;
+      v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
+  }
+  __device__ __forceinline__ uint32_t amax() const {
+    // magnitudes without their signs order as 16-bit integers, a NaN last
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu),
+                                __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    return max(m << 16, m & 0xffff0000u);
+  }
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
+
+// A warp takes kUnits pairs of groups (256 columns each) of a row at a time:
+// their loads in flight together, then a lane per group divides for the 16 that
+// hold it.
 template <typename Te>
 __global__ void __launch_bounds__(kThreads)
-    quantize_rows_kernel(const Te* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
+    quantize_rows_kernel(const Te* __restrict__ x, int64_t rows, int cols, int64_t ldx,
                          uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scales,
-                         int64_t scale_row_bytes, int vec_x, int vec_c, ZeroWords zero,
-                         const int32_t* __restrict__ k, int64_t n_k, int k_most,
+                         int64_t scale_row_bytes, int vec_x, int vec_c, uint32_t chunks,
+                         ZeroWords zero, const int32_t* __restrict__ k, int64_t n_k, int k_most,
                          uint32_t* err) {
   grid_dep_wait();
   grid_dep_launch();
@@ -78,38 +140,40 @@ __global__ void __launch_bounds__(kThreads)
     }
   }
   const int lane = threadIdx.x & 31;
-  const int64_t per_row = (cols + 255) / 256, units = rows * per_row;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
-  const int64_t w0 = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-  for (int64_t u0 = w0 * kUnits; u0 < units; u0 += warps * kUnits) {
-    float f[kUnits][8];
-    int64_t r[kUnits], c[kUnits];
-    r[0] = u0 / per_row;
-    c[0] = u0 - r[0] * per_row;
+  const int64_t units = rows * chunks;  // chunks of 1024 columns
+  const int64_t step = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+       u < units; u += step) {
+    const int64_t r = chunks == 1 ? u : units <= 0xffffffffll
+                                            ? static_cast<uint32_t>(u) / chunks : u / chunks;
+    const int c0 = static_cast<int>(u - r * chunks) * (256 * kUnits) + lane * 8;
+    const Te* row = x + r * ldx;
+    Raw8<Te> raw[kUnits];
 #pragma unroll
-    for (int i = 1; i < kUnits; ++i) {
-      const bool wrap = c[i - 1] + 1 == per_row;
-      r[i] = r[i - 1] + (wrap ? 1 : 0);
-      c[i] = wrap ? 0 : c[i - 1] + 1;
-    }
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      c[i] = c[i] * 256 + lane * 8;
-      if (r[i] < rows) {
-        load_elems(x + r[i] * ldx, c[i], cols, vec_x != 0, f[i]);
-      }
-    }
+    for (int i = 0; i < kUnits; ++i)
+      if (i == 0 || c0 - lane * 8 + i * 256 < cols) raw[i].load(row, c0 + i * 256, cols, vec_x != 0);
+    // the magnitude of group g (= 2 i + half) ends up in lane g
+    uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      if (r[i] >= rows) break;
-      uint32_t m = amax_bits(f[i]);
+      uint32_t m = 0;
+      if (i == 0 || c0 - lane * 8 + i * 256 < cols) m = raw[i].amax();
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float a = fp8_amax(m);
-      store_codes(codes + r[i] * ldc, c[i], cols, vec_c != 0, f[i], fp8_inverse(a));
-      if ((lane & 15) == 0 && c[i] < cols)
-        *reinterpret_cast<float*>(scales + r[i] * scale_row_bytes + (c[i] >> 7) * 4) =
-            __fdiv_rn(a, kE4m3Max);
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, m, 16);
+      if ((lane >> 1) == i) mine = (lane & 1) == (lane >> 4) ? m : other;
+    }
+    const float a = fp8_amax(mine), inv = fp8_inverse(a);
+    const int group = (c0 - lane * 8) / 128 + lane;
+    if (lane < 2 * kUnits && group * 128 < cols)
+      *reinterpret_cast<float*>(scales + r * scale_row_bytes + group * 4) = __fdiv_rn(a, kE4m3Max);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const float by = __shfl_sync(0xffffffffu, inv, 2 * i + (lane >> 4));
+      if (i > 0 && c0 - lane * 8 + i * 256 >= cols) break;
+      float f[8];
+      raw[i].widen(f);
+      store_codes(codes + r * ldc, c0 + i * 256, cols, vec_c != 0, f, by);
     }
   }
 }
@@ -157,16 +221,15 @@ bool aligned_rows(const Te* x, int64_t ld) {
 
 template <typename Te>
 cudaError_t rows_typed(const Te* x, const Fp8Rows& q, int num_sms, cudaStream_t stream) {
-  const int64_t units = q.rows * ((q.cols + 255) / 256);
-  int64_t grid = (units + 8 * kUnits - 1) / (8 * kUnits);
-  // short inputs spread over the SMs, one unit a warp, no matter the unroll
-  if (grid < num_sms) grid = std::min<int64_t>(num_sms, (units + 7) / 8);
-  grid = std::max<int64_t>(1, std::min<int64_t>(grid, 8 * num_sms));
-  return launch_pdl(quantize_rows_kernel<Te>, dim3(static_cast<unsigned>(grid)), dim3(kThreads),
-                    0, stream, x, q.rows, q.cols, q.ldx, q.codes, q.ldc, q.scales,
-                    q.scale_row_bytes, static_cast<int>(aligned_rows(x, q.ldx)),
-                    static_cast<int>(aligned_rows(q.codes, q.ldc)), q.zero, q.k, q.n_k, q.k_most,
-                    q.err);
+  const int64_t chunks = (q.cols + 256 * kUnits - 1) / (256 * kUnits);
+  const int64_t grid = (q.rows * chunks + kThreads / 32 - 1) / (kThreads / 32);
+  return launch_pdl(quantize_rows_kernel<Te>,
+                    dim3(static_cast<unsigned>(std::min<int64_t>(grid, 16 * num_sms))),
+                    dim3(kThreads), 0, stream, x, q.rows, static_cast<int>(q.cols), q.ldx,
+                    q.codes, q.ldc, q.scales, q.scale_row_bytes,
+                    static_cast<int>(aligned_rows(x, q.ldx)),
+                    static_cast<int>(aligned_rows(q.codes, q.ldc)),
+                    static_cast<uint32_t>(chunks), q.zero, q.k, q.n_k, q.k_most, q.err);
 }
 
 template <typename Te>
