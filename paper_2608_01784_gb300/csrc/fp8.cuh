@@ -57,6 +57,23 @@ cudaError_t launch_quantize_blocks(int dtype, const void* x, int64_t rows, int64
                                    int64_t ldx, uint8_t* codes, int64_t ldc, float* scales,
                                    int64_t lds, cudaStream_t stream);
 
+// The dense layer for up to four rows of x, in one launch (fp8_gemv.cu).
+struct Fp8LinearRows {
+  int64_t ldx;
+  const uint8_t* w;
+  int64_t ldw;
+  const float* w_scales;
+  int64_t ldws;
+  int M, N, K;
+  int out_f32;
+  void* out;
+  int64_t ldo;
+  ZeroWords zero;
+};
+bool linear_rows_fit(int M, int N, int K);
+cudaError_t launch_linear_rows(int dtype, const void* x, const Fp8LinearRows& p, int num_sms,
+                               cudaStream_t stream);
+
 // A row of codes with its scales behind it, in one piece that a row copy of
 // 16-byte vectors moves: codes [cols], scales from the next multiple of 4.
 inline int64_t fp8_scale_offset(int64_t cols) { return (cols + 3) / 4 * 4; }
@@ -80,7 +97,7 @@ struct Fp8GemmArgs {
   void* out;
   int64_t ldo;       // elements; SwiGLU: bytes of a packed row
   int out_f32;       // fp32 out (dense only), else bf16
-  int splits;        // CTAs of a cluster that share a tile's K: 1, 2, 4 or 8
+  int splits = 1;    // CTAs of a cluster that share a tile's K: 1, 2, 4 or 8 (dense only)
   uint32_t* err;
   int num_sms;
 };

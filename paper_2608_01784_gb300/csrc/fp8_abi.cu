@@ -20,6 +20,7 @@ using rx::WsHeader;
 constexpr size_t kAlign = 256;
 size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 int64_t blocks(int64_t n) { return (n + 127) / 128; }
+int64_t blocks2(int64_t n) { return (n + 255) / 256; }
 
 #define RX_CUDA(x)                                  \
   do {                                              \
@@ -47,11 +48,17 @@ bool code_map(CUtensorMap* m, const void* base, int64_t groups, int64_t rows, in
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// CTAs that share a tile's K: as many as the SMs leave free, each with two
-// blocks of K at least.
-int pick_splits(int64_t tiles, int64_t nkb, int sms) {
+// CTAs of a cluster that share a tile's K, where the tiles leave SMs free.  Adding
+// the parts costs 2 to 3 us for each 32 rows, a block of K 0.5 us, so taller
+// tiles are split at a long K only (N x K, one CTA a tile | split, us):
+//   M =   8, 4096 x 2048: 13 | 12 by 4, 20 by 8;   1024 x 8192: 34 | 18 by 4, 14 by 8
+//   M = 128, 4096 x 2048: 19 | 24 by 4, 45 by 8;   1024 x 8192: 41 | 29 by 8
+// Clusters of eight find room at once in half of the SMs only: more wait for a
+// second round, the 20 and 45 above.
+int pick_splits(int64_t M, int64_t tiles, int64_t nkb, int sms) {
+  if (M > 32 && nkb < 64) return 1;
   int s = 1;
-  while (s < 8 && tiles * s * 2 <= sms && nkb >= 4 * s) s *= 2;
+  while (s < 8 && nkb >= 4 * s && tiles * s * 2 <= (s < 4 ? sms : sms / 2)) s *= 2;
   return s;
 }
 
@@ -79,13 +86,18 @@ int matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t a_sca
   g.out = out;
   g.ldo = ldo;
   g.out_f32 = out_dtype == REFLEX_DTYPE_F32;
-  g.splits = pick_splits(blocks(M) * ((N + 255) / 256), blocks(K), sms);
+  g.splits = pick_splits(M, blocks(M) * blocks2(N), blocks(K), sms);
   g.err = err;
   g.num_sms = sms;
   RX_CUDA(rx::launch_fp8_matmul(g, s));
   return REFLEX_OK;
 }
 
+// Sizes that the kernels' 32-bit counts of tiles and columns hold.
+bool product_fits(int64_t M, int64_t N, int64_t K) {
+  constexpr int64_t most = int64_t{1} << 30;
+  return M <= most && N <= most && K <= most && blocks(M) * blocks2(N) <= most;
+}
 // Rows, columns and strides of a product that the kernels and maps can take.
 bool product_ok(int64_t M, int64_t N, int64_t K, int64_t ldb, int64_t ldbs, int32_t out_dtype,
                 int64_t ldo) {
@@ -155,6 +167,7 @@ int reflex_quantize_fp8(int32_t dtype, const void* x, int64_t rows, int64_t cols
   if (!dtype_ok(dtype) || rows < 0 || cols < 0 || (block_rows != 1 && block_rows != 128))
     return REFLEX_EINVAL;
   if (rows == 0 || cols == 0) return REFLEX_OK;
+  if (cols > (1 << 30)) return REFLEX_EUNSUPPORTED;
   if (x == nullptr || codes == nullptr || scales == nullptr || ldx < cols || ldc < cols ||
       lds < blocks(cols))
     return REFLEX_EINVAL;
@@ -175,6 +188,7 @@ int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int6
                       int32_t M, int32_t N, int32_t K, int32_t out_dtype, void* out, int64_t ldo,
                       int32_t* dev_status, void* stream) {
   if (!product_ok(M, N, K, ldb, ldbs, out_dtype, ldo)) return REFLEX_EINVAL;
+  if (!product_fits(M, N, K)) return REFLEX_EUNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));
   if (M == 0) return REFLEX_OK;
@@ -199,6 +213,7 @@ int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* 
                       size_t ws_bytes, void* stream) {
   if (!dtype_ok(dtype) || !product_ok(M, N, K, ldw, ldws, out_dtype, ldo) || ldx < K)
     return REFLEX_EINVAL;
+  if (!product_fits(M, N, K)) return REFLEX_EUNSUPPORTED;
   const LinearLayout L = linear_layout(M, K);
   if (workspace == nullptr || ws_bytes < L.total || !aligned(workspace, kAlign))
     return REFLEX_EWORKSPACE;
@@ -213,12 +228,19 @@ int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* 
   if (!aligned(x, dtype == REFLEX_DTYPE_F32 ? 4 : 2) || !aligned(w, 16) ||
       !aligned(w_scales, 4) || !aligned(out, out_dtype == REFLEX_DTYPE_F32 ? 4 : 2))
     return REFLEX_EINVAL;
+  rx::ZeroWords zero;
+  zero.words = reinterpret_cast<uint32_t*>(hdr);
+  zero.n = static_cast<int>(sizeof(WsHeader) / 4);
+  if (rx::linear_rows_fit(M, N, K)) {
+    const rx::Fp8LinearRows p{ldx, w, ldw, w_scales, ldws, M, N, K,
+                              out_dtype == REFLEX_DTYPE_F32, out, ldo, zero};
+    RX_CUDA(rx::launch_linear_rows(dtype, x, p, rx::device_sms(), s));
+    return REFLEX_OK;
+  }
   if (rx::tensor_map_encoder() == nullptr) return REFLEX_ECUDA;
   uint8_t* rows = ws + L.rows;
   uint8_t* scales = rows + rx::fp8_scale_offset(K);
-  rx::Fp8Rows q{M, K, ldx, rows, L.row_bytes, scales, L.row_bytes, {}};
-  q.zero.words = reinterpret_cast<uint32_t*>(hdr);
-  q.zero.n = static_cast<int>(sizeof(WsHeader) / 4);
+  const rx::Fp8Rows q{M, K, ldx, rows, L.row_bytes, scales, L.row_bytes, zero};
   RX_CUDA(rx::launch_quantize_rows(dtype, x, q, rx::device_sms(), s));
   return matmul(rows, L.row_bytes, scales, L.row_bytes, w, ldw, w_scales, ldws, M, N, K,
                 out_dtype, out, ldo, &hdr->err, s);
@@ -283,10 +305,6 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
       !code_map(&ma2, ws + L.act, 0, cap, inter, L.act_bytes, 0, kBox) ||
       !code_map(&mb2, w_down, E, d, inter, inter, static_cast<int64_t>(d) * inter, 128))
     return REFLEX_ECUDA;
-  // tiles that k_max / 2 experts a token give: one m-tile per expert with
-  // pairs, and what lies beyond
-  const int64_t pairs = (static_cast<int64_t>(T) * k_max + 1) / 2;
-  const int64_t mt = std::min<int64_t>(E, pairs) + pairs / 128;
   rx::Fp8GemmArgs g{};
   g.g = rx::GroupRows{I32(L.offsets), I32(L.mt_prefix), I32(L.mt2_prefix), &hdr->total_pairs,
                       E, 0, cap};
@@ -305,7 +323,6 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   up_args.b_scale_ld = blocks(d);
   up_args.out = ws + L.act;
   up_args.ldo = L.act_bytes;
-  up_args.splits = pick_splits(mt * blocks(inter), blocks(d), sms);
   RX_CUDA(rx::launch_fp8_swiglu(up_args, s));
   rx::Fp8GemmArgs dn = g;
   dn.map_a = &ma2;
@@ -319,7 +336,6 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   dn.b_scale_ld = blocks(inter);
   dn.out = ws + L.y;
   dn.ldo = d;
-  dn.splits = pick_splits(mt * ((d + 255) / 256), blocks(inter), sms);
   RX_CUDA(rx::launch_fp8_matmul(dn, s));
   const void* resid = (flags & REFLEX_FLAG_RESIDUAL) ? hidden : nullptr;
   RX_CUDA(rx::launch_combine(REFLEX_DTYPE_BF16, ws + L.y, nullptr, resid, I32(L.row_of), alpha, k,

@@ -14,17 +14,27 @@
 // MMAs of the next block run while the last one is read.
 //
 // Tiles: 128 rows of A x 256 rows of B (SwiGLU: 128 gate rows and the matching
-// 128 up rows, hence whole groups of act columns in one CTA).  Per block of K
-// a CTA reads 16 + 32 KB of codes and the MMAs take 512 cycles; reading the
-// accumulator back (128 KB) and 16384 packed fp32 FMAs fit beside them on
-// eight warps.
-//   warp 0      TMA producer: ring of four 48 KB stages, 128-byte swizzle;
-//   warp 1      allocates TMEM, issues the MMAs from one thread;
+// 128 up rows, hence whole groups of act columns in one CTA), taken from a grid of
+// one CTA an SM.
+//   warp 0      TMA producer: ring of three 48 KB stages, 128-byte swizzle;
+//   warp 1      allocates TMEM, issues the MMAs;
+//   warp 2      scales, 16 blocks of K ahead;
+//   warp 3      stores of finished bf16 tiles, which lie staged in 64 KB;
 //   warps 4-11  two warpgroups, each thread one row and 64 + 64 columns (64
 //               of either 128-row half of B): 128 accumulators in registers.
-// Split tiles (few tiles, long K): the CTAs of a cluster take a part of K
-// each and add their accumulators through distributed shared memory, 32 rows
+// Split tiles (few tiles, long K, dense only): the CTAs of a cluster take a part
+// of K each and add their accumulators through distributed shared memory, 32 rows
 // at a time in rank order, so the sums do not depend on timing.
+//
+// Bound: for many rows the sums in registers.  The MMAs of a block take 520
+// cycles; the eight warps that read it back (128 KB), scale it and hand the
+// accumulator on take 900, of which the reads and FMAs are 340 and the rest are
+// latencies of two barriers, of the scales' reads and of the look at TMEM that two
+// warps a scheduler cannot hide.  8192 x 8192 x 8192: 477 us, 2.31 PFLOP/s.
+// Sixteen warps of 64 accumulators took 552 us (the same latencies by twice the
+// warps), CTA pairs on a tile of 256 rows and accumulators of 128 columns no less
+// than this, more registers for the next block's scales spilled (654 us).  For few
+// rows the weights' bytes: 32 x 50000 x 2048 32 us, of which the bytes take 16.
 //
 // Every wait is bounded (2 s); on expiry the CTA records the timeout in the
 // error word, drains its loads and MMAs, frees TMEM and exits.
@@ -38,15 +48,17 @@ namespace {
 
 constexpr int BM = 128;
 constexpr int BN = 256;
-constexpr int kStages = 4;
+constexpr int kHalfB = BN / 2 * 128;  // 128 rows of B
 constexpr int kABytes = BM * 128;
-constexpr int kBBytes = BN * 128;
-constexpr int kStageBytes = kABytes + kBBytes;
-constexpr int kPatchBytes = 32 * 1024;  // 4 KB a warp, or 32 rows x 256 fp32
+constexpr int kBBytes = 2 * kHalfB;
+constexpr int kStages = 3;
+constexpr int kStageOut = 64 * 1024;  // a bf16 tile; else 32 rows x 256 fp32, or 4 KB a warp
+constexpr int kScaleChunk = 16;       // blocks of K whose scales are fetched together
+constexpr int kScaleBytes = 2 * kScaleChunk * (BM + 2) * 4;
 constexpr int kIndexInts = 320;
 constexpr int kBarBytes = 256;
-constexpr int kSmemBytes =
-    kStages * kStageBytes + kPatchBytes + kBarBytes + kIndexInts * 4 + 1024;
+constexpr int kSmemBytes = kStages * (kABytes + kBBytes) + kStageOut + kScaleBytes + kBarBytes +
+                           kIndexInts * 4 + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 // 384 x 168 registers at launch = 128 x 56 + 256 x 224 after the split
 constexpr int kThreads = 384;
@@ -91,17 +103,16 @@ __device__ __forceinline__ void mma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t 
       "l"(da), "l"(db), "r"(kIdesc), "r"(accumulate)
       : "memory");
 }
-// The registers of a tcgen05.ld may be used once this has returned.
-__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
-                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
-                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
-                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
-                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]),
-                 "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :
-               : "memory");
+
+// One lane of a converged warp.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(e));
+  return e;
 }
 
 // Two fp32 in one 64-bit register: one FMA instruction for both.
@@ -115,12 +126,26 @@ __device__ __forceinline__ float2 unpack2(uint64_t v) {
   asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
   return make_float2(__uint_as_float(lo), __uint_as_float(hi));
 }
-__device__ __forceinline__ void fma2(uint64_t& acc, uint64_t a, uint64_t b) {
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+// Waits for the TMEM loads in flight; r passes through, so that no use of it is
+// moved in front of the wait.
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]),
+                 "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
 }
+// acc += r * s, 32 columns of a row.
 __device__ __forceinline__ void scaled_add(uint64_t* acc, const uint32_t (&r)[32], uint64_t s2) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) fma2(acc[i], pack2(r[2 * i], r[2 * i + 1]), s2);
+  for (int i = 0; i < 16; ++i) {
+    const uint64_t x = pack2(r[2 * i], r[2 * i + 1]);
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[i]) : "l"(x), "l"(s2));
+  }
 }
 
 // ---- clusters ---------------------------------------------------------------
@@ -219,9 +244,19 @@ __device__ __forceinline__ bool decode_tile(const Params& p, const int32_t* pref
          row_hi <= static_cast<uint32_t>(p.g.cap_rows);
 }
 
+// The scales of half h of a tile's columns by blocks of K.  A half past the last
+// column has none: its columns are not stored.
+__device__ __forceinline__ const float* b_scale_row(const Params& p, int mode, const Tile& tl,
+                                                    int h) {
+  if (mode == kSwiGLU)
+    return p.b_scales + (2 * tl.e + h) * p.b_scale_group + tl.n * p.b_scale_ld;
+  const int block = 2 * tl.n + (tl.n * BN + 128 < p.n_out ? h : 0);
+  return p.b_scales + tl.e * p.b_scale_group + block * p.b_scale_ld;
+}
+
 // silu(g) u
 __device__ __forceinline__ float swiglu(float g, float u) {
-  return g / (1.0f + __expf(-g)) * u;
+  return __fdividef(g, 1.0f + __expf(-g)) * u;
 }
 
 template <int MODE, bool SPLIT>
@@ -233,8 +268,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sa = smem;
   uint8_t* sb = smem + kStages * kABytes;
-  uint8_t* patch = smem + kStages * kStageBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(patch + kPatchBytes);
+  uint8_t* patch = smem + kStages * (kABytes + kBBytes);
+  float* sc_a = reinterpret_cast<float*>(patch + kStageOut);  // [2][kScaleChunk][BM]
+  float* sc_b = sc_a + 2 * kScaleChunk * BM;                  // [2][kScaleChunk][2]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(patch + kStageOut + kScaleBytes);
   uint64_t* full = bars;                 // [kStages]
   uint64_t* empty = bars + kStages;      // [kStages]
   uint64_t* tfull = bars + 2 * kStages;  // [2] a TMEM accumulator is complete
@@ -242,17 +279,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* xbar = tempty + 2;           // [4] SwiGLU: row maxima of a quarter's two warps
   uint64_t* red_full = xbar + 4;         // split: every CTA's rows are in its patch
   uint64_t* red_empty = red_full + 1;    // split: every CTA has read them
-  uint64_t* drain = red_empty + 1;
+  uint64_t* sfull = red_empty + 1;       // [2] a chunk of scales is in place
+  uint64_t* sempty = sfull + 2;          // [2] it has been used
+  uint64_t* ofull = sempty + 2;          // a tile of bf16 is staged
+  uint64_t* oempty = ofull + 1;          // it has been stored
+  uint64_t* drain = oempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int32_t* cache = reinterpret_cast<int32_t*>(patch + kPatchBytes + kBarBytes);
+  int32_t* cache = reinterpret_cast<int32_t*>(bars + kBarBytes / 8);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   const int S = SPLIT ? p.splits : 1;
   const int rank = SPLIT ? static_cast<int>(cluster_rank()) : 0;
   const int t_first = blockIdx.x / S, t_step = gridDim.x / S;
-  const int kb0 = p.nkb * rank / S, kb1 = p.nkb * (rank + 1) / S;
+  const int kb0 = SPLIT ? p.nkb * rank / S : 0, kb1 = SPLIT ? p.nkb * (rank + 1) / S : p.nkb;
+  const bool staged = MODE == kMatmul && !SPLIT && !p.out_f32 && p.out_vec;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -263,6 +305,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&tfull[b], 1);
       mbar_init(&tempty[b], kPromoters);
     }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&sfull[b], 1);
+      mbar_init(&sempty[b], kPromoters);
+    }
+    mbar_init(ofull, kPromoters);
+    mbar_init(oempty, 1);
     for (int q = 0; q < 4; ++q) mbar_init(&xbar[q], 2);
     mbar_init(red_full, 2 * S);
     mbar_init(red_empty, kPromoters * S);
@@ -277,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (SPLIT) cluster_sync();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   grid_dep_wait();
   grid_dep_launch();
   const int32_t* pref = load_prefix(p, cache);
@@ -303,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int c1 = MODE == kSwiGLU ? tl.n * 128 : tl.n * BN;
         const int c2 = MODE == kSwiGLU ? 2 * tl.e : tl.e;
         const bool second = MODE == kSwiGLU || c1 + 128 < p.n_out;
-        const uint32_t bytes = boxes * p.a_box * 128 + (second ? 2 : 1) * (kBBytes / 2);
+        const uint32_t bytes = boxes * p.a_box * 128 + (second ? 2 : 1) * kHalfB;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
             ok = false;
@@ -315,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t b_dst = smem_addr(sb + stage * kBBytes);
           tma_load_3d(b_dst, &map_b, kb * 128, c1, c2, fb);
           if (second)
-            tma_load_3d(b_dst + kBBytes / 2, &map_b, kb * 128,
-                        MODE == kSwiGLU ? c1 : c1 + 128, MODE == kSwiGLU ? c2 + 1 : c2, fb);
+            tma_load_3d(b_dst + kHalfB, &map_b, kb * 128, MODE == kSwiGLU ? c1 : c1 + 128,
+                        MODE == kSwiGLU ? c2 + 1 : c2, fb);
           for (int i = 0; i < boxes; ++i)
             tma_load_2d(a_dst + i * p.a_box * 128, &map_a, kb * 128, tl.row0 + i * p.a_box, fb);
           issued_mask |= 1u << stage;
@@ -337,48 +385,133 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (issued_mask & (1u << s))
             mbar_wait(&full[s], (issued_phase >> s) & 1u, nullptr, kDrainNs);
       }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
+      // The whole warp walks the loop, so that descriptors and addresses stay in
+      // uniform registers, as tcgen05.mma takes them; one lane issues.
+      const uint32_t elected = elect_one();
       int stage = 0;
       uint32_t phase = 0;
       uint32_t it = 0;
       bool ok = true, issued_any = false;
+      const uint64_t da0 = desc_sw128(smem_addr(sa)), db0 = desc_sw128(smem_addr(sb));
       for (int t = t_first; t < ntiles && ok; t += t_step) {
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const int b = it & 1;
-          if (!mbar_wait(&tempty[b], ((it >> 1) & 1u) ^ 1u, abort_flag, kWaitNs) ||
-              !mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
-            ok = false;
-            break;
-          }
+          ok = mbar_wait(&full[stage], phase, abort_flag, kWaitNs) &&
+               mbar_wait(&tempty[b], ((it >> 1) & 1u) ^ 1u, abort_flag, kWaitNs);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
           tc_fence_after();
-          const uint32_t a0 = smem_addr(sa + stage * kABytes);
-          const uint32_t b0 = smem_addr(sb + stage * kBBytes);
+          // (addresses count 16 bytes in a descriptor's low bits)
+          const uint64_t da = da0 + static_cast<uint32_t>(stage * (kABytes >> 4));
+          const uint64_t db = db0 + static_cast<uint32_t>(stage * (kBBytes >> 4));
+          const uint32_t d = tmem_base + b * BN;
+          if (elected) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_e4m3(tmem_base + b * BN, desc_sw128(a0 + k * 32), desc_sw128(b0 + k * 32),
-                     k > 0 ? 1u : 0u);
+            for (int k = 0; k < 4; ++k) mma_e4m3(d, da + 2 * k, db + 2 * k, k > 0 ? 1u : 0u);
+            mma_commit(smem_addr(&tfull[b]));
+            mma_commit(smem_addr(&empty[stage]));
+          }
           issued_any = true;
-          mma_commit(smem_addr(&empty[stage]));
-          mma_commit(smem_addr(&tfull[b]));
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
         }
       }
-      if (!ok) {
+      if (!ok && elected) {
         if (!*abort_flag) set_err(p.err, kErrTimeout);
         *abort_flag = 1;
       }
-      if (*abort_flag && issued_any) {
+      __syncwarp();
+      if (*abort_flag && issued_any && elected) {
         // MMAs in flight must finish before TMEM is freed
         mma_commit(smem_addr(drain));
         mbar_wait(drain, 0, nullptr, kDrainNs);
       }
+    } else if (warp == 2) {
+      // ---------------- scales ----------------
+      // The scales of a row of A are fetched 16 blocks of K ahead, by themselves:
+      // global loads in the warps that hand accumulators back delay the hand-over
+      // by their latency (8192 x 8192 x 8192: some 30 us).
+      uint32_t slot = 0, phase = 0;
+      bool ok = true;
+      for (int t = t_first; t < ntiles && ok; t += t_step) {
+        Tile tl;
+        if (!decode_tile(p, pref, t, tl)) break;
+        const int rows = tl.rows;
+        const float* b0 = b_scale_row(p, MODE, tl, 0);
+        const float* b1 = b_scale_row(p, MODE, tl, 1);
+        for (int c0 = kb0; c0 < kb1; c0 += kScaleChunk) {
+          const int n = min(kScaleChunk, kb1 - c0);
+          ok = __all_sync(0xffffffffu, mbar_wait(&sempty[slot], phase ^ 1u, abort_flag, kWaitNs));
+          if (!ok) break;
+          float* to = sc_a + slot * kScaleChunk * BM;
+#pragma unroll 1
+          for (int r = lane; r < BM; r += 32) {
+            const float* from = reinterpret_cast<const float*>(
+                p.a_scales + static_cast<int64_t>(tl.row0 + (r < rows ? r : 0)) *
+                                 p.a_scale_row_bytes) + c0;
+#pragma unroll
+            for (int i0 = 0; i0 < kScaleChunk; i0 += 8) {
+              float v[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = i0 + i < n ? from[i0 + i] : 0.f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) to[(i0 + i) * BM + r] = v[i];
+            }
+          }
+          if (lane < 2 * n)
+            sc_b[slot * kScaleChunk * 2 + lane] = (lane & 1 ? b1 : b0)[c0 + (lane >> 1)];
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(smem_addr(&sfull[slot]));
+          slot ^= 1u;
+          if (slot == 0) phase ^= 1u;
+        }
+      }
+      if (!ok && lane == 0) {
+        if (!*abort_flag) set_err(p.err, kErrTimeout);
+        *abort_flag = 1;
+      }
+    } else if (warp == 3 && staged) {
+      // ---------------- stores of staged tiles ----------------
+      // (a row of 256 columns an instruction, while the next tile is summed)
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = t_first; t < ntiles && ok; t += t_step, phase ^= 1u) {
+        Tile tl;
+        if (!decode_tile(p, pref, t, tl)) break;
+        const int rows = tl.rows;
+        const int cols = min(BN, p.n_out - tl.n * BN);
+        uint16_t* o = static_cast<uint16_t*>(p.out) +
+                      static_cast<int64_t>(tl.row0) * p.ldo + tl.n * BN;
+        ok = __all_sync(0xffffffffu, mbar_wait(ofull, phase, abort_flag, kWaitNs));
+        if (!ok) break;
+        if (lane * 8 + 8 <= cols) {
+#pragma unroll 4
+          for (int r = 0; r < rows; ++r) {
+            const uint4 v =
+                *reinterpret_cast<const uint4*>(patch + r * 512 + ((lane ^ (r & 7)) << 4));
+            *reinterpret_cast<uint4*>(o + r * p.ldo + lane * 8) = v;
+          }
+        } else if (lane * 8 < cols) {  // the lane with the last columns
+          for (int r = 0; r < rows; ++r) {
+            const uint16_t* v =
+                reinterpret_cast<const uint16_t*>(patch + r * 512 + ((lane ^ (r & 7)) << 4));
+            for (int j = 0; j < cols - lane * 8; ++j) o[r * p.ldo + lane * 8 + j] = v[j];
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(oempty));
+      }
+      if (!ok && lane == 0) {
+        if (!*abort_flag) set_err(p.err, kErrTimeout);
+        *abort_flag = 1;
+      }
     }
   } else {
-    // ---------------- scales, sums and stores ----------------
+    // ---------------- sums and epilogue ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int quarter = warp & 3;          // TMEM lanes 32 * quarter ..
     const int wg = (warp - kFirstPromoter) >> 2;  // columns 64 wg .. of both halves
@@ -386,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int row = quarter * 32 + lane;
     uint8_t* my_patch = patch + pw * 4096;
     float* s_max = reinterpret_cast<float*>(patch);  // SwiGLU: [2][2][128] row maxima
-    uint32_t it = 0, red_phase = 0;
+    uint32_t it = 0, red_phase = 0, sc_slot = 0, sc_phase = 0, o_phase = 0;
     uint32_t xt = 0;  // SwiGLU tiles that this quarter has had rows in
     bool ok = true;
     for (int t = t_first; t < ntiles && ok; t += t_step) {
@@ -394,25 +527,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!decode_tile(p, pref, t, tl)) break;
       const bool live = quarter * 32 < tl.rows;
       const bool store = row < tl.rows;
-      const float* sb0 = MODE == kSwiGLU
-                             ? p.b_scales + (2 * tl.e) * p.b_scale_group + tl.n * p.b_scale_ld
-                             : p.b_scales + tl.e * p.b_scale_group + 2 * tl.n * p.b_scale_ld;
-      const float* sb1 = sb0;
-      if (MODE == kSwiGLU) sb1 += p.b_scale_group;
-      else if (tl.n * BN + 128 < p.n_out) sb1 += p.b_scale_ld;
-      const float* sa_row = reinterpret_cast<const float*>(
-          p.a_scales + static_cast<int64_t>(tl.row0 + (store ? row : 0)) * p.a_scale_row_bytes);
       uint64_t acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
-      float na = sa_row[kb0], n0 = sb0[kb0], n1 = sb1[kb0];
       for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const int b = it & 1;
-        const float s0 = na * n0, s1 = na * n1;
-        if (kb + 1 < kb1) {
-          na = sa_row[kb + 1];
-          n0 = sb0[kb + 1];
-          n1 = sb1[kb + 1];
+        const int b = it & 1, in = (kb - kb0) & (kScaleChunk - 1);  // place in the chunk
+        if (in == 0 &&
+            !__all_sync(0xffffffffu, mbar_wait(&sfull[sc_slot], sc_phase, abort_flag, kWaitNs))) {
+          ok = false;
+          break;
+        }
+        const float sa_r = sc_a[(sc_slot * kScaleChunk + in) * BM + row];
+        const float2 sb_r =
+            *reinterpret_cast<const float2*>(sc_b + (sc_slot * kScaleChunk + in) * 2);
+        const float s0 = sa_r * sb_r.x, s1 = sa_r * sb_r.y;
+        if (in == kScaleChunk - 1 || kb + 1 == kb1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(smem_addr(&sempty[sc_slot]));
+          sc_slot ^= 1u;
+          if (sc_slot == 0) sc_phase ^= 1u;
         }
         if (!__all_sync(0xffffffffu, mbar_wait(&tfull[b], (it >> 1) & 1u, abort_flag, kWaitNs))) {
           ok = false;
@@ -424,22 +557,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                               static_cast<uint32_t>(b * BN + wg * 64);
           const uint64_t p0 = pack2(__float_as_uint(s0), __float_as_uint(s0));
           const uint64_t p1 = pack2(__float_as_uint(s1), __float_as_uint(s1));
-          uint32_t r0[32], r1[32];
+          uint32_t r0[32];
           tmem_ld32(ta, r0);
-          tmem_ld_wait_for(r0);
-          tmem_ld32(ta + 32, r1);
+          tmem_ld_wait(r0);
           scaled_add(acc, r0, p0);
-          tmem_ld_wait_for(r1);
+          tmem_ld32(ta + 32, r0);
+          tmem_ld_wait(r0);
+          scaled_add(acc + 16, r0, p0);
           tmem_ld32(ta + 128, r0);
-          scaled_add(acc + 16, r1, p0);
-          tmem_ld_wait_for(r0);
-          tmem_ld32(ta + 160, r1);
+          tmem_ld_wait(r0);
           scaled_add(acc + 32, r0, p1);
-          tmem_ld_wait_for(r1);
+          tmem_ld32(ta + 160, r0);
+          tmem_ld_wait(r0);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive1(smem_addr(&tempty[b]));
-          scaled_add(acc + 48, r1, p1);
+          scaled_add(acc + 48, r0, p1);
         } else if (lane == 0) {
           mbar_arrive1(smem_addr(&tempty[b]));
         }
@@ -469,58 +602,47 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = __all_sync(0xffffffffu, mbar_wait_cluster(red_full, red_phase, abort_flag));
           if (!ok) break;
           for (int i = rank + S * pw; i < 32 && q * 32 + i < tl.rows; i += S * kPromoters) {
+            // (all ranks' rows in flight, then summed in rank order)
             float v[2][4] = {};
+            float4 x[8], y[8];
             const uint32_t at = smem_addr(red + i * BN);
-            for (int s = 0; s < S; ++s) {
-              const uint32_t from = peer_addr(at, s);
-              const float4 x = ld_peer4(from + ((lane ^ (i & 7)) << 4));
-              const float4 y = ld_peer4(from + (((32 + lane) ^ (i & 7)) << 4));
-              v[0][0] += x.x; v[0][1] += x.y; v[0][2] += x.z; v[0][3] += x.w;
-              v[1][0] += y.x; v[1][1] += y.y; v[1][2] += y.z; v[1][3] += y.w;
-            }
-            const int64_t r = tl.row0 + q * 32 + i;
-            if (MODE == kSwiGLU) {
-              const int col = tl.n * 128 + lane * 4;
-              float a[4];
-              uint32_t m = 0;
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                a[j] = col + j < p.n_out ? swiglu(v[0][j], v[1][j]) : 0.f;
-                m = max(m, __float_as_uint(a[j]) & 0x7fffffffu);
+            for (int s = 0; s < 8; ++s)
+              if (s < S) {
+                const uint32_t from = peer_addr(at, s);
+                x[s] = ld_peer4(from + ((lane ^ (i & 7)) << 4));
+                y[s] = ld_peer4(from + (((32 + lane) ^ (i & 7)) << 4));
               }
-              const float am = fp8_amax(__reduce_max_sync(0xffffffffu, m));
-              const float inv = fp8_inverse(am);
-              uint8_t* o = static_cast<uint8_t*>(p.out) + r * p.ldo;
-              if (col < p.n_out)  // n_out is a multiple of 64
-                *reinterpret_cast<uint32_t*>(o + col) =
-                    e4m3x4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
-              if (lane == 0)
-                reinterpret_cast<float*>(o + p.scale_offset)[tl.n] = __fdiv_rn(am, kE4m3Max);
-            } else {
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int col = tl.n * BN + h * 128 + lane * 4;
-                const bool whole = p.out_vec && col + 4 <= p.n_out;
-                if (p.out_f32) {
-                  float* o = static_cast<float*>(p.out) + r * p.ldo + col;
-                  if (whole) {
-                    *reinterpret_cast<float4*>(o) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
-                  } else {
+            for (int s = 0; s < 8; ++s)
+              if (s < S) {
+                v[0][0] += x[s].x; v[0][1] += x[s].y; v[0][2] += x[s].z; v[0][3] += x[s].w;
+                v[1][0] += y[s].x; v[1][1] += y[s].y; v[1][2] += y[s].z; v[1][3] += y[s].w;
+              }
+            const int64_t r = tl.row0 + q * 32 + i;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                      if (col + j < p.n_out) o[j] = v[h][j];
-                  }
+            for (int h = 0; h < 2; ++h) {
+              const int col = tl.n * BN + h * 128 + lane * 4;
+              const bool whole = p.out_vec && col + 4 <= p.n_out;
+              if (p.out_f32) {
+                float* o = static_cast<float*>(p.out) + r * p.ldo + col;
+                if (whole) {
+                  *reinterpret_cast<float4*>(o) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
                 } else {
-                  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + r * p.ldo + col;
-                  if (whole) {
-                    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v[h][0], v[h][1]),
-                                           __floats2bfloat162_rn(v[h][2], v[h][3])};
-                    *reinterpret_cast<uint2*>(o) = *reinterpret_cast<uint2*>(w);
-                  } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                      if (col + j < p.n_out) o[j] = __float2bfloat16_rn(v[h][j]);
-                  }
+                  for (int j = 0; j < 4; ++j)
+                    if (col + j < p.n_out) o[j] = v[h][j];
+                }
+              } else {
+                __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + r * p.ldo + col;
+                if (whole) {
+                  __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v[h][0], v[h][1]),
+                                         __floats2bfloat162_rn(v[h][2], v[h][3])};
+                  *reinterpret_cast<uint2*>(o) = *reinterpret_cast<uint2*>(w);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    if (col + j < p.n_out) o[j] = __float2bfloat16_rn(v[h][j]);
                 }
               }
             }
@@ -528,6 +650,33 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane < S) mbar_arrive_peer(peer_addr(smem_addr(red_empty), lane));
         }
+        continue;
+      }
+
+      if (staged) {
+        // hand the tile to the store warp (16-byte chunks swizzled by the row)
+        ok = __all_sync(0xffffffffu, mbar_wait(oempty, o_phase ^ 1u, abort_flag, kWaitNs));
+        if (!ok) break;
+        o_phase ^= 1u;
+        if (live) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              uint32_t w[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float2 v = unpack2(acc[h * 32 + 4 * j + i]);
+                __nv_bfloat162 b2 = __floats2bfloat162_rn(v.x, v.y);
+                w[i] = *reinterpret_cast<uint32_t*>(&b2);
+              }
+              *reinterpret_cast<uint4*>(patch + row * 512 +
+                                        (((h * 16 + wg * 8 + j) ^ (row & 7)) << 4)) =
+                  make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(ofull));
         continue;
       }
 
@@ -574,71 +723,59 @@ __global__ void __launch_bounds__(kThreads, 1)
             reinterpret_cast<float*>(o + p.scale_offset)[tl.n] = __fdiv_rn(am, kE4m3Max);
         }
       } else {
-        // through a 32-row patch of 128-byte rows (16-byte chunks swizzled by
-        // the row), so that a store instruction writes four whole lines
-        const int es = p.out_f32 ? 4 : 2;
+        // fp32, or bf16 rows at any multiple of 2 bytes: 32 columns at a time through
+        // a 32-row patch of 128-byte rows (16-byte chunks swizzled by the row), so
+        // that a store instruction writes whole lines
         const int64_t row_base = tl.row0 + quarter * 32;
         const int rows = min(32, tl.rows - quarter * 32);
-        for (int part = 0; part < es; ++part) {
-          // part: (half, and which 32 of its 64 columns in fp32)
-          const int h = p.out_f32 ? part >> 1 : part;
-          const int sub = p.out_f32 ? (part & 1) * 32 : 0;
+        auto at = [&](int r, int c) {
+          return *reinterpret_cast<const float*>(my_patch + r * 128 + (((c >> 2) ^ (r & 7)) << 4) +
+                                                 (c & 3) * 4);
+        };
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
           __syncwarp();
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            if (hh != h) continue;
-            if (p.out_f32) {
-#pragma unroll
-              for (int ss = 0; ss < 2; ++ss) {
-                if (ss * 32 != sub) continue;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const float2 v0 = unpack2(acc[hh * 32 + ss * 16 + 2 * j]);
-                  const float2 v1 = unpack2(acc[hh * 32 + ss * 16 + 2 * j + 1]);
-                  *reinterpret_cast<float4*>(my_patch + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                      make_float4(v0.x, v0.y, v1.x, v1.y);
-                }
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float2 v = unpack2(acc[hh * 32 + 4 * j + i]);
-                  __nv_bfloat162 b2 = __floats2bfloat162_rn(v.x, v.y);
-                  w[i] = *reinterpret_cast<uint32_t*>(&b2);
-                }
-                *reinterpret_cast<uint4*>(my_patch + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                    make_uint4(w[0], w[1], w[2], w[3]);
-              }
-            }
+          for (int j = 0; j < 8; ++j) {
+            const float2 v0 = unpack2(acc[part * 16 + 2 * j]);
+            const float2 v1 = unpack2(acc[part * 16 + 2 * j + 1]);
+            *reinterpret_cast<float4*>(my_patch + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_float4(v0.x, v0.y, v1.x, v1.y);
           }
           __syncwarp();
-          const int chunk = lane & 7;
-          const int col = tl.n * BN + h * 128 + wg * 64 + sub + chunk * (16 / es);
+          const int first = tl.n * BN + (part >> 1) * 128 + wg * 64 + (part & 1) * 32;
+          const int cols = min(32, p.n_out - first);
+          if (p.out_f32 && p.out_vec && cols == 32) {
+            const int chunk = lane & 7;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3);
-            const uint4 v =
-                *reinterpret_cast<const uint4*>(my_patch + r * 128 + ((chunk ^ (r & 7)) << 4));
-            if (r >= rows) continue;
-            uint8_t* o = static_cast<uint8_t*>(p.out) + ((row_base + r) * p.ldo + col) * es;
-            if (p.out_vec && col + 16 / es <= p.n_out) {
-              *reinterpret_cast<uint4*>(o) = v;
-            } else {
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-              if (p.out_f32) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (col + j < p.n_out) reinterpret_cast<uint32_t*>(o)[j] = w[j];
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  if (col + j < p.n_out)
-                    reinterpret_cast<uint16_t*>(o)[j] =
-                        static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
-              }
+            for (int i = 0; i < 8; ++i) {
+              const int r = i * 4 + (lane >> 3);
+              const float4 v =
+                  *reinterpret_cast<const float4*>(my_patch + r * 128 + ((chunk ^ (r & 7)) << 4));
+              if (r < rows)
+                *reinterpret_cast<float4*>(static_cast<float*>(p.out) + (row_base + r) * p.ldo +
+                                           first + chunk * 4) = v;
+            }
+          } else if (p.out_f32) {  // a lane a column
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r)
+              if (lane < cols)
+                static_cast<float*>(p.out)[(row_base + r) * p.ldo + first + lane] = at(r, lane);
+          } else {
+            // two rows an instruction: words of two columns from the row's first 4-byte
+            // boundary on, what is left in front and behind by itself
+#pragma unroll 4
+            for (int r = lane >> 4; r < rows; r += 2) {
+              __nv_bfloat16* o =
+                  static_cast<__nv_bfloat16*>(p.out) + (row_base + r) * p.ldo + first;
+              const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1);
+              const int c = 2 * (lane & 15) + odd;
+              if (c + 1 < cols)
+                *reinterpret_cast<__nv_bfloat162*>(o + c) =
+                    __floats2bfloat162_rn(at(r, c), at(r, c + 1));
+              else if (c < cols)
+                o[c] = __float2bfloat16_rn(at(r, c));
+              if ((lane & 15) == 0 && odd && cols > 0) o[0] = __float2bfloat16_rn(at(r, 0));
             }
           }
         }
@@ -668,12 +805,13 @@ cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
                                        kSmemBytes);
   if (e != cudaSuccess) return e;
   Params p{};
+  static_assert(!(SPLIT && MODE == kSwiGLU), "only dense products are split");
   p.nkb = (a.K + 127) / 128;
   p.n_out = a.n_out;
   p.n_tiles = MODE == kSwiGLU ? (a.n_out + 127) / 128 : (a.n_out + BN - 1) / BN;
   p.g = a.g;
-  p.max_mtiles = a.g.offsets != nullptr ? a.g.E + (a.g.cap_rows + BM - 1) / BM
-                                        : (a.g.dense_rows + BM - 1) / BM;
+  p.max_mtiles = ((a.g.offsets != nullptr ? a.g.cap_rows : a.g.dense_rows) + BM - 1) / BM +
+                 (a.g.offsets != nullptr ? a.g.E : 0);
   p.a_box = a.a_box;
   p.a_scales = a.a_scales;
   p.a_scale_row_bytes = a.a_scale_row_bytes;
@@ -689,13 +827,13 @@ cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
   p.splits = a.splits;
   p.err = a.err;
   const int64_t most = static_cast<int64_t>(p.max_mtiles) * p.n_tiles;
-  int64_t grid = std::min<int64_t>(a.num_sms / a.splits, most) * a.splits;
-  if (grid < a.splits) grid = a.splits;
+  const int per_tile = a.splits;
+  const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(a.num_sms / per_tile, most)) * per_tile;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {static_cast<unsigned>(a.splits), 1, 1};
+  attr[1].val.clusterDim = {static_cast<unsigned>(per_tile), 1, 1};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(grid));
   cfg.blockDim = dim3(kThreads);
@@ -709,8 +847,7 @@ cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t launch_fp8_swiglu(const Fp8GemmArgs& a, cudaStream_t stream) {
-  return a.splits > 1 ? launch_impl<kSwiGLU, true>(a, stream)
-                      : launch_impl<kSwiGLU, false>(a, stream);
+  return launch_impl<kSwiGLU, false>(a, stream);
 }
 cudaError_t launch_fp8_matmul(const Fp8GemmArgs& a, cudaStream_t stream) {
   return a.splits > 1 ? launch_impl<kMatmul, true>(a, stream)

@@ -91,7 +91,11 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
 def _output(out, M: int, N: int, dtype, device) -> torch.Tensor:
     _want(dtype in _DTYPES, "outputs are fp32 or bf16")
     if out is None:
-        return torch.empty((M, N), dtype=dtype, device=device)
+        # rows on 16-byte boundaries, where a row is a few vectors long at least
+        # (999 x 50001 x 2048 to bf16: 105 us, packed rows 236)
+        unit = 16 // dtype.itemsize
+        ld = -(-N // unit) * unit if N >= 4 * unit else N
+        return torch.empty((M, ld), dtype=dtype, device=device)[:, :N]
     _rows(out, "out", _DTYPES)
     _want(tuple(out.shape) == (M, N) and out.device == device, "out: shape or device")
     return out
