@@ -447,7 +447,8 @@ int reflex_quantize_fp8(int32_t dtype, const void* x, int64_t rows, int64_t cols
  * a and b start on 16-byte boundaries.  M == 0 computes nothing.  Any N, K
  * >= 1; the same bits for a row whatever M and the other rows are, as long as
  * the number of CTAs that share a tile's K stays the same (it is chosen from M,
- * N and K).
+ * N and K).  Sizes up to 2^30, and up to 2^30 tiles of 128 x 256 (else
+ * REFLEX_EUNSUPPORTED).  Rows of out on 16-byte boundaries are stored fastest.
  */
 int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int64_t ldas,
                       const uint8_t* b, int64_t ldb, const float* b_scales, int64_t ldbs,
@@ -460,7 +461,8 @@ int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int6
  * with the codes w [N, K] and w_scales as by reflex_matmul_fp8.
  *   workspace  >= reflex_linear_fp8_workspace_size(M, K) bytes, 256-B aligned;
  *              its first word is the call's error word (reflex_moe_status).
- * A workspace sized for M rows serves every smaller batch.
+ * A workspace sized for M rows serves every smaller batch.  One to four rows are
+ * summed in another order than more, where that is faster (chosen from M, N, K).
  */
 size_t reflex_linear_fp8_workspace_size(int32_t M, int32_t K);
 int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* w,

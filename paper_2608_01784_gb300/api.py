@@ -209,6 +209,12 @@ class MoELayer:
         nbytes = n * torch.empty((), dtype=dtype).element_size()
         return self.ws[off:off + nbytes].view(dtype)
 
+    def routing(self):
+        """Views of the last forward's (ids int32, alpha fp32), both [T, k_max]."""
+        T, km = self._T, self.k_max
+        return (self._view(self.rec.ids, T * km).view(T, km),
+                self._view(self.rec.alpha, T * km, torch.float32).view(T, km))
+
     def record(self) -> dict:
         """Views (no copies) of the routing record of the last forward."""
         T, km, E = self._T, self.k_max, self.E

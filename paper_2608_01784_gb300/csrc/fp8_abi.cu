@@ -189,15 +189,17 @@ int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int6
                       int32_t* dev_status, void* stream) {
   if (!product_ok(M, N, K, ldb, ldbs, out_dtype, ldo)) return REFLEX_EINVAL;
   if (!product_fits(M, N, K)) return REFLEX_EUNSUPPORTED;
+  if (M > 0) {
+    if (a == nullptr || a_scales == nullptr || b == nullptr || b_scales == nullptr ||
+        out == nullptr || lda < K || lda % 16 != 0 || ldas < blocks(K))
+      return REFLEX_EINVAL;
+    if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) ||
+        !aligned(out, out_dtype == REFLEX_DTYPE_F32 ? 4 : 2))
+      return REFLEX_EINVAL;
+  }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));
   if (M == 0) return REFLEX_OK;
-  if (a == nullptr || a_scales == nullptr || b == nullptr || b_scales == nullptr ||
-      out == nullptr || lda < K || lda % 16 != 0 || ldas < blocks(K))
-    return REFLEX_EINVAL;
-  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) ||
-      !aligned(out, out_dtype == REFLEX_DTYPE_F32 ? 4 : 2))
-    return REFLEX_EINVAL;
   return matmul(a, lda, reinterpret_cast<const uint8_t*>(a_scales), ldas * 4, b, ldb, b_scales,
                 ldbs, M, N, K, out_dtype, out, ldo, reinterpret_cast<uint32_t*>(dev_status), s);
 }

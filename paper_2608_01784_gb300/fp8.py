@@ -164,6 +164,17 @@ class ExpertsFp8:
 
     def __init__(self, weights: dict, *, d: int, E: int, inter: int, k_max: int,
                  max_tokens: int):
+        self.w, self.d, self.E, self.inter = weights, d, E, inter
+        self.k_max, self.max_tokens = k_max, max_tokens
+        self.ws_bytes = B.reflex_experts_fp8_workspace_size(max_tokens, d, E, inter, k_max)
+        _want(self.ws_bytes > 0, "unsupported MoE layer shape")
+        self.check_weights(weights)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=weights["w_down"].device)
+
+    def check_weights(self, weights: dict):
+        """Refuses weights that this layer's shape does not fit; `w` may be set to
+        others of the same shape (layers that share the workspace)."""
+        d, E, inter = self.d, self.E, self.inter
         shapes = dict(w_gate_up=(E, 2 * inter, d), w_down=(E, d, inter),
                       w_gate_up_scales=(E, 2, _blocks(inter), _blocks(d)),
                       w_down_scales=(E, _blocks(d), _blocks(inter)))
@@ -172,11 +183,6 @@ class ExpertsFp8:
             dt = torch.float32 if name.endswith("scales") else torch.float8_e4m3fn
             _want(t.is_cuda and t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous(),
                   f"{name}: a contiguous CUDA tensor {shape} of {dt}")
-        self.w, self.d, self.E, self.inter = weights, d, E, inter
-        self.k_max, self.max_tokens = k_max, max_tokens
-        self.ws_bytes = B.reflex_experts_fp8_workspace_size(max_tokens, d, E, inter, k_max)
-        _want(self.ws_bytes > 0, "unsupported MoE layer shape")
-        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=weights["w_down"].device)
 
     def forward(self, hidden: torch.Tensor, ids: torch.Tensor, alpha: torch.Tensor,
                 k: torch.Tensor, out: torch.Tensor | None = None, residual: bool = False,
