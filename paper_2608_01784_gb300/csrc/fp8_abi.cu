@@ -48,6 +48,20 @@ bool code_map(CUtensorMap* m, const void* base, int64_t groups, int64_t rows, in
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Rows of out as the kernel stores them, 32 x 128 bytes at a time with the same
+// swizzle.
+bool out_map(CUtensorMap* m, void* base, bool bf16, int64_t rows, int64_t cols, int64_t row_bytes) {
+  auto fn = rx::tensor_map_encoder();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(row_bytes)};
+  const cuuint32_t box[2] = {bf16 ? 64u : 128u, 32};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base,
+            dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // CTAs of a cluster that share a tile's K, where the tiles leave SMs free.  Adding
 // the parts costs 2 to 3 us for each 32 rows, a block of K 0.5 us, so taller
 // tiles are split at a long K only (N x K, one CTA a tile | split, us):
@@ -89,6 +103,11 @@ int matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t a_sca
   g.splits = pick_splits(M, blocks(M) * blocks2(N), blocks(K), sms);
   g.err = err;
   g.num_sms = sms;
+  CUtensorMap mo;
+  if (g.splits == 1 && !g.out_f32 && aligned(out, 16) && ldo % 8 == 0) {
+    if (!out_map(&mo, out, true, M, N, ldo * 2)) return REFLEX_ECUDA;
+    g.map_out = &mo;
+  }
   RX_CUDA(rx::launch_fp8_matmul(g, s));
   return REFLEX_OK;
 }
@@ -299,13 +318,15 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   RX_CUDA(rx::launch_dispatch_gather(REFLEX_DTYPE_BF16, ws + L.x, ids, k, T, E, k_max, cap,
                                      static_cast<int>(L.x_bytes / 2), b, ws + L.xperm, sms, s));
 
-  CUtensorMap ma1, mb1, ma2, mb2;
+  CUtensorMap ma1, mb1, mo1, ma2, mb2, mo2;
   constexpr int kBox = 32;
   if (!code_map(&ma1, ws + L.xperm, 0, cap, d, L.x_bytes, 0, kBox) ||
       !code_map(&mb1, w_gate_up, 2 * static_cast<int64_t>(E), inter, d, d,
                 static_cast<int64_t>(inter) * d, 128) ||
       !code_map(&ma2, ws + L.act, 0, cap, inter, L.act_bytes, 0, kBox) ||
-      !code_map(&mb2, w_down, E, d, inter, inter, static_cast<int64_t>(d) * inter, 128))
+      !code_map(&mb2, w_down, E, d, inter, inter, static_cast<int64_t>(d) * inter, 128) ||
+      !out_map(&mo1, ws + L.act, false, cap, inter, L.act_bytes) ||
+      !out_map(&mo2, ws + L.y, true, cap, d, static_cast<int64_t>(d) * 2))
     return REFLEX_ECUDA;
   rx::Fp8GemmArgs g{};
   g.g = rx::GroupRows{I32(L.offsets), I32(L.mt_prefix), I32(L.mt2_prefix), &hdr->total_pairs,
@@ -316,6 +337,7 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   rx::Fp8GemmArgs up_args = g;
   up_args.map_a = &ma1;
   up_args.map_b = &mb1;
+  up_args.map_out = &mo1;
   up_args.K = d;
   up_args.n_out = inter;
   up_args.a_scales = ws + L.xperm + rx::fp8_scale_offset(d);
@@ -329,6 +351,7 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   rx::Fp8GemmArgs dn = g;
   dn.map_a = &ma2;
   dn.map_b = &mb2;
+  dn.map_out = &mo2;
   dn.K = inter;
   dn.n_out = d;
   dn.a_scales = ws + L.act + rx::fp8_scale_offset(inter);

@@ -18,23 +18,31 @@
 // one CTA an SM.
 //   warp 0      TMA producer: ring of three 48 KB stages, 128-byte swizzle;
 //   warp 1      allocates TMEM, issues the MMAs;
-//   warp 2      scales, 16 blocks of K ahead;
-//   warp 3      stores of finished bf16 tiles, which lie staged in 64 KB;
+//   warp 2      the tiles and their scales, up to 16 blocks of K ahead;
+//   warp 3      TMA stores of finished tiles (bf16, act codes), which lie staged in
+//               64 KB while the next tile is summed;
 //   warps 4-11  two warpgroups, each thread one row and 64 + 64 columns (64
 //               of either 128-row half of B): 128 accumulators in registers.
 // Split tiles (few tiles, long K, dense only): the CTAs of a cluster take a part
 // of K each and add their accumulators through distributed shared memory, 32 rows
 // at a time in rank order, so the sums do not depend on timing.
 //
-// Bound: for many rows the sums in registers.  The MMAs of a block take 520
-// cycles; the eight warps that read it back (128 KB), scale it and hand the
-// accumulator on take 900, of which the reads and FMAs are 340 and the rest are
-// latencies of two barriers, of the scales' reads and of the look at TMEM that two
-// warps a scheduler cannot hide.  8192 x 8192 x 8192: 477 us, 2.31 PFLOP/s.
-// Sixteen warps of 64 accumulators took 552 us (the same latencies by twice the
-// warps), CTA pairs on a tile of 256 rows and accumulators of 128 columns no less
-// than this, more registers for the next block's scales spilled (654 us).  For few
-// rows the weights' bytes: 32 x 50000 x 2048 32 us, of which the bytes take 16.
+// Bound: for many rows the sums in registers, and close behind them the codes'
+// way from L2.  The MMAs of a block take 520 cycles; the eight warps that read it
+// back (128 KB), scale it and hand the accumulator on take about 1000, of which the
+// reads and FMAs by themselves are 340 and the rest are latencies of two barriers,
+// of the scales' reads and of TMEM that two warps a scheduler cannot hide.
+// 8192 x 8192 x 8192: 485 us, 2.27 PFLOP/s; with a quarter of the MMAs 475, without
+// the sums 426, without these and the loads of B 358.  Sixteen warps of 64
+// accumulators took 552 us (the same latencies by twice the warps); CTA pairs on a
+// tile of 256 rows, accumulators of 128 columns, scalar FMAs and reading the next
+// block's scales ahead were no faster.  For few rows the weights' bytes:
+// 32 x 50000 x 2048 30 us, of which the bytes take 16.
+//
+// Short K (512 in a down product) shows what a tile costs besides its blocks: finding
+// it takes some 2000 cycles (warps 0 and 2 do it ahead) and storing it 8000 by one
+// warp's vectors, 900 to 3000 by TMA.  61,000 pairs of 256 experts, d = 2048, inter
+// = 512: layer 458 us without these two, 385 with.
 //
 // Every wait is bounded (2 s); on expiry the CTA records the timeout in the
 // error word, drains its loads and MMAs, frees TMEM and exits.
@@ -52,8 +60,11 @@ constexpr int kHalfB = BN / 2 * 128;  // 128 rows of B
 constexpr int kABytes = BM * 128;
 constexpr int kBBytes = 2 * kHalfB;
 constexpr int kStages = 3;
-constexpr int kStageOut = 64 * 1024;  // a bf16 tile; else 32 rows x 256 fp32, or 4 KB a warp
-constexpr int kScaleChunk = 16;       // blocks of K whose scales are fetched together
+// a staged tile, boxes of 128 rows x 128 bytes with the swizzle of the stages: bf16
+// four of them, act codes one; else 32 rows x 256 fp32, or 4 KB a warp
+constexpr int kBoxOut = BM * 128;
+constexpr int kStageOut = 4 * kBoxOut;
+constexpr int kScaleChunk = 16;  // blocks of K whose scales are fetched together
 constexpr int kScaleBytes = 2 * kScaleChunk * (BM + 2) * 4;
 constexpr int kIndexInts = 320;
 constexpr int kBarBytes = 256;
@@ -85,6 +96,7 @@ struct Params {
   void* out;
   int64_t ldo;
   int out_f32;
+  int staged;   // out goes through shared memory and map_out
   int out_vec;  // rows of out start on 16-byte boundaries
   int64_t scale_offset;  // SwiGLU: the scales' place in a packed row
   int splits;
@@ -148,6 +160,15 @@ __device__ __forceinline__ void scaled_add(uint64_t* acc, const uint32_t (&r)[32
   }
 }
 
+// A box of shared memory to global memory, clipped to the map's extents.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t from, int c0,
+                                             int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map),
+      "r"(from), "r"(c0), "r"(c1)
+      : "memory");
+}
+
 // ---- clusters ---------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -194,7 +215,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
 }
 
 // ---- tiles ------------------------------------------------------------------
-struct Tile {
+struct __align__(16) Tile {
   int e, n, row0, rows;
 };
 
@@ -262,7 +283,8 @@ __device__ __forceinline__ float swiglu(float g, float u) {
 template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
     fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a,
-                    const __grid_constant__ CUtensorMap map_b, const Params p) {
+                    const __grid_constant__ CUtensorMap map_b,
+                    const __grid_constant__ CUtensorMap map_out, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -286,6 +308,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain = oempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  Tile* s_tile = reinterpret_cast<Tile*>(tmem_slot + 2);  // [2] whose scales these are
+  Tile* o_tile = s_tile + 2;                              // the staged one
+  static_assert(2 * kStages + 17 == 23 && 23 * 8 + 8 + 3 * 16 <= kBarBytes, "barriers");
   int32_t* cache = reinterpret_cast<int32_t*>(bars + kBarBytes / 8);
 
   const int warp = threadIdx.x >> 5;
@@ -294,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = SPLIT ? static_cast<int>(cluster_rank()) : 0;
   const int t_first = blockIdx.x / S, t_step = gridDim.x / S;
   const int kb0 = SPLIT ? p.nkb * rank / S : 0, kb1 = SPLIT ? p.nkb * (rank + 1) / S : p.nkb;
-  const bool staged = MODE == kMatmul && !SPLIT && !p.out_f32 && p.out_vec;
+  const bool staged = MODE == kSwiGLU || (!SPLIT && p.staged);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -319,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
     prefetch_map(&map_a);
     prefetch_map(&map_b);
+    if (staged) prefetch_map(&map_out);
   }
   if (warp == 1) tmem_alloc(smem_addr(tmem_slot), 2 * BN);
   tc_fence_before();
@@ -339,13 +365,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       int stage = 0;
       uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
       bool ok = true;
+      Tile next;
+      bool valid = t_first >= ntiles || decode_tile(p, pref, t_first, next);
       for (int t = t_first; t < ntiles && ok; t += t_step) {
-        Tile tl;
-        if (!decode_tile(p, pref, t, tl)) {
+        if (!valid) {
           set_err(p.err, kErrIndex);
           *abort_flag = 1;
           break;
         }
+        const Tile tl = next;
         // rows of a box past the tile's last row are of no use: leave them out
         const int boxes = (tl.rows + p.a_box - 1) / p.a_box;
         const int c1 = MODE == kSwiGLU ? tl.n * 128 : tl.n * BN;
@@ -373,6 +401,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             stage = 0;
             phase ^= 1u;
           }
+          // (the ring is full: time for the next tile, some 2000 cycles)
+          if (kb == min(kb0 + kStages, kb1) - 1 && t + t_step < ntiles)
+            valid = decode_tile(p, pref, t + t_step, next);
         }
       }
       if (!ok) {
@@ -447,21 +478,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int n = min(kScaleChunk, kb1 - c0);
           ok = __all_sync(0xffffffffu, mbar_wait(&sempty[slot], phase ^ 1u, abort_flag, kWaitNs));
           if (!ok) break;
-          float* to = sc_a + slot * kScaleChunk * BM;
+          float* to = sc_a + slot * kScaleChunk * BM + lane;
+          const uint8_t* from[BM / 32];
+#pragma unroll
+          for (int r = 0; r < BM / 32; ++r)
+            from[r] = p.a_scales + c0 * 4 +
+                      static_cast<int64_t>(tl.row0 + (r * 32 + lane < rows ? r * 32 + lane : 0)) *
+                          p.a_scale_row_bytes;
+          // (four loads in flight; eight spill)
 #pragma unroll 1
-          for (int r = lane; r < BM; r += 32) {
-            const float* from = reinterpret_cast<const float*>(
-                p.a_scales + static_cast<int64_t>(tl.row0 + (r < rows ? r : 0)) *
-                                 p.a_scale_row_bytes) + c0;
+          for (int i = 0; i < n; ++i) {
+            float v[BM / 32];
 #pragma unroll
-            for (int i0 = 0; i0 < kScaleChunk; i0 += 8) {
-              float v[8];
+            for (int r = 0; r < BM / 32; ++r) v[r] = reinterpret_cast<const float*>(from[r])[i];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = i0 + i < n ? from[i0 + i] : 0.f;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) to[(i0 + i) * BM + r] = v[i];
-            }
+            for (int r = 0; r < BM / 32; ++r) to[i * BM + r * 32] = v[r];
           }
+          if (c0 == kb0 && lane == 0) s_tile[slot] = tl;
           if (lane < 2 * n)
             sc_b[slot * kScaleChunk * 2 + lane] = (lane & 1 ? b1 : b0)[c0 + (lane >> 1)];
           __syncwarp();
@@ -476,35 +509,38 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     } else if (warp == 3 && staged) {
       // ---------------- stores of staged tiles ----------------
-      // (a row of 256 columns an instruction, while the next tile is summed)
+      // (while the next tile is summed: boxes of 32 rows, of a group's last rows each
+      // by itself, because another group's follow them)
+      constexpr int kBoxes = MODE == kSwiGLU ? 1 : 4;  // of 128 bytes across
+      constexpr int kEach = MODE == kSwiGLU ? 128 : 64;
       uint32_t phase = 0;
       bool ok = true;
       for (int t = t_first; t < ntiles && ok; t += t_step, phase ^= 1u) {
-        Tile tl;
-        if (!decode_tile(p, pref, t, tl)) break;
-        const int rows = tl.rows;
-        const int cols = min(BN, p.n_out - tl.n * BN);
-        uint16_t* o = static_cast<uint16_t*>(p.out) +
-                      static_cast<int64_t>(tl.row0) * p.ldo + tl.n * BN;
         ok = __all_sync(0xffffffffu, mbar_wait(ofull, phase, abort_flag, kWaitNs));
         if (!ok) break;
-        if (lane * 8 + 8 <= cols) {
+        const Tile tl = *o_tile;
+        const int col0 = tl.n * kBoxes * kEach;
+        const int boxes = p.g.offsets == nullptr ? (tl.rows + 31) / 32 : tl.rows / 32;
+        const int box = lane % kBoxes, first = lane / kBoxes * 32;
+        if (lane < boxes * kBoxes && col0 + box * kEach < p.n_out)
+          tma_store_2d(&map_out, smem_addr(patch + box * kBoxOut + first * 128),
+                       col0 + box * kEach, tl.row0 + first);
+        // (8 lanes across a box)
+        const int r_box = (lane >> 3) % kBoxes, c = col0 + r_box * kEach + (lane & 7) * (kEach / 8);
+        uint8_t* o = static_cast<uint8_t*>(p.out) +
+                     (static_cast<int64_t>(tl.row0) * p.ldo + c) * (128 / kEach);
+        if (c < p.n_out)  // (n_out of groups is a multiple of 64)
 #pragma unroll 4
-          for (int r = 0; r < rows; ++r) {
-            const uint4 v =
-                *reinterpret_cast<const uint4*>(patch + r * 512 + ((lane ^ (r & 7)) << 4));
-            *reinterpret_cast<uint4*>(o + r * p.ldo + lane * 8) = v;
-          }
-        } else if (lane * 8 < cols) {  // the lane with the last columns
-          for (int r = 0; r < rows; ++r) {
-            const uint16_t* v =
-                reinterpret_cast<const uint16_t*>(patch + r * 512 + ((lane ^ (r & 7)) << 4));
-            for (int j = 0; j < cols - lane * 8; ++j) o[r * p.ldo + lane * 8 + j] = v[j];
-          }
-        }
+          for (int r = boxes * 32 + (lane >> 3) / kBoxes; r < tl.rows; r += 4 / kBoxes)
+            *reinterpret_cast<uint4*>(o + r * p.ldo * (128 / kEach)) =
+                *reinterpret_cast<const uint4*>(patch + r_box * kBoxOut + r * 128 +
+                                                (((lane & 7) ^ (r & 7)) << 4));
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive1(smem_addr(oempty));
       }
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       if (!ok && lane == 0) {
         if (!*abort_flag) set_err(p.err, kErrTimeout);
         *abort_flag = 1;
@@ -518,66 +554,66 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int pw = warp - kFirstPromoter;
     const int row = quarter * 32 + lane;
     uint8_t* my_patch = patch + pw * 4096;
-    float* s_max = reinterpret_cast<float*>(patch);  // SwiGLU: [2][2][128] row maxima
+    float* s_max = reinterpret_cast<float*>(patch + kBoxOut);  // SwiGLU: [2][2][128] row maxima
     uint32_t it = 0, red_phase = 0, sc_slot = 0, sc_phase = 0, o_phase = 0;
     uint32_t xt = 0;  // SwiGLU tiles that this quarter has had rows in
     bool ok = true;
     for (int t = t_first; t < ntiles && ok; t += t_step) {
-      Tile tl;
-      if (!decode_tile(p, pref, t, tl)) break;
+      // the tile comes with its first scales (an invalid one does not: abort)
+      ok = __all_sync(0xffffffffu, mbar_wait(&sfull[sc_slot], sc_phase, abort_flag, kWaitNs));
+      if (!ok) break;
+      const Tile tl = s_tile[sc_slot];
       const bool live = quarter * 32 < tl.rows;
       const bool store = row < tl.rows;
       uint64_t acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const int b = it & 1, in = (kb - kb0) & (kScaleChunk - 1);  // place in the chunk
-        if (in == 0 &&
-            !__all_sync(0xffffffffu, mbar_wait(&sfull[sc_slot], sc_phase, abort_flag, kWaitNs))) {
-          ok = false;
-          break;
+      auto scales_done = [&] {
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(&sempty[sc_slot]));
+        sc_slot ^= 1u;
+        if (sc_slot == 0) sc_phase ^= 1u;
+      };
+      int in = 0;  // place in the chunk of scales
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int b = it & 1;
+        if (kb > kb0 && ++in == kScaleChunk) {
+          in = 0;
+          scales_done();
+          ok = __all_sync(0xffffffffu, mbar_wait(&sfull[sc_slot], sc_phase, abort_flag, kWaitNs));
+          if (!ok) break;
         }
-        const float sa_r = sc_a[(sc_slot * kScaleChunk + in) * BM + row];
-        const float2 sb_r =
-            *reinterpret_cast<const float2*>(sc_b + (sc_slot * kScaleChunk + in) * 2);
+        const int at = sc_slot * kScaleChunk + in;
+        const float sa_r = sc_a[at * BM + row];
+        const float2 sb_r = *reinterpret_cast<const float2*>(sc_b + at * 2);
         const float s0 = sa_r * sb_r.x, s1 = sa_r * sb_r.y;
-        if (in == kScaleChunk - 1 || kb + 1 == kb1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive1(smem_addr(&sempty[sc_slot]));
-          sc_slot ^= 1u;
-          if (sc_slot == 0) sc_phase ^= 1u;
-        }
-        if (!__all_sync(0xffffffffu, mbar_wait(&tfull[b], (it >> 1) & 1u, abort_flag, kWaitNs))) {
-          ok = false;
-          break;
-        }
-        if (live) {
-          tc_fence_after();
-          const uint32_t ta = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
-                              static_cast<uint32_t>(b * BN + wg * 64);
-          const uint64_t p0 = pack2(__float_as_uint(s0), __float_as_uint(s0));
-          const uint64_t p1 = pack2(__float_as_uint(s1), __float_as_uint(s1));
-          uint32_t r0[32];
-          tmem_ld32(ta, r0);
-          tmem_ld_wait(r0);
-          scaled_add(acc, r0, p0);
-          tmem_ld32(ta + 32, r0);
-          tmem_ld_wait(r0);
-          scaled_add(acc + 16, r0, p0);
-          tmem_ld32(ta + 128, r0);
-          tmem_ld_wait(r0);
-          scaled_add(acc + 32, r0, p1);
-          tmem_ld32(ta + 160, r0);
-          tmem_ld_wait(r0);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive1(smem_addr(&tempty[b]));
-          scaled_add(acc + 48, r0, p1);
-        } else if (lane == 0) {
-          mbar_arrive1(smem_addr(&tempty[b]));
-        }
+        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[b], (it >> 1) & 1u, abort_flag, kWaitNs));
+        if (!ok) break;
+        const uint32_t ta = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                            static_cast<uint32_t>(b * BN + wg * 64);
+        const uint64_t p0 = pack2(__float_as_uint(s0), __float_as_uint(s0));
+        const uint64_t p1 = pack2(__float_as_uint(s1), __float_as_uint(s1));
+        uint32_t r[32];
+        tc_fence_after();
+        tmem_ld32(ta, r);
+        tmem_ld_wait(r);
+        scaled_add(acc, r, p0);
+        tmem_ld32(ta + 32, r);
+        tmem_ld_wait(r);
+        scaled_add(acc + 16, r, p0);
+        tmem_ld32(ta + 128, r);
+        tmem_ld_wait(r);
+        scaled_add(acc + 32, r, p1);
+        tmem_ld32(ta + 160, r);
+        tmem_ld_wait(r);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(&tempty[b]));
+        ++it;
+        scaled_add(acc + 48, r, p1);
       }
       if (!ok) break;
+      scales_done();
 
       if (SPLIT) {
         // the cluster's accumulators, 32 rows at a time: rows i = rank, rank +
@@ -653,12 +689,53 @@ __global__ void __launch_bounds__(kThreads, 1)
         continue;
       }
 
+      if (MODE == kSwiGLU && live) {
+        // act in place of the gate sums, codes in place of the up sums
+        uint32_t m = 0;
+        const bool in = tl.n * 128 + wg * 64 < p.n_out;  // n_out is a multiple of 64
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float2 g = unpack2(acc[i]), u = unpack2(acc[32 + i]);
+          const float a0 = swiglu(g.x, u.x), a1 = swiglu(g.y, u.y);
+          m = max(m, max(__float_as_uint(a0) & 0x7fffffffu, __float_as_uint(a1) & 0x7fffffffu));
+          acc[i] = pack2(__float_as_uint(a0), __float_as_uint(a1));
+        }
+        if (!in) m = 0;
+        // the row's maximum over both warps.  Two buffers: a warp that is a tile
+        // ahead has seen the other's arrival for this tile, which follows its reads
+        // of the tile before
+        float* mine = s_max + (xt & 1) * 256;
+        mine[wg * 128 + row] = __uint_as_float(m);
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(&xbar[quarter]));
+        ok = __all_sync(0xffffffffu, mbar_wait(&xbar[quarter], xt & 1, abort_flag, kWaitNs));
+        ++xt;
+        if (!ok) break;
+        m = max(m, __float_as_uint(mine[(wg ^ 1) * 128 + row]));
+        const float am = fp8_amax(m), inv = fp8_inverse(am);
+        if (store && wg == 0)
+          *reinterpret_cast<float*>(static_cast<uint8_t*>(p.out) +
+                                    static_cast<int64_t>(tl.row0 + row) * p.ldo +
+                                    p.scale_offset + tl.n * 4) = __fdiv_rn(am, kE4m3Max);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 x0 = unpack2(acc[4 * j]), x1 = unpack2(acc[4 * j + 1]);
+          const float2 x2 = unpack2(acc[4 * j + 2]), x3 = unpack2(acc[4 * j + 3]);
+          acc[32 + j] = pack2(e4m3x4(x0.x * inv, x0.y * inv, x1.x * inv, x1.y * inv),
+                              e4m3x4(x2.x * inv, x2.y * inv, x3.x * inv, x3.y * inv));
+        }
+      }
       if (staged) {
-        // hand the tile to the store warp (16-byte chunks swizzled by the row)
+        // hand the tile to the store warp
         ok = __all_sync(0xffffffffu, mbar_wait(oempty, o_phase ^ 1u, abort_flag, kWaitNs));
         if (!ok) break;
         o_phase ^= 1u;
-        if (live) {
+        if (live && MODE == kSwiGLU) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<ulonglong2*>(patch + row * 128 + (((wg * 4 + j) ^ (row & 7)) << 4)) =
+                make_ulonglong2(acc[32 + 2 * j], acc[33 + 2 * j]);
+        } else if (live) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -670,59 +747,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __nv_bfloat162 b2 = __floats2bfloat162_rn(v.x, v.y);
                 w[i] = *reinterpret_cast<uint32_t*>(&b2);
               }
-              *reinterpret_cast<uint4*>(patch + row * 512 +
-                                        (((h * 16 + wg * 8 + j) ^ (row & 7)) << 4)) =
+              *reinterpret_cast<uint4*>(patch + (h * 2 + wg) * kBoxOut + row * 128 +
+                                        ((j ^ (row & 7)) << 4)) =
                   make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
+        if (threadIdx.x == kFirstPromoter * 32) *o_tile = tl;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive1(smem_addr(ofull));
         continue;
       }
 
       if (!live) continue;
-      if (MODE == kSwiGLU) {
-        // act in place of the gate sums; the row's maximum over both warps
-        uint32_t m = 0;
-        const int col0 = tl.n * 128 + wg * 64;
-        const bool in = col0 < p.n_out;  // n_out is a multiple of 64
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float2 g = unpack2(acc[i]), u = unpack2(acc[32 + i]);
-          const float a0 = swiglu(g.x, u.x), a1 = swiglu(g.y, u.y);
-          m = max(m, max(__float_as_uint(a0) & 0x7fffffffu, __float_as_uint(a1) & 0x7fffffffu));
-          acc[i] = pack2(__float_as_uint(a0), __float_as_uint(a1));
-        }
-        if (!in) m = 0;
-        // two buffers: a warp that is a tile ahead has seen the other's
-        // arrival for this tile, which follows its reads of the tile before
-        float* mine = s_max + (xt & 1) * 256;
-        mine[wg * 128 + row] = __uint_as_float(m);
-        __syncwarp();
-        if (lane == 0) mbar_arrive1(smem_addr(&xbar[quarter]));
-        ok = __all_sync(0xffffffffu, mbar_wait(&xbar[quarter], xt & 1, abort_flag, kWaitNs));
-        ++xt;
-        if (!ok) break;
-        m = max(m, __float_as_uint(mine[(wg ^ 1) * 128 + row]));
-        const float am = fp8_amax(m), inv = fp8_inverse(am);
-        if (store) {
-          uint8_t* o = static_cast<uint8_t*>(p.out) + static_cast<int64_t>(tl.row0 + row) * p.ldo;
-          if (in) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              uint32_t w[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float2 x = unpack2(acc[8 * v + 2 * j]), y = unpack2(acc[8 * v + 2 * j + 1]);
-                w[j] = e4m3x4(x.x * inv, x.y * inv, y.x * inv, y.y * inv);
-              }
-              *reinterpret_cast<uint4*>(o + col0 + 16 * v) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-          }
-          if (wg == 0)
-            reinterpret_cast<float*>(o + p.scale_offset)[tl.n] = __fdiv_rn(am, kE4m3Max);
-        }
-      } else {
+      {
         // fp32, or bf16 rows at any multiple of 2 bytes: 32 columns at a time through
         // a 32-row patch of 128-byte rows (16-byte chunks swizzled by the row), so
         // that a store instruction writes whole lines
@@ -821,6 +859,7 @@ cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
   p.out = a.out;
   p.ldo = a.ldo;
   p.out_f32 = a.out_f32;
+  p.staged = !SPLIT && a.map_out != nullptr;
   p.out_vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
               a.ldo * (a.out_f32 ? 4 : 2) % 16 == 0;
   p.scale_offset = fp8_scale_offset(a.n_out);
@@ -841,7 +880,8 @@ cudaError_t launch_impl(const Fp8GemmArgs& a, cudaStream_t stream) {
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = SPLIT ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, *a.map_a, *a.map_b, p);
+  return cudaLaunchKernelEx(&cfg, kernel, *a.map_a, *a.map_b,
+                            p.staged ? *a.map_out : *a.map_a, p);
 }
 
 }  // namespace
