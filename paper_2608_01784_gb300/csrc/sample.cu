@@ -32,7 +32,9 @@
 //
 // Bound: instruction issue, about 15 instructions a token for weights (fp32 in
 // packed pairs), 8 for counts, against the 12 cycles that HBM gives an SM for 128
-// bf16 tokens.
+// bf16 tokens.  2048 rows of 131072 in bf16 (their bytes take 79 us): greedy 114 us,
+// no filters 199, top-k 50 232, top-p 0.9 540.  One such row: 24 us with every filter,
+// a dozen of the cluster's barriers one after another.
 #include <algorithm>
 #include <type_traits>
 
@@ -500,8 +502,13 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
   const uint4* my_vec = reinterpret_cast<const uint4*>(base + my_pos);
   constexpr int kStepVecs = kStep / kVec;
   // visit(i, z, raw) for the steps from i0 to i1 - 1, `kAhead` loads in flight
-  constexpr int kAhead = kStream ? (sizeof(Te) == 2 ? 4 : 2) : 1;
+  // Streamed bf16: two.  With four the loops outgrow the instruction caches that two
+  // CTAs in different rows' filters share (a quarter of the stalls; 2048 rows of
+  // 131072 without filters 194 us, two 199, top-p 573, 540, mixed filters 414, 341).
+  constexpr int kAhead = kStream && sizeof(Te) == 2 ? 2 : 1;
+  constexpr int kSample = kStream ? 32 / sizeof(Te) / 4 : 1;  // steps that top-k looks at first
   auto each_step = [&](int i0, int i1, auto visit) {
+#pragma unroll 1
     for (int i = i0; i < i1; i += kAhead) {
       uint4 raw[kAhead][kRaw];
       if (kStream && i >= in0 && i + kAhead <= in1) {
@@ -759,20 +766,20 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
       if (same_t) count_pass(std::true_type(), i0, i1);
       else count_pass(std::false_type(), i0, i1);
     };
-    if (kStream && by_k && steps >= 4 * kAhead && top_k < a.vocab / 16) {
+    if (kStream && by_k && steps >= 4 * kSample && top_k < a.vocab / 16) {
       // Top-k of few: the counts of a sample (the first steps of every warp)
       // name the bins that hold three times as many tokens; these make the
       // list, and the other steps are not counted (2048 rows of 131072, top-k
-      // 50: 313 us with counts, 249 us without).  Should the list be too short
+      // 50: 313 us with counts, 232 us without).  Should the list be too short
       // all the same, or too long, the whole row is searched.
-      counts(0, kAhead);
+      counts(0, kSample);
       __syncthreads();
       if (warp == 0) {
         constexpr int kPer = kFine / 32;
         uint32_t n = 0;
         for (int i = 0; i < kPer; ++i) n += s.fine[lane * kPer + i];
         uint32_t upto = warp_before(n);
-        const uint32_t want = 3u * top_k * kAhead / steps + 48;
+        const uint32_t want = 3u * top_k * kSample / steps + 48;
         uint32_t b = kFine - 1;
         for (int i = kPer - 1; i >= 0; --i) {  // the first bin at which `want` is reached
           if (upto + n >= want) b = lane * kPer + i;
@@ -784,12 +791,12 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
       }
       __syncthreads();
       const float flo = key_value<Te>(s.klo);
-      each_step(kAhead, steps, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
+      each_step(kSample, steps, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) add_exp(add2(pk(z[j], z[j + 1]), pk(neg_m, neg_m)));
         enlist(true, flo, m, i, z, raw);
       });
-      each_step(0, kAhead, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
+      each_step(0, kSample, [&](int i, const float (&z)[8], const uint4 (&raw)[kRaw]) {
         enlist(true, flo, m, i, z, raw);
       });
       for (int g = lane; g < segs; g += 32) set_seg(g, 0, 0);
