@@ -8,8 +8,8 @@ import numpy as np
 import torch
 
 from . import _binding as B
-from .fp8 import (ExpertsFp8, LinearFp8, matmul_fp8, quantize_experts,  # noqa: F401
-                  quantize_fp8)
+from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, matmul_fp8,  # noqa: F401
+                  quantize_experts, quantize_fp8)
 
 
 def _dev(a: np.ndarray, device, dtype=None) -> torch.Tensor:
@@ -310,23 +310,22 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor |
     """reflex_sample of logits [rows, vocab] (fp32 or bf16) with uniforms u
     [rows] -> (tokens int32 [rows], conf fp32 [rows]).  Every setting is one
     value per row; rows with masked == 0 get token -1 and confidence 0."""
-    kinds = {torch.float32: B.REFLEX_DTYPE_F32, torch.bfloat16: B.REFLEX_DTYPE_BF16}
-    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in kinds:
-        raise ValueError("logits: a CUDA matrix of fp32 or bf16")
-    rows, vocab = int(logits.shape[0]), int(logits.shape[1])
-    if (vocab > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
-        raise ValueError("logits: rows must be contiguous and must not overlap")
-    tokens = (torch.empty(rows, dtype=torch.int32, device=logits.device)
-              if tokens is None else tokens)
-    conf = torch.empty(rows, dtype=torch.float32, device=logits.device) if conf is None else conf
-    for t, dt, what in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"),
-                        (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
-                        (min_p, torch.float32, "min_p"), (masked, torch.uint8, "masked"),
-                        (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf")):
-        if t is not None and (t.dtype != dt or t.numel() != rows or not t.is_contiguous()
-                              or t.device != logits.device):
+    rows, vocab, ld = _matrix(logits, "logits", _DTYPES)
+    dev = logits.device
+    def check(t, dt, what):
+        if t.dtype != dt or t.numel() != rows or not t.is_contiguous() or t.device != dev:
             raise ValueError(f"{what}: {rows} values of {dt} on the logits' device")
-    ld = int(logits.stride(0)) if rows > 1 else vocab
-    B.reflex_sample(kinds[logits.dtype], logits, ld, rows, vocab, temperature, top_k, top_p, min_p,
+    check(u, torch.float32, "u")
+    for t, dt, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"),
+                        (masked, torch.uint8, "masked"), (tokens, torch.int32, "tokens"),
+                        (conf, torch.float32, "conf")):
+        if t is not None:
+            check(t, dt, what)
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+    if conf is None:
+        conf = torch.empty(rows, dtype=torch.float32, device=dev)
+    B.reflex_sample(_DTYPES[logits.dtype], logits, ld, rows, vocab, temperature, top_k, top_p, min_p,
                     u, masked, tokens, conf, status, stream)
     return tokens, conf

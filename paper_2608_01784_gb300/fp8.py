@@ -21,17 +21,24 @@ def _want(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _rows(t: torch.Tensor, what: str, dtypes) -> torch.Tensor:
-    """A device matrix whose rows are contiguous (any row stride)."""
-    _want(t.is_cuda and t.dim() == 2 and t.dtype in dtypes, f"{what}: a CUDA matrix of " +
-          " or ".join(str(d) for d in dtypes))
-    _want(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
-    _want(t.shape[0] <= 1 or t.stride(0) >= t.shape[1], f"{what}: rows must not overlap")
-    return t
+def _matrix(t: torch.Tensor, what: str, dtypes):
+    """(rows, columns, row stride) of a device matrix whose rows are contiguous,
+    any row stride; of one row, its length."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+        raise ValueError(f"{what}: a CUDA matrix of " + " or ".join(str(d) for d in dtypes))
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
+        raise ValueError(f"{what}: rows must not overlap")
+    return rows, cols, ld
 
 
-def _ld(t: torch.Tensor) -> int:
-    return max(int(t.stride(0)) if t.shape[0] > 1 else 0, int(t.shape[1]))
+_F32 = (torch.float32,)
+_E4M3 = (torch.float8_e4m3fn,)
 
 
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | None = None,
@@ -39,34 +46,39 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
     """reflex_quantize_fp8 of x [rows, cols] (fp32 or bf16) -> (codes [rows,
     cols] float8_e4m3fn, scales [ceil(rows / block_rows), ceil(cols / 128)]).
     New codes have rows on 16-byte boundaries, as the products take them."""
-    _rows(x, "x", _DTYPES)
-    rows, cols = int(x.shape[0]), int(x.shape[1])
+    rows, cols, ldx = _matrix(x, "x", _DTYPES)
     _want(block_rows in (1, 128), "block_rows is 1 or 128")
+    shape = -(-rows // block_rows), _blocks(cols)
     if codes is None:
-        ld = -(-cols // 16) * 16
-        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=x.device)[:, :cols]
+        ldc = -(-cols // 16) * 16
+        codes = torch.empty((rows, ldc), dtype=torch.float8_e4m3fn, device=x.device)
+        if ldc != cols:
+            codes = codes[:, :cols]
+    else:
+        r, c, ldc = _matrix(codes, "codes", _E4M3)
+        _want((r, c) == (rows, cols), "codes: another shape than x")
+        _want(codes.device == x.device, "tensors on several devices")
     if scales is None:
-        scales = torch.empty((-(-rows // block_rows), _blocks(cols)), dtype=torch.float32,
-                             device=x.device)
-    _rows(codes, "codes", (torch.float8_e4m3fn,))
-    _rows(scales, "scales", (torch.float32,))
-    _want(tuple(codes.shape) == (rows, cols), "codes: another shape than x")
-    _want(tuple(scales.shape) == (-(-rows // block_rows), _blocks(cols)), "scales: shape")
-    _want(codes.device == x.device and scales.device == x.device, "tensors on several devices")
-    B.reflex_quantize_fp8(_DTYPES[x.dtype], x, rows, cols, _ld(x), block_rows, codes, _ld(codes),
-                          scales, _ld(scales), stream)
+        scales = torch.empty(shape, dtype=torch.float32, device=x.device)
+        lds = shape[1]
+    else:
+        r, c, lds = _matrix(scales, "scales", _F32)
+        _want((r, c) == shape, "scales: shape")
+        _want(scales.device == x.device, "tensors on several devices")
+    B.reflex_quantize_fp8(_DTYPES[x.dtype], x, rows, cols, ldx, block_rows, codes, ldc, scales,
+                          lds, stream)
     return codes, scales
 
 
-def _code_rows(codes: torch.Tensor, what: str):
-    _rows(codes, what, (torch.float8_e4m3fn,))
-    _want(_code_ld(codes) % 16 == 0 and codes.data_ptr() % 16 == 0,
+def _codes(codes: torch.Tensor, what: str):
+    """(rows, columns, row stride) of codes as the products take them; the stride
+    of a single row is its length in whole 16-byte vectors."""
+    rows, cols, ld = _matrix(codes, what, _E4M3)
+    if rows <= 1:
+        ld = -(-cols // 16) * 16
+    _want(ld % 16 == 0 and codes.data_ptr() % 16 == 0,
           f"{what}: rows start on 16-byte boundaries (as quantize_fp8 lays them out)")
-
-
-def _code_ld(codes: torch.Tensor) -> int:
-    """Row stride; of a single row, its length in whole 16-byte vectors."""
-    return int(codes.stride(0)) if codes.shape[0] > 1 else -(-int(codes.shape[1]) // 16) * 16
+    return rows, cols, ld
 
 
 def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
@@ -74,31 +86,32 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
                status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """reflex_matmul_fp8: A B^T of codes a [M, K] (scales per row and 128
     columns) and b [N, K] (scales per 128 x 128 block) -> [M, N]."""
-    _code_rows(a, "a")
-    _code_rows(b, "b")
-    M, K, N = int(a.shape[0]), int(a.shape[1]), int(b.shape[0])
-    _want(int(b.shape[1]) == K, "a and b disagree on K")
-    _rows(a_scales, "a_scales", (torch.float32,))
-    _rows(b_scales, "b_scales", (torch.float32,))
-    _want(tuple(a_scales.shape) == (M, _blocks(K)), "a_scales: shape")
-    _want(tuple(b_scales.shape) == (_blocks(N), _blocks(K)), "b_scales: shape")
-    out = _output(out, M, N, out_dtype, a.device)
-    B.reflex_matmul_fp8(a, _code_ld(a), a_scales, _ld(a_scales), b, _code_ld(b), b_scales,
-                        _ld(b_scales), M, N, K, _DTYPES[out.dtype], out, _ld(out), status, stream)
+    M, K, lda = _codes(a, "a")
+    N, kb, ldb = _codes(b, "b")
+    _want(kb == K, "a and b disagree on K")
+    ra, ca, ldas = _matrix(a_scales, "a_scales", _F32)
+    rb, cb, ldbs = _matrix(b_scales, "b_scales", _F32)
+    _want((ra, ca) == (M, _blocks(K)), "a_scales: shape")
+    _want((rb, cb) == (_blocks(N), _blocks(K)), "b_scales: shape")
+    out, ldo = _output(out, M, N, out_dtype, a.device)
+    B.reflex_matmul_fp8(a, lda, a_scales, ldas, b, ldb, b_scales, ldbs, M, N, K,
+                        _DTYPES[out.dtype], out, ldo, status, stream)
     return out
 
 
-def _output(out, M: int, N: int, dtype, device) -> torch.Tensor:
+def _output(out, M: int, N: int, dtype, device):
+    """The output (given, or new) and its row stride."""
+    if out is not None:
+        r, c, ldo = _matrix(out, "out", _DTYPES)
+        _want((r, c) == (M, N) and out.device == device, "out: shape or device")
+        return out, ldo
     _want(dtype in _DTYPES, "outputs are fp32 or bf16")
-    if out is None:
-        # rows on 16-byte boundaries, where a row is a few vectors long at least
-        # (999 x 50001 x 2048 to bf16: 105 us, packed rows 236)
-        unit = 16 // dtype.itemsize
-        ld = -(-N // unit) * unit if N >= 4 * unit else N
-        return torch.empty((M, ld), dtype=dtype, device=device)[:, :N]
-    _rows(out, "out", _DTYPES)
-    _want(tuple(out.shape) == (M, N) and out.device == device, "out: shape or device")
-    return out
+    # rows on 16-byte boundaries, where a row is a few vectors long at least
+    # (999 x 50001 x 2048 to bf16: 105 us, packed rows 236)
+    unit = 16 // dtype.itemsize
+    ldo = -(-N // unit) * unit if N >= 4 * unit else N
+    out = torch.empty((M, ldo), dtype=dtype, device=device)
+    return (out if ldo == N else out[:, :N]), ldo
 
 
 class LinearFp8:
@@ -108,30 +121,27 @@ class LinearFp8:
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, *, max_rows: int,
                  out_dtype: torch.dtype = torch.bfloat16):
-        _code_rows(codes, "codes")
-        _rows(scales, "scales", (torch.float32,))
         self.codes, self.scales = codes, scales
-        self.N, self.K = int(codes.shape[0]), int(codes.shape[1])
-        _want(tuple(scales.shape) == (_blocks(self.N), _blocks(self.K)), "scales: shape")
+        self.N, self.K, self._w_ld = _codes(codes, "codes")
+        r, c, self._s_ld = _matrix(scales, "scales", _F32)
+        _want((r, c) == (_blocks(self.N), _blocks(self.K)), "scales: shape")
         _want(out_dtype in _DTYPES, "outputs are fp32 or bf16")
         self.max_rows, self.out_dtype = max_rows, out_dtype
         self.ws_bytes = B.reflex_linear_fp8_workspace_size(max_rows, self.K)
         _want(self.ws_bytes > 0, "unsupported shape")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=codes.device)
-        self._w_ld, self._s_ld = _code_ld(codes), _ld(scales)
 
     def forward(self, x: torch.Tensor, out: torch.Tensor | None = None, stream=None,
                 check: bool = True) -> torch.Tensor:
         """x [M, K] fp32 or bf16 -> [M, N] of the layer's output type (or out's)."""
-        _rows(x, "x", _DTYPES)
-        M = int(x.shape[0])
-        _want(int(x.shape[1]) == self.K, "x: another number of columns than the weights")
-        _want(x.device == self.codes.device, "x is on another device than the weights")
+        M, K, ldx = _matrix(x, "x", _DTYPES)
+        _want(K == self.K, "x: another number of columns than the weights")
+        _want(x.device == self.ws.device, "x is on another device than the weights")
         _want(M <= self.max_rows, "more rows than the workspace was sized for")
-        out = _output(out, M, self.N, self.out_dtype, x.device)
-        B.reflex_linear_fp8(_DTYPES[x.dtype], x, _ld(x), self.codes, self._w_ld, self.scales,
-                            self._s_ld, M, self.N, self.K, _DTYPES[out.dtype], out, _ld(out),
-                            self.ws, self.ws_bytes, stream, check)
+        out, ldo = _output(out, M, self.N, self.out_dtype, x.device)
+        B.reflex_linear_fp8(_DTYPES[x.dtype], x, ldx, self.codes, self._w_ld, self.scales,
+                            self._s_ld, M, self.N, K, _DTYPES[out.dtype], out, ldo, self.ws,
+                            self.ws_bytes, stream, check)
         return out
 
     def status(self, stream=None) -> int:
