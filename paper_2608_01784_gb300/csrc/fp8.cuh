@@ -85,8 +85,9 @@ inline int64_t fp8_packed_bytes(int64_t cols) {
 struct Fp8GemmArgs {
   const CUtensorMap* map_a;  // A codes [rows, K]: boxes of {128, a_box}
   const CUtensorMap* map_b;  // B codes {K, rows of a group, groups}: {128, 128, 1}
-  // out, boxes of 32 rows x 128 bytes (bf16: 64 columns, act codes: 128), where its rows
-  // lie on 16-byte boundaries and it is not fp32 or split; else null
+  // out, boxes of 32 rows x 128 bytes (bf16: 64 columns, act codes: 128) over the columns
+  // up to the last whole multiple of 8, where its rows lie on 16-byte boundaries and it is
+  // not fp32 or split; else null
   const CUtensorMap* map_out = nullptr;
   int K;
   int n_out;  // columns of out per group (SwiGLU: inter)

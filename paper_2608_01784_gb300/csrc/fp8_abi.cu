@@ -49,7 +49,7 @@ bool code_map(CUtensorMap* m, const void* base, int64_t groups, int64_t rows, in
 }
 
 // Rows of out as the kernel stores them, 32 x 128 bytes at a time with the same
-// swizzle.
+// swizzle; rows of whole 16-byte vectors.
 bool out_map(CUtensorMap* m, void* base, bool bf16, int64_t rows, int64_t cols, int64_t row_bytes) {
   auto fn = rx::tensor_map_encoder();
   if (fn == nullptr) return false;
@@ -104,8 +104,8 @@ int matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t a_sca
   g.err = err;
   g.num_sms = sms;
   CUtensorMap mo;
-  if (g.splits == 1 && !g.out_f32 && aligned(out, 16) && ldo % 8 == 0) {
-    if (!out_map(&mo, out, true, M, N, ldo * 2)) return REFLEX_ECUDA;
+  if (g.splits == 1 && !g.out_f32 && aligned(out, 16) && ldo % 8 == 0 && N >= 8) {
+    if (!out_map(&mo, out, true, M, N / 8 * 8, ldo * 2)) return REFLEX_ECUDA;
     g.map_out = &mo;
   }
   RX_CUDA(rx::launch_fp8_matmul(g, s));

@@ -513,6 +513,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       // by itself, because another group's follow them)
       constexpr int kBoxes = MODE == kSwiGLU ? 1 : 4;  // of 128 bytes across
       constexpr int kEach = MODE == kSwiGLU ? 128 : 64;
+      // the map ends with the last whole 16 bytes of a row: a box is clipped in units of
+      // these, and would write over what follows the row
+      const int whole_cols = p.n_out & ~7;
       uint32_t phase = 0;
       bool ok = true;
       for (int t = t_first; t < ntiles && ok; t += t_step, phase ^= 1u) {
@@ -522,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int col0 = tl.n * kBoxes * kEach;
         const int boxes = p.g.offsets == nullptr ? (tl.rows + 31) / 32 : tl.rows / 32;
         const int box = lane % kBoxes, first = lane / kBoxes * 32;
-        if (lane < boxes * kBoxes && col0 + box * kEach < p.n_out)
+        if (lane < boxes * kBoxes && col0 + box * kEach < whole_cols)
           tma_store_2d(&map_out, smem_addr(patch + box * kBoxOut + first * 128),
                        col0 + box * kEach, tl.row0 + first);
         // (8 lanes across a box)
@@ -535,6 +538,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             *reinterpret_cast<uint4*>(o + r * p.ldo * (128 / kEach)) =
                 *reinterpret_cast<const uint4*>(patch + r_box * kBoxOut + r * 128 +
                                                 (((lane & 7) ^ (r & 7)) << 4));
+        const int at = whole_cols - col0;  // the row's last columns, fewer than eight
+        if (MODE == kMatmul && whole_cols < p.n_out && at < BN) {
+          for (int r = lane; r < tl.rows; r += 32) {
+            const uint16_t* from = reinterpret_cast<const uint16_t*>(
+                patch + (at >> 6) * kBoxOut + r * 128 + (((at >> 3 & 7) ^ (r & 7)) << 4));
+            uint16_t* to = static_cast<uint16_t*>(p.out) + (tl.row0 + r) * p.ldo + whole_cols;
+            for (int j = 0; j < p.n_out - whole_cols; ++j) to[j] = from[j];
+          }
+        }
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();

@@ -1,0 +1,122 @@
+"""The 8-bit products where their kernels change over: few rows, split K, edges of
+the boxes that tiles are stored in, groups around them, rows far apart."""
+import pytest
+import torch
+
+from paper_2608_01784_gb300 import _binding as B
+from paper_2608_01784_gb300 import api
+from tests.test_gpu_fp8 import (BF16, E4M3, F32, check_experts, check_product, codes_of, experts64,
+                                experts_layer, normal, product_bound, same_codes)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("n", [1, 3, 5, 130])
+@pytest.mark.parametrize("k", [1, 15, 16, 511, 513, 2048, 4100, 16384, 16400])
+def test_few_rows(n, k, dtype, out_dtype):
+    w, ws = api.quantize_fp8(normal(n + k, n, k, std=0.02), 128)
+    x = normal(k, 5, k, dtype=dtype)
+    codes, scales = codes_of(x, 1)
+    ref, bound = product_bound(codes.cuda(), scales.cuda(), w, ws)
+    lin = api.LinearFp8(w, ws, max_rows=5)
+    whole = torch.full((5, n + 1), 7.0, dtype=out_dtype, device="cuda")  # rows off 4 bytes
+    for m in range(1, 6):
+        lin.forward(x[:m], out=whole[:m, 1:])
+        check_product(whole[:m, 1:], ref[:m], bound[:m], out_dtype == F32)
+        assert bool((whole[:, 0] == 7.0).all()) and bool((whole[m:] == 7.0).all())
+        assert lin.status() == B.REFLEX_OK
+
+
+@pytest.mark.parametrize("m", [1, 31, 32, 33, 128, 129, 161, 256])
+@pytest.mark.parametrize("n", [8, 63, 64, 72, 130, 200, 257, 264])
+def test_edges_of_stored_boxes(m, n):
+    """bf16 rows on 16-byte boundaries: nothing outside [m, n] is written."""
+    k = 200
+    a, sa = api.quantize_fp8(normal(m, m, k))
+    b, sb = api.quantize_fp8(normal(n, n, k, std=0.05), 128)
+    whole = torch.full((m + 40, -(-n // 8) * 8 + 16), 7.0, dtype=BF16, device="cuda")
+    out = api.matmul_fp8(a, sa, b, sb, out=whole[2:m + 2, 8:n + 8])
+    check_product(out, *product_bound(a, sa, b, sb), False)
+    out.fill_(7.0)
+    assert bool((whole == 7.0).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(8, 1024, 8192), (33, 256, 8300), (128, 1000, 8192),
+                                   (300, 300, 8320), (5, 5000, 1024), (32, 777, 1500)])
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+def test_shared_tiles_of_long_rows(m, n, k, out_dtype):
+    a, sa = api.quantize_fp8(normal(m, m, k))
+    b, sb = api.quantize_fp8(normal(n, n, k, std=0.05), 128)
+    ref, bound = product_bound(a, sa, b, sb)
+    whole = torch.full((m, n + 3), 7.0, dtype=out_dtype, device="cuda")
+    check_product(api.matmul_fp8(a, sa, b, sb, out=whole[:, :n]), ref, bound, out_dtype == F32)
+    assert bool((whole[:, n:] == 7.0).all())
+    out = api.matmul_fp8(a, sa, b, sb, out_dtype=out_dtype)
+    check_product(out, ref, bound, out_dtype == F32)
+    assert torch.equal(out, whole[:, :n])
+
+
+@pytest.mark.parametrize("n", [7, 31, 33, 5001])
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+def test_new_outputs_have_aligned_rows(n, out_dtype):
+    w, ws = api.quantize_fp8(normal(n, n, 300, std=0.05), 128)
+    x = normal(1, 40, 300, dtype=BF16)
+    lin = api.LinearFp8(w, ws, max_rows=40, out_dtype=out_dtype)
+    out = lin.forward(x)
+    assert out.shape == (40, n) and out.dtype == out_dtype
+    unit = 16 // out.element_size()
+    assert out.stride(0) % unit == 0 if n >= 4 * unit else out.stride(0) == n
+    packed = torch.empty((40, n), dtype=out_dtype, device="cuda")
+    assert torch.equal(lin.forward(x, packed), out)
+
+
+@pytest.mark.parametrize("inter", [64, 192, 256])
+def test_groups_of_any_size(inter):
+    """Pairs of an expert just below, at and above the stored boxes and the tiles."""
+    sizes = [0, 1, 31, 32, 33, 63, 64, 65, 127, 0, 128, 129, 159, 160, 161, 255, 256, 257, 300, 0]
+    E, d = len(sizes), 256
+    ids = torch.repeat_interleave(torch.arange(E), torch.tensor(sizes)).int()
+    T = ids.numel()
+    ids = ids[torch.randperm(T, generator=torch.Generator().manual_seed(inter))].cuda()[:, None]
+    alpha = normal(3, T, 1).abs()
+    k = torch.ones(T, dtype=torch.int32, device="cuda")
+    w = experts_layer(inter, d, E, inter)
+    h = normal(4, T, d, dtype=BF16)
+    op = api.ExpertsFp8(w, d=d, E=E, inter=inter, k_max=1, max_tokens=T)
+    out = op.forward(h, ids.contiguous(), alpha, k)
+    assert op.status() == B.REFLEX_OK
+    check_experts(out, experts64(h, ids, alpha, w, inter))
+
+
+def far(rows, cols, dtype):
+    """Rows further apart than 32 bits of bytes reach."""
+    ld = (1 << 31) // torch.empty((), dtype=dtype).element_size() + 16
+    return torch.empty(rows * ld, dtype=dtype, device="cuda").as_strided((rows, cols), (ld, 1))
+
+
+def test_rows_far_apart():
+    m, n, k = 3, 300, 200
+    x = far(m, k, BF16)
+    x.copy_(normal(1, m, k))
+    a, sa = api.quantize_fp8(x, 1, far(m, k, E4M3), far(m, 2, F32))
+    want, scales = api.quantize_fp8(x.contiguous())
+    assert same_codes(a, want) and torch.equal(sa, scales)
+    b, sb = api.quantize_fp8(normal(2, n, k, std=0.05), 128)
+    ref, bound = product_bound(want, scales, b, sb)
+    for out_dtype in (F32, BF16):
+        check_product(api.matmul_fp8(a, sa, b, sb, out=far(m, n, out_dtype)), ref, bound,
+                      out_dtype == F32)
+    lin = api.LinearFp8(b, sb, max_rows=m)
+    check_product(lin.forward(x, far(m, n, BF16)), ref, bound, False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logits_far_apart(dtype):
+    z = far(3, 1000, dtype)
+    z.copy_(normal(5, 3, 1000, std=3.0))
+    u = torch.tensor([0.1, 0.5, 0.9], device="cuda")
+    top = torch.full((3,), 40, dtype=torch.int32, device="cuda")
+    for kw in ({}, dict(top_k=top)):
+        got, want = api.sample(z, u, **kw), api.sample(z.contiguous(), u, **kw)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
