@@ -6,7 +6,7 @@ import torch
 from paper_2608_01784_gb300 import _binding as B
 from paper_2608_01784_gb300 import api
 from tests.test_gpu_fp8 import (BF16, E4M3, F32, check_experts, check_product, codes_of, experts64,
-                                experts_layer, normal, product_bound, same_codes)
+                                experts_layer, normal, product_bound, routing, same_codes)
 
 pytestmark = pytest.mark.gpu
 
@@ -120,3 +120,40 @@ def test_logits_far_apart(dtype):
     for kw in ({}, dict(top_k=top)):
         got, want = api.sample(z, u, **kw), api.sample(z.contiguous(), u, **kw)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 100), (2, 300, 17), (40, 300, 1000), (200, 130, 77),
+                                   (33, 64, 8201)])
+def test_what_follows_a_row_is_not_read(m, n, k):
+    """NaN codes between the rows of A and B, and in a workspace used before."""
+    def spread(codes):
+        wide = torch.full((codes.shape[0], -(-k // 16) * 16 + 16), 0x7f, dtype=torch.uint8,
+                          device="cuda")
+        wide[:, :k] = codes.view(torch.uint8)
+        return wide.view(E4M3)[:, :k]
+    x = normal(m, m, k)
+    a, sa = api.quantize_fp8(x)
+    b, sb = api.quantize_fp8(normal(n, n, k, std=0.05), 128)
+    ref, bound = product_bound(a, sa, b, sb)
+    wide = spread(b)
+    check_product(api.matmul_fp8(spread(a), sa, wide, sb, out_dtype=F32), ref, bound, True)
+    lin = api.LinearFp8(wide, sb, max_rows=m, out_dtype=F32)
+    lin.ws.fill_(0x7f)
+    check_product(lin.forward(x), ref, bound, True)
+    assert lin.status() == B.REFLEX_OK
+
+
+@pytest.mark.parametrize("T,d,E,inter,k_max", [(1, 64, 4, 64, 2), (70, 320, 6, 192, 4),
+                                               (900, 256, 5, 128, 3)])
+def test_experts_whatever_the_workspace_holds(T, d, E, inter, k_max):
+    w = experts_layer(T, d, E, inter)
+    h = normal(2, T, d, dtype=BF16)
+    ids, alpha, k = routing(T, T, E, k_max)
+    op = api.ExpertsFp8(w, d=d, E=E, inter=inter, k_max=k_max, max_tokens=T)
+    outs = []
+    for byte in (0x00, 0x7f, 0xff):
+        op.ws.fill_(byte)
+        outs.append(op.forward(h, ids, alpha, k))
+        assert op.status() == B.REFLEX_OK
+    check_experts(outs[0], experts64(h, ids, alpha, w, inter))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
