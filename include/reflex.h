@@ -493,8 +493,9 @@ int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* 
  *                  shapes that are not supported), 256-B aligned; reads as
  *                  reflex_moe_forward's with reflex_moe_status.
  *   out            [T, d] bf16.
- * hidden, out and the codes start on 16-byte boundaries.  Shape rules: d % 64
- * == 0, inter % 64 == 0, 1 <= E <= 1024, 1 <= k_max <= 32, T >= 0.
+ * hidden, out and the codes start on 16-byte boundaries.  A few pairs (chosen
+ * from T, k_max, d and inter) are summed in another order than more.  Shape
+ * rules: d % 64 == 0, inter % 64 == 0, 1 <= E <= 1024, 1 <= k_max <= 32, T >= 0.
  */
 size_t reflex_experts_fp8_workspace_size(int32_t T, int32_t d, int32_t E, int32_t inter,
                                          int32_t k_max);

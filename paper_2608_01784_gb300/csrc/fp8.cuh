@@ -36,6 +36,11 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return lo | hi << 16;
 }
 
+// silu(g) u
+__device__ __forceinline__ float swiglu(float g, float u) {
+  return __fdividef(g, 1.0f + __expf(-g)) * u;
+}
+
 // Rows to codes and scales.  The scale of row r, group g lies at scales +
 // r * scale_row_bytes + 4 g.  The first CTA clears the zero words and, with
 // k, flags counts outside [1, k_most] in err.
@@ -73,6 +78,27 @@ struct Fp8LinearRows {
 bool linear_rows_fit(int M, int N, int K);
 cudaError_t launch_linear_rows(int dtype, const void* x, const Fp8LinearRows& p, int num_sms,
                                cudaStream_t stream);
+
+// The routed experts for few pairs, in two launches (fp8_gemv.cu).
+struct Fp8ExpertsRows {
+  const __nv_bfloat16* hidden;
+  const int32_t* ids;
+  const float* alpha;
+  const int32_t* k;
+  const uint8_t* w_gate_up;
+  const float* gate_up_scales;
+  const uint8_t* w_down;
+  const float* down_scales;
+  int T, d, E, inter, k_max, k_most;
+  int residual;
+  float* act;  // [T k_max, inter]
+  __nv_bfloat16* out;
+  ZeroWords zero;
+  uint32_t* err;
+};
+constexpr int kFp8ExpertsRowsSlots = 128;  // the most slots (T k_max) it serves
+bool experts_rows_fit(int T, int k_max, int d, int inter);
+cudaError_t launch_experts_rows(const Fp8ExpertsRows& p, cudaStream_t stream);
 
 // A row of codes with its scales behind it, in one piece that a row copy of
 // 16-byte vectors moves: codes [cols], scales from the next multiple of 4.

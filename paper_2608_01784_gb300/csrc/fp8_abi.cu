@@ -139,7 +139,7 @@ LinearLayout linear_layout(int64_t M, int64_t K) {
 
 struct ExpertsLayout {
   size_t hdr, x, blk_count, blk_mask, blk_off, counts, offsets, mt_prefix, mt2_prefix, perm,
-      row_of, xperm, act, y, total;
+      row_of, xperm, act, y, act_rows, total;
   int64_t cap, x_bytes, act_bytes;
 };
 ExpertsLayout experts_layout(int32_t T, int32_t d, int32_t E, int32_t inter, int32_t k_max) {
@@ -168,6 +168,7 @@ ExpertsLayout experts_layout(int32_t T, int32_t d, int32_t E, int32_t inter, int
   L.xperm = take(L.cap * L.x_bytes);
   L.act = take(L.cap * L.act_bytes);
   L.y = take(L.cap * d * 2);
+  L.act_rows = take(std::min<int64_t>(L.cap, rx::kFp8ExpertsRowsSlots) * inter * 4);
   L.total = o;
   return L;
 }
@@ -296,6 +297,19 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
       !aligned(w_down, 16) || !aligned(ids, 4) || !aligned(alpha, 4) || !aligned(k, 4) ||
       !aligned(gate_up_scales, 4) || !aligned(down_scales, 4))
     return REFLEX_EINVAL;
+  rx::ZeroWords zero;
+  zero.words = reinterpret_cast<uint32_t*>(hdr);
+  zero.n = static_cast<int>(sizeof(WsHeader) / 4);
+  const int k_most = k_max < E ? k_max : E;
+  if (rx::experts_rows_fit(T, k_max, d, inter)) {
+    const rx::Fp8ExpertsRows p{static_cast<const __nv_bfloat16*>(hidden), ids, alpha, k, w_gate_up,
+                               gate_up_scales, w_down, down_scales, T, d, E, inter, k_max, k_most,
+                               (flags & REFLEX_FLAG_RESIDUAL) != 0,
+                               reinterpret_cast<float*>(ws + L.act_rows),
+                               static_cast<__nv_bfloat16*>(out), zero, &hdr->err};
+    RX_CUDA(rx::launch_experts_rows(p, s));
+    return REFLEX_OK;
+  }
   if (rx::tensor_map_encoder() == nullptr) return REFLEX_ECUDA;
   const int sms = rx::device_sms();
   const int cap = static_cast<int>(L.cap);
@@ -305,11 +319,10 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   // rows to codes once per token; the dispatch copies packed rows, half of
   // the bytes of bf16 ones
   rx::Fp8Rows q{T, d, d, ws + L.x, L.x_bytes, ws + L.x + rx::fp8_scale_offset(d), L.x_bytes, {}};
-  q.zero.words = reinterpret_cast<uint32_t*>(hdr);
-  q.zero.n = static_cast<int>(sizeof(WsHeader) / 4);
+  q.zero = zero;
   q.k = k;
   q.n_k = T;
-  q.k_most = k_max < E ? k_max : E;
+  q.k_most = k_most;
   q.err = err;
   RX_CUDA(rx::launch_quantize_rows(REFLEX_DTYPE_BF16, hidden, q, sms, s));
   rx::DispatchBufs b{I32(L.blk_count), I32(L.blk_off),    I32(L.counts), I32(L.offsets),

@@ -275,11 +275,6 @@ __device__ __forceinline__ const float* b_scale_row(const Params& p, int mode, c
   return p.b_scales + tl.e * p.b_scale_group + block * p.b_scale_ld;
 }
 
-// silu(g) u
-__device__ __forceinline__ float swiglu(float g, float u) {
-  return __fdividef(g, 1.0f + __expf(-g)) * u;
-}
-
 template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
     fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a,

@@ -1,14 +1,17 @@
-// fp8_gemv.cu — the dense layer of reflex_linear_fp8 for one to four rows:
-// x quantised, then multiplied with e4m3 weights, in one launch.
+// fp8_gemv.cu — 8-bit products of a few rows without the tensor cores: the dense
+// layer of reflex_linear_fp8 for one to four rows in one launch, and the routed
+// experts of reflex_experts_fp8 for a few pairs in two.
 //
 // Bound: the weights' bytes (65536 x 2048, one row: 27 us, 73 % of the measured
-// copy rate; 4096 x 2048: 4.8 us, of which the bytes take 1.2 and one launch, one
-// trip to HBM and the quantisation the rest).  A warp takes four rows of the weights at a time and 512 columns a step,
-// 16 bytes of each row a lane, so a step has 2 KB in flight and x is read from
-// shared memory once for four rows.  Every CTA quantises x by itself (the codes
-// of reflex_quantize_fp8 bit for bit): a second launch would take longer.  The 16
-// products of a lane lie in one block of K: they are summed in fp32, scaled once
-// by the weights' scale (x's scale is in x), and the lanes' sums added at the end.
+// copy rate) and, when they are few, launches and trips to HBM (4096 x 2048: 4.8 us,
+// of which the bytes take 1.2; one token of 64 experts of 1024 18 us, 6).
+// A warp takes four rows of the weights (experts: eight) at a time and 512 columns a
+// step, 16 bytes of each row a lane, two steps in flight, and the rows of x are read
+// from shared memory once for all of them.  Every CTA quantises its rows of x by
+// itself (the codes of reflex_quantize_fp8 bit for bit): a launch more would take
+// longer.  The 16 products of a lane lie in one block of K: they are summed in fp32,
+// scaled once by the weights' scale (x's scale is in x), and the lanes' sums added
+// at the end.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
@@ -40,6 +43,29 @@ __device__ __forceinline__ int place(int k) {
   return (k >> 9) * kChunk + ((k >> 2) & 3) * 128 + ((k >> 4) & 31) * 4 + (k & 3);
 }
 
+// 256 columns of a row (8 a lane, from c on) as the values of their codes, 16 lanes
+// a group of 128 as in the quantisation kernel.
+template <typename Te>
+__device__ __forceinline__ void quantise_pair(const Te* row, int c, int K, float* xs) {
+  float f[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f[i] = c + i < K ? to_f32(row[c + i]) : 0.f;
+    top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float a = fp8_amax(top), inv = fp8_inverse(a), s = __fdiv_rn(a, kE4m3Max);
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const uint32_t q = e4m3x4(f[i] * inv, f[i + 1] * inv, f[i + 2] * inv, f[i + 3] * inv);
+    const float2 lo = e4m3x2(q & 0xffffu), hi = e4m3x2(q >> 16);
+    *reinterpret_cast<float4*>(xs + place(c + i)) =
+        make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+  }
+}
+
 template <typename Te, int M>
 __global__ void __launch_bounds__(kThreads)
     linear_rows_kernel(const Te* __restrict__ x, int64_t ldx, const uint8_t* __restrict__ w,
@@ -51,28 +77,10 @@ __global__ void __launch_bounds__(kThreads)
   if (blockIdx.x == 0) clear_words(zero);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = (K + kChunk - 1) / kChunk, row_floats = chunks * kChunk;
-  // x: 16 lanes a group of 128, as the quantisation kernel
   const int pairs = row_floats / 256;
   for (int u = warp; u < M * pairs; u += kWarps) {
-    const int m = u / pairs, c = (u - m * pairs) * 256 + lane * 8;
-    const Te* row = x + m * ldx;
-    float f[8];
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f[i] = c + i < K ? to_f32(row[c + i]) : 0.f;
-      top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-    }
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float a = fp8_amax(top), inv = fp8_inverse(a), s = __fdiv_rn(a, kE4m3Max);
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      const uint32_t q = e4m3x4(f[i] * inv, f[i + 1] * inv, f[i + 2] * inv, f[i + 3] * inv);
-      const float2 lo = e4m3x2(q & 0xffffu), hi = e4m3x2(q >> 16);
-      *reinterpret_cast<float4*>(xs + m * row_floats + place(c + i)) =
-          make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
-    }
+    const int m = u / pairs;
+    quantise_pair(x + m * ldx, (u - m * pairs) * 256 + lane * 8, K, xs + m * row_floats);
   }
   __syncthreads();
 
@@ -158,6 +166,177 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
+// ---- routed experts, few pairs ------------------------------------------------
+// kAhead steps of R rows of a matrix, K a multiple of 16: their loads, then their
+// products with xs.
+template <int R>
+struct Steps {
+  uint4 q[kAhead][R];
+  float s[kAhead][R / 4];  // scales of the first rows of each four (blocks of 128)
+};
+template <int R>
+__device__ __forceinline__ void load_steps(Steps<R>& v, const uint8_t* const (&rows)[R],
+                                           const float* const (&sc)[R / 4], int c0, int K) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) {
+    const bool in = (c0 + a) * kChunk + lane * 16 < K;
+#pragma unroll
+    for (int g = 0; g < R / 4; ++g) v.s[a][g] = in ? sc[g][(c0 + a) * (kChunk / 128)] : 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      v.q[a][r] = in ? __ldcs(reinterpret_cast<const uint4*>(rows[r] + (c0 + a) * kChunk))
+                     : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+template <int R>
+__device__ __forceinline__ void add_steps(const Steps<R>& v, const float* xs, int c0, int chunks,
+                                          float (&acc)[R]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) {
+    if (c0 + a >= chunks) break;
+    float2 sum[R] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 x =
+          *reinterpret_cast<const float4*>(xs + (c0 + a) * kChunk + j * 128 + lane * 4);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const uint4& q = v.q[a][r];
+        const uint32_t word = j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w;
+        fma2(sum[r], e4m3x2(word & 0xffffu), make_float2(x.x, x.y));
+        fma2(sum[r], e4m3x2(word >> 16), make_float2(x.z, x.w));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = fmaf(sum[r].x + sum[r].y, v.s[a][r / 4], acc[r]);
+  }
+}
+template <int R>
+__device__ __forceinline__ void sum_lanes(float (&acc)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+}
+
+// act of one slot (token, j): a warp takes four columns (four gate and four up rows).
+// Every CTA quantises its token.
+__global__ void __launch_bounds__(kThreads) experts_up_rows_kernel(const Fp8ExpertsRows p) {
+  extern __shared__ __align__(16) float xs[];
+  grid_dep_wait();
+  grid_dep_launch();
+  if (blockIdx.x == 0 && blockIdx.y == 0) {
+    clear_words(p.zero);
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.T * p.k_max; i += kThreads) {
+      const int t = i / p.k_max, j = i - t * p.k_max, k = p.k[t];
+      if (k < 1 || k > p.k_most) set_err(p.err, kErrKRange);
+      if (j < min(max(k, 1), p.k_most) && (p.ids[i] < 0 || p.ids[i] >= p.E))
+        set_err(p.err, kErrIndex);
+    }
+  }
+  const int slot = blockIdx.y, t = slot / p.k_max;
+  const int e = p.ids[slot];
+  if (slot - t * p.k_max >= min(max(p.k[t], 1), p.k_most) || e < 0 || e >= p.E) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int col = blockIdx.x * (4 * kWarps) + warp * 4;
+  const bool on = col < p.inter;  // inter is a multiple of 64
+  const int chunks = (p.d + kChunk - 1) / kChunk;
+  const int kb = (p.d + 127) / 128, ib = (p.inter + 127) / 128;
+  const uint8_t* rows[8];
+  const float* sc[2];
+  Steps<8> v;
+  if (on) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      rows[r] = p.w_gate_up +
+                ((2 * static_cast<int64_t>(e) + (r >> 2)) * p.inter + col + (r & 3)) * p.d +
+                lane * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sc[h] = p.gate_up_scales +
+              ((2 * static_cast<int64_t>(e) + h) * ib + col / 128) * kb + (lane >> 3);
+    load_steps(v, rows, sc, 0, p.d);
+  }
+  for (int u = warp; u < chunks * kChunk / 256; u += kWarps)
+    quantise_pair(p.hidden + static_cast<int64_t>(t) * p.d, u * 256 + lane * 8, p.d, xs);
+  __syncthreads();
+  if (!on) return;
+  float acc[8] = {};
+  for (int c0 = 0; c0 < chunks; c0 += kAhead) {
+    if (c0 > 0) load_steps(v, rows, sc, c0, p.d);
+    add_steps(v, xs, c0, chunks, acc);
+  }
+  sum_lanes(acc);
+  float mine = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (lane == i) mine = swiglu(acc[i], acc[4 + i]);
+  if (lane < 4) p.act[static_cast<int64_t>(slot) * p.inter + col + lane] = mine;
+}
+
+// out of one token, eight columns a CTA: a warp takes a slot's product (its act
+// quantised by the warp itself), and the slots are added in order.
+__global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8ExpertsRows p) {
+  extern __shared__ __align__(16) float xs[];  // [kWarps][chunks * kChunk]
+  __shared__ float y[32][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t = blockIdx.y, n0 = blockIdx.x * 8;
+  const int chunks = (p.inter + kChunk - 1) / kChunk;
+  const int ib = (p.inter + 127) / 128, db = (p.d + 127) / 128;
+  const int kt = min(max(p.k[t], 1), p.k_most);
+  float* my_xs = xs + warp * chunks * kChunk;
+  const int32_t* ids = p.ids + t * p.k_max;
+  bool waited = false;
+  for (int j = warp; j < kt; j += kWarps) {
+    const int e = ids[j];
+    if (e < 0 || e >= p.E) {
+      if (lane < 8) y[j][lane] = 0.f;
+      continue;
+    }
+    const uint8_t* rows[8];
+    const float* sc[2];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      rows[r] = p.w_down + (static_cast<int64_t>(e) * p.d + n0 + r) * p.inter + lane * 16;
+    sc[0] = sc[1] = p.down_scales + (static_cast<int64_t>(e) * db + n0 / 128) * ib + (lane >> 3);
+    Steps<8> v;
+    load_steps(v, rows, sc, 0, p.inter);
+    // the weights are not the launch's before: only act waits for it
+    if (!waited) grid_dep_wait();
+    waited = true;
+    const float* act = p.act + (static_cast<int64_t>(t) * p.k_max + j) * p.inter;
+    for (int u = 0; u < chunks * kChunk / 256; ++u)
+      quantise_pair(act, u * 256 + lane * 8, p.inter, my_xs);
+    __syncwarp();
+    float acc[8] = {};
+    for (int c0 = 0; c0 < chunks; c0 += kAhead) {
+      if (c0 > 0) load_steps(v, rows, sc, c0, p.inter);
+      add_steps(v, my_xs, c0, chunks, acc);
+    }
+    sum_lanes(acc);
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (lane == r) y[j][r] = __bfloat162float(__float2bfloat16_rn(acc[r]));
+  }
+  if (!waited) grid_dep_wait();
+  grid_dep_launch();
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    float sum = 0.f;
+    for (int j = 0; j < kt; ++j) {
+      const int e = ids[j];
+      if (e >= 0 && e < p.E) sum = fmaf(p.alpha[t * p.k_max + j], y[j][threadIdx.x], sum);
+    }
+    const int64_t at = static_cast<int64_t>(t) * p.d + n0 + threadIdx.x;
+    if (p.residual) sum += __bfloat162float(p.hidden[at]);
+    p.out[at] = __float2bfloat16_rn(sum);
+  }
+}
+
 template <typename Te, int M>
 cudaError_t launch_m(const Te* x, const Fp8LinearRows& p, int num_sms, cudaStream_t stream) {
   auto kernel = linear_rows_kernel<Te, M>;
@@ -186,7 +365,44 @@ cudaError_t launch_typed(const Te* x, const Fp8LinearRows& p, int num_sms, cudaS
   }
 }
 
+template <typename K>
+cudaError_t launch_wide(K kernel, dim3 grid, size_t smem, const Fp8ExpertsRows& p,
+                        cudaStream_t stream) {
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(
+        kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(kernel, grid, dim3(kThreads), smem, stream, p);
+}
+
+size_t row_bytes(int cols) {
+  return static_cast<size_t>((cols + kChunk - 1) / kChunk) * kChunk * sizeof(float);
+}
+
 }  // namespace
+
+// Two launches instead of six pay while the slots' weights, read again for every
+// slot, are few.  Layer in us, here | tiles:
+//   d 2048, inter 1024, k_max 12: 1 token (12 slots, 75 MB) 18 | 34, 2 31 | 39,
+//   3 (226 MB) 42 | 43, 4 61 | 60; k_max 8: 3 (151 MB) 37 | 40, 4 (201 MB) 44 | 42;
+//   d 2048, inter 512, k_max 12: 1 14 | 32, 4 (151 MB) 39 | 43, 6 (226 MB) 56 | 54;
+//   d 1024, inter 512, k_max 8: 1 10 | 26, 8 (101 MB) 28 | 29, 16 (201 MB) 49 | 32;
+//   d 256, inter 128, k_max 4: 1 7 | 21, 32 (128 slots) 20 | 22.
+// Both kernels' rows lie in shared memory.
+bool experts_rows_fit(int T, int k_max, int d, int inter) {
+  const int64_t slots = static_cast<int64_t>(T) * k_max;
+  return slots <= kFp8ExpertsRowsSlots && slots * 3 * d * inter <= (int64_t{160} << 20) &&
+         row_bytes(d) <= 128 * 1024 && row_bytes(inter) * kWarps <= 128 * 1024;
+}
+
+cudaError_t launch_experts_rows(const Fp8ExpertsRows& p, cudaStream_t stream) {
+  const dim3 up((p.inter + 4 * kWarps - 1) / (4 * kWarps), p.T * p.k_max);
+  const cudaError_t e = launch_wide(experts_up_rows_kernel, up, row_bytes(p.d), p, stream);
+  if (e != cudaSuccess) return e;
+  return launch_wide(experts_down_rows_kernel, dim3(p.d / 8, p.T), row_bytes(p.inter) * kWarps, p,
+                     stream);
+}
 
 // x fits in shared memory, and the products of each of up to four rows by
 // themselves take no longer than the tensor cores' tiles of 128 (us, here |

@@ -157,3 +157,52 @@ def test_experts_whatever_the_workspace_holds(T, d, E, inter, k_max):
         assert op.status() == B.REFLEX_OK
     check_experts(outs[0], experts64(h, ids, alpha, w, inter))
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("T,d,inter,k_max", [
+    (64, 128, 64, 2), (65, 128, 64, 2),            # 128 and 130 slots
+    (4, 2048, 1024, 6), (5, 2048, 1024, 6),        # 151 and 189 MB of the slots' weights
+    (1, 576, 320, 32), (3, 64, 64, 32), (2, 4096, 192, 3), (1, 640, 4160, 2)])
+def test_few_pairs_and_more(T, d, inter, k_max):
+    """Around the sizes from which tiles of the tensor cores take over."""
+    E = 40
+    w = experts_layer(T + d, d, E, inter)
+    h = normal(T, T, d, dtype=BF16)
+    ids, alpha, k = routing(T + E, T, E, k_max)
+    op = api.ExpertsFp8(w, d=d, E=E, inter=inter, k_max=k_max, max_tokens=T)
+    out = op.forward(h, ids, alpha, k)
+    assert op.status() == B.REFLEX_OK
+    ref = experts64(h, ids, alpha, w, inter)
+    check_experts(out, ref)
+    assert torch.equal(op.forward(h, ids, alpha, k), out)
+    both = op.forward(h, ids, alpha, k, residual=True).double() - (h.double() + ref)
+    assert float(both.norm() / (h.double() + ref).norm()) <= 6e-3
+
+
+@pytest.mark.parametrize("T", [7, 200])
+def test_experts_errors_and_nan(T):
+    d, E, inter, k_max = 192, 4, 128, 2
+    w = experts_layer(4, d, E, inter)
+    op = api.ExpertsFp8(w, d=d, E=E, inter=inter, k_max=k_max, max_tokens=T)
+    h = normal(1, T, d, dtype=BF16)
+    ids, alpha, k = routing(1, T, E, k_max, lo=2)
+    want = op.forward(h, ids, alpha, k)
+    rest = torch.arange(T, device="cuda") != 3
+    for bad in (E, -7):
+        wrong = ids.clone()
+        wrong[3, 1] = bad
+        out = op.forward(h, wrong, alpha, k)
+        assert op.status() == B.REFLEX_EINVAL and torch.equal(out[rest], want[rest])
+        only = alpha.clone()
+        only[3, 1] = 0.0
+        check_experts(out, experts64(h, ids, only, w, inter))
+    for count, same in ((3, 2), (0, 1), (-5, 1)):
+        counts = k.clone()
+        counts[3] = count
+        out = op.forward(h, ids, alpha, counts)
+        assert op.status() == B.REFLEX_EKRANGE and torch.equal(out[rest], want[rest])
+        counts[3] = same
+        assert torch.equal(out, op.forward(h, ids, alpha, counts)) and op.status() == B.REFLEX_OK
+    h[3, 5] = float("nan")
+    out = op.forward(h, ids, alpha, k)
+    assert bool(out[3].isnan().all()) and torch.equal(out[rest], want[rest])
