@@ -24,7 +24,7 @@ namespace rx {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnits = 4;  // pairs of groups that a warp has in flight
+constexpr int kUnits = 4;  // groups that a half of a warp has in flight
 
 // 8 elements from column c on; those at or past cols are 0.
 template <typename Te>
@@ -118,14 +118,14 @@ struct Raw8<__nv_bfloat16> {
   }
 };
 
-// A warp takes kUnits pairs of groups (256 columns each) of a row at a time:
-// their loads in flight together, then a lane per group divides for the 16 that
-// hold it.
-template <typename Te>
+// A warp takes 2 kUnits groups at a time: their loads in flight together (16 lanes a
+// group), then a lane per group divides for the 16 that hold it.  kPacked: of
+// several rows, one group after another, where a row has few.
+template <typename Te, bool kPacked>
 __global__ void __launch_bounds__(kThreads)
     quantize_rows_kernel(const Te* __restrict__ x, int64_t rows, int cols, int64_t ldx,
                          uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scales,
-                         int64_t scale_row_bytes, int vec_x, int vec_c, uint32_t chunks,
+                         int64_t scale_row_bytes, int vec_x, int vec_c, uint32_t groups,
                          ZeroWords zero, const int32_t* __restrict__ k, int64_t n_k, int k_most,
                          uint32_t* err) {
   grid_dep_wait();
@@ -139,41 +139,63 @@ __global__ void __launch_bounds__(kThreads)
       if (bad) set_err(err, kErrKRange);
     }
   }
-  const int lane = threadIdx.x & 31;
-  const int64_t units = rows * chunks;  // chunks of 1024 columns
+  const int lane = threadIdx.x & 31, half = lane >> 4;
+  constexpr int kGroups = 2 * kUnits;
+  const uint32_t chunks = (groups + kGroups - 1) / kGroups;  // of a row
+  const int64_t total = rows * groups;
+  const int64_t units = kPacked ? (total + kGroups - 1) / kGroups : rows * chunks;
   const int64_t step = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
        u < units; u += step) {
-    const int64_t r = chunks == 1 ? u : units <= 0xffffffffll
-                                            ? static_cast<uint32_t>(u) / chunks : u / chunks;
-    const int c0 = static_cast<int>(u - r * chunks) * (256 * kUnits) + lane * 8;
-    const Te* row = x + r * ldx;
+    // the unit's first group, and its groups
+    const int64_t first = kPacked ? u * kGroups : u;
+    const uint32_t per_row = kPacked ? groups : chunks;
+    const int64_t r0 = (kPacked ? total : units) <= 0xffffffffll
+                           ? static_cast<uint32_t>(first) / per_row : first / per_row;
+    const uint32_t g0 = static_cast<uint32_t>(first - r0 * per_row) * (kPacked ? 1 : kGroups);
+    const int left = static_cast<int>(
+        min(static_cast<int64_t>(kGroups), kPacked ? total - first : int64_t{groups} - g0));
+    auto locate = [&](int n, int64_t& r, uint32_t& g) {
+      const uint32_t over = kPacked ? (g0 + n) / groups : 0u;
+      g = g0 + n - over * groups;
+      r = r0 + over;
+    };
     Raw8<Te> raw[kUnits];
+    int64_t row[kUnits];
+    int col[kUnits];
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i)
-      if (i == 0 || c0 - lane * 8 + i * 256 < cols) raw[i].load(row, c0 + i * 256, cols, vec_x != 0);
-    // the magnitude of group g (= 2 i + half) ends up in lane g
+    for (int i = 0; i < kUnits; ++i) {
+      uint32_t g;
+      locate(2 * i + half, row[i], g);
+      col[i] = static_cast<int>(g) * 128 + (lane & 15) * 8;
+      if (2 * i + half < left) raw[i].load(x + row[i] * ldx, col[i], cols, vec_x != 0);
+    }
+    // the magnitude of the n-th group ends up in lane n
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       uint32_t m = 0;
-      if (i == 0 || c0 - lane * 8 + i * 256 < cols) m = raw[i].amax();
+      if (2 * i + half < left) m = raw[i].amax();
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
       const uint32_t other = __shfl_xor_sync(0xffffffffu, m, 16);
-      if ((lane >> 1) == i) mine = (lane & 1) == (lane >> 4) ? m : other;
+      if ((lane >> 1) == i) mine = (lane & 1) == half ? m : other;
     }
     const float a = fp8_amax(mine), inv = fp8_inverse(a);
-    const int group = (c0 - lane * 8) / 128 + lane;
-    if (lane < 2 * kUnits && group * 128 < cols)
-      *reinterpret_cast<float*>(scales + r * scale_row_bytes + group * 4) = __fdiv_rn(a, kE4m3Max);
+    if (lane < left) {
+      int64_t r;
+      uint32_t g;
+      locate(lane, r, g);
+      *reinterpret_cast<float*>(scales + r * scale_row_bytes + static_cast<int64_t>(g) * 4) =
+          __fdiv_rn(a, kE4m3Max);
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const float by = __shfl_sync(0xffffffffu, inv, 2 * i + (lane >> 4));
-      if (i > 0 && c0 - lane * 8 + i * 256 >= cols) break;
+      const float by = __shfl_sync(0xffffffffu, inv, 2 * i + half);
+      if (2 * i + half >= left) continue;
       float f[8];
       raw[i].widen(f);
-      store_codes(codes + r * ldc, c0 + i * 256, cols, vec_c != 0, f, by);
+      store_codes(codes + row[i] * ldc, col[i], cols, vec_c != 0, f, by);
     }
   }
 }
@@ -221,15 +243,20 @@ bool aligned_rows(const Te* x, int64_t ld) {
 
 template <typename Te>
 cudaError_t rows_typed(const Te* x, const Fp8Rows& q, int num_sms, cudaStream_t stream) {
-  const int64_t chunks = (q.cols + 256 * kUnits - 1) / (256 * kUnits);
-  const int64_t grid = (q.rows * chunks + kThreads / 32 - 1) / (kThreads / 32);
-  return launch_pdl(quantize_rows_kernel<Te>,
+  const int64_t groups = (q.cols + 127) / 128;
+  // (30 million bf16 in rows of 64, 128, 256 and 384: packed 60, 24, 23 and 24 us, a
+  // row a warp 150, 80, 36 and 35; in rows of 513 and 1000 40 and 25, here 38 and 21)
+  const bool packed = groups <= kUnits;
+  const int64_t units = packed ? (q.rows * groups + 2 * kUnits - 1) / (2 * kUnits)
+                               : q.rows * ((groups + 2 * kUnits - 1) / (2 * kUnits));
+  const int64_t grid = (units + kThreads / 32 - 1) / (kThreads / 32);
+  return launch_pdl(packed ? quantize_rows_kernel<Te, true> : quantize_rows_kernel<Te, false>,
                     dim3(static_cast<unsigned>(std::min<int64_t>(grid, 16 * num_sms))),
                     dim3(kThreads), 0, stream, x, q.rows, static_cast<int>(q.cols), q.ldx,
                     q.codes, q.ldc, q.scales, q.scale_row_bytes,
                     static_cast<int>(aligned_rows(x, q.ldx)),
                     static_cast<int>(aligned_rows(q.codes, q.ldc)),
-                    static_cast<uint32_t>(chunks), q.zero, q.k, q.n_k, q.k_most, q.err);
+                    static_cast<uint32_t>(groups), q.zero, q.k, q.n_k, q.k_most, q.err);
 }
 
 template <typename Te>

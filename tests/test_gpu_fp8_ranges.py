@@ -206,3 +206,17 @@ def test_experts_errors_and_nan(T):
     h[3, 5] = float("nan")
     out = op.forward(h, ids, alpha, k)
     assert bool(out[3].isnan().all()) and torch.equal(out[rest], want[rest])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,extra", [(1001, 1, 0), (77, 100, 4), (3, 128, 0), (123, 300, 1),
+                                             (9, 512, 8), (10, 513, 0), (70001, 129, 0),
+                                             (5, 1025, 7)])
+def test_narrow_and_wide_rows_quantised(rows, cols, extra, dtype):
+    x = torch.full((rows, cols + extra), float("nan"), dtype=dtype, device="cuda")
+    x[:, :cols] = normal(rows + cols, rows, cols)
+    whole = torch.full((rows + 1, cols + 3), 0x55, dtype=torch.uint8, device="cuda")
+    codes, scales = api.quantize_fp8(x[:, :cols], 1, whole.view(E4M3)[:rows, :cols])
+    want, want_scales = codes_of(x[:, :cols], 1)
+    assert same_codes(codes, want) and torch.equal(scales.cpu(), want_scales)
+    assert bool((whole[:, cols:] == 0x55).all()) and bool((whole[rows:] == 0x55).all())
