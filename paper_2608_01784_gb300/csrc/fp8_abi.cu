@@ -63,14 +63,15 @@ bool out_map(CUtensorMap* m, void* base, bool bf16, int64_t rows, int64_t cols, 
 }
 
 // CTAs of a cluster that share a tile's K, where the tiles leave SMs free.  Adding
-// the parts costs 2 to 3 us for each 32 rows, a block of K 0.5 us, so taller
-// tiles are split at a long K only (N x K, one CTA a tile | split, us):
+// the parts costs some 3 us for each 32 rows of a tile, a block of K 0.5 us, so taller
+// tiles are split at a longer K only (N x K, one CTA a tile | split, us):
 //   M =   8, 4096 x 2048: 13 | 12 by 4, 20 by 8;   1024 x 8192: 34 | 18 by 4, 14 by 8
-//   M = 128, 4096 x 2048: 19 | 24 by 4, 45 by 8;   1024 x 8192: 41 | 29 by 8
+//   M =  64, 512 x 2048: 14 | 14;  512 x 3200: 20 | 16;  512 x 8000: 38 | 20
+//   M = 128, 512 x 3200: 21 | 24;  512 x 5120: 28 | 25;  512 x 8000: 39 | 28
 // Clusters of eight find room at once in half of the SMs only: more wait for a
-// second round, the 20 and 45 above.
+// second round, the 20 by 8 above.
 int pick_splits(int64_t M, int64_t tiles, int64_t nkb, int sms) {
-  if (M > 32 && nkb < 64) return 1;
+  if (M > 32 && nkb < 10 * std::min<int64_t>(4, (M + 31) / 32)) return 1;
   int s = 1;
   while (s < 8 && nkb >= 4 * s && tiles * s * 2 <= (s < 4 ? sms : sms / 2)) s *= 2;
   return s;
