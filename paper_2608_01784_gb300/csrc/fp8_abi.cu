@@ -68,13 +68,15 @@ bool out_map(CUtensorMap* m, void* base, bool bf16, int64_t rows, int64_t cols, 
 //   M =   8, 4096 x 2048: 13 | 12 by 4, 20 by 8;   1024 x 8192: 34 | 18 by 4, 14 by 8
 //   M =  64, 512 x 2048: 14 | 14;  512 x 3200: 20 | 16;  512 x 8000: 38 | 20
 //   M = 128, 512 x 3200: 21 | 24;  512 x 5120: 28 | 25;  512 x 8000: 39 | 28
+//   M = 256, 8192 x 8000: 43 | 51 by 2;   M = 300, 2048 x 5120: 29 | 29 by 4
 // Clusters of eight find room at once in half of the SMs only: more wait for a
 // second round, the 20 by 8 above.
 int pick_splits(int64_t M, int64_t tiles, int64_t nkb, int sms) {
-  if (M > 32 && nkb < 10 * std::min<int64_t>(4, (M + 31) / 32)) return 1;
   int s = 1;
   while (s < 8 && nkb >= 4 * s && tiles * s * 2 <= (s < 4 ? sms : sms / 2)) s *= 2;
-  return s;
+  // the blocks that a CTA is spared, against 8.5 for each 32 rows
+  const int64_t quarters = std::min<int64_t>(4, (M + 31) / 32);
+  return M > 32 && 2 * nkb * (s - 1) < 17 * quarters * s ? 1 : s;
 }
 
 int matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t a_scale_row_bytes,
