@@ -475,8 +475,8 @@ int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* 
  * routing that the caller holds (the ids, alpha of a route record):
  *   out_t = sum_{j < k_t} alpha[t, j] E_{ids[t, j]}(h_t)   (+ h_t)
  * with h_t quantised in rows, the activation silu(g) u of each pair quantised
- * again in rows of 128 columns, and the pairs' outputs rounded to bf16 before
- * the weighted fp32 sum.
+ * again in rows of 128 columns; the weighted sum is in fp32, of outputs that
+ * tiles of many pairs store as bf16 and a few pairs keep in fp32.
  *   hidden         [T, d] bf16.
  *   ids, alpha     [T, k_max]: slots j < k[t] are read; an id outside [0, E)
  *                  there sets REFLEX_EINVAL in the error word and its pair

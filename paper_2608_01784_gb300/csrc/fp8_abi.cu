@@ -170,6 +170,11 @@ ExpertsLayout experts_layout(int32_t T, int32_t d, int32_t E, int32_t inter, int
   L.row_of = take(L.cap * 4);
   L.xperm = take(L.cap * L.x_bytes);
   L.act = take(L.cap * L.act_bytes);
+  // Tiles leave the pairs' outputs in memory as bf16, in which the layer's output is
+  // rounded anyway; fp32 ones take twice the bytes through two kernels and bring the
+  // error against 64 bits down by 1 % (k_max 12, d 2048, bf16 | fp32; relative error, us):
+  //   64 x 1024, 32 tokens 2.62e-3, 83 | 2.60e-3, 89; 1024 tokens 2.57e-3, 123 | 2.55e-3, 140;
+  //   256 x 512, 8192 tokens 11.7e-3, 377 | 11.6e-3, 489.
   L.y = take(L.cap * d * 2);
   L.act_rows = take(std::min<int64_t>(L.cap, rx::kFp8ExpertsRowsSlots) * inter * 4);
   L.total = o;

@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(kThreads) experts_up_rows_kernel(const Fp8Expe
 }
 
 // out of one token, eight columns a CTA: a warp takes a slot's product (its act
-// quantised by the warp itself), and the slots are added in order.
+// quantised by the warp itself), and the slots are added in order.  The products stay
+// in fp32 until the sum is rounded: they never leave the CTA.
 __global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8ExpertsRows p) {
   extern __shared__ __align__(16) float xs[];  // [kWarps][chunks * kChunk]
   __shared__ float y[32][8];
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8Ex
     __syncwarp();
 #pragma unroll
     for (int r = 0; r < 8; ++r)
-      if (lane == r) y[j][r] = __bfloat162float(__float2bfloat16_rn(acc[r]));
+      if (lane == r) y[j][r] = acc[r];
   }
   if (!waited) grid_dep_wait();
   grid_dep_launch();
