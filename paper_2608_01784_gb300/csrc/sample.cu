@@ -637,7 +637,8 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
         }
     }
     fix = fix_inf = kStream;
-    if (lane_max == m) lane_max = 0.0f;
+    // (a lane without one has none of the largest logit now, whatever it had before)
+    lane_max = lane_max == m ? 0.0f : minus_inf;
     m = 0.0f;
   }
   const float neg_m = -m;
@@ -755,11 +756,11 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
     if (lane_max == m) {  // the lane's first token of the largest logit
       float z[8];
       load(own + max_step * kStep, z);
-      int first = 7;
+      int first = -1;
 #pragma unroll
-      for (int j = 6; j >= 0; --j)
+      for (int j = 7; j >= 0; --j)
         if (z[j] == m) first = j;
-      atomicMin(&s.first, my_pos + max_step * kStep + first);
+      if (first >= 0) atomicMin(&s.first, my_pos + max_step * kStep + first);
     }
   } else if (cut_any) {
     auto counts = [&](int i0, int i1) {
