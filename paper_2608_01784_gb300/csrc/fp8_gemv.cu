@@ -9,9 +9,9 @@
 // step, 16 bytes of each row a lane, two steps in flight, and the rows of x are read
 // from shared memory once for all of them.  Every CTA quantises its rows of x by
 // itself (the codes of reflex_quantize_fp8 bit for bit): a launch more would take
-// longer.  The 16 products of a lane lie in one block of K: they are summed in fp32,
-// scaled once by the weights' scale (x's scale is in x), and the lanes' sums added
-// at the end.
+// longer.  The 16 products of a lane lie in one block of K: the codes' products are
+// summed in fp32 and scaled once by both scales, as the tiles do (a scale folded into
+// x first would overflow for rows above 1e34), and the lanes' sums added at the end.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
@@ -37,16 +37,18 @@ __device__ __forceinline__ void fma2(float2& acc, float2 a, float2 b) {
       : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
 }
 
-// Element k of a row of x in shared memory: a lane's 16 columns as four vectors,
-// each vector of all lanes in a row, so that no two lanes share a bank.
+// A row of x in shared memory: its codes as fp32, and behind them the scales of its
+// blocks.  Element k: a lane's 16 columns as four vectors, each vector of all lanes in
+// a row, so that no two lanes share a bank.
+__host__ __device__ constexpr int row_floats(int chunks) { return chunks * (kChunk + kChunk / 128); }
 __device__ __forceinline__ int place(int k) {
   return (k >> 9) * kChunk + ((k >> 2) & 3) * 128 + ((k >> 4) & 31) * 4 + (k & 3);
 }
 
-// 256 columns of a row (8 a lane, from c on) as the values of their codes, 16 lanes
-// a group of 128 as in the quantisation kernel.
+// 256 columns of a row (8 a lane, from c on) to codes and scales, 16 lanes a group of
+// 128 as in the quantisation kernel.
 template <typename Te>
-__device__ __forceinline__ void quantise_pair(const Te* row, int c, int K, float* xs) {
+__device__ __forceinline__ void quantise_pair(const Te* row, int c, int K, float* xs, int chunks) {
   float f[8];
   uint32_t top = 0;
 #pragma unroll
@@ -56,13 +58,13 @@ __device__ __forceinline__ void quantise_pair(const Te* row, int c, int K, float
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const float a = fp8_amax(top), inv = fp8_inverse(a), s = __fdiv_rn(a, kE4m3Max);
+  const float a = fp8_amax(top), inv = fp8_inverse(a);
+  if (c % 128 == 0) xs[chunks * kChunk + c / 128] = __fdiv_rn(a, kE4m3Max);
 #pragma unroll
   for (int i = 0; i < 8; i += 4) {
     const uint32_t q = e4m3x4(f[i] * inv, f[i + 1] * inv, f[i + 2] * inv, f[i + 3] * inv);
     const float2 lo = e4m3x2(q & 0xffffu), hi = e4m3x2(q >> 16);
-    *reinterpret_cast<float4*>(xs + place(c + i)) =
-        make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+    *reinterpret_cast<float4*>(xs + place(c + i)) = make_float4(lo.x, lo.y, hi.x, hi.y);
   }
 }
 
@@ -71,16 +73,16 @@ __global__ void __launch_bounds__(kThreads)
     linear_rows_kernel(const Te* __restrict__ x, int64_t ldx, const uint8_t* __restrict__ w,
                        int64_t ldw, const float* __restrict__ w_scales, int64_t ldws, int N,
                        int K, int out_f32, void* __restrict__ out, int64_t ldo, ZeroWords zero) {
-  extern __shared__ __align__(16) float xs[];  // [M][chunks * kChunk], see place()
+  extern __shared__ __align__(16) float xs[];  // [M][row_floats(chunks)]
   grid_dep_wait();
   grid_dep_launch();
   if (blockIdx.x == 0) clear_words(zero);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int chunks = (K + kChunk - 1) / kChunk, row_floats = chunks * kChunk;
-  const int pairs = row_floats / 256;
+  const int chunks = (K + kChunk - 1) / kChunk, ld = row_floats(chunks);
+  const int pairs = chunks * kChunk / 256;
   for (int u = warp; u < M * pairs; u += kWarps) {
     const int m = u / pairs;
-    quantise_pair(x + m * ldx, (u - m * pairs) * 256 + lane * 8, K, xs + m * row_floats);
+    quantise_pair(x + m * ldx, (u - m * pairs) * 256 + lane * 8, K, xs + m * ld, chunks);
   }
   __syncthreads();
 
@@ -127,8 +129,8 @@ __global__ void __launch_bounds__(kThreads)
           float4 xv[M];
 #pragma unroll
           for (int m = 0; m < M; ++m)
-            xv[m] = *reinterpret_cast<const float4*>(xs + m * row_floats + (c0 + d) * kChunk +
-                                                     j * 128 + lane * 4);
+            xv[m] = *reinterpret_cast<const float4*>(xs + m * ld + (c0 + d) * kChunk + j * 128 +
+                                                     lane * 4);
 #pragma unroll
           for (int r = 0; r < kRows; ++r) {
             const uint32_t word = j == 0 ? q[d][r].x : j == 1 ? q[d][r].y
@@ -141,11 +143,14 @@ __global__ void __launch_bounds__(kThreads)
             }
           }
         }
+        const float* sx = xs + chunks * kChunk + (c0 + d) * (kChunk / 128) + (lane >> 3);
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
+        for (int m = 0; m < M; ++m) {
+          const float both = s[d] * sx[m * ld];
 #pragma unroll
-          for (int m = 0; m < M; ++m)
-            acc[r][m] = fmaf(sum[r][m].x + sum[r][m].y, s[d], acc[r][m]);
+          for (int r = 0; r < kRows; ++r)
+            acc[r][m] = fmaf(sum[r][m].x + sum[r][m].y, both, acc[r][m]);
+        }
       }
     }
     float mine = 0.f;
@@ -209,8 +214,9 @@ __device__ __forceinline__ void add_steps(const Steps<R>& v, const float* xs, in
         fma2(sum[r], e4m3x2(word >> 16), make_float2(x.z, x.w));
       }
     }
+    const float sx = xs[chunks * kChunk + (c0 + a) * (kChunk / 128) + (lane >> 3)];
 #pragma unroll
-    for (int r = 0; r < R; ++r) acc[r] = fmaf(sum[r].x + sum[r].y, v.s[a][r / 4], acc[r]);
+    for (int r = 0; r < R; ++r) acc[r] = fmaf(sum[r].x + sum[r].y, v.s[a][r / 4] * sx, acc[r]);
   }
 }
 template <int R>
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) experts_up_rows_kernel(const Fp8Expe
     load_steps(v, rows, sc, 0, p.d);
   }
   for (int u = warp; u < chunks * kChunk / 256; u += kWarps)
-    quantise_pair(p.hidden + static_cast<int64_t>(t) * p.d, u * 256 + lane * 8, p.d, xs);
+    quantise_pair(p.hidden + static_cast<int64_t>(t) * p.d, u * 256 + lane * 8, p.d, xs, chunks);
   __syncthreads();
   if (!on) return;
   float acc[8] = {};
@@ -281,14 +287,14 @@ __global__ void __launch_bounds__(kThreads) experts_up_rows_kernel(const Fp8Expe
 // quantised by the warp itself), and the slots are added in order.  The products stay
 // in fp32 until the sum is rounded: they never leave the CTA.
 __global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8ExpertsRows p) {
-  extern __shared__ __align__(16) float xs[];  // [kWarps][chunks * kChunk]
+  extern __shared__ __align__(16) float xs[];  // [kWarps][row_floats(chunks)]
   __shared__ float y[32][8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = blockIdx.y, n0 = blockIdx.x * 8;
   const int chunks = (p.inter + kChunk - 1) / kChunk;
   const int ib = (p.inter + 127) / 128, db = (p.d + 127) / 128;
   const int kt = min(max(p.k[t], 1), p.k_most);
-  float* my_xs = xs + warp * chunks * kChunk;
+  float* my_xs = xs + warp * row_floats(chunks);
   const int32_t* ids = p.ids + t * p.k_max;
   bool waited = false;
   for (int j = warp; j < kt; j += kWarps) {
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8Ex
     waited = true;
     const float* act = p.act + (static_cast<int64_t>(t) * p.k_max + j) * p.inter;
     for (int u = 0; u < chunks * kChunk / 256; ++u)
-      quantise_pair(act, u * 256 + lane * 8, p.inter, my_xs);
+      quantise_pair(act, u * 256 + lane * 8, p.inter, my_xs, chunks);
     __syncwarp();
     float acc[8] = {};
     for (int c0 = 0; c0 < chunks; c0 += kAhead) {
@@ -342,7 +348,7 @@ template <typename Te, int M>
 cudaError_t launch_m(const Te* x, const Fp8LinearRows& p, int num_sms, cudaStream_t stream) {
   auto kernel = linear_rows_kernel<Te, M>;
   const int chunks = (p.K + kChunk - 1) / kChunk;
-  const size_t smem = static_cast<size_t>(M) * chunks * kChunk * sizeof(float);
+  const size_t smem = static_cast<size_t>(M) * row_floats(chunks) * sizeof(float);
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(
         kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
@@ -378,7 +384,7 @@ cudaError_t launch_wide(K kernel, dim3 grid, size_t smem, const Fp8ExpertsRows& 
 }
 
 size_t row_bytes(int cols) {
-  return static_cast<size_t>((cols + kChunk - 1) / kChunk) * kChunk * sizeof(float);
+  return static_cast<size_t>((cols + kChunk - 1) / kChunk) * row_floats(1) * sizeof(float);
 }
 
 }  // namespace
@@ -394,7 +400,7 @@ size_t row_bytes(int cols) {
 bool experts_rows_fit(int T, int k_max, int d, int inter) {
   const int64_t slots = static_cast<int64_t>(T) * k_max;
   return slots <= kFp8ExpertsRowsSlots && slots * 3 * d * inter <= (int64_t{160} << 20) &&
-         row_bytes(d) <= 128 * 1024 && row_bytes(inter) * kWarps <= 128 * 1024;
+         row_bytes(d) <= 130 * 1024 && row_bytes(inter) * kWarps <= 130 * 1024;
 }
 
 cudaError_t launch_experts_rows(const Fp8ExpertsRows& p, cudaStream_t stream) {
