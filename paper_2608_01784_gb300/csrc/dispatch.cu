@@ -261,8 +261,11 @@ __global__ void __launch_bounds__(1024)
 // every SM gets work.  Lane j of a warp of token t places pair (t, j) at
 // offsets[e] + block prefix + the popcount of the lower tokens' bits in its
 // block's KW mask words of expert e (the pairs of expert e in token order);
-// the warp of the row's first segment writes perm and row_of.
-template <typename Te, int KW>
+// the warp of the row's first segment writes perm and row_of (kWeights: and the weights
+// of a caller's routing, which may be any in a slot without a row.  A choice between
+// weight and zero in the combine's sums costs that kernel its sixth CTA an SM: 8192
+// tokens of 2048 x 12 slots 62 us, here 47).
+template <typename Te, int KW, bool kWeights>
 __global__ void __launch_bounds__(256)
     gather_scatter_kernel(const Te* __restrict__ x, const int32_t* __restrict__ ids,
                           const int32_t* __restrict__ k, const uint32_t* __restrict__ blk_mask,
@@ -270,6 +273,7 @@ __global__ void __launch_bounds__(256)
                           const int32_t* __restrict__ offsets, int E, int k_max, int cap_rows,
                           int T, int d, int wpt, int32_t* __restrict__ perm,
                           int32_t* __restrict__ row_of, Te* __restrict__ xp,
+                          const float* __restrict__ alpha, float* __restrict__ weights,
                           uint32_t* __restrict__ err) {
   constexpr int kVecElems = 16 / sizeof(Te);
   constexpr int kMaxVec = 8;
@@ -329,6 +333,7 @@ __global__ void __launch_bounds__(256)
       }
       if (seg == 0) {
         row_of[o] = my_row;
+        if constexpr (kWeights) weights[o] = my_row >= 0 ? alpha[o] : 0.f;
         if (my_row >= 0) perm[my_row] = static_cast<int32_t>(o);
       }
     }
@@ -416,10 +421,15 @@ static cudaError_t launch_gather_scatter(const Te* hidden, const int32_t* ids, c
                                          cudaStream_t stream) {
   int wpt, grid;
   gather_shape(sizeof(Te) == 4 ? 0 : 1, T, d, num_sms, x_perm != nullptr, &wpt, &grid);
-  return launch_pdl(gather_scatter_kernel<Te, KW>, dim3(grid), dim3(256), 0, stream, hidden,
-                    ids, k, static_cast<const uint32_t*>(b.blk_mask),
+  auto kernel = gather_scatter_kernel<Te, KW, false>;
+  if constexpr (sizeof(Te) == 2) {  // (packed rows of codes come as bf16)
+    if (b.weights != nullptr) kernel = gather_scatter_kernel<Te, KW, true>;
+  }
+  return launch_pdl(kernel, dim3(grid), dim3(256), 0, stream, hidden, ids, k,
+                    static_cast<const uint32_t*>(b.blk_mask),
                     static_cast<const int32_t*>(b.blk_off), static_cast<const int32_t*>(b.offsets),
-                    E, k_max, cap_rows, T, d, wpt, b.perm, b.row_of, x_perm, b.err);
+                    E, k_max, cap_rows, T, d, wpt, b.perm, b.row_of, x_perm, b.alpha, b.weights,
+                    b.err);
 }
 
 template <typename Te>

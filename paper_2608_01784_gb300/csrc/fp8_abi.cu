@@ -142,7 +142,7 @@ LinearLayout linear_layout(int64_t M, int64_t K) {
 
 struct ExpertsLayout {
   size_t hdr, x, blk_count, blk_mask, blk_off, counts, offsets, mt_prefix, mt2_prefix, perm,
-      row_of, xperm, act, y, act_rows, total;
+      row_of, weights, xperm, act, y, act_rows, total;
   int64_t cap, x_bytes, act_bytes;
 };
 ExpertsLayout experts_layout(int32_t T, int32_t d, int32_t E, int32_t inter, int32_t k_max) {
@@ -168,6 +168,7 @@ ExpertsLayout experts_layout(int32_t T, int32_t d, int32_t E, int32_t inter, int
   L.mt2_prefix = take(static_cast<size_t>(E + 1) * 4);
   L.perm = take(L.cap * 4);
   L.row_of = take(L.cap * 4);
+  L.weights = take(L.cap * 4);
   L.xperm = take(L.cap * L.x_bytes);
   L.act = take(L.cap * L.act_bytes);
   // Tiles leave the pairs' outputs in memory as bf16, in which the layer's output is
@@ -335,7 +336,8 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   RX_CUDA(rx::launch_quantize_rows(REFLEX_DTYPE_BF16, hidden, q, sms, s));
   rx::DispatchBufs b{I32(L.blk_count), I32(L.blk_off),    I32(L.counts), I32(L.offsets),
                      I32(L.mt_prefix), I32(L.mt2_prefix), I32(L.perm),   I32(L.row_of),
-                     &hdr->total_pairs, err, reinterpret_cast<uint32_t*>(ws + L.blk_mask)};
+                     &hdr->total_pairs, err, reinterpret_cast<uint32_t*>(ws + L.blk_mask),
+                     alpha, reinterpret_cast<float*>(ws + L.weights)};
   RX_CUDA(rx::launch_dispatch_gather(REFLEX_DTYPE_BF16, ws + L.x, ids, k, T, E, k_max, cap,
                                      static_cast<int>(L.x_bytes / 2), b, ws + L.xperm, sms, s));
 
@@ -384,8 +386,9 @@ int reflex_experts_fp8(const void* hidden, const int32_t* ids, const float* alph
   dn.ldo = d;
   RX_CUDA(rx::launch_fp8_matmul(dn, s));
   const void* resid = (flags & REFLEX_FLAG_RESIDUAL) ? hidden : nullptr;
-  RX_CUDA(rx::launch_combine(REFLEX_DTYPE_BF16, ws + L.y, nullptr, resid, I32(L.row_of), alpha, k,
-                             T, d, k_max, cap, out, err, sms, s));
+  RX_CUDA(rx::launch_combine(REFLEX_DTYPE_BF16, ws + L.y, nullptr, resid, I32(L.row_of),
+                             reinterpret_cast<const float*>(ws + L.weights), k, T, d, k_max, cap,
+                             out, err, sms, s));
   return REFLEX_OK;
 }
 

@@ -138,6 +138,10 @@ struct DispatchBufs {
   int32_t* totals;     // header: total_pairs, total_mtiles, total_mtiles2
   uint32_t* err;
   uint32_t* blk_mask;  // [nblk, E, BLK / 32] token bits of each block and expert
+  // a caller's routing: its weights [T*k_max], and the same with 0 in slots without a
+  // row (clamped away or refused), as the combine takes them; null otherwise
+  const float* alpha = nullptr;
+  float* weights = nullptr;
 };
 constexpr int kDispatchBlock = 256;       // tokens per dispatch block, large batches
 constexpr int kDispatchBlockSmall = 32;   // tokens per dispatch block up to 4096 tokens
