@@ -8,7 +8,7 @@ import numpy as np
 import torch
 
 from . import _binding as B
-from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, matmul_fp8,  # noqa: F401
+from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, _new, matmul_fp8,  # noqa: F401
                   quantize_experts, quantize_fp8)
 
 
@@ -309,7 +309,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor |
            status: torch.Tensor | None = None, stream=None):
     """reflex_sample of logits [rows, vocab] (fp32 or bf16) with uniforms u
     [rows] -> (tokens int32 [rows], conf fp32 [rows]).  Every setting is one
-    value per row; rows with masked == 0 get token -1 and confidence 0."""
+    value per row; rows with masked == 0 get token -1 and confidence 0.  New
+    outputs belong to `stream`."""
     rows, vocab, ld = _matrix(logits, "logits", _DTYPES)
     dev = logits.device
     def check(t, dt, what):
@@ -323,9 +324,9 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor |
         if t is not None:
             check(t, dt, what)
     if tokens is None:
-        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+        tokens = _new(rows, torch.int32, dev, stream)
     if conf is None:
-        conf = torch.empty(rows, dtype=torch.float32, device=dev)
+        conf = _new(rows, torch.float32, dev, stream)
     B.reflex_sample(_DTYPES[logits.dtype], logits, ld, rows, vocab, temperature, top_k, top_p, min_p,
                     u, masked, tokens, conf, status, stream)
     return tokens, conf

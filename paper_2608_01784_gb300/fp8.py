@@ -1,7 +1,8 @@
 """Torch-facing convenience over the 8-bit entry points: quantisation, the
 dense layer and the routed experts.  Codes are torch.float8_e4m3fn tensors,
 scales fp32; a scale covers 128 columns of a row (activations) or a 128 x 128
-block (weights).  Every step runs in libreflex.so's kernels.
+block (weights).  Every step runs in libreflex.so's kernels.  With a `stream`, new
+outputs belong to it: to use them on another, wait for it, as torch's own rules have it.
 """
 from __future__ import annotations
 
@@ -19,6 +20,17 @@ def _blocks(n: int) -> int:
 def _want(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _new(shape, dtype: torch.dtype, device, stream=None) -> torch.Tensor:
+    """An empty tensor in the memory of the stream that writes it: what another stream
+    has freed may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _matrix(t: torch.Tensor, what: str, dtypes):
@@ -51,7 +63,7 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
     shape = -(-rows // block_rows), _blocks(cols)
     if codes is None:
         ldc = -(-cols // 16) * 16
-        codes = torch.empty((rows, ldc), dtype=torch.float8_e4m3fn, device=x.device)
+        codes = _new((rows, ldc), torch.float8_e4m3fn, x.device, stream)
         if ldc != cols:
             codes = codes[:, :cols]
     else:
@@ -59,7 +71,7 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
         _want((r, c) == (rows, cols), "codes: another shape than x")
         _want(codes.device == x.device, "tensors on several devices")
     if scales is None:
-        scales = torch.empty(shape, dtype=torch.float32, device=x.device)
+        scales = _new(shape, torch.float32, x.device, stream)
         lds = shape[1]
     else:
         r, c, lds = _matrix(scales, "scales", _F32)
@@ -93,13 +105,13 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     rb, cb, ldbs = _matrix(b_scales, "b_scales", _F32)
     _want((ra, ca) == (M, _blocks(K)), "a_scales: shape")
     _want((rb, cb) == (_blocks(N), _blocks(K)), "b_scales: shape")
-    out, ldo = _output(out, M, N, out_dtype, a.device)
+    out, ldo = _output(out, M, N, out_dtype, a.device, stream)
     B.reflex_matmul_fp8(a, lda, a_scales, ldas, b, ldb, b_scales, ldbs, M, N, K,
                         _DTYPES[out.dtype], out, ldo, status, stream)
     return out
 
 
-def _output(out, M: int, N: int, dtype, device):
+def _output(out, M: int, N: int, dtype, device, stream):
     """The output (given, or new) and its row stride."""
     if out is not None:
         r, c, ldo = _matrix(out, "out", _DTYPES)
@@ -110,7 +122,7 @@ def _output(out, M: int, N: int, dtype, device):
     # (999 x 50001 x 2048 to bf16: 105 us, packed rows 236)
     unit = 16 // dtype.itemsize
     ldo = -(-N // unit) * unit if N >= 4 * unit else N
-    out = torch.empty((M, ldo), dtype=dtype, device=device)
+    out = _new((M, ldo), dtype, device, stream)
     return (out if ldo == N else out[:, :N]), ldo
 
 
@@ -138,7 +150,7 @@ class LinearFp8:
         _want(K == self.K, "x: another number of columns than the weights")
         _want(x.device == self.ws.device, "x is on another device than the weights")
         _want(M <= self.max_rows, "more rows than the workspace was sized for")
-        out, ldo = _output(out, M, self.N, self.out_dtype, x.device)
+        out, ldo = _output(out, M, self.N, self.out_dtype, x.device, stream)
         B.reflex_linear_fp8(_DTYPES[x.dtype], x, ldx, self.codes, self._w_ld, self.scales,
                             self._s_ld, M, self.N, K, _DTYPES[out.dtype], out, ldo, self.ws,
                             self.ws_bytes, stream, check)
@@ -155,10 +167,11 @@ def quantize_experts(w_gate_up: torch.Tensor, w_down: torch.Tensor, stream=None)
     e, two, d = (int(n) for n in w_gate_up.shape)
     inter = two // 2
     _want(two == 2 * inter and tuple(w_down.shape) == (e, d, inter), "weights: shapes")
-    gu = torch.empty((e, 2 * inter, d), dtype=torch.float8_e4m3fn, device=w_gate_up.device)
-    dn = torch.empty((e, d, inter), dtype=torch.float8_e4m3fn, device=w_down.device)
-    gus = torch.empty((e, 2, _blocks(inter), _blocks(d)), device=w_gate_up.device)
-    dns = torch.empty((e, _blocks(d), _blocks(inter)), device=w_down.device)
+    dev = w_gate_up.device
+    gu = _new((e, 2 * inter, d), torch.float8_e4m3fn, dev, stream)
+    dn = _new((e, d, inter), torch.float8_e4m3fn, dev, stream)
+    gus = _new((e, 2, _blocks(inter), _blocks(d)), torch.float32, dev, stream)
+    dns = _new((e, _blocks(d), _blocks(inter)), torch.float32, dev, stream)
     for i in range(e):
         for h in range(2):
             part = slice(h * inter, (h + 1) * inter)
@@ -202,7 +215,7 @@ class ExpertsFp8:
         T = int(hidden.shape[0])
         _want(T <= self.max_tokens, "more tokens than the workspace was sized for")
         if out is None:
-            out = torch.empty((T, self.d), dtype=torch.bfloat16, device=hidden.device)
+            out = _new((T, self.d), torch.bfloat16, hidden.device, stream)
         for t, dt, shape, what in ((hidden, torch.bfloat16, (T, self.d), "hidden"),
                                    (ids, torch.int32, (T, self.k_max), "ids"),
                                    (alpha, torch.float32, (T, self.k_max), "alpha"),
