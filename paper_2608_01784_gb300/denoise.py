@@ -26,6 +26,17 @@ def quantize_layer(w_router: torch.Tensor, w_gate_up: torch.Tensor, w_down: torc
     return dict(w_router=w_router, **api.quantize_experts(w_gate_up, w_down, stream))
 
 
+def _a_header_a_layer(op, layers: int) -> list:
+    """The operator's workspace for one call a layer, each 256 bytes after the one
+    before: a call's error word lies in front of all that later calls write, so every
+    layer's can be read at the end."""
+    nbytes, device = op.ws_bytes, op.ws.device
+    op.ws = None
+    ws = torch.empty(nbytes + 256 * (layers - 1), dtype=torch.uint8, device=device)
+    ws[:256 * layers].zero_()
+    return [ws[256 * i:256 * i + nbytes] for i in range(layers)]
+
+
 class DenoiserFp8:
     """Layers (quantize_layer) of one shape, without a shared expert, and an
     output head (codes, scales: quantize_fp8 of [vocab, d] in 128 x 128 blocks),
@@ -43,6 +54,9 @@ class DenoiserFp8:
         self.experts = api.ExpertsFp8(layers[0], **shape)
         for w in layers[1:]:
             self.experts.check_weights(w)
+        self._ws = list(zip(_a_header_a_layer(self.router, len(layers)),
+                            _a_header_a_layer(self.experts, len(layers))))
+        self.router.ws, self.experts.ws = self._ws[0]
         self.head = api.LinearFp8(*head, max_rows=max_tokens)
         if self.head.K != d:
             raise ValueError("the head takes another width than the layers give")
@@ -68,6 +82,7 @@ class DenoiserFp8:
         for i, w in enumerate(self.layers):
             out = self._h[i & 1][:T]
             self.router.w = self.experts.w = w
+            self.router.ws, self.experts.ws = self._ws[i]
             if i == 0:  # counts and the first router in one call
                 self.router.step(state, params, h, out=out, k_out=k, k_sum=self.k_sum,
                                  status=self._status[:1], flags=route)
@@ -94,10 +109,10 @@ class DenoiserFp8:
                                 status=self._status[2:])
 
     def status(self) -> int:
-        """The first error of the last forward's steps, of the layers the last one's
-        (waits)."""
+        """The first error of the last forward's steps, in any layer (waits)."""
         codes = [B.reflex_read_status(self._status[i:i + 1]) for i in range(3)]
-        codes += [self.router.status(), self.experts.status(), self.head.status()]
+        codes += [B.reflex_moe_status(ws) for pair in self._ws for ws in pair]
+        codes.append(self.head.status())
         return next((c for c in codes if c != B.REFLEX_OK), B.REFLEX_OK)
 
 
