@@ -37,6 +37,12 @@ def _a_header_a_layer(op, layers: int) -> list:
     return [ws[256 * i:256 * i + nbytes] for i in range(layers)]
 
 
+def _check(t: torch.Tensor, shape: tuple, what: str, device=None):
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == shape
+            and t.is_contiguous() and t.device == (device or t.device)):
+        raise ValueError(f"{what}: a contiguous CUDA tensor {shape} of torch.bfloat16")
+
+
 class DenoiserFp8:
     """Layers (quantize_layer) of one shape, without a shared expert, and an
     output head (codes, scales: quantize_fp8 of [vocab, d] in 128 x 128 blocks),
@@ -54,6 +60,8 @@ class DenoiserFp8:
         self.experts = api.ExpertsFp8(layers[0], **shape)
         for w in layers[1:]:
             self.experts.check_weights(w)
+        for w in layers:
+            _check(w["w_router"], (E, d), "w_router")
         self._ws = list(zip(_a_header_a_layer(self.router, len(layers)),
                             _a_header_a_layer(self.experts, len(layers))))
         self.router.ws, self.experts.ws = self._ws[0]
@@ -77,6 +85,7 @@ class DenoiserFp8:
         T = int(hidden.shape[0])
         if T > self.max_tokens:
             raise ValueError("more tokens than the buffers were sized for")
+        _check(hidden, (T, self.experts.d), "hidden", self.k.device)
         k, route = self.k[:T], self.flags | B.REFLEX_STAGE_ROUTE
         h = hidden
         for i, w in enumerate(self.layers):
