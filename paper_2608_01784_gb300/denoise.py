@@ -77,6 +77,7 @@ class DenoiserFp8:
         self.k = torch.empty(max_tokens, dtype=torch.int32, device=dev)
         self.k_sum = torch.zeros(1, dtype=torch.int64, device=dev)
         self._status = torch.zeros(3, dtype=torch.int32, device=dev)
+        self._committed = torch.empty(max_tokens, dtype=torch.int32, device=dev)
 
     def logits(self, state: dict, params: B.reflex_alloc_params,
                hidden: torch.Tensor) -> torch.Tensor:
@@ -108,12 +109,17 @@ class DenoiserFp8:
         """One forward on device tensors: `state` moves on by one (update_state);
         tokens int32 [T] and conf fp32 [T] receive what every position that was
         masked would take (-1 and 0 elsewhere).  u [T] holds the uniforms, and
-        settings are sample()'s temperature, top_k, top_p and min_p."""
+        settings are sample()'s temperature, top_k, top_p and min_p.  Returns the
+        numbers of commits, in `committed` or in a buffer that the next forward
+        overwrites (up to max_tokens sequences)."""
         masked = state["masked"]
         self._status.zero_()
         logits = self.logits(state, params, hidden)
         api.sample(logits, u, masked=masked, tokens=tokens, conf=conf, status=self._status[1:2],
                    **settings)
+        sequences = int(state["active_block"].numel())
+        if committed is None and sequences <= self.max_tokens:
+            committed = self._committed[:sequences]
         return api.update_state(state, conf, num_blocks, theta_commit, committed=committed,
                                 status=self._status[2:])
 
