@@ -8,8 +8,8 @@ import numpy as np
 import torch
 
 from . import _binding as B
-from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, _new, matmul_fp8,  # noqa: F401
-                  quantize_experts, quantize_fp8)
+from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, _new, _status_word,  # noqa: F401
+                  matmul_fp8, quantize_experts, quantize_fp8)
 
 
 def _dev(a: np.ndarray, device, dtype=None) -> torch.Tensor:
@@ -323,6 +323,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor |
                         (conf, torch.float32, "conf")):
         if t is not None:
             check(t, dt, what)
+    _status_word(status, dev)
     if tokens is None:
         tokens = _new(rows, torch.int32, dev, stream)
     if conf is None:

@@ -49,6 +49,13 @@ def _matrix(t: torch.Tensor, what: str, dtypes):
     return rows, cols, ld
 
 
+def _status_word(status: torch.Tensor | None, device):
+    """Refuses an error word that a kernel on `device` could not write."""
+    _want(status is None or (status.dtype == torch.int32 and status.numel() == 1
+                             and status.device == device),
+          "status: one int32 on the device of the inputs")
+
+
 _F32 = (torch.float32,)
 _E4M3 = (torch.float8_e4m3fn,)
 
@@ -105,6 +112,9 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     rb, cb, ldbs = _matrix(b_scales, "b_scales", _F32)
     _want((ra, ca) == (M, _blocks(K)), "a_scales: shape")
     _want((rb, cb) == (_blocks(N), _blocks(K)), "b_scales: shape")
+    _want(a.device == a_scales.device == b.device == b_scales.device,
+          "tensors on several devices")
+    _status_word(status, a.device)
     out, ldo = _output(out, M, N, out_dtype, a.device, stream)
     B.reflex_matmul_fp8(a, lda, a_scales, ldas, b, ldb, b_scales, ldbs, M, N, K,
                         _DTYPES[out.dtype], out, ldo, status, stream)
@@ -137,6 +147,7 @@ class LinearFp8:
         self.N, self.K, self._w_ld = _codes(codes, "codes")
         r, c, self._s_ld = _matrix(scales, "scales", _F32)
         _want((r, c) == (_blocks(self.N), _blocks(self.K)), "scales: shape")
+        _want(scales.device == codes.device, "tensors on several devices")
         _want(out_dtype in _DTYPES, "outputs are fp32 or bf16")
         self.max_rows, self.out_dtype = max_rows, out_dtype
         self.ws_bytes = B.reflex_linear_fp8_workspace_size(max_rows, self.K)
@@ -204,8 +215,9 @@ class ExpertsFp8:
         for name, shape in shapes.items():
             t = weights[name]
             dt = torch.float32 if name.endswith("scales") else torch.float8_e4m3fn
-            _want(t.is_cuda and t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous(),
-                  f"{name}: a contiguous CUDA tensor {shape} of {dt}")
+            _want(t.is_cuda and t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous()
+                  and t.device == weights["w_down"].device,
+                  f"{name}: a contiguous CUDA tensor {shape} of {dt}, all on one device")
 
     def forward(self, hidden: torch.Tensor, ids: torch.Tensor, alpha: torch.Tensor,
                 k: torch.Tensor, out: torch.Tensor | None = None, residual: bool = False,
