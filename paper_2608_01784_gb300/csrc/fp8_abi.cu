@@ -226,6 +226,7 @@ int reflex_matmul_fp8(const uint8_t* a, int64_t lda, const float* a_scales, int6
         !aligned(out, out_dtype == REFLEX_DTYPE_F32 ? 4 : 2))
       return REFLEX_EINVAL;
   }
+  if (!aligned(dev_status, 4)) return REFLEX_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));
   if (M == 0) return REFLEX_OK;
@@ -402,6 +403,12 @@ int reflex_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, i
   if (logits == nullptr || u == nullptr || tokens_out == nullptr || conf_out == nullptr ||
       !aligned(logits, dtype == REFLEX_DTYPE_F32 ? 4 : 2))
     return REFLEX_EINVAL;
+  for (const void* words : {static_cast<const void*>(temperature), static_cast<const void*>(top_k),
+                            static_cast<const void*>(top_p), static_cast<const void*>(min_p),
+                            static_cast<const void*>(u), static_cast<const void*>(tokens_out),
+                            static_cast<const void*>(conf_out),
+                            static_cast<const void*>(dev_status)})
+    if (!aligned(words, 4)) return REFLEX_EINVAL;
   const rx::SampleArgs a{logits, ld, rows,   vocab,      temperature, top_k, top_p,
                          min_p,  u,  masked, tokens_out, conf_out,
                          reinterpret_cast<uint32_t*>(dev_status)};
