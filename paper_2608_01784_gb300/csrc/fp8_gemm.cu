@@ -44,8 +44,10 @@
 // warp's vectors, 900 to 3000 by TMA.  61,000 pairs of 256 experts, d = 2048, inter
 // = 512: layer 458 us without these two, 385 with.
 //
-// Every wait is bounded (2 s); on expiry the CTA records the timeout in the
-// error word, drains its loads and MMAs, frees TMEM and exits.
+// Every wait on a barrier in shared memory is bounded (2 s); on expiry the CTA records
+// the timeout in the error word, drains its loads and MMAs, frees TMEM and exits.  The
+// two barriers of a cluster (its CTAs run together; each comes to the last one past
+// bounded waits alone) have no limit.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "internal.h"
@@ -193,6 +195,7 @@ __device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
   return v;
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();  // the barrier takes whole warps, whatever branch a lane comes from
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
