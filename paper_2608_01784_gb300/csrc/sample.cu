@@ -35,6 +35,8 @@
 // bf16 tokens.  2048 rows of 131072 in bf16 (their bytes take 79 us): greedy 114 us,
 // no filters 199, top-k 50 232, top-p 0.9 540.  One such row: 24 us with every filter,
 // a dozen of the cluster's barriers one after another.
+#include <float.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -433,7 +435,7 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
   const float min_p = a.min_p ? a.min_p[row] : 0.0f;
   float u = a.u[row];
   const bool out = a.masked != nullptr && a.masked[row] == 0;
-  const bool bad = !(temp >= 0.0f && temp <= 3.4e38f) || !(top_p > 0.0f) || !(min_p <= 1.0f) ||
+  const bool bad = !(temp >= 0.0f && temp <= FLT_MAX) || !(top_p > 0.0f) || !(min_p <= 1.0f) ||
                    !(u == u);
   if (out || bad) {
     if (leader) {
@@ -627,7 +629,7 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
     }
     return;
   }
-  if (m > 3.4028234e38f) {  // +inf: those tokens alone, alike
+  if (m > FLT_MAX) {  // +inf: those tokens alone, alike
     if (!kStream) {
       for (int i = 0; i < steps; ++i)
 #pragma unroll
@@ -642,7 +644,7 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
     m = 0.0f;
   }
   const float neg_m = -m;
-  const float c = fminf(__fdiv_rn(kLog2e, temp), 3.4028234e38f);
+  const float c = fminf(__fdiv_rn(kLog2e, temp), FLT_MAX);
   const bool by_k = !greedy && top_k > 0, by_p = !greedy && top_p < 1.0f;
   const bool cut_any = by_k || by_p;
   const uint32_t w_min =
