@@ -33,7 +33,7 @@
 // Bound: instruction issue, about 15 instructions a token for weights (fp32 in
 // packed pairs), 8 for counts, against the 12 cycles that HBM gives an SM for 128
 // bf16 tokens.  2048 rows of 131072 in bf16 (their bytes take 79 us): greedy 114 us,
-// no filters 199, top-k 50 232, top-p 0.9 540.  One such row: 24 us with every filter,
+// no filters 197, top-k 50 228, top-p 0.5 to 0.9999 between 420 and 525.  One such row: 24 us with every filter,
 // a dozen of the cluster's barriers one after another.
 #include <float.h>
 
@@ -884,13 +884,14 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
           for (int i = 0; i < kPer; ++i) n[i] = s.fine[bin0 + i];
         }
       }
-      float w[kPer];  // the bins' middle weights, relative
-      w[0] = exp2f(static_cast<float>(threadIdx.x) * (-kPer / 32.0f));
-      uint32_t own_n = n[0];
-      float own_m = n[0] * w[0];
+      float w[kPer];  // the bins' middle weights, rounded down as every weight is
+      float middle = exp2f(31.0f - static_cast<float>(threadIdx.x) * (kPer / 32.0f));
+      uint32_t own_n = 0;
+      float own_m = 0.0f;
 #pragma unroll
-      for (int i = 1; i < kPer; ++i) {
-        w[i] = w[i - 1] * 0.97857206208770013f;  // 2^(-1/32)
+      for (int i = 0; i < kPer; ++i) {
+        w[i] = floorf(middle);
+        middle *= 0.97857206208770013f;  // 2^(-1/32)
         own_n += n[i];
         own_m += n[i] * w[i];
       }
@@ -901,7 +902,9 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
         s.warp_f[warp] = est + own_m;
       }
       if (threadIdx.x < 4) {
-        s.bin[threadIdx.x] = kFine;
+        // (top-p: a bin that rounding keeps from being named is the last one, below
+        // which no weight counts)
+        s.bin[threadIdx.x] = by_k ? kFine : kFine - 1;
         s.at[threadIdx.x] = 0;
       }
       __syncthreads();
@@ -913,10 +916,20 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
         }
         whole += s.warp_f[i];
       }
-      // top-p: a bin's weights are within 1.1% of the middle one, so that the
-      // first pair of bins cannot miss; the second does not where the tokens
-      // spread over their bins
-      const float want = top_p * whole;
+      // top-p: a bin's weights are within 1.1 % of the middle one.  The cut is taken to
+      // lie no earlier than the first bin up to which the sum may reach top_p of the
+      // whole, and no later than the first at which it must, by the weights up to a
+      // bin or by those behind it, of which 1 - top_p is left: next to top_p = 1 they
+      // alone tell bins apart.  The second pair is closer, for rows whose first holds
+      // too many tokens.  A pair that misses is found out by the search, which adds
+      // the weights up exactly, and costs time alone.
+      const float want = top_p * whole, rest = (1.0f - top_p) * whole;
+      auto may = [&](float e, float off) {
+        return e * (1.0f + off) >= want && (whole - e) * (1.0f - off) <= rest;
+      };
+      auto must = [&](float e, float off) {
+        return e * (1.0f - off) >= want || (whole - e) * (1.0f + off) <= rest;
+      };
       uint32_t c0 = cnt;
       float e0 = est;
 #pragma unroll
@@ -930,10 +943,10 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
         } else {
           // (a little less: the threads' running sums round differently)
           const float d0 = (e0 - n[i] * w[i]) * 0.9999f;
-          if (e0 * 1.012f >= want && d0 * 1.012f < want) atomicMin(&s.bin[0], b);
-          if (e0 * 0.988f >= want && d0 * 0.988f < want) atomicMin(&s.bin[1], b);
-          if (e0 * 1.003f >= want && d0 * 1.003f < want) atomicMin(&s.bin[2], b);
-          if (e0 * 0.997f >= want && d0 * 0.997f < want) atomicMin(&s.bin[3], b);
+          if (may(e0, 0.012f) && !may(d0, 0.012f)) atomicMin(&s.bin[0], b);
+          if (must(e0, 0.012f) && !must(d0, 0.012f)) atomicMin(&s.bin[1], b);
+          if (may(e0, 0.003f) && !may(d0, 0.003f)) atomicMin(&s.bin[2], b);
+          if (must(e0, 0.003f) && !must(d0, 0.003f)) atomicMin(&s.bin[3], b);
         }
       }
       __syncthreads();
