@@ -33,8 +33,8 @@
 // Bound: instruction issue, about 15 instructions a token for weights (fp32 in
 // packed pairs), 8 for counts, against the 12 cycles that HBM gives an SM for 128
 // bf16 tokens.  2048 rows of 131072 in bf16 (their bytes take 79 us): greedy 114 us,
-// no filters 197, top-k 50 228, top-p 0.5 to 0.9999 between 420 and 525.  One such row: 24 us with every filter,
-// a dozen of the cluster's barriers one after another.
+// no filters 197, top-k 50 228, 5000 423, top-p 0.5 to 0.9999 between 410 and 525.  One
+// such row: 24 us with every filter, a dozen of the cluster's barriers one after another.
 #include <float.h>
 
 #include <algorithm>
@@ -769,12 +769,15 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
       if (same_t) count_pass(std::true_type(), i0, i1);
       else count_pass(std::false_type(), i0, i1);
     };
-    if (kStream && by_k && steps >= 4 * kSample && top_k < a.vocab / 16) {
+    if (kStream && by_k && steps >= 4 * kSample && top_k < a.vocab / 16 &&
+        4 * top_k <= kList) {
       // Top-k of few: the counts of a sample (the first steps of every warp)
       // name the bins that hold three times as many tokens; these make the
       // list, and the other steps are not counted (2048 rows of 131072, top-k
-      // 50: 313 us with counts, 232 us without).  Should the list be too short
-      // all the same, or too long, the whole row is searched.
+      // 50: 313 us with counts, 228 us without).  Should the list be too short
+      // all the same, or too long, the whole row is searched, so a quarter of the list
+      // is the most that is asked for (top-k 3000 and 5000 there, 9000 and 15000 tokens
+      // for 10240 places: 590 and 2910 us).
       counts(0, kSample);
       __syncthreads();
       if (warp == 0) {

@@ -84,3 +84,20 @@ def test_far_cuts_cost_no_walk_over_every_token(kind):
     near = time(top_p=0.9)
     for p in (0.985, 0.99, 0.999, 0.9999):
         assert time(top_p=p) <= 2 * near, (p, near)
+
+
+@pytest.mark.parametrize("kind", ["spread", "peaked"])
+def test_top_k_of_thousands_costs_no_walk_over_every_token(kind):
+    """The same rows: six times as long where the list cannot hold what is asked for."""
+    rows, vocab = 304, 131072
+    z = logits_of(1, rows, vocab, BF16) if kind == "spread" else peaked(rows, vocab, BF16)
+    u = torch.tensor(uniforms(1, rows), device="cuda")
+    tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
+    conf = torch.empty(rows, device="cuda")
+
+    def time(k):
+        k = torch.full((rows,), k, dtype=torch.int32, device="cuda")
+        return us(lambda: api.sample(z, u, tokens=tokens, conf=conf, top_k=k))
+    near = time(9000)
+    for k in (2000, 2560, 3000, 3500, 5000, 8000):
+        assert time(k) <= 2 * near, (k, near)
