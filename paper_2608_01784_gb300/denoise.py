@@ -131,8 +131,9 @@ class DenoiserFp8:
         return next((c for c in codes if c != B.REFLEX_OK), B.REFLEX_OK)
 
 
-def main(seed: int = 0) -> dict:
-    """Two sequences of a small random model from all masked to all committed."""
+def main(seed: int = 0, most: int | None = None) -> dict:
+    """Two sequences of a small random model from all masked to all committed, or as
+    far as `most` forwards take them."""
     from . import trajectory, workloads
     cfg = workloads.CONFIGS["tiny_fp32"].with_(dtype="bf16", n_seq=2)
     vocab, layers = 1000, 2
@@ -156,7 +157,7 @@ def main(seed: int = 0) -> dict:
     settings = dict(temperature=torch.full((cfg.T,), 0.8, device="cuda"),
                     top_p=torch.full((cfg.T,), 0.95, device="cuda"))
     forwards = 0
-    while bool((state["active_block"] <= blocks).any()):
+    while forwards != most and bool((state["active_block"] <= blocks).any()):
         known = (text >= 0)[:, None]
         hidden = (torch.where(known, embed[text.clamp(min=0).long()], mask_row) + place)
         before = state["masked"].clone()
