@@ -12,7 +12,11 @@
 // c1 .. c5 interpolate (2^f - 1) / f at the five Chebyshev nodes of [-1/2,
 // 1/2]; p is within 3e-7 of 2^f.  Weights are 2^31 at the largest logit and 0
 // from about 2^-31 of it down; sums of 2^18 of them fit 64 bits and are exact
-// in a double, in which the comparisons with p * mass and u * mass are made.
+// in a double, in which the comparisons with p * mass and u * mass are made.  The
+// confidence is the library's exponential of the token over an fp32 sum of e^(z - m);
+// the sum's terms, one a token, are hardware exponentials of a rounded exponent (each
+// within 2^-22 and 2^-24 of its exponent; the terms that count are near the largest
+// logit, and the library's would double the instructions of a token).
 //
 // Two shapes of one kernel.  Few rows, or short ones: a row is held in the shared
 // memory of a cluster of 1 to 8 CTAs.  Many long rows: one CTA of 512 threads
@@ -1303,7 +1307,7 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
               }
             }
             a.tokens[row] = pos0 + off + pick - shift;
-            a.conf[row] = ex2((zt + neg_m) * kLog2e) / esum;
+            a.conf[row] = expf(zt + neg_m) / esum;
           }
           break;
         }
