@@ -436,7 +436,7 @@ int reflex_quantize_fp8(int32_t dtype, const void* x, int64_t rows, int64_t cols
  * reflex_matmul_fp8 — out = A B^T over codes:
  *   out[m, n] = sum_b sa[m, b] sb[n / 128, b] sum_{k in block b} A[m, k] B[n, k]
  * with fp32 sums; each block of K is summed by the tensor cores and scaled
- * once.
+ * once, by the product of both scales in fp32 (which has to be finite).
  *   a         [M, K] codes, row stride lda (a multiple of 16, >= K);
  *             a_scales [M, ceil(K / 128)], row stride ldas.
  *   b         [N, K] codes, row stride ldb (a multiple of 16, >= K);
@@ -480,7 +480,7 @@ int reflex_linear_fp8(int32_t dtype, const void* x, int64_t ldx, const uint8_t* 
  *   hidden         [T, d] bf16.
  *   ids, alpha     [T, k_max]: slots j < k[t] are read; an id outside [0, E)
  *                  there sets REFLEX_EINVAL in the error word and its pair
- *                  is left out.
+ *                  is left out, whatever its weight is.
  *   k              [T] int32 counts in [1, min(k_max, E)] (else REFLEX_EKRANGE
  *                  in the error word and the count is clamped).
  *   w_gate_up      [E, 2 inter, d] codes: gate rows, then up rows;

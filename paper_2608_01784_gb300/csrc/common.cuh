@@ -44,8 +44,12 @@ constexpr int kTileM = 128;  // rows per grouped-GEMM tile (M of tcgen05.mma)
 // current one drains and runs its prologue (barrier setup, TMEM allocation)
 // early.  grid_dep_wait() returns once the preceding kernel has completed and
 // its writes are visible; every kernel calls it before its first global
-// memory access, so stream order is kept exactly.  grid_dep_launch() allows
-// the following kernel to be scheduled.  Both are no-ops for plain launches.
+// memory access, so stream order is kept exactly.  (One reads earlier:
+// experts_down_rows_kernel, and only what was written before the kernel in front of
+// it, its own call's experts_up_rows_kernel.  That kernel allows the launch after its
+// own wait alone, so all that came before it is complete and visible by then.)
+// grid_dep_launch() allows the following kernel to be scheduled: it comes after the
+// wait.  Both are no-ops for plain launches.
 __device__ __forceinline__ void grid_dep_wait() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }

@@ -32,11 +32,13 @@
 // back (128 KB), scale it and hand the accumulator on take about 1000, of which the
 // reads and FMAs by themselves are 340 and the rest are latencies of two barriers,
 // of the scales' reads and of TMEM that two warps a scheduler cannot hide.
-// 8192 x 8192 x 8192: 485 us, 2.27 PFLOP/s; with a quarter of the MMAs 475, without
-// the sums 426, without these and the loads of B 358.  Sixteen warps of 64
+// 8192 x 8192 x 8192: 452 us, 2.43 PFLOP/s, on one card, 485 on the one that these
+// were timed on: with a quarter of the MMAs 475, without the sums 426, without these
+// and the loads of B 358, so no one of them is the limit by itself.  Sixteen warps of 64
 // accumulators took 552 us (the same latencies by twice the warps); CTA pairs on a
 // tile of 256 rows, accumulators of 128 columns, scalar FMAs and reading the next
-// block's scales ahead were no faster.  For few rows the weights' bytes:
+// block's scales ahead were no faster as they were tried.  fp32 out (stored by the
+// summing warps): 483 us where bf16 takes 452.  For few rows the weights' bytes:
 // 32 x 50000 x 2048 30 us, of which the bytes take 16.
 //
 // Short K (512 in a down product) shows what a tile costs besides its blocks: finding

@@ -2,9 +2,10 @@
 // layer of reflex_linear_fp8 for one to four rows in one launch, and the routed
 // experts of reflex_experts_fp8 for a few pairs in two.
 //
-// Bound: the weights' bytes (65536 x 2048, one row: 27 us, 73 % of the measured
+// Bound: the weights' bytes (65536 x 2048, one row: 25 us, 80 % of the measured
 // copy rate) and, when they are few, launches and trips to HBM (4096 x 2048: 4.8 us,
-// of which the bytes take 1.2; one token of 64 experts of 1024 18 us, 6).
+// of which the bytes take 1.2, 3.7 with the weights in L2; twelve experts of 1024 for
+// one token 25 us, 11).  Times are of replayed graphs.
 // A warp takes four rows of the weights (experts: eight) at a time and 512 columns a
 // step, 16 bytes of each row a lane, two steps in flight, and the rows of x are read
 // from shared memory once for all of them.  Every CTA quantises its rows of x by
@@ -311,7 +312,8 @@ __global__ void __launch_bounds__(kThreads) experts_down_rows_kernel(const Fp8Ex
     sc[0] = sc[1] = p.down_scales + (static_cast<int64_t>(e) * db + n0 / 128) * ib + (lane >> 3);
     Steps<8> v;
     load_steps(v, rows, sc, 0, p.inter);
-    // the weights are not the launch's before: only act waits for it
+    // (k, ids, the weights and their scales are older than the launch before, which
+    // allowed this one after its own wait: only act waits for it)
     if (!waited) grid_dep_wait();
     waited = true;
     const float* act = p.act + (static_cast<int64_t>(t) * p.k_max + j) * p.inter;
@@ -390,12 +392,12 @@ size_t row_bytes(int cols) {
 }  // namespace
 
 // Two launches instead of six pay while the slots' weights, read again for every
-// slot, are few.  Layer in us, here | tiles:
-//   d 2048, inter 1024, k_max 12: 1 token (12 slots, 75 MB) 18 | 34, 2 31 | 39,
-//   3 (226 MB) 42 | 43, 4 61 | 60; k_max 8: 3 (151 MB) 37 | 40, 4 (201 MB) 44 | 42;
-//   d 2048, inter 512, k_max 12: 1 14 | 32, 4 (151 MB) 39 | 43, 6 (226 MB) 56 | 54;
-//   d 1024, inter 512, k_max 8: 1 10 | 26, 8 (101 MB) 28 | 29, 16 (201 MB) 49 | 32;
-//   d 256, inter 128, k_max 4: 1 7 | 21, 32 (128 slots) 20 | 22.
+// slot, are few.  Layer in us, every slot in use, here | tiles:
+//   d 2048, inter 1024, k_max 12: 1 token (12 slots, 75 MB) 25 | 35, 2 45 | 57,
+//   3 (226 MB) 64 | 59, 4 82 | 61; k_max 8: 3 (151 MB) 44 | 55, 4 (201 MB) 55 | 57;
+//   d 2048, inter 512, k_max 12: 1 16 | 32, 4 (151 MB) 50 | 56, 6 (226 MB) 67 | 63;
+//   d 1024, inter 512, k_max 8: 1 9 | 26, 8 (101 MB) 34 | 35, 16 (201 MB) 60 | 38;
+//   d 256, inter 128, k_max 4: 1 6 | 20, 32 (128 slots) 19 | 21.
 // Both kernels' rows lie in shared memory.
 bool experts_rows_fit(int T, int k_max, int d, int inter) {
   const int64_t slots = static_cast<int64_t>(T) * k_max;
@@ -413,8 +415,9 @@ cudaError_t launch_experts_rows(const Fp8ExpertsRows& p, cudaStream_t stream) {
 
 // x fits in shared memory, and the products of each of up to four rows by
 // themselves take no longer than the tensor cores' tiles of 128 (us, here |
-// quantisation and tiles): 4096 x 2048 at M = 1..4 4.8, 5.8, 6.7, 7.9 | 11.4;
-// 4096 x 4096 at 4 13.7 | 14.1; 65536 x 2048 at 1, 2, 4 27, 35, 57 | 30.
+// quantisation and tiles; weights from HBM): 4096 x 2048 at M = 1..4 4.8, 5.8, 6.8,
+// 8.0 | 11.8 to 12.1; 4096 x 4096 at 4 13.7 | 14.9; 65536 x 2048 at 1, 2, 4 25, 34,
+// 56 | 28.
 bool linear_rows_fit(int M, int N, int K) {
   return M <= 4 && static_cast<int64_t>(M) * ((static_cast<int64_t>(K) + kChunk - 1) / kChunk *
                                               kChunk) <= 16384 &&

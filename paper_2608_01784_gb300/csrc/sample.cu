@@ -16,7 +16,8 @@
 // confidence is the library's exponential of the token over an fp32 sum of e^(z - m);
 // the sum's terms, one a token, are hardware exponentials of a rounded exponent (each
 // within 2^-22 and 2^-24 of its exponent; the terms that count are near the largest
-// logit, and the library's would double the instructions of a token).
+// logit.  2048 rows of 131072 bf16, greedy 112 us, T = 0.7 206, top-k 50 228; with the
+// library's 145, 255 and 260).
 //
 // Two shapes of one kernel.  Few rows, or short ones: a row is held in the shared
 // memory of a cluster of 1 to 8 CTAs.  Many long rows: one CTA of 512 threads
@@ -510,7 +511,8 @@ __device__ __forceinline__ void sample_row(const Args& a, Shared<kStream>& s, Te
   // visit(i, z, raw) for the steps from i0 to i1 - 1, `kAhead` loads in flight
   // Streamed bf16: two.  With four the loops outgrow the instruction caches that two
   // CTAs in different rows' filters share (a quarter of the stalls; 2048 rows of
-  // 131072 without filters 194 us, two 199, top-p 573, 540, mixed filters 414, 341).
+  // 131072 without filters 191 us, two 198, top-p 0.9 499, 471, 4096 mixed rows 417,
+  // 331).
   constexpr int kAhead = kStream && sizeof(Te) == 2 ? 2 : 1;
   constexpr int kSample = kStream ? 32 / sizeof(Te) / 4 : 1;  // steps that top-k looks at first
   auto each_step = [&](int i0, int i1, auto visit) {
@@ -1376,8 +1378,8 @@ cudaError_t launch_typed(Args a, int rows, int num_sms, cudaStream_t stream) {
   while (C < 8 && slice_of(C, kGrain) * sizeof(Te) > 56 * 1024) ++C;
   // A row that no CTA holds is streamed as soon as the rows fill half of the SMs
   // (rows of 131072 bf16 logits, cluster / stream in us, plain, top-k 50, top-p
-  // 0.9: 32 rows 17, 25, 37 / 23, 29, 66; 76 rows 25, 45, 70 / 23, 29, 66; 304
-  // rows 64, 112, 176 / 33, 42, 93).
+  // 0.9: 32 rows 17, 26, 34 / 21, 27, 50; 76 rows 20, 29, 39 / 21, 27, 50; 100 rows
+  // 28, 49, 60 / 22, 27, 49; 304 rows 59, 99, 131 / 34, 36, 75).
   if (C > 1 && 2 * static_cast<int64_t>(rows) >= num_sms) {
     a.slice = slice_of(1, Shape<true>::kWarps * kStep);
     return launch_shape<Te, true>(a, rows, 1, stream);

@@ -46,7 +46,9 @@ def _check(t: torch.Tensor, shape: tuple, what: str, device=None):
 class DenoiserFp8:
     """Layers (quantize_layer) of one shape, without a shared expert, and an
     output head (codes, scales: quantize_fp8 of [vocab, d] in 128 x 128 blocks),
-    with buffers for `max_tokens` tokens."""
+    with buffers for `max_tokens` tokens.  The router's workspace is that of a whole
+    bf16 layer (2.4 GB at 32768 tokens, d = 2048, 64 experts of 1024, 12 slots), of
+    which a forward uses the scores and the record alone."""
 
     def __init__(self, layers: list, head: tuple, *, d: int, E: int, inter: int, k_max: int,
                  max_tokens: int, flags: int = B.REFLEX_FLAG_RENORM_TOPK):
