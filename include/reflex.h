@@ -551,6 +551,116 @@ int reflex_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, i
                   const float* min_p, const float* u, const uint8_t* masked,
                   int32_t* tokens_out, float* conf_out, int32_t* dev_status, void* stream);
 
+/*
+ * ---- around the experts, with gradients -------------------------------------
+ */
+
+/*
+ * reflex_block_norm — root-mean-square norms around a block, with its gate and
+ * scale, on the residual stream.  With r(v) = 1 / sqrt(mean(v^2) + eps), per row:
+ *   a = y r(y) w_after,   out = h + scale * gate * a,   norm = out r(out) w_before
+ * in fp32 from the inputs to each output's one rounding (norm is taken from out
+ * before that is rounded).
+ *   dtype     REFLEX_DTYPE_F32 or REFLEX_DTYPE_BF16, of every tensor.
+ *   h         [rows, d] the stream, row stride ldh >= d elements.
+ *   y         [rows, d] the block's output (ldy), nullable: out = h.
+ *   w_after   [d], nullable: a = y.
+ *   gate      [rows, d] with row stride ldg >= d, or [d] with ldg == 0; nullable: 1.
+ *   w_before  [d]; needed for norm.
+ *   scale, eps  finite, eps >= 0.
+ *   out, norm [rows, d] (ldo, ldn), either nullable.
+ * w_after and gate need y.  An output may be h, y or a [rows, d] gate itself (the
+ * same address and stride); else outputs overlap nothing.  Any d from 1 to 16384
+ * (above: REFLEX_EUNSUPPORTED), any strides; rows on 16-byte boundaries with d a
+ * multiple of 8 are fastest.  A row's bits do not depend on the other rows.
+ */
+int reflex_block_norm(int32_t dtype, const void* h, int64_t ldh, const void* y, int64_t ldy,
+                      const void* w_after, const void* gate, int64_t ldg, const void* w_before,
+                      float scale, float eps, int64_t rows, int32_t d, void* out, int64_t ldo,
+                      void* norm, int64_t ldn, void* stream);
+
+/*
+ * reflex_block_norm_backward — its gradients, from d_out and d_norm, those of out
+ * and of norm (one of them may be NULL; d_norm comes with w_before).
+ *   d_h, d_y  [rows, d]; d_y comes with y.
+ *   d_gate, d_w_after, d_w_before  of their inputs' shapes; nullable: not wanted.
+ *             Those of a [d] input are sums over the rows, in fp32 and in an order
+ *             that depends on rows, d and the GPU alone.
+ *   workspace >= reflex_block_norm_workspace_size(rows, d) bytes (0 for widths that
+ *             are not supported), 256-B aligned; one for more rows serves fewer of
+ *             the same width.
+ * An output may be an input of its own shape, as above.  rows == 0 leaves zeros in
+ * the sums.
+ */
+size_t reflex_block_norm_workspace_size(int64_t rows, int32_t d);
+int reflex_block_norm_backward(int32_t dtype, const void* h, int64_t ldh, const void* y,
+                               int64_t ldy, const void* w_after, const void* gate, int64_t ldg,
+                               const void* w_before, float scale, float eps, int64_t rows,
+                               int32_t d, const void* d_out, int64_t ld_d_out,
+                               const void* d_norm, int64_t ld_d_norm, void* d_h, int64_t ld_d_h,
+                               void* d_y, int64_t ld_d_y, void* d_gate, int64_t ld_d_gate,
+                               void* d_w_after, void* d_w_before, void* workspace,
+                               size_t ws_bytes, void* stream);
+
+/*
+ * reflex_expert_plan — the rows of token-expert pairs in expert order, as in the
+ * record of reflex_moe_forward, for a routing that the caller holds.  Pairs (t, j)
+ * are numbered in order of (expert, token, slot).
+ *   ids       [T, k_max]; without k a negative id marks an unused slot.
+ *   k         [T] int32, nullable: slots j < k[t] are used.  A count outside
+ *             [0, k_max] sets REFLEX_EKRANGE in the error word and is clamped.
+ *   row_of    [T, k_max] the pair's row, -1 without one: unused slots, pairs whose
+ *             id is outside [0, E) (REFLEX_EINVAL in the error word) and pairs past
+ *             the first cap_rows rows (REFLEX_ECAPACITY).
+ *   counts    [E], offsets [E + 1]: rows of expert e are offsets[e] .. offsets[e + 1]
+ *             - 1 (before the cut at cap_rows).
+ *   perm      [>= pairs] nullable: row -> t * k_max + j.
+ *   dev_status nullable device error word, cleared by this call.
+ *   workspace >= reflex_expert_plan_workspace_size(...) bytes (0 for shapes that are
+ *             not supported), 256-B aligned; one for more tokens serves fewer.
+ * An expert may come several times in a token.  Shape rules: 1 <= E <= 1024,
+ * 1 <= k_max <= 32, 0 <= T * k_max <= 2^30.
+ */
+size_t reflex_expert_plan_workspace_size(int64_t T, int32_t E, int32_t k_max);
+int reflex_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, int32_t E, int32_t k_max,
+                       int64_t cap_rows, int32_t* row_of, int32_t* counts, int32_t* offsets,
+                       int32_t* perm, int32_t* dev_status, void* workspace, size_t ws_bytes,
+                       void* stream);
+
+/*
+ * reflex_expert_rows — tokens to their experts: rows[row_of[t, j]] = x[t].
+ *   x         [T, d] (ldx); rows [cap_rows, d] (ldr).  Rows without a pair are
+ *             left as they are.  row_of outside [0, cap_rows) is an unused slot.
+ * Its gradient is reflex_expert_combine with alpha == NULL and no residual.
+ */
+int reflex_expert_rows(int32_t dtype, const void* x, int64_t ldx, const int32_t* row_of,
+                       int64_t T, int32_t d, int32_t k_max, int64_t cap_rows, void* rows,
+                       int64_t ldr, void* stream);
+
+/*
+ * reflex_expert_combine — and back: out[t] = sum_j alpha[t, j] rows[row_of[t, j]]
+ * (+ residual[t]), summed in fp32 in the order of j and rounded once.
+ *   alpha     [T, k_max] fp32, of used slots; NULL: 1.
+ *   residual  [T, d] (ldres), nullable; out [T, d] (ldo), which may be residual.
+ */
+int reflex_expert_combine(int32_t dtype, const void* rows, int64_t ldr, const float* alpha,
+                          const int32_t* row_of, const void* residual, int64_t ldres, int64_t T,
+                          int32_t d, int32_t k_max, int64_t cap_rows, void* out, int64_t ldo,
+                          void* stream);
+
+/*
+ * reflex_expert_combine_backward — its gradients (that of the residual is d_out):
+ *   d_rows[row_of[t, j]] = alpha[t, j] d_out[t]   [cap_rows, d], nullable; rows
+ *             without a pair are left as they are.  d_rows may be rows.
+ *   d_alpha[t, j] = <d_out[t], rows[row_of[t, j]]>  [T, k_max] fp32, nullable; 0 in
+ *             unused slots.
+ */
+int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_d_out,
+                                   const void* rows, int64_t ldr, const float* alpha,
+                                   const int32_t* row_of, int64_t T, int32_t d, int32_t k_max,
+                                   int64_t cap_rows, void* d_rows, int64_t ld_d_rows,
+                                   float* d_alpha, void* stream);
+
 /* Synchronises `stream` and returns the status recorded in the workspace's
  * device error word by the last forward (REFLEX_OK if clean). */
 int reflex_moe_status(const void* workspace, void* stream);

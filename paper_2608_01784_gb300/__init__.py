@@ -15,7 +15,10 @@ from ._binding import (  # noqa: F401
     REFLEX_STAGE_DISPATCH, REFLEX_STAGE_EXPERT_DOWN, REFLEX_STAGE_EXPERT_UP,
     REFLEX_STAGE_ROUTE,
     ReflexError, load, make_params, reflex_abi_version, reflex_allocate,
+    reflex_block_norm, reflex_block_norm_backward, reflex_block_norm_workspace_size,
     reflex_default_params, reflex_experts_fp8, reflex_experts_fp8_workspace_size,
+    reflex_expert_combine, reflex_expert_combine_backward, reflex_expert_plan,
+    reflex_expert_plan_workspace_size, reflex_expert_rows,
     reflex_linear_fp8, reflex_linear_fp8_workspace_size, reflex_matmul_fp8,
     reflex_moe_forward, reflex_moe_status, reflex_moe_workspace_size,
     reflex_quantize_fp8, reflex_read_status, reflex_sample,

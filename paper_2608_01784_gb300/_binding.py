@@ -53,6 +53,9 @@ EXPORTED = (
     "reflex_step", "reflex_quantize_fp8", "reflex_matmul_fp8",
     "reflex_linear_fp8_workspace_size", "reflex_linear_fp8",
     "reflex_experts_fp8_workspace_size", "reflex_experts_fp8", "reflex_sample",
+    "reflex_block_norm", "reflex_block_norm_workspace_size", "reflex_block_norm_backward",
+    "reflex_expert_plan_workspace_size", "reflex_expert_plan", "reflex_expert_rows",
+    "reflex_expert_combine", "reflex_expert_combine_backward",
 )
 
 
@@ -150,6 +153,27 @@ def load():
                                        ctypes.c_uint32, P, sz, P, P]
     lib.reflex_sample.restype = ctypes.c_int
     lib.reflex_sample.argtypes = [i32, P, i64, i32, i32, P, P, P, P, P, P, P, P, P, P]
+    f32 = ctypes.c_float
+    lib.reflex_block_norm.restype = ctypes.c_int
+    lib.reflex_block_norm.argtypes = [i32, P, i64, P, i64, P, P, i64, P, f32, f32, i64, i32, P,
+                                      i64, P, i64, P]
+    lib.reflex_block_norm_workspace_size.restype = sz
+    lib.reflex_block_norm_workspace_size.argtypes = [i64, i32]
+    lib.reflex_block_norm_backward.restype = ctypes.c_int
+    lib.reflex_block_norm_backward.argtypes = [i32, P, i64, P, i64, P, P, i64, P, f32, f32, i64,
+                                               i32, P, i64, P, i64, P, i64, P, i64, P, i64, P, P,
+                                               P, sz, P]
+    lib.reflex_expert_plan_workspace_size.restype = sz
+    lib.reflex_expert_plan_workspace_size.argtypes = [i64, i32, i32]
+    lib.reflex_expert_plan.restype = ctypes.c_int
+    lib.reflex_expert_plan.argtypes = [P, P, i64, i32, i32, i64, P, P, P, P, P, P, sz, P]
+    lib.reflex_expert_rows.restype = ctypes.c_int
+    lib.reflex_expert_rows.argtypes = [i32, P, i64, P, i64, i32, i32, i64, P, i64, P]
+    lib.reflex_expert_combine.restype = ctypes.c_int
+    lib.reflex_expert_combine.argtypes = [i32, P, i64, P, P, P, i64, i64, i32, i32, i64, P, i64, P]
+    lib.reflex_expert_combine_backward.restype = ctypes.c_int
+    lib.reflex_expert_combine_backward.argtypes = [i32, P, i64, P, i64, P, P, i64, i32, i32, i64,
+                                                   P, i64, P, P]
     if lib.reflex_abi_version() != ABI_VERSION:
         raise ImportError(f"{_LIB_PATH} has ABI version {lib.reflex_abi_version()}, "
                           f"this binding needs {ABI_VERSION}: rebuild it")
@@ -355,4 +379,80 @@ def reflex_sample(dtype: int, logits, ld: int, rows: int, vocab: int, temperatur
                               _ptr(conf_out), _ptr(dev_status), _stream(stream))
     if check and rc != REFLEX_OK:
         raise ReflexError(rc, "reflex_sample")
+    return rc
+
+
+def reflex_block_norm(dtype: int, h, ldh: int, y, ldy: int, w_after, gate, ldg: int, w_before,
+                      scale: float, eps: float, rows: int, d: int, out, ldo: int, norm, ldn: int,
+                      stream=None, check: bool = True) -> int:
+    rc = load().reflex_block_norm(dtype, _ptr(h), ldh, _ptr(y), ldy, _ptr(w_after), _ptr(gate),
+                                  ldg, _ptr(w_before), scale, eps, rows, d, _ptr(out), ldo,
+                                  _ptr(norm), ldn, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_block_norm")
+    return rc
+
+
+def reflex_block_norm_workspace_size(rows: int, d: int) -> int:
+    return int(load().reflex_block_norm_workspace_size(rows, d))
+
+
+def reflex_block_norm_backward(dtype: int, h, ldh: int, y, ldy: int, w_after, gate, ldg: int,
+                               w_before, scale: float, eps: float, rows: int, d: int, d_out,
+                               ld_d_out: int, d_norm, ld_d_norm: int, d_h, ld_d_h: int, d_y,
+                               ld_d_y: int, d_gate, ld_d_gate: int, d_w_after, d_w_before,
+                               workspace, ws_bytes: int, stream=None, check: bool = True) -> int:
+    rc = load().reflex_block_norm_backward(
+        dtype, _ptr(h), ldh, _ptr(y), ldy, _ptr(w_after), _ptr(gate), ldg, _ptr(w_before), scale,
+        eps, rows, d, _ptr(d_out), ld_d_out, _ptr(d_norm), ld_d_norm, _ptr(d_h), ld_d_h,
+        _ptr(d_y), ld_d_y, _ptr(d_gate), ld_d_gate, _ptr(d_w_after), _ptr(d_w_before),
+        _ptr(workspace), ws_bytes, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_block_norm_backward")
+    return rc
+
+
+def reflex_expert_plan_workspace_size(T: int, E: int, k_max: int) -> int:
+    return int(load().reflex_expert_plan_workspace_size(T, E, k_max))
+
+
+def reflex_expert_plan(ids, k, T: int, E: int, k_max: int, cap_rows: int, row_of, counts, offsets,
+                       perm, dev_status, workspace, ws_bytes: int, stream=None,
+                       check: bool = True) -> int:
+    rc = load().reflex_expert_plan(_ptr(ids), _ptr(k), T, E, k_max, cap_rows, _ptr(row_of),
+                                   _ptr(counts), _ptr(offsets), _ptr(perm), _ptr(dev_status),
+                                   _ptr(workspace), ws_bytes, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_expert_plan")
+    return rc
+
+
+def reflex_expert_rows(dtype: int, x, ldx: int, row_of, T: int, d: int, k_max: int, cap_rows: int,
+                       rows, ldr: int, stream=None, check: bool = True) -> int:
+    rc = load().reflex_expert_rows(dtype, _ptr(x), ldx, _ptr(row_of), T, d, k_max, cap_rows,
+                                   _ptr(rows), ldr, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_expert_rows")
+    return rc
+
+
+def reflex_expert_combine(dtype: int, rows, ldr: int, alpha, row_of, residual, ldres: int, T: int,
+                          d: int, k_max: int, cap_rows: int, out, ldo: int, stream=None,
+                          check: bool = True) -> int:
+    rc = load().reflex_expert_combine(dtype, _ptr(rows), ldr, _ptr(alpha), _ptr(row_of),
+                                      _ptr(residual), ldres, T, d, k_max, cap_rows, _ptr(out), ldo,
+                                      _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_expert_combine")
+    return rc
+
+
+def reflex_expert_combine_backward(dtype: int, d_out, ld_d_out: int, rows, ldr: int, alpha, row_of,
+                                   T: int, d: int, k_max: int, cap_rows: int, d_rows,
+                                   ld_d_rows: int, d_alpha, stream=None, check: bool = True) -> int:
+    rc = load().reflex_expert_combine_backward(
+        dtype, _ptr(d_out), ld_d_out, _ptr(rows), ldr, _ptr(alpha), _ptr(row_of), T, d, k_max,
+        cap_rows, _ptr(d_rows), ld_d_rows, _ptr(d_alpha), _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_expert_combine_backward")
     return rc

@@ -283,4 +283,64 @@ struct SampleArgs {
 int sample_max_vocab();
 cudaError_t launch_sample(int dtype, const SampleArgs& p, int num_sms, cudaStream_t stream);
 
+// ---- norms around a block (block_norm.cu) -------------------------------------
+struct BlockNormArgs {
+  int64_t rows;
+  int d, tpr;  // tpr: threads that share a row (set by the launcher)
+  float scale, eps;
+  const void* h;
+  int64_t ldh;
+  const void* y;  // nullable
+  int64_t ldy;
+  const void* w_after;  // nullable
+  const void* gate;     // nullable; ldg == 0: one row for all
+  int64_t ldg;
+  const void* w_before;  // nullable
+  void* out;             // forward
+  int64_t ldo;
+  void* norm;
+  int64_t ldn;
+  const void* d_out;  // backward; nullable
+  int64_t ld_d_out;
+  const void* d_norm;
+  int64_t ld_d_norm;
+  void* d_h;
+  int64_t ld_d_h;
+  void* d_y;
+  int64_t ld_d_y;
+  void* d_gate;  // nullable, like the next two
+  int64_t ld_d_gate;
+  void* d_w_after;
+  void* d_w_before;
+  float* partial;  // [3][block_norm_parts][d]: sums of the weights' gradients
+};
+int block_norm_max_width();
+int64_t block_norm_parts(int64_t rows, int d, int sms);
+cudaError_t launch_block_norm(int dtype, const BlockNormArgs& p, bool backward, int sms,
+                              cudaStream_t s);
+
+// ---- tokens to experts and back (expert_rows.cu) --------------------------------
+// CTAs of a plan of so many pairs or fewer
+int64_t expert_plan_blocks_most(int64_t pairs, int sms);
+cudaError_t launch_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, int E, int k_max,
+                               int cap_rows, int32_t* row_of, int32_t* counts, int32_t* offsets,
+                               int32_t* perm, uint32_t* err, int32_t* blk_count, int sms,
+                               cudaStream_t s);
+struct ExpertRowsArgs {
+  const int32_t* row_of;
+  int64_t T;
+  int d, k_max, cap_rows;
+  const void* x;  // by token: tokens, residual (nullable), gradient of the output
+  int64_t ldx;
+  const void* rows;  // by pair
+  int64_t ldr;
+  const float* alpha;  // nullable in sums: 1
+  void* out;           // what is written: rows, sums, gradient of the rows (nullable)
+  int64_t ldo;
+  float* d_alpha;  // nullable
+};
+cudaError_t launch_expert_rows(int dtype, const ExpertRowsArgs& p, int sms, cudaStream_t s);
+cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backward, int sms,
+                                  cudaStream_t s);
+
 }  // namespace rx

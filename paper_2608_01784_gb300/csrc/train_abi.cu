@@ -1,0 +1,281 @@
+// train_abi.cu — C entry points of what stands around the experts, with gradients:
+// norms around a block, tokens to experts and back.  Argument checks and workspace
+// carving; the kernels are in block_norm.cu and expert_rows.cu.
+#include <limits.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "common.cuh"
+#include "internal.h"
+#include "reflex.h"
+
+namespace rx {
+int device_sms();
+}  // namespace rx
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+#define RX_CUDA(x)                                  \
+  do {                                              \
+    if ((x) != cudaSuccess) return REFLEX_ECUDA;    \
+  } while (0)
+
+bool dtype_ok(int32_t t) { return t == REFLEX_DTYPE_F32 || t == REFLEX_DTYPE_BF16; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// A matrix argument: a pointer on its element's boundary and rows that hold `cols`.
+struct Matrix {
+  const void* p;
+  int64_t ld;
+};
+bool matrix_ok(const Matrix& m, int64_t cols, size_t es) {
+  return m.p != nullptr && aligned(m.p, es) && m.ld >= cols;
+}
+
+bool norm_ok(int32_t dtype, const Matrix& h, const Matrix& y, const void* w_after,
+             const Matrix& gate, const void* w_before, float scale, float eps, int64_t rows,
+             int32_t d) {
+  if (!dtype_ok(dtype) || rows < 0 || d < 1 || !std::isfinite(scale) || !(eps >= 0.f) ||
+      !std::isfinite(eps))
+    return false;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  // what scales the block's output needs one
+  if (rows > 0 && y.p == nullptr && (w_after != nullptr || gate.p != nullptr)) return false;
+  if (rows > 0 && !matrix_ok(h, d, es)) return false;
+  if (rows > 0 && y.p != nullptr && !matrix_ok(y, d, es)) return false;
+  if (gate.p != nullptr && ((gate.ld != 0 && gate.ld < d) || !aligned(gate.p, es))) return false;
+  return aligned(w_after, es) && aligned(w_before, es);
+}
+
+bool plan_ok(int64_t T, int32_t E, int32_t k_max) {
+  return T >= 0 && E >= 1 && E <= 1024 && k_max >= 1 && k_max <= 32 &&
+         T <= (int64_t{1} << 30) / k_max;
+}
+bool rows_ok(int32_t dtype, int64_t T, int32_t d, int32_t k_max, int64_t cap_rows) {
+  return dtype_ok(dtype) && d >= 1 && plan_ok(T, 1, k_max) && cap_rows >= 0 &&
+         cap_rows <= INT32_MAX;
+}
+
+}  // namespace
+
+extern "C" {
+
+int reflex_block_norm(int32_t dtype, const void* h, int64_t ldh, const void* y, int64_t ldy,
+                      const void* w_after, const void* gate, int64_t ldg, const void* w_before,
+                      float scale, float eps, int64_t rows, int32_t d, void* out, int64_t ldo,
+                      void* norm, int64_t ldn, void* stream) {
+  if (!norm_ok(dtype, {h, ldh}, {y, ldy}, w_after, {gate, ldg}, w_before, scale, eps, rows, d) ||
+      (norm != nullptr && w_before == nullptr) ||
+      (rows > 0 && out == nullptr && norm == nullptr))
+    return REFLEX_EINVAL;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if ((out != nullptr && !matrix_ok({out, ldo}, d, es)) ||
+      (norm != nullptr && !matrix_ok({norm, ldn}, d, es)))
+    return REFLEX_EINVAL;
+  if (d > rx::block_norm_max_width()) return REFLEX_EUNSUPPORTED;
+  if (rows == 0) return REFLEX_OK;
+  rx::BlockNormArgs a{};
+  a.rows = rows;
+  a.d = d;
+  a.scale = scale;
+  a.eps = eps;
+  a.h = h;
+  a.ldh = ldh;
+  a.y = y;
+  a.ldy = ldy;
+  a.w_after = w_after;
+  a.gate = gate;
+  a.ldg = ldg;
+  a.w_before = norm != nullptr ? w_before : nullptr;
+  a.out = out;
+  a.ldo = ldo;
+  a.norm = norm;
+  a.ldn = ldn;
+  RX_CUDA(rx::launch_block_norm(dtype, a, false, rx::device_sms(),
+                                static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+size_t reflex_block_norm_workspace_size(int64_t rows, int32_t d) {
+  if (rows < 0 || d < 1 || d > rx::block_norm_max_width()) return 0;
+  const int64_t parts = std::max<int64_t>(1, rx::block_norm_parts(rows, d, rx::device_sms()));
+  return up(3 * static_cast<size_t>(parts) * d * sizeof(float));
+}
+
+int reflex_block_norm_backward(int32_t dtype, const void* h, int64_t ldh, const void* y,
+                               int64_t ldy, const void* w_after, const void* gate, int64_t ldg,
+                               const void* w_before, float scale, float eps, int64_t rows,
+                               int32_t d, const void* d_out, int64_t ld_d_out,
+                               const void* d_norm, int64_t ld_d_norm, void* d_h, int64_t ld_d_h,
+                               void* d_y, int64_t ld_d_y, void* d_gate, int64_t ld_d_gate,
+                               void* d_w_after, void* d_w_before, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  if (!norm_ok(dtype, {h, ldh}, {y, ldy}, w_after, {gate, ldg}, w_before, scale, eps, rows, d) ||
+      (rows > 0 && ((d_norm != nullptr) != (w_before != nullptr) ||
+                    (d_out == nullptr && d_norm == nullptr))) ||
+      (d_w_after != nullptr && w_after == nullptr) || (d_gate != nullptr && gate == nullptr) ||
+      (d_w_before != nullptr && w_before == nullptr))
+    return REFLEX_EINVAL;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if (rows > 0 && (!matrix_ok({d_h, ld_d_h}, d, es) ||
+                   (d_out != nullptr && !matrix_ok({d_out, ld_d_out}, d, es)) ||
+                   (d_norm != nullptr && !matrix_ok({d_norm, ld_d_norm}, d, es)) ||
+                   (y != nullptr && !matrix_ok({d_y, ld_d_y}, d, es)) ||
+                   (d_gate != nullptr && ldg != 0 && ld_d_gate < d)))
+    return REFLEX_EINVAL;
+  if (!aligned(d_gate, es) || !aligned(d_w_after, es) || !aligned(d_w_before, es))
+    return REFLEX_EINVAL;
+  if (d > rx::block_norm_max_width()) return REFLEX_EUNSUPPORTED;
+  if (workspace == nullptr || ws_bytes < reflex_block_norm_workspace_size(rows, d) ||
+      !aligned(workspace, kAlign))
+    return REFLEX_EWORKSPACE;
+  rx::BlockNormArgs a{};
+  a.rows = rows;
+  a.d = d;
+  a.scale = scale;
+  a.eps = eps;
+  a.h = h;
+  a.ldh = ldh;
+  a.y = y;
+  a.ldy = ldy;
+  a.w_after = w_after;
+  a.gate = gate;
+  a.ldg = ldg;
+  a.w_before = w_before;
+  a.d_out = d_out;
+  a.ld_d_out = ld_d_out;
+  a.d_norm = d_norm;
+  a.ld_d_norm = ld_d_norm;
+  a.d_h = d_h;
+  a.ld_d_h = ld_d_h;
+  a.d_y = d_y;
+  a.ld_d_y = ld_d_y;
+  a.d_gate = d_gate;
+  a.ld_d_gate = ld_d_gate;
+  a.d_w_after = d_w_after;
+  a.d_w_before = d_w_before;
+  a.partial = static_cast<float*>(workspace);
+  RX_CUDA(rx::launch_block_norm(dtype, a, true, rx::device_sms(),
+                                static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+size_t reflex_expert_plan_workspace_size(int64_t T, int32_t E, int32_t k_max) {
+  if (!plan_ok(T, E, k_max)) return 0;
+  return up(static_cast<size_t>(rx::expert_plan_blocks_most(T * k_max, rx::device_sms())) * E * 4);
+}
+
+int reflex_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, int32_t E, int32_t k_max,
+                       int64_t cap_rows, int32_t* row_of, int32_t* counts, int32_t* offsets,
+                       int32_t* perm, int32_t* dev_status, void* workspace, size_t ws_bytes,
+                       void* stream) {
+  if (!plan_ok(T, E, k_max) || cap_rows < 0) return REFLEX_EINVAL;
+  if (counts == nullptr || offsets == nullptr || (T > 0 && (ids == nullptr || row_of == nullptr)))
+    return REFLEX_EINVAL;
+  for (const void* p : {static_cast<const void*>(ids), static_cast<const void*>(k),
+                        static_cast<const void*>(row_of), static_cast<const void*>(counts),
+                        static_cast<const void*>(offsets), static_cast<const void*>(perm),
+                        static_cast<const void*>(dev_status)})
+    if (!aligned(p, 4)) return REFLEX_EINVAL;
+  if (workspace == nullptr || ws_bytes < reflex_expert_plan_workspace_size(T, E, k_max) ||
+      !aligned(workspace, kAlign))
+    return REFLEX_EWORKSPACE;
+  const int cap = static_cast<int>(std::min<int64_t>(cap_rows, INT32_MAX));
+  RX_CUDA(rx::launch_expert_plan(ids, k, T, E, k_max, cap, row_of, counts, offsets, perm,
+                                 reinterpret_cast<uint32_t*>(dev_status),
+                                 static_cast<int32_t*>(workspace), rx::device_sms(),
+                                 static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+int reflex_expert_rows(int32_t dtype, const void* x, int64_t ldx, const int32_t* row_of,
+                       int64_t T, int32_t d, int32_t k_max, int64_t cap_rows, void* rows,
+                       int64_t ldr, void* stream) {
+  if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
+  if (T == 0 || cap_rows == 0) return REFLEX_OK;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if (!matrix_ok({x, ldx}, d, es) || !matrix_ok({rows, ldr}, d, es) || row_of == nullptr ||
+      !aligned(row_of, 4))
+    return REFLEX_EINVAL;
+  rx::ExpertRowsArgs a{};
+  a.row_of = row_of;
+  a.T = T;
+  a.d = d;
+  a.k_max = k_max;
+  a.cap_rows = static_cast<int>(cap_rows);
+  a.x = x;
+  a.ldx = ldx;
+  a.out = rows;
+  a.ldo = ldr;
+  RX_CUDA(rx::launch_expert_rows(dtype, a, rx::device_sms(), static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+int reflex_expert_combine(int32_t dtype, const void* rows, int64_t ldr, const float* alpha,
+                          const int32_t* row_of, const void* residual, int64_t ldres, int64_t T,
+                          int32_t d, int32_t k_max, int64_t cap_rows, void* out, int64_t ldo,
+                          void* stream) {
+  if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
+  if (T == 0) return REFLEX_OK;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if (!matrix_ok({out, ldo}, d, es) || (cap_rows > 0 && !matrix_ok({rows, ldr}, d, es)) ||
+      (residual != nullptr && !matrix_ok({residual, ldres}, d, es)) || row_of == nullptr ||
+      !aligned(row_of, 4) || !aligned(alpha, 4))
+    return REFLEX_EINVAL;
+  rx::ExpertRowsArgs a{};
+  a.row_of = row_of;
+  a.T = T;
+  a.d = d;
+  a.k_max = k_max;
+  a.cap_rows = static_cast<int>(cap_rows);
+  a.x = residual;
+  a.ldx = ldres;
+  a.rows = rows;
+  a.ldr = ldr;
+  a.alpha = alpha;
+  a.out = out;
+  a.ldo = ldo;
+  RX_CUDA(rx::launch_expert_combine(dtype, a, false, rx::device_sms(),
+                                    static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_d_out,
+                                   const void* rows, int64_t ldr, const float* alpha,
+                                   const int32_t* row_of, int64_t T, int32_t d, int32_t k_max,
+                                   int64_t cap_rows, void* d_rows, int64_t ld_d_rows,
+                                   float* d_alpha, void* stream) {
+  if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
+  if (T == 0) return REFLEX_OK;
+  const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if (!matrix_ok({d_out, ld_d_out}, d, es) || alpha == nullptr || row_of == nullptr ||
+      (d_rows == nullptr && d_alpha == nullptr) || !aligned(row_of, 4) || !aligned(alpha, 4) ||
+      !aligned(d_alpha, 4))
+    return REFLEX_EINVAL;
+  if (cap_rows > 0 && ((d_rows != nullptr && !matrix_ok({d_rows, ld_d_rows}, d, es)) ||
+                       (d_alpha != nullptr && !matrix_ok({rows, ldr}, d, es))))
+    return REFLEX_EINVAL;
+  rx::ExpertRowsArgs a{};
+  a.row_of = row_of;
+  a.T = T;
+  a.d = d;
+  a.k_max = k_max;
+  a.cap_rows = static_cast<int>(cap_rows);
+  a.x = d_out;
+  a.ldx = ld_d_out;
+  a.rows = rows;
+  a.ldr = ldr;
+  a.alpha = alpha;
+  a.out = d_rows;
+  a.ldo = ld_d_rows;
+  a.d_alpha = d_alpha;
+  RX_CUDA(rx::launch_expert_combine(dtype, a, true, rx::device_sms(),
+                                    static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,234 @@
+"""Torch-facing convenience over the entry points around the experts that have
+gradients: norms around a block, tokens to experts and back.  A gradient is a call of
+its own (no autograd graph is kept), takes the forward call's inputs again and
+allocates only what it returns and a workspace, so each can be captured in a CUDA
+graph.  With a `stream`, new outputs belong to it: to use them on another, wait for
+it, as torch's own rules have it.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _binding as B
+from .fp8 import _DTYPES, _matrix, _new, _want
+
+
+def _here(device):
+    """A launch goes to the current device; tensors of another one are refused."""
+    _want(device.index == torch.cuda.current_device(),
+          "the tensors are on another device than the current one")
+
+
+def _like(t: torch.Tensor, x: torch.Tensor, what: str) -> int:
+    """The row stride of t, which has x's shape, type and device."""
+    rows, cols, ld = _matrix(t, what, (x.dtype,))
+    _want((rows, cols) == tuple(x.shape) and t.device == x.device, f"{what}: shape or device")
+    return ld
+
+
+def _vector(t: torch.Tensor | None, d: int, x: torch.Tensor, what: str):
+    _want(t is None or (t.dtype == x.dtype and t.device == x.device and tuple(t.shape) == (d,)
+                        and (d == 1 or t.stride(0) == 1)),
+          f"{what}: {d} contiguous values of the stream's type on its device")
+
+
+def _norm_inputs(h, y, w_after, w_before, gate):
+    """Checks them; (rows, d, ldh, ldy, ldg)."""
+    rows, d, ldh = _matrix(h, "h", _DTYPES)
+    _want(d > 0, "h: at least one column")
+    _here(h.device)
+    ldy = _like(y, h, "y") if y is not None else 0
+    _vector(w_after, d, h, "w_after")
+    _vector(w_before, d, h, "w_before")
+    _want(y is not None or (w_after is None and gate is None), "w_after and gate need y")
+    ldg = 0
+    if gate is not None and gate.dim() == 2:
+        ldg = _like(gate, h, "gate")
+    else:
+        _vector(gate, d, h, "gate")
+    return rows, d, ldh, ldy, ldg
+
+
+def block_norm(h: torch.Tensor, y: torch.Tensor | None = None, *,
+               w_after: torch.Tensor | None = None, w_before: torch.Tensor | None = None,
+               gate: torch.Tensor | None = None, scale: float = 1.0, eps: float = 1e-6,
+               out: torch.Tensor | None = None, norm: torch.Tensor | None = None, stream=None):
+    """reflex_block_norm: (h + scale * gate * norm(y) w_after, its own norm times
+    w_before).  h, y [rows, d] fp32 or bf16, gate [d] or [rows, d]; without w_after
+    y is not normalised, without y the stream is h itself, without w_before the
+    second value is None.  `out` and `norm` may be h or y."""
+    rows, d, ldh, ldy, ldg = _norm_inputs(h, y, w_after, w_before, gate)
+    _want(norm is None or w_before is not None, "norm needs w_before")
+    if out is None:
+        out = _new((rows, d), h.dtype, h.device, stream)
+    if norm is None and w_before is not None:
+        norm = _new((rows, d), h.dtype, h.device, stream)
+    ldo = _like(out, h, "out")
+    ldn = _like(norm, h, "norm") if norm is not None else 0
+    B.reflex_block_norm(_DTYPES[h.dtype], h, ldh, y, ldy, w_after, gate, ldg, w_before, scale, eps,
+                        rows, d, out, ldo, norm, ldn, stream)
+    return out, norm
+
+
+def block_norm_backward(h: torch.Tensor, y: torch.Tensor | None, d_out: torch.Tensor | None,
+                        d_norm: torch.Tensor | None, *, w_after: torch.Tensor | None = None,
+                        w_before: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                        scale: float = 1.0, eps: float = 1e-6, d_h: torch.Tensor | None = None,
+                        d_y: torch.Tensor | None = None, stream=None) -> dict:
+    """reflex_block_norm_backward: the gradients of block_norm's inputs from those of
+    its outputs (d_out may be None; d_norm comes with w_before), as a dict of "h", "y",
+    "gate", "w_after" and "w_before", None for inputs that are not given.  `d_h` and
+    `d_y` may be any [rows, d] input."""
+    rows, d, ldh, ldy, ldg = _norm_inputs(h, y, w_after, w_before, gate)
+    _want((d_norm is not None) == (w_before is not None), "d_norm comes with w_before")
+    _want(d_out is not None or d_norm is not None, "no gradient of an output")
+    _want(d_y is None or y is not None, "d_y needs y")
+    ld_d_out = _like(d_out, h, "d_out") if d_out is not None else 0
+    ld_d_norm = _like(d_norm, h, "d_norm") if d_norm is not None else 0
+
+    def new(like, *shape):
+        return None if like is None else _new(shape, h.dtype, h.device, stream)
+    d_h = new(h, rows, d) if d_h is None else d_h
+    d_y = new(y, rows, d) if d_y is None else d_y
+    ld_d_h = _like(d_h, h, "d_h")
+    ld_d_y = _like(d_y, h, "d_y") if d_y is not None else 0
+    got = dict(w_after=new(w_after, d), w_before=new(w_before, d),
+               gate=new(gate, rows, d) if ldg else new(gate, d), h=d_h, y=d_y)
+    ws_bytes = B.reflex_block_norm_workspace_size(rows, d)
+    _want(ws_bytes > 0, "unsupported width")
+    ws = _new(ws_bytes, torch.uint8, h.device, stream)
+    B.reflex_block_norm_backward(_DTYPES[h.dtype], h, ldh, y, ldy, w_after, gate, ldg, w_before,
+                                 scale, eps, rows, d, d_out, ld_d_out, d_norm, ld_d_norm, d_h,
+                                 ld_d_h, d_y, ld_d_y, got["gate"], d, got["w_after"],
+                                 got["w_before"], ws, ws_bytes, stream)
+    return got
+
+
+class ExpertPlan:
+    """Where the pairs of a routing lie in expert order (reflex_expert_plan): row_of
+    int32 [T, k_max], counts [E], offsets [E + 1], all on the device; the pairs' rows
+    are 0 .. offsets[E] - 1 of at most cap_rows."""
+
+    def __init__(self, T: int, E: int, k_max: int, cap_rows: int, device, stream=None):
+        def new(*shape):
+            return _new(shape, torch.int32, device, stream)
+        self.T, self.E, self.k_max, self.cap_rows = T, E, k_max, cap_rows
+        self.row_of, self.counts, self.offsets = new(T, k_max), new(E), new(E + 1)
+        self.error = new(1)
+        self.ws_bytes = B.reflex_expert_plan_workspace_size(T, E, k_max)
+        _want(self.ws_bytes > 0, "unsupported shape: E up to 1024, k_max up to 32")
+        self.ws = _new(self.ws_bytes, torch.uint8, device, stream)
+
+    def status(self, stream=None) -> int:
+        """What the last plan found wrong with its routing (waits)."""
+        return B.reflex_read_status(self.error, stream)
+
+
+def expert_plan(ids: torch.Tensor, *, E: int, k: torch.Tensor | None = None,
+                cap_rows: int | None = None, plan: ExpertPlan | None = None,
+                perm: torch.Tensor | None = None, stream=None) -> ExpertPlan:
+    """reflex_expert_plan of ids int32 [T, k_max]: slots j < k[t] are used, or, without
+    k, those with ids >= 0.  `plan` (of the same T, E, k_max and cap_rows) is filled
+    again instead of a new one; `perm` int32 [T * k_max] receives row -> t * k_max + j."""
+    _want(ids.is_cuda and ids.dim() == 2 and ids.dtype == torch.int32 and ids.is_contiguous(),
+          "ids: a contiguous CUDA matrix of torch.int32")
+    _here(ids.device)
+    T, k_max = ids.shape
+    for t, n, what in ((k, T, "k"), (perm, T * k_max, "perm")):
+        _want(t is None or (t.dtype == torch.int32 and tuple(t.shape) == (n,)
+                            and t.is_contiguous() and t.device == ids.device),
+              f"{what}: {n} contiguous values of torch.int32 on the device of ids")
+    if plan is None:
+        plan = ExpertPlan(T, E, k_max, T * k_max if cap_rows is None else cap_rows, ids.device,
+                          stream)
+    _want((plan.T, plan.E, plan.k_max) == (T, E, k_max) and plan.row_of.device == ids.device
+          and cap_rows in (None, plan.cap_rows), "plan: made for another shape or device")
+    B.reflex_expert_plan(ids, k, T, E, k_max, plan.cap_rows, plan.row_of, plan.counts,
+                         plan.offsets, perm, plan.error, plan.ws, plan.ws_bytes, stream)
+    return plan
+
+
+def _pair_rows(rows: torch.Tensor, plan: ExpertPlan, what: str):
+    """(d, row stride) of the pairs' rows of a plan."""
+    n, d, ld = _matrix(rows, what, _DTYPES)
+    _want(n >= plan.cap_rows and rows.device == plan.row_of.device,
+          f"{what}: fewer rows than the plan's cap_rows, or another device")
+    _want(d > 0, f"{what}: at least one column")
+    _here(rows.device)
+    return d, ld
+
+
+def _tokens(x: torch.Tensor, plan: ExpertPlan, d: int, dtype, what: str) -> int:
+    rows, cols, ld = _matrix(x, what, (dtype,))
+    _want((rows, cols) == (plan.T, d) and x.device == plan.row_of.device,
+          f"{what}: a row for each of the plan's tokens, of the rows' width and device")
+    return ld
+
+
+def _weights(alpha: torch.Tensor, plan: ExpertPlan, what: str):
+    _want(alpha.dtype == torch.float32 and tuple(alpha.shape) == (plan.T, plan.k_max)
+          and alpha.is_contiguous() and alpha.device == plan.row_of.device,
+          f"{what}: a contiguous tensor of torch.float32 of the plan's [T, k_max]")
+
+
+def expert_rows(x: torch.Tensor, plan: ExpertPlan, *, rows: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """reflex_expert_rows: x [T, d] (fp32 or bf16) laid out by expert, [cap_rows, d].
+    `rows` behind the last pair are left as they are; of a new tensor they are not set."""
+    _, d, ldx = _matrix(x, "x", _DTYPES)
+    _want(d > 0, "x: at least one column")
+    if rows is None:
+        rows = _new((plan.cap_rows, d), x.dtype, x.device, stream)
+    dr, ldr = _pair_rows(rows, plan, "rows")
+    _want(dr == d, "rows: another width than x")
+    _tokens(x, plan, d, rows.dtype, "x")
+    B.reflex_expert_rows(_DTYPES[x.dtype], x, ldx, plan.row_of, plan.T, d, plan.k_max,
+                         plan.cap_rows, rows, ldr, stream)
+    return rows
+
+
+def _sum(rows, alpha, plan, residual, out, stream):
+    d, ldr = _pair_rows(rows, plan, "rows")
+    ldres = _tokens(residual, plan, d, rows.dtype, "residual") if residual is not None else 0
+    if out is None:
+        out = _new((plan.T, d), rows.dtype, rows.device, stream)
+    ldo = _tokens(out, plan, d, rows.dtype, "out")
+    B.reflex_expert_combine(_DTYPES[rows.dtype], rows, ldr, alpha, plan.row_of, residual, ldres,
+                            plan.T, d, plan.k_max, plan.cap_rows, out, ldo, stream)
+    return out
+
+
+def expert_rows_backward(d_rows: torch.Tensor, plan: ExpertPlan, *,
+                         out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of expert_rows' x from that of its rows: their sums by token."""
+    return _sum(d_rows, None, plan, None, out, stream)
+
+
+def expert_combine(rows: torch.Tensor, alpha: torch.Tensor, plan: ExpertPlan, *,
+                   residual: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+    """reflex_expert_combine: out[t] = sum_j alpha[t, j] rows[row_of[t, j]] (+ residual[t]);
+    alpha fp32 [T, k_max].  `out` may be residual."""
+    _weights(alpha, plan, "alpha")
+    return _sum(rows, alpha, plan, residual, out, stream)
+
+
+def expert_combine_backward(d_out: torch.Tensor, rows: torch.Tensor, alpha: torch.Tensor,
+                            plan: ExpertPlan, *, d_rows: torch.Tensor | None = None,
+                            d_alpha: torch.Tensor | None = None, stream=None):
+    """reflex_expert_combine_backward: (gradient of the rows, of alpha); that of the
+    residual is d_out.  `d_rows` may be rows; behind the last pair it is left as it is."""
+    d, ldr = _pair_rows(rows, plan, "rows")
+    ldd = _tokens(d_out, plan, d, rows.dtype, "d_out")
+    _weights(alpha, plan, "alpha")
+    if d_rows is None:
+        d_rows = _new((plan.cap_rows, d), rows.dtype, rows.device, stream)
+    if d_alpha is None:
+        d_alpha = _new((plan.T, plan.k_max), torch.float32, rows.device, stream)
+    dd, lddr = _pair_rows(d_rows, plan, "d_rows")
+    _want(dd == d and d_rows.dtype == rows.dtype, "d_rows: another width or type than rows")
+    _weights(d_alpha, plan, "d_alpha")
+    B.reflex_expert_combine_backward(_DTYPES[rows.dtype], d_out, ldd, rows, ldr, alpha,
+                                     plan.row_of, plan.T, d, plan.k_max, plan.cap_rows, d_rows,
+                                     lddr, d_alpha, stream)
+    return d_rows, d_alpha
