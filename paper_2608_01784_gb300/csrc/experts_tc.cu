@@ -38,6 +38,7 @@
 #include "common.cuh"
 #include "internal.h"
 #include "tcgen05.cuh"
+#include "tcgen05_pair.cuh"
 
 namespace rx {
 namespace {
@@ -739,51 +740,6 @@ constexpr int kEpiWarps2 = 8;
 constexpr int kGatherWarps = 4;
 constexpr int kThreads2Up = kThreads2 + 32 * kGatherWarps;
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  __syncwarp();  // the barrier takes whole warps, whatever branch a lane comes from
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
-               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// shared::cta address -> the same variable's shared::cluster address in CTA `rank`
-__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-// Byte-count announcement on the leader's barrier from the peer CTA: no
-// release needed (the bytes themselves arrive by TMA complete_tx).
-__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cl_bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cl_bar),
-               "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx_only_cluster(uint32_t cl_bar, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(cl_bar),
-               "r"(bytes)
-               : "memory");
-}
-// Arrival that orders nothing but the arriving thread's own progress: used to
-// hand a TMEM accumulator back once its last tcgen05.ld has completed
-// (tcgen05.wait::ld); the epilogue's global stores need not be visible to
-// the MMA issuer, so no release fence makes them drain first.
-__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cl_bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cl_bar)
-               : "memory");
-}
-// TMA tile load whose completion is counted on a barrier in either CTA of the pair.
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int c0,
-                                                 int c1, uint32_t cl_bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-      " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(cl_bar)
-      : "memory");
-}
 __device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap* map, int c0,
                                                  int c3, int c4, uint32_t cl_bar) {
   asm volatile(
@@ -825,59 +781,6 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait_but() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// mbar_wait that also acquires what the other CTA's warps released
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity,
-                                                  const volatile int* abort, uint64_t limit_ns) {
-  uint64_t t0 = 0;
-  for (;;) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}\n"
-        : "=r"(ok)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if (abort != nullptr && *abort) return false;
-    const uint64_t now = global_ns();
-    if (t0 == 0) t0 = now;
-    if (now - t0 > limit_ns) return false;
-  }
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cl_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cl_bar)
-               : "memory");
-}
-__device__ __forceinline__ void mma_bf16_pair(uint32_t tmem_d, uint64_t da, uint64_t db,
-                                              uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(tmem_d),
-      "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// Arrive on the barrier at this shared-memory offset in both CTAs of the pair
-// once all prior MMAs of this thread have completed.
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-      " [%0], %1;" ::"r"(bar),
-      "h"(static_cast<uint16_t>(0x3))
-      : "memory");
-}
-__device__ __forceinline__ void tmem_alloc_pair(uint32_t slot, uint32_t ncols) {
-  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
-               "r"(ncols)
-               : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
-  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
-               : "memory");
-}
-
 struct Cfg2 {
   static constexpr int BN = 256;                 // most token rows of a tile
   static constexpr int KS = 2;                   // 64-k blocks per stage
@@ -893,26 +796,6 @@ struct Cfg2 {
       kStages * kStageBytes + 256 + kEpiWarps2 * kStagingBytes + kIndexInts * 4 + 1024;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 };
-
-// TMA tile store of a shared-memory box (bulk-group completion) and its waits.
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0,
-                                             int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1)
-               : "memory");
-}
-__device__ __forceinline__ void bulk_commit() {
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-// all stores but the latest N have read their shared-memory source
-template <int N>
-__device__ __forceinline__ void bulk_wait_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
-}
-// ... and completed
-__device__ __forceinline__ void bulk_wait_all() {
-  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-}
 
 // The epilogue's bf16 outputs reach global memory through staging tiles of 32
 // token rows x 64 output columns (128 bytes a row, 16-byte chunk j at
@@ -946,10 +829,6 @@ __device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32
 // address of 16-byte chunk j of row `row` of a staging tile
 __device__ __forceinline__ uint32_t stage_addr(uint32_t stg, int row, int j) {
   return stg + static_cast<uint32_t>(row * 128 + ((j ^ (row & 7)) << 4));
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  __nv_bfloat162 h2 = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&h2);
 }
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
   return pack_bf16(__uint_as_float(lo), __uint_as_float(hi));
