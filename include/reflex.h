@@ -661,6 +661,54 @@ int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_
                                    int64_t cap_rows, void* d_rows, int64_t ld_d_rows,
                                    float* d_alpha, void* stream);
 
+/*
+ * reflex_head_loss — softmax cross entropy of a vocabulary head, with no logits kept:
+ *   z[r, v] = sum_k hidden[r, k] w[v, k],  lse[r] = log sum_v exp z[r, v],
+ *   loss[r] = lse[r] - z[r, targets[r]]
+ * for the rows with a target; loss and lse are 0 for the others, whose hidden row is
+ * not read.  Sums, exponentials and logits are fp32.
+ *   hidden    [rows, k] bf16, row stride ld_hidden >= k, any alignment of 2 bytes.
+ *   w         [vocab, k] bf16, row stride ldw >= k: rows start on 16-byte boundaries
+ *             (w and ldw * 2 are multiples of 16).
+ *   targets   [rows] int32; a negative one leaves its row out, one >= vocab too, with
+ *             REFLEX_EINVAL in the error word.
+ *   loss, lse [rows] fp32.
+ *   dev_status nullable device error word, cleared by this call.
+ *   workspace >= reflex_head_loss_workspace_size(...) bytes (0 for shapes that are not
+ *             supported), 256-B aligned.
+ * Any sizes up to 2^24 rows, 2^24 columns of the vocabulary and k = 2^20 (above:
+ * REFLEX_EUNSUPPORTED).  A row's results have the same bits on every run, whatever
+ * the other rows are.  Logits are finite; a row with one that is not has a loss that is
+ * not, and no influence on others.
+ */
+size_t reflex_head_loss_workspace_size(int32_t rows, int32_t vocab, int32_t k);
+int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
+                     const int32_t* targets, int32_t rows, int32_t vocab, int32_t k, float* loss,
+                     float* lse, int32_t* dev_status, void* workspace, size_t ws_bytes,
+                     void* stream);
+
+/*
+ * reflex_head_loss_backward — its gradients from grad[r], the gradient of loss[r] (that
+ * of a mean is 1 / rows, of a weighted loss the weight), and the forward call's lse:
+ *   G[r, v] = grad[r] (exp(z[r, v] - lse[r]) - [v == targets[r]]),  in bf16
+ *   d_hidden = G w  [rows, k], zeros in rows left out;  d_w = G^T hidden  [vocab, k]
+ * with sums in fp32.  The logits are computed again, a piece of the vocabulary at a
+ * time.
+ *   lse, grad [rows] fp32, of rows with a target.
+ *   d_hidden, d_w  fp32 or bf16 by their dtype argument, any strides; either may be
+ *             NULL (not wanted).  Rows of d_w on 16-byte boundaries are stored fastest.
+ *   workspace >= reflex_head_loss_backward_workspace_size(...) bytes (for these very
+ *             sizes), 256-B aligned.
+ * The rest as in reflex_head_loss; the same bits on every run.
+ */
+size_t reflex_head_loss_backward_workspace_size(int32_t rows, int32_t vocab, int32_t k);
+int reflex_head_loss_backward(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
+                              const int32_t* targets, const float* lse, const float* grad,
+                              int32_t rows, int32_t vocab, int32_t k, int32_t d_hidden_dtype,
+                              void* d_hidden, int64_t ld_d_hidden, int32_t d_w_dtype, void* d_w,
+                              int64_t ld_d_w, int32_t* dev_status, void* workspace,
+                              size_t ws_bytes, void* stream);
+
 /* Synchronises `stream` and returns the status recorded in the workspace's
  * device error word by the last forward (REFLEX_OK if clean). */
 int reflex_moe_status(const void* workspace, void* stream);

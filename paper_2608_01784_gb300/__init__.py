@@ -19,6 +19,8 @@ from ._binding import (  # noqa: F401
     reflex_default_params, reflex_experts_fp8, reflex_experts_fp8_workspace_size,
     reflex_expert_combine, reflex_expert_combine_backward, reflex_expert_plan,
     reflex_expert_plan_workspace_size, reflex_expert_rows,
+    reflex_head_loss, reflex_head_loss_backward,
+    reflex_head_loss_backward_workspace_size, reflex_head_loss_workspace_size,
     reflex_linear_fp8, reflex_linear_fp8_workspace_size, reflex_matmul_fp8,
     reflex_moe_forward, reflex_moe_status, reflex_moe_workspace_size,
     reflex_quantize_fp8, reflex_read_status, reflex_sample,

@@ -56,6 +56,8 @@ EXPORTED = (
     "reflex_block_norm", "reflex_block_norm_workspace_size", "reflex_block_norm_backward",
     "reflex_expert_plan_workspace_size", "reflex_expert_plan", "reflex_expert_rows",
     "reflex_expert_combine", "reflex_expert_combine_backward",
+    "reflex_head_loss_workspace_size", "reflex_head_loss",
+    "reflex_head_loss_backward_workspace_size", "reflex_head_loss_backward",
 )
 
 
@@ -174,6 +176,14 @@ def load():
     lib.reflex_expert_combine_backward.restype = ctypes.c_int
     lib.reflex_expert_combine_backward.argtypes = [i32, P, i64, P, i64, P, P, i64, i32, i32, i64,
                                                    P, i64, P, P]
+    for f in (lib.reflex_head_loss_workspace_size, lib.reflex_head_loss_backward_workspace_size):
+        f.restype = sz
+        f.argtypes = [i32, i32, i32]
+    lib.reflex_head_loss.restype = ctypes.c_int
+    lib.reflex_head_loss.argtypes = [P, i64, P, i64, P, i32, i32, i32, P, P, P, P, sz, P]
+    lib.reflex_head_loss_backward.restype = ctypes.c_int
+    lib.reflex_head_loss_backward.argtypes = [P, i64, P, i64, P, P, P, i32, i32, i32, i32, P, i64,
+                                              i32, P, i64, P, P, sz, P]
     if lib.reflex_abi_version() != ABI_VERSION:
         raise ImportError(f"{_LIB_PATH} has ABI version {lib.reflex_abi_version()}, "
                           f"this binding needs {ABI_VERSION}: rebuild it")
@@ -455,4 +465,36 @@ def reflex_expert_combine_backward(dtype: int, d_out, ld_d_out: int, rows, ldr: 
         cap_rows, _ptr(d_rows), ld_d_rows, _ptr(d_alpha), _stream(stream))
     if check and rc != REFLEX_OK:
         raise ReflexError(rc, "reflex_expert_combine_backward")
+    return rc
+
+
+def reflex_head_loss_workspace_size(rows: int, vocab: int, k: int) -> int:
+    return int(load().reflex_head_loss_workspace_size(rows, vocab, k))
+
+
+def reflex_head_loss(hidden, ld_hidden: int, w, ldw: int, targets, rows: int, vocab: int, k: int,
+                     loss, lse, dev_status, workspace, ws_bytes: int, stream=None,
+                     check: bool = True) -> int:
+    rc = load().reflex_head_loss(_ptr(hidden), ld_hidden, _ptr(w), ldw, _ptr(targets), rows, vocab,
+                                 k, _ptr(loss), _ptr(lse), _ptr(dev_status), _ptr(workspace),
+                                 ws_bytes, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_head_loss")
+    return rc
+
+
+def reflex_head_loss_backward_workspace_size(rows: int, vocab: int, k: int) -> int:
+    return int(load().reflex_head_loss_backward_workspace_size(rows, vocab, k))
+
+
+def reflex_head_loss_backward(hidden, ld_hidden: int, w, ldw: int, targets, lse, grad, rows: int,
+                              vocab: int, k: int, d_hidden_dtype: int, d_hidden,
+                              ld_d_hidden: int, d_w_dtype: int, d_w, ld_d_w: int, dev_status,
+                              workspace, ws_bytes: int, stream=None, check: bool = True) -> int:
+    rc = load().reflex_head_loss_backward(
+        _ptr(hidden), ld_hidden, _ptr(w), ldw, _ptr(targets), _ptr(lse), _ptr(grad), rows, vocab,
+        k, d_hidden_dtype, _ptr(d_hidden), ld_d_hidden, d_w_dtype, _ptr(d_w), ld_d_w,
+        _ptr(dev_status), _ptr(workspace), ws_bytes, _stream(stream))
+    if check and rc != REFLEX_OK:
+        raise ReflexError(rc, "reflex_head_loss_backward")
     return rc

@@ -11,7 +11,8 @@ from . import _binding as B
 from .fp8 import (_DTYPES, ExpertsFp8, LinearFp8, _matrix, _new, _status_word,  # noqa: F401
                   matmul_fp8, quantize_experts, quantize_fp8)
 from .train import (ExpertPlan, block_norm, block_norm_backward, expert_combine,  # noqa: F401
-                    expert_combine_backward, expert_plan, expert_rows, expert_rows_backward)
+                    expert_combine_backward, expert_plan, expert_rows, expert_rows_backward,
+                    head_loss, head_loss_backward)
 
 
 def _dev(a: np.ndarray, device, dtype=None) -> torch.Tensor:

@@ -1,0 +1,879 @@
+// head_loss.cu — softmax cross entropy of a vocabulary head without its logits in
+// memory, and its gradients, on the 5th-generation tensor cores:
+//   z = h W^T,  lse[r] = log sum_v exp z[r, v],  loss[r] = lse[r] - z[r, target[r]]
+//   G[r, v] = c[r] (exp(z[r, v] - lse[r]) - [v = target[r]]),  Dh = G W,  DW = G^T h
+// for the rows r with a target, which lie packed in front (head_rows_kernel); c[r] is
+// the gradient of loss[r].
+//
+// Every product is made of tiles of 256 x 256 by pairs of CTAs (cta_group::2, M = 256,
+// two accumulators of 256 columns in all of TMEM), fed by TMA through a ring of six
+// stages of 64 along the reduction:
+//   loss    z tile -> each thread has a row of 128 columns in fp32, of which it leaves
+//           the maximum, the sum of exponentials and, where it has it, the target's z;
+//   grad    z tile -> G in bf16, a piece of the vocabulary at a time (MN-major operands
+//           of the next two, straight from row-major memory);
+//   hidden  G W of a part of the piece, added in fp32 where the last piece left off;
+//   weight  G^T h, stored as it is wanted.
+// A launch of the backward pass holds the hidden and weight tiles of one piece and the
+// grad tiles of the next, which do not depend on each other, so that a launch has but
+// one tail; pairs take tiles from a queue, the long ones first.  Every tile is summed
+// by one pair in one order, wherever it runs: results do not depend on timing.
+//
+// G is rounded to bf16 (2^-9 of each term, as the products take them); z, the sums of
+// exponentials and all accumulators are fp32.  exp(z - m) is taken as 2^(z c - m c), c =
+// log2 e, with the rounding error of m c, the same for all terms, put back at the end.
+//
+// Every wait on a barrier in shared memory is bounded (2 s); on expiry the CTA records
+// the timeout in the error word, drains its loads and MMAs, frees TMEM and exits.
+#include <algorithm>
+
+#include "common.cuh"
+#include "internal.h"
+#include "tcgen05.cuh"
+#include "tcgen05_pair.cuh"
+
+namespace rx {
+namespace {
+
+constexpr int kTile = kHeadTile;      // rows and columns of a pair's tile
+constexpr int BK = 64;                // of the reduction in a stage: 128 bytes
+constexpr int kHalf = kTile / 2;      // rows of A and of B in a CTA
+constexpr int kOperand = kHalf * 128;  // 16 KB
+constexpr int kStages = 6;
+constexpr int kStageBytes = 2 * kOperand;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kStaging = 32 * 128;  // of an epilogue warp
+constexpr int kJobs = 4;            // tiles that are known ahead
+constexpr int kSmemBytes = kStages * kStageBytes + kEpiWarps * kStaging + 512 + 1024;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
+constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr uint64_t kDrainNs = 1000000000ull;
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
+
+// kind::f16, bf16 operands, fp32 accumulator, M = N = 256; bits 15 and 16: A, B MN-major.
+constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) |
+                            (static_cast<uint32_t>(kTile >> 3) << 17) |
+                            (static_cast<uint32_t>(kTile >> 4) << 24);
+
+// Shared-memory descriptor of an MN-major operand: boxes of 64 (M or N) x 64 (K), 128
+// bytes a K row, with the 128-byte swizzle; 8 K rows are 1024 bytes, boxes 8 KB apart.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
+  uint64_t desc = static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
+  desc |= static_cast<uint64_t>(8192 >> 4) << 16;
+  desc |= static_cast<uint64_t>(1024 >> 4) << 32;
+  desc |= static_cast<uint64_t>(1) << 46;
+  desc |= static_cast<uint64_t>(2) << 61;
+  return desc;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A staged box added to global memory in fp32.
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+      ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(src)
+      : "memory");
+}
+
+// ---- rows that count ----------------------------------------------------------
+constexpr int kRowsThreads = 256;
+
+// Each CTA counts the rows in front of its own by itself (the targets of a batch are
+// few bytes), so that packing them takes one launch.
+__global__ void __launch_bounds__(kRowsThreads)
+    head_rows_kernel(const HeadRows p, bool vec) {
+  __shared__ int s_count[3][kRowsThreads / 32];
+  __shared__ int s_at[kRowsThreads];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int64_t per = (p.rows + gridDim.x - 1) / gridDim.x;
+  const int64_t lo = min(p.rows, blockIdx.x * per), hi = min(p.rows, lo + per);
+  int before = 0, total = 0, wrong = 0;
+#pragma unroll 4
+  for (int64_t r = tid; r < p.rows; r += kRowsThreads) {
+    const int t = p.targets[r];
+    const bool live = t >= 0 && t < p.vocab;
+    total += live;
+    before += live && r < lo;
+    wrong |= t >= p.vocab;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+    total += __shfl_xor_sync(0xffffffffu, total, o);
+    wrong |= __shfl_xor_sync(0xffffffffu, wrong, o);
+  }
+  if (lane == 0) {
+    s_count[0][w] = before;
+    s_count[1][w] = total;
+    s_count[2][w] = wrong;
+  }
+  __syncthreads();
+  before = total = wrong = 0;
+  for (int i = 0; i < kRowsThreads / 32; ++i) {
+    before += s_count[0][i];
+    total += s_count[1][i];
+    wrong |= s_count[2][i];
+  }
+  if (blockIdx.x == 0) {
+    if (tid == 0) {
+      *p.live = total;
+      if (p.err != nullptr) *p.err = wrong ? kErrIndex : 0u;
+    }
+    for (int i = tid; i < p.n_queue; i += kRowsThreads) p.queue[i] = 0u;
+  }
+  auto copy_row = [&](int64_t at, const __nv_bfloat16* from) {  // a warp; zeros from nullptr
+    __nv_bfloat16* to = p.packed + at * p.ld_packed;
+    if (vec) {
+      for (int c = lane * 8; c < p.k; c += 256)
+        *reinterpret_cast<uint4*>(to + c) =
+            from ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      for (int c = lane; c < p.k; c += 32) to[c] = from ? from[c] : __float2bfloat16_rn(0.f);
+    }
+  };
+  for (int64_t r0 = lo; r0 < hi; r0 += kRowsThreads) {
+    const int64_t r = r0 + tid;
+    const int t = r < hi ? p.targets[r] : -1;
+    const bool live = t >= 0 && t < p.vocab;
+    const uint32_t mask = __ballot_sync(0xffffffffu, live);
+    __syncthreads();  // (earlier readers of both arrays)
+    if (lane == 0) s_count[0][w] = __popc(mask);
+    __syncthreads();
+    int at = before + __popc(mask & ((1u << lane) - 1u));
+    int in_chunk = 0;
+    for (int i = 0; i < kRowsThreads / 32; ++i) {
+      if (i < w) at += s_count[0][i];
+      in_chunk += s_count[0][i];
+    }
+    before += in_chunk;
+    s_at[tid] = live ? at : -1;
+    if (r < hi) {
+      if (p.place != nullptr) p.place[r] = live ? at : -1;
+      if (live) {
+        p.row[at] = static_cast<int>(r);
+        p.target[at] = t;
+        if (p.grad != nullptr) p.row_grad[at] = p.grad[r];
+        if (p.lse != nullptr) p.row_lse[at] = p.lse[r];
+      } else if (p.loss_out != nullptr) {
+        p.loss_out[r] = 0.f;
+        p.lse_out[r] = 0.f;
+      }
+    }
+    __syncthreads();
+    const int n = static_cast<int>(min(static_cast<int64_t>(kRowsThreads), hi - r0));
+    for (int i = w; i < n; i += kRowsThreads / 32)
+      if (s_at[i] >= 0) copy_row(s_at[i], p.hidden + (r0 + i) * p.ld_hidden);
+  }
+  // rows of zeros up to whole tiles
+  const int64_t most = (total + kTile - 1) / kTile * kTile;
+  for (int64_t i = total + static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + w; i < most;
+       i += static_cast<int64_t>(gridDim.x) * (kRowsThreads / 32)) {
+    copy_row(i, nullptr);
+    if (lane == 0) {
+      p.target[i] = -1;
+      if (p.grad != nullptr) p.row_grad[i] = 0.f;
+      if (p.lse != nullptr) p.row_lse[i] = 0.f;
+    }
+  }
+}
+
+// ---- tiles --------------------------------------------------------------------
+enum { kLoss = 0, kGrad = 1, kHidden = 2, kWeight = 3 };
+
+struct Maps {
+  CUtensorMap h_rows;   // packed rows, boxes of 64 columns x 128 rows
+  CUtensorMap w_rows;   // W, the same
+  CUtensorMap h_cols;   // packed rows, boxes of 64 x 64
+  CUtensorMap w_cols;   // W, the same
+  CUtensorMap g_rows;   // the piece of G that is read, 64 x 128
+  CUtensorMap g_cols;   // the same, 64 x 64
+  CUtensorMap g_out;    // the piece of G that is written, 64 columns x 32 rows
+  CUtensorMap dw_out;   // gradient of W, 64 (fp32: 32) columns x 32 rows
+  CUtensorMap dh_out;   // [splits x rows] fp32 sums, 32 x 32
+};
+
+struct Tile {
+  int kind;
+  int row0;      // rows of the tile: packed rows, weight: rows of the piece
+  int col0;      // columns: vocabulary (grad: in the piece) or hidden columns
+  int kb0, kb1;  // stages of the reduction
+  int part;      // hidden: which part of the piece
+};
+
+// How many tiles of each kind the launch has, for `live` rows.
+struct Counts {
+  int mt;         // tiles of rows
+  int grad, hidden, weight;
+  __device__ __forceinline__ int all() const { return grad + hidden + weight; }
+};
+__device__ __forceinline__ Counts count_tiles(const HeadTiles& p, int live, bool loss) {
+  Counts c;
+  c.mt = (live + kTile - 1) / kTile;
+  c.grad = c.mt * p.vt_next;
+  c.hidden = loss ? 0 : c.mt * p.kt * p.parts;
+  c.weight = loss || p.dw == nullptr ? 0 : p.vt * p.kt;
+  return c;
+}
+
+__device__ __forceinline__ Tile decode(const HeadTiles& p, const Counts& c, int live, bool loss,
+                                       int j) {
+  Tile t{};
+  if (!loss) {
+    // hidden tiles and weight tiles, the longer ones first; the parts and columns of a
+    // panel of G next to one another
+    const int first = p.hidden_first ? c.hidden : c.weight;
+    const bool in_first = j < first;
+    if (j < c.hidden + c.weight) {
+      const int i = in_first ? j : j - first;
+      t.kind = in_first == p.hidden_first ? kHidden : kWeight;
+      t.col0 = i % p.kt * kTile;
+      if (t.kind == kHidden) {
+        t.part = i / p.kt % p.parts;
+        t.row0 = i / p.kt / p.parts * kTile;
+        t.kb0 = t.part * p.part_blocks;
+        t.kb1 = min(t.kb0 + p.part_blocks, p.vt * (kTile / BK));
+      } else {
+        t.row0 = i / p.kt * kTile;
+        t.kb1 = (live + BK - 1) / BK;
+      }
+      return t;
+    }
+    j -= c.hidden + c.weight;
+  }
+  t.kind = loss ? kLoss : kGrad;
+  // groups of kHeadGroup tiles of rows stay in L2 while W passes by
+  const int per = kHeadGroup * p.vt_next;
+  const int m0 = j / per * kHeadGroup, r = j % per;
+  const int gm = min(kHeadGroup, c.mt - m0);
+  t.row0 = (m0 + r % gm) * kTile;
+  t.col0 = r / gm * kTile;
+  t.kb1 = (p.k + BK - 1) / BK;
+  return t;
+}
+
+// Running maximum and sum of 2^((z - m) log2 e).
+struct Stats {
+  float m, s;
+};
+__device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ void add_chunk(Stats& st, const float (&z)[32]) {
+  float top[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top[i] = fmaxf(fmaxf(z[i], z[i + 8]), fmaxf(z[i + 16], z[i + 24]));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], top[i + 4]);
+  const float m = fmaxf(st.m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+  const float ref = safe_max(m);
+  const float mc = ref * kLog2e;
+  const float lost = __fmaf_rn(ref, kLog2e, -mc);  // exponents are too large by this
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 32; ++i) sum[i & 3] += exp2_fast(__fmaf_rn(z[i], kLog2e, -mc));
+  const float chunk = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  st.s = __fmaf_rn(st.s, exp2_fast((st.m - ref) * kLog2e), __fmaf_rn(-lost * kLn2, chunk, chunk));
+  st.m = m;
+}
+
+template <bool LOSS>
+__global__ void __launch_bounds__(kThreads, 1)
+    head_tiles_kernel(const __grid_constant__ Maps maps, const HeadTiles p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sa = smem;
+  uint8_t* sb = smem + kStages * kOperand;
+  uint8_t* staging = smem + kStages * kStageBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + kEpiWarps * kStaging);
+  uint64_t* full = bars;                     // leader's is the one used
+  uint64_t* empty = full + kStages;          // per CTA
+  uint64_t* acc_full = empty + kStages;      // [2] per CTA
+  uint64_t* acc_empty = acc_full + 2;        // [2] leader's is the one used
+  uint64_t* job_full = acc_empty + 2;        // [kJobs] per CTA: the tile's number is there
+  uint64_t* job_empty = job_full + kJobs;    // [kJobs] leader's: everyone has read it
+  uint64_t* drain = job_empty + kJobs;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* s_job = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [kJobs]
+  static_assert((2 * kStages + 4 + 2 * kJobs + 1) * 8 + 8 + kJobs * 4 <= 512, "barriers");
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const bool leader = rank == 0;
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 2);  // an expect_tx of each CTA
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], 2 * kEpiWarps);
+    }
+    for (int j = 0; j < kJobs; ++j) {
+      mbar_init(&job_full[j], 1);
+      // the epilogue warps of both CTAs, the MMA issuer, the peer's producer
+      mbar_init(&job_empty[j], 2 * kEpiWarps + 2);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_map(&maps.h_rows);
+    prefetch_map(&maps.w_rows);
+  }
+  cluster_sync_all();  // barriers of both CTAs initialised; the peer is running
+  if (warp == 1) tmem_alloc_pair(smem_addr(tmem_slot), 2 * kTile);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int live = min(max(*p.live, 0), p.rows);
+  const Counts counts = count_tiles(p, live, LOSS);
+  const int njobs = counts.all();
+
+  // The number of the n-th tile of this pair; -1 after the last one.  Arrives for the
+  // calling thread; false on a timeout.
+  auto next_job = [&](uint32_t n, int& j) {
+    const int slot = n % kJobs;
+    if (!mbar_wait_cluster(&job_full[slot], (n / kJobs) & 1u, abort_flag, kWaitNs)) return false;
+    j = s_job[slot];
+    mbar_arrive_cluster(map_to_rank(smem_addr(&job_empty[slot]), 0));
+    return true;
+  };
+  auto give_up = [&](bool timeout) {
+    if (timeout && !*abort_flag) set_err(p.err, kErrTimeout);
+    *abort_flag = 1;
+  };
+
+  if (warp == 0 && lane == 0) {
+    // ---------------- tiles and TMA loads ----------------
+    int stage = 0;
+    uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
+    bool ok = true;
+    int next = pair < njobs ? pair : -1;  // leader
+    for (uint32_t n = 0; ok; ++n) {
+      int j = next;
+      if (leader) {
+        const int slot = n % kJobs;
+        if (!mbar_wait_cluster(&job_empty[slot], ((n / kJobs) & 1u) ^ 1u, abort_flag, kWaitNs)) {
+          ok = false;
+          break;
+        }
+        s_job[slot] = j;
+        const uint32_t there = map_to_rank(smem_addr(const_cast<int*>(&s_job[slot])), 1);
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(there), "r"(j) : "memory");
+        mbar_arrive_cluster(map_to_rank(smem_addr(&job_full[slot]), 0));
+        mbar_arrive_cluster(map_to_rank(smem_addr(&job_full[slot]), 1));
+      } else if (!next_job(n, j)) {
+        ok = false;
+        break;
+      }
+      if (j < 0) break;
+      const Tile t = decode(p, counts, live, LOSS, j);
+      const int ra = t.row0 + static_cast<int>(rank) * kHalf;
+      const int rb = t.col0 + static_cast<int>(rank) * kHalf;
+      bool fetched = false;
+      auto fetch = [&] {
+        if (leader) {
+          const uint32_t q = atomicAdd(p.queue, 1u) + static_cast<uint32_t>(npairs);
+          next = q < static_cast<uint32_t>(njobs) ? static_cast<int>(q) : -1;
+        }
+        fetched = true;
+      };
+      for (int kb = t.kb0; kb < t.kb1; ++kb) {
+        if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
+          ok = false;
+          break;
+        }
+        const uint32_t fb = map_to_rank(smem_addr(&full[stage]), 0);
+        if (leader) mbar_expect_tx(smem_addr(&full[stage]), kStageBytes);
+        else mbar_expect_tx_cluster(fb, kStageBytes);
+        const uint32_t a = smem_addr(sa + stage * kOperand), b = smem_addr(sb + stage * kOperand);
+        const int k0 = kb * BK;
+        if (LOSS || t.kind == kGrad) {
+          tma_load_2d_pair(a, &maps.h_rows, k0, ra, fb);
+          tma_load_2d_pair(b, &maps.w_rows, k0, p.v_next + rb, fb);
+        } else if (t.kind == kHidden) {
+          tma_load_2d_pair(a, &maps.g_rows, k0, ra, fb);
+          tma_load_2d_pair(b, &maps.w_cols, rb, p.v0 + k0, fb);
+          tma_load_2d_pair(b + kOperand / 2, &maps.w_cols, rb + 64, p.v0 + k0, fb);
+        } else {
+          tma_load_2d_pair(a, &maps.g_cols, ra, k0, fb);
+          tma_load_2d_pair(a + kOperand / 2, &maps.g_cols, ra + 64, k0, fb);
+          tma_load_2d_pair(b, &maps.h_cols, rb, k0, fb);
+          tma_load_2d_pair(b + kOperand / 2, &maps.h_cols, rb + 64, k0, fb);
+        }
+        issued_mask |= 1u << stage;
+        issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+        if (kb + 1 == t.kb1) fetch();
+      }
+      if (!fetched) fetch();
+    }
+    if (!ok) give_up(true);
+    if (*abort_flag && leader) {
+      // every issued load must land before the CTA may exit
+      for (int s = 0; s < kStages; ++s)
+        if (issued_mask & (1u << s))
+          mbar_wait(&full[s], (issued_phase >> s) & 1u, nullptr, kDrainNs);
+    }
+  } else if (warp == 1 && lane == 0 && leader) {
+    // ---------------- MMAs ----------------
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true, issued_any = false;
+    for (uint32_t n = 0; ok; ++n) {
+      int j;
+      if (!next_job(n, j)) {
+        ok = false;
+        break;
+      }
+      if (j < 0) break;
+      const Tile t = decode(p, counts, live, LOSS, j);
+      const bool a_mn = !LOSS && t.kind == kWeight, b_mn = !LOSS && t.kind >= kHidden;
+      const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+      // 16 along the reduction: 32 bytes of a row, or 16 rows of 128 bytes
+      const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+      const int ab = n & 1;
+      if (!mbar_wait(&acc_empty[ab], ((n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t d = tmem_base + static_cast<uint32_t>(ab * kTile);
+      for (int kb = t.kb0; kb < t.kb1; ++kb) {
+        if (!mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t a = smem_addr(sa + stage * kOperand), b = smem_addr(sb + stage * kOperand);
+        const uint64_t da = a_mn ? desc_mn(a) : desc_sw128(a);
+        const uint64_t db = b_mn ? desc_mn(b) : desc_sw128(b);
+#pragma unroll
+        for (int u = 0; u < BK / 16; ++u)
+          mma_bf16_pair(d, da + u * a_step, db + u * b_step, idesc,
+                        (kb > t.kb0 || u > 0) ? 1u : 0u);
+        issued_any = true;
+        mma_commit_pair(smem_addr(&empty[stage]));
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+      if (!ok) break;
+      mma_commit_pair(smem_addr(&acc_full[ab]));
+    }
+    if (!ok) give_up(true);
+    if (*abort_flag && issued_any) {
+      mma_commit_pair(smem_addr(drain));
+      mbar_wait(drain, 0, nullptr, kDrainNs);
+    }
+  } else if (warp >= 2) {
+    // ---------------- epilogue ----------------
+    const int quarter = warp & 3;
+    const int half = (warp - 2) >> 2;  // columns 128 half .. of the tile
+    uint8_t* stg = staging + (warp - 2) * kStaging;
+    const uint32_t stg_s = smem_addr(stg);
+    // 16-byte chunk c of this thread's row in the staged box
+    auto chunk_at = [&](int c) { return stg_s + lane * 128 + ((c ^ (lane & 7)) << 4); };
+    auto put = [&](int c, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk_at(c)), "r"(x), "r"(y),
+                   "r"(z), "r"(w)
+                   : "memory");
+    };
+    // the store that last used the box has read it
+    auto box_free = [&] {
+      if (lane == 0) bulk_wait_read<0>();
+      __syncwarp();
+    };
+    auto box_filled = [&] {
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    for (uint32_t n = 0;; ++n) {
+      int j = -1, ok = 1;
+      if (lane == 0) ok = next_job(n, j) ? 1 : 0;
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      j = __shfl_sync(0xffffffffu, j, 0);
+      if (!ok) {
+        if (lane == 0) give_up(true);
+        break;
+      }
+      if (j < 0) break;
+      const Tile t = decode(p, counts, live, LOSS, j);
+      const int ab = n & 1;
+      const int row = t.row0 + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
+      const int warp_row = row - lane;
+      const int col0 = t.col0 + half * 128;
+      int target = -1;
+      float c_row = 0.f, lse_c = 0.f;
+      if (LOSS || t.kind == kGrad) {
+        target = p.target[row] - (LOSS ? 0 : p.v_next);  // (rows up to whole tiles have one)
+        if (!LOSS) {
+          c_row = p.row_grad[row];
+          lse_c = p.row_lse[row] * kLog2e;
+        }
+      }
+      if (lane == 0) ok = mbar_wait(&acc_full[ab], (n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) {
+        if (lane == 0) give_up(true);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t tm = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                          static_cast<uint32_t>(ab * kTile + half * 128);
+      auto hand_back = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_rank(smem_addr(&acc_empty[ab]), 0));
+      };
+      float z[32];
+      auto load = [&](int c) {  // 32 columns from 32 c
+        uint32_t r[32];
+        tmem_ld32(tm + 32 * c, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(r[i]);
+        if (c == 3) hand_back();
+      };
+      if (LOSS) {
+        Stats st{-INFINITY, 0.f};
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          load(c);
+          const int v = col0 + 32 * c;
+          if (v + 32 > p.vocab)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (v + i >= p.vocab) z[i] = -INFINITY;
+          const uint32_t at = static_cast<uint32_t>(target - v);
+          if (at < 32u) {
+            float zt = z[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) zt = at == static_cast<uint32_t>(i) ? z[i] : zt;
+            p.z_target[row] = zt;
+          }
+          if (v < p.vocab) add_chunk(st, z);
+        }
+        p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
+      } else if (t.kind == kGrad) {
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          load(c);
+          const int v = col0 + 32 * c;  // in the piece
+          const uint32_t at = static_cast<uint32_t>(target - v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float g = exp2_fast(__fmaf_rn(z[i], kLog2e, -lse_c));
+            g = at == static_cast<uint32_t>(i) ? g - 1.f : g;
+            z[i] = c_row * g;
+          }
+          if (p.v_next + v + 32 > p.vocab)  // zeros behind the last column
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (p.v_next + v + i >= p.vocab) z[i] = 0.f;
+          if ((c & 1) == 0) box_free();
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            put((c & 1) * 4 + q, pack_bf16(z[8 * q], z[8 * q + 1]),
+                pack_bf16(z[8 * q + 2], z[8 * q + 3]), pack_bf16(z[8 * q + 4], z[8 * q + 5]),
+                pack_bf16(z[8 * q + 6], z[8 * q + 7]));
+          if (c & 1) {
+            box_filled();
+            if (lane == 0) {
+              tma_store_2d(&maps.g_out, stg_s, v - 32, warp_row);
+              bulk_commit();
+            }
+          }
+        }
+      } else if (t.kind == kHidden) {
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          load(c);
+          if (col0 + 32 * c >= p.ld_sums) continue;
+          box_free();
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            put(q, __float_as_uint(z[4 * q]), __float_as_uint(z[4 * q + 1]),
+                __float_as_uint(z[4 * q + 2]), __float_as_uint(z[4 * q + 3]));
+          box_filled();
+          if (lane == 0) {
+            const int at = t.part * p.rows_up + warp_row;
+            if (p.v0 == 0) tma_store_2d(&maps.dh_out, stg_s, col0 + 32 * c, at);
+            else tma_add_2d(&maps.dh_out, stg_s, col0 + 32 * c, at);
+            bulk_commit();
+          }
+        }
+      } else {
+        // boxes of 128 bytes: 64 bf16 or 32 fp32 columns
+        const int64_t out_row = static_cast<int64_t>(p.v0) + warp_row;
+        const int rows = min(32, p.vocab - p.v0 - warp_row);
+        auto flush = [&](int col, int cols) {
+          const int n_cols = min(cols, p.k - col);
+          if (rows <= 0 || n_cols <= 0) return;
+          const int es = p.dw_f32 ? 4 : 2;
+          int done = 0;  // columns that the map covers
+          if (p.dw_mapped) {
+            done = min(n_cols, max(0, p.k / (16 / es) * (16 / es) - col));
+            if (lane == 0) {
+              if (done > 0) tma_store_2d(&maps.dw_out, stg_s, col, static_cast<int>(out_row));
+              bulk_commit();
+            }
+          }
+          if (done == n_cols) return;
+          for (int i = lane; i < rows * (n_cols - done); i += 32) {
+            const int r = i / (n_cols - done), x = done + i % (n_cols - done);
+            const uint8_t* from = stg + r * 128 + (((x * es >> 4) ^ (r & 7)) << 4) + (x * es & 15);
+            const int64_t to = (out_row + r) * p.ld_dw + col + x;
+            if (p.dw_f32)
+              static_cast<float*>(p.dw)[to] = *reinterpret_cast<const float*>(from);
+            else
+              static_cast<uint16_t*>(p.dw)[to] = *reinterpret_cast<const uint16_t*>(from);
+          }
+          __syncwarp();
+        };
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          load(c);
+          if (t.kb1 == 0)  // no rows: nothing was added up
+#pragma unroll
+            for (int i = 0; i < 32; ++i) z[i] = 0.f;
+          const int col = col0 + 32 * c;
+          if (p.dw_f32) {
+            box_free();
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              put(q, __float_as_uint(z[4 * q]), __float_as_uint(z[4 * q + 1]),
+                  __float_as_uint(z[4 * q + 2]), __float_as_uint(z[4 * q + 3]));
+            box_filled();
+            flush(col, 32);
+            continue;
+          }
+          if ((c & 1) == 0) box_free();
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            put((c & 1) * 4 + q, pack_bf16(z[8 * q], z[8 * q + 1]),
+                pack_bf16(z[8 * q + 2], z[8 * q + 3]), pack_bf16(z[8 * q + 4], z[8 * q + 5]),
+                pack_bf16(z[8 * q + 6], z[8 * q + 7]));
+          if (c & 1) {
+            box_filled();
+            flush(col - 32, 64);
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();  // every store written before exit
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // the pair's MMAs and TMEM reads are done in both CTAs
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc_pair(tmem_base, 2 * kTile);
+  }
+}
+
+// ---- ends ---------------------------------------------------------------------
+// The maxima and sums of a row's slices to its lse and loss: 32 rows x 32 groups of
+// slices a CTA.
+__global__ void __launch_bounds__(1024)
+    head_loss_kernel(const float2* __restrict__ stats, int64_t ld_stats, int slices,
+                     const int* __restrict__ live, const int* __restrict__ row,
+                     const float* __restrict__ z_target, float* __restrict__ loss,
+                     float* __restrict__ lse) {
+  __shared__ float2 s_part[32][33];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int n = *live;
+  if (blockIdx.x * 32 >= static_cast<unsigned>(n)) return;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t i = blockIdx.x * 32 + x;
+  float2 st = make_float2(-INFINITY, 0.f);
+  auto merge = [](float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x), ref = safe_max(m);
+    return make_float2(m, a.y * exp2_fast((a.x - ref) * kLog2e) +
+                              b.y * exp2_fast((b.x - ref) * kLog2e));
+  };
+  // (a NaN maximum is lost in fmaxf, its sum is not)
+  for (int s = y; s < slices; s += 32) st = merge(st, stats[s * ld_stats + i]);
+  s_part[y][x] = st;
+  __syncthreads();
+  if (y >= 1 || i >= n) return;
+  for (int s = 1; s < 32; ++s) st = merge(st, s_part[s][x]);
+  const float ln = logf(st.y), m = safe_max(st.x);
+  const int r = row[i];
+  lse[r] = m + ln;
+  loss[r] = (m - z_target[i]) + ln;  // (m is often the target's own logit)
+}
+
+// Dh of the rows that count, the sums of its parts in their order; zeros elsewhere.
+template <typename Te>
+__global__ void __launch_bounds__(256)
+    head_hidden_kernel(const float* __restrict__ sums, int64_t ld_sums, int64_t part_stride,
+                       int parts, const int* __restrict__ place, int64_t rows, int k,
+                       Te* __restrict__ out, int64_t ldo) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const int lane = threadIdx.x & 31;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 8;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); r < rows; r += step) {
+    const int at = place[r];
+    const float* from = sums + at * ld_sums;
+    for (int c = lane; c < k; c += 32) {
+      float sum = 0.f;
+      if (at >= 0)
+        for (int s = 0; s < parts; ++s) sum += from[s * part_stride + c];
+      out[r * ldo + c] = from_f32<Te>(sum);
+    }
+  }
+}
+
+bool box_map(CUtensorMap* m, PFN_cuTensorMapEncodeTiled_v12000 fn, const void* base, bool f32,
+             int64_t rows, int64_t cols, int64_t ld, int box_cols, int box_rows) {
+  const cuuint64_t es = f32 ? 4 : 2;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols),
+                             static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool LOSS>
+cudaError_t launch_tiles(const Maps& maps, const HeadTiles& p, int64_t jobs, int sms,
+                         cudaStream_t stream) {
+  auto kernel = head_tiles_kernel<LOSS>;
+  cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const int64_t pairs = jobs < sms / 2 ? jobs : sms / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, maps, p);
+}
+
+}  // namespace
+
+cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream) {
+  const bool vec = p.k % 8 == 0 && reinterpret_cast<uintptr_t>(p.hidden) % 16 == 0 &&
+                   p.ld_hidden % 8 == 0;
+  const int64_t ctas = p.rows < 2 * sms ? p.rows : 2 * sms;
+  return launch_pdl(head_rows_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kRowsThreads), 0,
+                    stream, p, vec);
+}
+
+cudaError_t launch_head_loss(const HeadProblem& h, HeadTiles p, float* loss, float* lse, int sms,
+                             cudaStream_t stream) {
+  Maps maps;
+  if (!box_map(&maps.h_rows, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, kHalf) ||
+      !box_map(&maps.w_rows, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, kHalf))
+    return cudaErrorInvalidValue;
+  p.vt_next = static_cast<int>((static_cast<int64_t>(p.vocab) + kTile - 1) / kTile);
+  p.v_next = 0;
+  const int64_t mt = p.rows_up / kTile;
+  cudaError_t e = launch_tiles<true>(maps, p, mt * p.vt_next, sms, stream);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(head_loss_kernel, dim3(static_cast<unsigned>((p.rows + 31) / 32)), dim3(1024),
+                    0, stream, static_cast<const float2*>(p.stats), p.ld_stats, 2 * p.vt_next,
+                    p.live, p.row, static_cast<const float*>(p.z_target), loss, lse);
+}
+
+cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const HeadPieces& q,
+                                      const int* place, int64_t rows, void* d_hidden,
+                                      int64_t ld_d_hidden, bool d_hidden_f32, int sms,
+                                      cudaStream_t stream) {
+  Maps maps;
+  p.kt = (p.k + kTile - 1) / kTile;
+  const int es = p.dw_f32 ? 4 : 2, unit = 16 / es;
+  p.dw_mapped = reinterpret_cast<uintptr_t>(p.dw) % 16 == 0 && p.ld_dw % unit == 0 && p.k >= unit;
+  p.dw_mapped = p.dw_mapped && p.dw != nullptr;
+  if (!box_map(&maps.h_rows, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, kHalf) ||
+      !box_map(&maps.h_cols, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, 64, BK) ||
+      !box_map(&maps.w_rows, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, kHalf) ||
+      !box_map(&maps.w_cols, h.encode, h.w, false, p.vocab, p.k, h.ldw, 64, BK) ||
+      (q.sums != nullptr &&
+       !box_map(&maps.dh_out, h.encode, q.sums, true, static_cast<int64_t>(q.parts) * p.rows_up,
+                p.ld_sums, p.ld_sums, 32, 32)) ||
+      (p.dw_mapped && !box_map(&maps.dw_out, h.encode, p.dw, p.dw_f32, p.vocab, p.k / unit * unit,
+                               p.ld_dw, 128 / es, 32)))
+    return cudaErrorInvalidValue;
+  const int64_t vt = (static_cast<int64_t>(p.vocab) + kTile - 1) / kTile;
+  const int pieces = static_cast<int>((vt + q.piece_tiles - 1) / q.piece_tiles);
+  const int64_t mt = p.rows_up / kTile;
+  uint32_t* queue = p.queue;
+  for (int i = 0; i <= pieces; ++i) {
+    // hidden and weight tiles of piece i - 1, grad tiles of piece i
+    const int64_t now = i > 0 ? std::min<int64_t>(q.piece_tiles, vt - (i - 1) * int64_t{q.piece_tiles}) : 0;
+    const int64_t next = i < pieces ? std::min<int64_t>(q.piece_tiles, vt - i * int64_t{q.piece_tiles}) : 0;
+    const int64_t ld_g = int64_t{q.piece_tiles} * kTile;
+    const int64_t g_size = p.rows_up * ld_g;
+    void* g_now = q.g + (pieces > 1 ? (i + 1) & 1 : 0) * g_size;
+    void* g_next = q.g + (pieces > 1 ? i & 1 : 0) * g_size;
+    if (!box_map(&maps.g_rows, h.encode, g_now, false, p.rows_up, ld_g, ld_g, BK, kHalf) ||
+        !box_map(&maps.g_cols, h.encode, g_now, false, p.rows_up, ld_g, ld_g, 64, BK) ||
+        !box_map(&maps.g_out, h.encode, g_next, false, p.rows_up, ld_g, ld_g, 64, 32))
+      return cudaErrorInvalidValue;
+    p.vt = static_cast<int>(now);
+    p.v0 = (i - 1) * q.piece_tiles * kTile;
+    p.vt_next = static_cast<int>(next);
+    p.v_next = i * q.piece_tiles * kTile;
+    const int blocks = p.vt * (kTile / BK);
+    p.part_blocks = q.part_blocks;
+    p.parts = q.sums != nullptr ? (blocks + q.part_blocks - 1) / q.part_blocks : 0;
+    p.hidden_first = q.sums != nullptr && p.part_blocks * BK >= p.rows;
+    p.queue = queue + i;
+    const int64_t jobs = mt * next + mt * p.kt * p.parts + (p.dw != nullptr ? now * p.kt : 0);
+    if (jobs == 0) continue;
+    const cudaError_t e = launch_tiles<false>(maps, p, jobs, sms, stream);
+    if (e != cudaSuccess) return e;
+  }
+  if (q.sums == nullptr) return cudaSuccess;
+  const int64_t ctas = std::min<int64_t>((rows + 7) / 8, int64_t{sms} * 8);
+  // parts of the first piece; a shorter last piece adds to fewer of them
+  const int64_t first = std::min<int64_t>(q.piece_tiles, vt) * (kTile / BK);
+  const int parts = static_cast<int>((first + q.part_blocks - 1) / q.part_blocks);
+  const int64_t stride = static_cast<int64_t>(p.rows_up) * p.ld_sums;
+  if (d_hidden_f32)
+    return launch_pdl(head_hidden_kernel<float>, dim3(static_cast<unsigned>(ctas)), dim3(256), 0,
+                      stream, static_cast<const float*>(q.sums), p.ld_sums, stride, parts, place,
+                      rows, p.k, static_cast<float*>(d_hidden), ld_d_hidden);
+  return launch_pdl(head_hidden_kernel<__nv_bfloat16>, dim3(static_cast<unsigned>(ctas)),
+                    dim3(256), 0, stream, static_cast<const float*>(q.sums), p.ld_sums, stride,
+                    parts, place, rows, p.k, static_cast<__nv_bfloat16*>(d_hidden), ld_d_hidden);
+}
+
+}  // namespace rx

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -342,5 +343,78 @@ struct ExpertRowsArgs {
 cudaError_t launch_expert_rows(int dtype, const ExpertRowsArgs& p, int sms, cudaStream_t s);
 cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backward, int sms,
                                   cudaStream_t s);
+
+// ---- loss of a vocabulary head (head_loss.cu) --------------------------------------
+constexpr int kHeadTile = 256;  // rows and columns of a tile of any of its products
+constexpr int kHeadGroup = 32;  // tiles of rows that stay in L2 while the weights pass by
+
+// The rows with a target in [0, vocab) to the front, zeros behind them up to whole
+// tiles; what the other kernels read of each.  Clears the queue and sets the error word.
+struct HeadRows {
+  int64_t rows;
+  int vocab, k;
+  const int32_t* targets;
+  const __nv_bfloat16* hidden;
+  int64_t ld_hidden;
+  const float* lse;   // nullable, with row_lse
+  const float* grad;  // nullable, with row_grad
+  __nv_bfloat16* packed;
+  int64_t ld_packed;
+  int* row;     // [rows] packed row -> row
+  int* target;  // [rows up to whole tiles], like the next two
+  float* row_lse;
+  float* row_grad;
+  int* place;  // [rows] nullable: row -> packed row or -1
+  int* live;
+  uint32_t* queue;
+  int n_queue;
+  float* loss_out;  // nullable: zeros for the rows left out
+  float* lse_out;
+  uint32_t* err;  // nullable
+};
+cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream);
+
+struct HeadProblem {
+  PFN_cuTensorMapEncodeTiled_v12000 encode;
+  const __nv_bfloat16* packed;
+  int64_t ld_packed;
+  const void* w;
+  int64_t ldw;
+};
+struct HeadTiles {
+  int rows, vocab, k;
+  int rows_up;  // rows up to whole tiles
+  const int* live;
+  const int* row;
+  const int* target;
+  const float* row_lse;
+  const float* row_grad;
+  float* z_target;  // [rows_up]
+  float2* stats;    // [2 * tiles of the vocabulary][rows_up]: maximum, sum
+  int64_t ld_stats;
+  uint32_t* queue;
+  uint32_t* err;
+  void* dw;  // nullable
+  int64_t ld_dw;
+  int dw_f32;
+  int ld_sums;
+  // set by the launchers: the piece whose gradients are taken (vt tiles from column v0)
+  // and the one whose G is made (vt_next from v_next)
+  int vt, v0, vt_next, v_next;
+  int kt, parts, part_blocks, hidden_first, dw_mapped;
+};
+// G in pieces of piece_tiles tiles of the vocabulary (two of them, or one if that is
+// all), the sums of Dh in parts of part_blocks stages each.
+struct HeadPieces {
+  int piece_tiles, part_blocks, parts;
+  __nv_bfloat16* g;
+  float* sums;  // [parts][rows_up][ld_sums]; nullable: no gradient of the rows
+};
+cudaError_t launch_head_loss(const HeadProblem& h, HeadTiles p, float* loss, float* lse, int sms,
+                             cudaStream_t stream);
+cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const HeadPieces& q,
+                                      const int* place, int64_t rows, void* d_hidden,
+                                      int64_t ld_d_hidden, bool d_hidden_f32, int sms,
+                                      cudaStream_t stream);
 
 }  // namespace rx

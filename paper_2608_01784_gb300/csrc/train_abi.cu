@@ -1,6 +1,7 @@
 // train_abi.cu — C entry points of what stands around the experts, with gradients:
-// norms around a block, tokens to experts and back.  Argument checks and workspace
-// carving; the kernels are in block_norm.cu and expert_rows.cu.
+// norms around a block, tokens to experts and back, the loss of a vocabulary head.
+// Argument checks and workspace carving; the kernels are in block_norm.cu,
+// expert_rows.cu and head_loss.cu.
 #include <limits.h>
 
 #include <algorithm>
@@ -11,6 +12,7 @@
 #include "reflex.h"
 
 namespace rx {
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 int device_sms();
 }  // namespace rx
 
@@ -58,6 +60,118 @@ bool plan_ok(int64_t T, int32_t E, int32_t k_max) {
 bool rows_ok(int32_t dtype, int64_t T, int32_t d, int32_t k_max, int64_t cap_rows) {
   return dtype_ok(dtype) && d >= 1 && plan_ok(T, 1, k_max) && cap_rows >= 0 &&
          cap_rows <= INT32_MAX;
+}
+
+using rx::kHeadTile;
+constexpr int32_t kHeadMost = 1 << 24;  // rows, and columns of the vocabulary
+
+int64_t tiles(int64_t n) { return (n + kHeadTile - 1) / kHeadTile; }
+bool head_size_ok(int32_t rows, int32_t vocab, int32_t k) {
+  return rows >= 0 && vocab >= 1 && k >= 1;
+}
+bool head_size_fits(int32_t rows, int32_t vocab, int32_t k) {
+  return rows <= kHeadMost && vocab <= kHeadMost && k <= (1 << 20) &&
+         tiles(rows) * tiles(vocab) <= (1 << 30);
+}
+bool head_ok(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
+             const int32_t* targets, int32_t rows, int32_t vocab, int32_t k) {
+  if (!head_size_ok(rows, vocab, k) || w == nullptr || !aligned(w, 16) || ldw < k || ldw % 8 != 0)
+    return false;
+  return rows == 0 || (matrix_ok({hidden, ld_hidden}, k, 2) && targets != nullptr &&
+                       aligned(targets, 4));
+}
+
+// What both directions keep of the rows that count.
+struct HeadLayout {
+  size_t live, queue, row, target, packed, z_target, stats;  // forward
+  size_t row_lse, row_grad, place, g, sums;                  // backward
+  size_t total;
+  int64_t rows_up, ld_packed, ld_sums;
+  int n_queue, piece_tiles, part_blocks, parts;
+};
+struct Carve {
+  size_t at = 0;
+  size_t operator()(size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return here;
+  }
+};
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t k, bool backward) {
+  HeadLayout L{};
+  L.rows_up = tiles(rows) * kHeadTile;
+  L.ld_packed = (k + 7) / 8 * 8;
+  L.ld_sums = (k + 31) / 32 * 32;
+  L.n_queue = 1;
+  const int64_t vt = tiles(vocab);
+  if (backward) {
+    // pieces of G of some 128 MB: what is written for the next products is mostly still
+    // in L2 when they read it
+    const int64_t most = std::max<int64_t>(1, (int64_t{128} << 20) / (L.rows_up * kHeadTile * 2));
+    L.piece_tiles = static_cast<int>(std::min(most, vt));
+    L.n_queue = static_cast<int>(tiles(vocab) / L.piece_tiles) + 2;
+    // parts of Dh: enough tiles for all pairs of SMs, so that none is long for the launch
+    const int64_t mt = tiles(rows), kt = tiles(k), blocks = L.piece_tiles * (kHeadTile / 64);
+    const int64_t want = std::min<int64_t>((100 + mt * kt - 1) / std::max<int64_t>(1, mt * kt), 64);
+    L.part_blocks = static_cast<int>((blocks + want - 1) / want);
+    L.parts = static_cast<int>((blocks + L.part_blocks - 1) / L.part_blocks);
+  }
+  Carve take;
+  L.live = take(sizeof(int));
+  L.queue = take(static_cast<size_t>(L.n_queue) * 4);
+  L.row = take(rows * 4);
+  L.target = take(L.rows_up * 4);
+  L.packed = take(L.rows_up * L.ld_packed * 2);
+  if (!backward) {
+    L.z_target = take(L.rows_up * 4);
+    L.stats = take(2 * vt * L.rows_up * sizeof(float2));
+  } else {
+    L.row_lse = take(L.rows_up * 4);
+    L.row_grad = take(L.rows_up * 4);
+    L.place = take(rows * 4);
+    const int buffers = L.piece_tiles < vt ? 2 : 1;
+    L.g = take(buffers * L.rows_up * L.piece_tiles * kHeadTile * 2);
+    L.sums = take(L.parts * L.rows_up * L.ld_sums * 4);
+  }
+  L.total = take.at;
+  return L;
+}
+template <typename T>
+T* at(void* ws, size_t offset) {
+  return reinterpret_cast<T*>(static_cast<uint8_t*>(ws) + offset);
+}
+rx::HeadRows head_rows(const HeadLayout& L, void* ws, const void* hidden, int64_t ld_hidden,
+                       const int32_t* targets, int32_t rows, int32_t vocab, int32_t k,
+                       int32_t* dev_status) {
+  rx::HeadRows r{};
+  r.rows = rows;
+  r.vocab = vocab;
+  r.k = k;
+  r.targets = targets;
+  r.hidden = static_cast<const __nv_bfloat16*>(hidden);
+  r.ld_hidden = ld_hidden;
+  r.packed = at<__nv_bfloat16>(ws, L.packed);
+  r.ld_packed = L.ld_packed;
+  r.row = at<int>(ws, L.row);
+  r.target = at<int>(ws, L.target);
+  r.live = at<int>(ws, L.live);
+  r.queue = at<uint32_t>(ws, L.queue);
+  r.n_queue = L.n_queue;
+  r.err = reinterpret_cast<uint32_t*>(dev_status);
+  return r;
+}
+rx::HeadTiles head_tiles(const HeadLayout& L, const rx::HeadRows& r) {
+  rx::HeadTiles t{};
+  t.rows = static_cast<int>(r.rows);
+  t.vocab = r.vocab;
+  t.k = r.k;
+  t.rows_up = static_cast<int>(L.rows_up);
+  t.live = r.live;
+  t.row = r.row;
+  t.target = r.target;
+  t.queue = r.queue;
+  t.err = r.err;
+  return t;
 }
 
 }  // namespace
@@ -275,6 +389,102 @@ int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_
   a.d_alpha = d_alpha;
   RX_CUDA(rx::launch_expert_combine(dtype, a, true, rx::device_sms(),
                                     static_cast<cudaStream_t>(stream)));
+  return REFLEX_OK;
+}
+
+size_t reflex_head_loss_workspace_size(int32_t rows, int32_t vocab, int32_t k) {
+  if (!head_size_ok(rows, vocab, k) || !head_size_fits(rows, vocab, k)) return 0;
+  return head_layout(rows, vocab, k, false).total;
+}
+
+int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
+                     const int32_t* targets, int32_t rows, int32_t vocab, int32_t k, float* loss,
+                     float* lse, int32_t* dev_status, void* workspace, size_t ws_bytes,
+                     void* stream) {
+  if (!head_ok(hidden, ld_hidden, w, ldw, targets, rows, vocab, k) || !aligned(dev_status, 4) ||
+      (rows > 0 && (loss == nullptr || lse == nullptr)) || !aligned(loss, 4) || !aligned(lse, 4))
+    return REFLEX_EINVAL;
+  if (!head_size_fits(rows, vocab, k)) return REFLEX_EUNSUPPORTED;
+  const HeadLayout L = head_layout(rows, vocab, k, false);
+  if (workspace == nullptr || ws_bytes < L.total || !aligned(workspace, kAlign))
+    return REFLEX_EWORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));
+    return REFLEX_OK;
+  }
+  const auto encode = rx::tensor_map_encoder();
+  if (encode == nullptr) return REFLEX_ECUDA;
+  const int sms = rx::device_sms();
+  rx::HeadRows r =
+      head_rows(L, workspace, hidden, ld_hidden, targets, rows, vocab, k, dev_status);
+  r.loss_out = loss;
+  r.lse_out = lse;
+  RX_CUDA(rx::launch_head_rows(r, sms, s));
+  rx::HeadTiles t = head_tiles(L, r);
+  t.z_target = at<float>(workspace, L.z_target);
+  t.stats = at<float2>(workspace, L.stats);
+  t.ld_stats = L.rows_up;
+  RX_CUDA(rx::launch_head_loss({encode, r.packed, L.ld_packed, w, ldw}, t, loss, lse, sms, s));
+  return REFLEX_OK;
+}
+
+size_t reflex_head_loss_backward_workspace_size(int32_t rows, int32_t vocab, int32_t k) {
+  if (!head_size_ok(rows, vocab, k) || !head_size_fits(rows, vocab, k)) return 0;
+  return head_layout(rows, vocab, k, true).total;
+}
+
+int reflex_head_loss_backward(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
+                              const int32_t* targets, const float* lse, const float* grad,
+                              int32_t rows, int32_t vocab, int32_t k, int32_t d_hidden_dtype,
+                              void* d_hidden, int64_t ld_d_hidden, int32_t d_w_dtype, void* d_w,
+                              int64_t ld_d_w, int32_t* dev_status, void* workspace,
+                              size_t ws_bytes, void* stream) {
+  if (!head_ok(hidden, ld_hidden, w, ldw, targets, rows, vocab, k) || !aligned(dev_status, 4) ||
+      (rows > 0 && (lse == nullptr || grad == nullptr)) || !aligned(lse, 4) || !aligned(grad, 4) ||
+      (rows > 0 && d_hidden == nullptr && d_w == nullptr))
+    return REFLEX_EINVAL;
+  if (!dtype_ok(d_hidden_dtype) || !dtype_ok(d_w_dtype)) return REFLEX_EINVAL;
+  const size_t es_h = d_hidden_dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  const size_t es_w = d_w_dtype == REFLEX_DTYPE_F32 ? 4 : 2;
+  if ((d_hidden != nullptr && !matrix_ok({d_hidden, ld_d_hidden}, k, es_h)) ||
+      (d_w != nullptr && !matrix_ok({d_w, ld_d_w}, k, es_w)))
+    return REFLEX_EINVAL;
+  if (!head_size_fits(rows, vocab, k)) return REFLEX_EUNSUPPORTED;
+  const HeadLayout L = head_layout(rows, vocab, k, true);
+  if (workspace == nullptr || ws_bytes < L.total || !aligned(workspace, kAlign))
+    return REFLEX_EWORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));
+    if (d_w != nullptr)
+      RX_CUDA(cudaMemset2DAsync(d_w, ld_d_w * es_w, 0, k * es_w, vocab, s));
+    return REFLEX_OK;
+  }
+  const auto encode = rx::tensor_map_encoder();
+  if (encode == nullptr) return REFLEX_ECUDA;
+  const int sms = rx::device_sms();
+  rx::HeadRows r =
+      head_rows(L, workspace, hidden, ld_hidden, targets, rows, vocab, k, dev_status);
+  r.lse = lse;
+  r.grad = grad;
+  r.row_lse = at<float>(workspace, L.row_lse);
+  r.row_grad = at<float>(workspace, L.row_grad);
+  r.place = at<int>(workspace, L.place);
+  RX_CUDA(rx::launch_head_rows(r, sms, s));
+  rx::HeadTiles t = head_tiles(L, r);
+  t.row_lse = r.row_lse;
+  t.row_grad = r.row_grad;
+  t.dw = d_w;
+  t.ld_dw = ld_d_w;
+  t.dw_f32 = d_w_dtype == REFLEX_DTYPE_F32;
+  t.ld_sums = static_cast<int>(L.ld_sums);
+  const rx::HeadPieces q{L.piece_tiles, L.part_blocks, L.parts,
+                         at<__nv_bfloat16>(workspace, L.g),
+                         d_hidden != nullptr ? at<float>(workspace, L.sums) : nullptr};
+  RX_CUDA(rx::launch_head_loss_backward({encode, r.packed, L.ld_packed, w, ldw}, t, q, r.place,
+                                        rows, d_hidden, ld_d_hidden,
+                                        d_hidden_dtype == REFLEX_DTYPE_F32, sms, s));
   return REFLEX_OK;
 }
 

@@ -1,5 +1,5 @@
 """Torch-facing convenience over the entry points around the experts that have
-gradients: norms around a block, tokens to experts and back.  A gradient is a call of
+gradients: norms around a block, tokens to experts and back, the loss of a head.  A gradient is a call of
 its own (no autograd graph is kept), takes the forward call's inputs again and
 allocates only what it returns and a workspace, so each can be captured in a CUDA
 graph.  With a `stream`, new outputs belong to it: to use them on another, wait for
@@ -10,7 +10,7 @@ from __future__ import annotations
 import torch
 
 from . import _binding as B
-from .fp8 import _DTYPES, _matrix, _new, _want
+from .fp8 import _DTYPES, _matrix, _new, _status_word, _want
 
 
 def _here(device):
@@ -232,3 +232,92 @@ def expert_combine_backward(d_out: torch.Tensor, rows: torch.Tensor, alpha: torc
                                      plan.row_of, plan.T, d, plan.k_max, plan.cap_rows, d_rows,
                                      lddr, d_alpha, stream)
     return d_rows, d_alpha
+
+
+_BF16 = (torch.bfloat16,)
+
+
+def _head(hidden, weight, targets, status):
+    """Checks them; (rows, vocab, k, ld_hidden, ldw)."""
+    rows, k, ld_hidden = _matrix(hidden, "hidden", _BF16)
+    vocab, kw, ldw = _matrix(weight, "weight", _BF16)
+    _want(k > 0 and vocab > 0 and kw == k, "hidden and weight disagree on their columns")
+    if vocab == 1:
+        ldw = -(-k // 8) * 8
+    _want(ldw % 8 == 0 and weight.data_ptr() % 16 == 0,
+          "weight: rows start on 16-byte boundaries")
+    _want(hidden.device == weight.device, "tensors on several devices")
+    _here(hidden.device)
+    _rows(targets, rows, torch.int32, hidden.device, "targets")
+    _status_word(status, hidden.device)
+    return rows, vocab, k, ld_hidden, ldw
+
+
+def _rows(t: torch.Tensor, rows: int, dtype, device, what: str):
+    _want(t.dtype == dtype and tuple(t.shape) == (rows,) and t.is_contiguous()
+          and t.device == device, f"{what}: {rows} contiguous values of {dtype}")
+
+
+def head_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
+              loss: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+              status: torch.Tensor | None = None, stream=None):
+    """reflex_head_loss: (loss, lse) fp32 [rows] of the softmax of hidden weight^T at
+    targets int32 [rows], zeros where a target is negative.  hidden [rows, k] and weight
+    [vocab, k] are bf16; the logits are not kept."""
+    rows, vocab, k, ld_hidden, ldw = _head(hidden, weight, targets, status)
+    if loss is None:
+        loss = _new(rows, torch.float32, hidden.device, stream)
+    if lse is None:
+        lse = _new(rows, torch.float32, hidden.device, stream)
+    _rows(loss, rows, torch.float32, hidden.device, "loss")
+    _rows(lse, rows, torch.float32, hidden.device, "lse")
+    ws_bytes = B.reflex_head_loss_workspace_size(rows, vocab, k)
+    _want(ws_bytes > 0, "unsupported sizes")
+    ws = _new(ws_bytes, torch.uint8, hidden.device, stream)
+    B.reflex_head_loss(hidden, ld_hidden, weight, ldw, targets, rows, vocab, k, loss, lse, status,
+                       ws, ws_bytes, stream)
+    return loss, lse
+
+
+def _gradient(out, rows: int, cols: int, device, stream, what: str):
+    """A gradient (given, or new in bf16 with rows on 16-byte boundaries) and its stride."""
+    if out is None:
+        ld = -(-cols // 8) * 8
+        out = _new((rows, ld), torch.bfloat16, device, stream)
+        return (out if ld == cols else out[:, :cols]), ld
+    r, c, ld = _matrix(out, what, _DTYPES)
+    _want((r, c) == (rows, cols) and out.device == device, f"{what}: shape or device")
+    return out, ld
+
+
+def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                       lse: torch.Tensor, grad: torch.Tensor, *,
+                       d_hidden: torch.Tensor | None = None,
+                       d_weight: torch.Tensor | None = None, need_hidden: bool = True,
+                       need_weight: bool = True, status: torch.Tensor | None = None,
+                       stream=None):
+    """reflex_head_loss_backward: the gradients (of hidden, of weight) from grad fp32
+    [rows], that of each row's loss, and head_loss's lse.  They come in bf16, or in the
+    type of `d_hidden` and `d_weight` (fp32 or bf16); the one that is not needed is None."""
+    rows, vocab, k, ld_hidden, ldw = _head(hidden, weight, targets, status)
+    dev = hidden.device
+    _rows(lse, rows, torch.float32, dev, "lse")
+    _rows(grad, rows, torch.float32, dev, "grad")
+    _want(need_hidden or need_weight, "no gradient wanted")
+    _want((need_hidden or d_hidden is None) and (need_weight or d_weight is None),
+          "a place for a gradient that is not needed")
+    ld_dh = ld_dw = k
+    dt_h = dt_w = B.REFLEX_DTYPE_BF16
+    if need_hidden:
+        d_hidden, ld_dh = _gradient(d_hidden, rows, k, dev, stream, "d_hidden")
+        dt_h = _DTYPES[d_hidden.dtype]
+    if need_weight:
+        d_weight, ld_dw = _gradient(d_weight, vocab, k, dev, stream, "d_weight")
+        dt_w = _DTYPES[d_weight.dtype]
+    ws_bytes = B.reflex_head_loss_backward_workspace_size(rows, vocab, k)
+    _want(ws_bytes > 0, "unsupported sizes")
+    ws = _new(ws_bytes, torch.uint8, dev, stream)
+    B.reflex_head_loss_backward(hidden, ld_hidden, weight, ldw, targets, lse, grad, rows, vocab, k,
+                                dt_h, d_hidden, ld_dh, dt_w, d_weight, ld_dw, status, ws, ws_bytes,
+                                stream)
+    return d_hidden, d_weight

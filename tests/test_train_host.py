@@ -125,3 +125,41 @@ def test_no_tokens(B):
     assert call(B.reflex_expert_combine, COMBINE, rows=None, out=None, **none) == B.REFLEX_OK
     assert call(B.reflex_expert_combine_backward, COMBINE_GRAD, d_out=None, rows=None,
                 d_rows=None, d_alpha=None, **none) == B.REFLEX_OK
+
+
+HEAD = dict(hidden=P, ld_hidden=100, w=P, ldw=104, targets=P, rows=4, vocab=50, k=100, loss=P,
+            lse=P, dev_status=P, workspace=P, ws_bytes=1 << 40)
+HEAD_GRAD = dict(hidden=P, ld_hidden=100, w=P, ldw=104, targets=P, lse=P, grad=P, rows=4, vocab=50,
+                 k=100, d_hidden_dtype=1, d_hidden=P, ld_d_hidden=100, d_w_dtype=1, d_w=P,
+                 ld_d_w=100, dev_status=P, workspace=P, ws_bytes=1 << 40)
+BAD_HEAD = [dict(rows=-1), dict(vocab=0), dict(k=0), dict(hidden=None), dict(hidden=P + 1),
+            dict(ld_hidden=99), dict(w=None), dict(w=P + 8), dict(ldw=96), dict(ldw=101),
+            dict(targets=None), dict(targets=P + 2), dict(lse=None), dict(lse=P + 2),
+            dict(dev_status=P + 2)]
+
+
+@pytest.mark.parametrize("changes", BAD_HEAD + [dict(loss=None), dict(loss=P + 2)])
+def test_head_loss_refuses(B, changes):
+    assert call(B.reflex_head_loss, HEAD, **changes) == B.REFLEX_EINVAL
+
+
+@pytest.mark.parametrize("changes", BAD_HEAD + [
+    dict(grad=None), dict(grad=P + 2), dict(d_hidden=None, d_w=None), dict(d_hidden_dtype=2),
+    dict(d_w_dtype=2), dict(ld_d_hidden=99), dict(ld_d_w=99), dict(d_hidden=P + 1),
+    dict(d_w=P + 1), dict(d_hidden_dtype=0, d_hidden=P + 2), dict(d_w_dtype=0, d_w=P + 2)])
+def test_head_loss_backward_refuses(B, changes):
+    assert call(B.reflex_head_loss_backward, HEAD_GRAD, **changes) == B.REFLEX_EINVAL
+
+
+def test_head_loss_sizes_and_workspace(B):
+    huge = (1 << 24) + 1
+    for fn, good, size in ((B.reflex_head_loss, HEAD, B.reflex_head_loss_workspace_size),
+                           (B.reflex_head_loss_backward, HEAD_GRAD,
+                            B.reflex_head_loss_backward_workspace_size)):
+        for changes in (dict(rows=huge), dict(vocab=huge), dict(rows=1 << 24, vocab=1 << 24)):
+            assert call(fn, good, **changes) == B.REFLEX_EUNSUPPORTED
+            assert size(*({**good, **changes}[n] for n in ("rows", "vocab", "k"))) == 0
+        need = size(4, 50, 100)
+        assert 0 < need < size(4, 5000, 100)
+        for changes in (dict(workspace=None), dict(workspace=P + 64), dict(ws_bytes=need - 1)):
+            assert call(fn, good, **changes) == B.REFLEX_EWORKSPACE
