@@ -830,9 +830,6 @@ __device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32
 __device__ __forceinline__ uint32_t stage_addr(uint32_t stg, int row, int j) {
   return stg + static_cast<uint32_t>(row * 128 + ((j ^ (row & 7)) << 4));
 }
-__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
-  return pack_bf16(__uint_as_float(lo), __uint_as_float(hi));
-}
 // named barrier of `threads` threads; the second form returns whether v held
 // in every one of them
 __device__ __forceinline__ void group_sync(int id, int threads) {

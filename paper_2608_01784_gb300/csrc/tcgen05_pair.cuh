@@ -132,5 +132,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 h2 = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&h2);
 }
+__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
+  return pack_bf16(__uint_as_float(lo), __uint_as_float(hi));
+}
 
 }  // namespace rx
