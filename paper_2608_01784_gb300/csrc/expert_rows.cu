@@ -13,6 +13,7 @@
 // HBM once.  Unused slots contribute nothing, whatever their weights are; rows behind
 // the last pair are neither read nor written.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -185,39 +186,42 @@ __global__ void __launch_bounds__(kPlanThreads)
 
 // ---- copies and sums ---------------------------------------------------------
 constexpr int kThreads = 256;
-constexpr int VE = 8;         // columns of a lane
-constexpr int kSpan = 32 * VE;  // columns of a warp's turn
 
-// Columns c0 + 8 lane .. + 7 of a row, or, element by element, c0 + lane + 32 i.
-template <bool VEC>
-struct Span {
-  int d, c0, lane;
-  __device__ __forceinline__ int col(int i) const {
-    return VEC ? c0 + lane * VE + i : c0 + lane + 32 * i;
+// A lane's share of `kVecs` turns over a row, as stored: 16-byte vectors one warp apart,
+// or, where rows or columns do not allow it, elements.
+template <typename Te, bool VEC, int kVecs>
+struct Share {
+  static constexpr int kEach = VEC ? 16 / static_cast<int>(sizeof(Te)) : 1;
+  static constexpr int kSpan = 32 * kEach * kVecs;  // columns of a warp
+  static constexpr int kElems = kEach * kVecs;
+  // (as words: elements of two bytes by themselves would take a register each)
+  using Unit = std::conditional_t<VEC, uint4, Te>;
+  Unit u[kVecs];
+  static __device__ __forceinline__ int col(int c0, int i) {
+    return c0 + (i * 32 + static_cast<int>(threadIdx.x & 31)) * kEach;
   }
-  template <typename Te>
-  __device__ __forceinline__ void load(const Te* row, float* f) const {
-    if constexpr (VEC) {
-      if (col(0) < d) {
-        load8(row + col(0), f);
-        return;
-      }
+  __device__ __forceinline__ void load(const Te* row, int c0, int d) {
 #pragma unroll
-      for (int i = 0; i < VE; ++i) f[i] = 0.f;
+    for (int i = 0; i < kVecs; ++i)
+      if (col(c0, i) < d) u[i] = *reinterpret_cast<const Unit*>(row + col(c0, i));
+  }
+  // (elements past the row are not set)
+  __device__ __forceinline__ float at(int i, int e) const {
+    if constexpr (!VEC) {
+      return to_f32(u[i]);
     } else {
-#pragma unroll
-      for (int i = 0; i < VE; ++i) f[i] = col(i) < d ? to_f32(row[col(i)]) : 0.f;
+      const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+      if constexpr (sizeof(Te) == 4) return __uint_as_float(w[e]);
+      return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     }
   }
-  template <typename Te>
-  __device__ __forceinline__ void store(Te* row, const float* f) const {
-    if constexpr (VEC) {
-      if (col(0) < d) store8(row + col(0), f);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VE; ++i)
-        if (col(i) < d) row[col(i)] = from_f32<Te>(f[i]);
-    }
+  // unit i, kEach floats
+  static __device__ __forceinline__ void store(Te* row, int c0, int d, int i, const float* f) {
+    if (col(c0, i) >= d) return;
+    Te* to = row + col(c0, i);
+    if constexpr (!VEC) *to = from_f32<Te>(f[0]);
+    else if constexpr (sizeof(Te) == 2) store8(to, f);
+    else *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
   }
 };
 
@@ -274,15 +278,17 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-constexpr int kBatch = 4;  // pair rows whose loads are under way together
-
-// alpha == nullptr: weight 1.
+// A warp for a token and kCombineVecs turns of its columns, four pair rows under way
+// together.  alpha == nullptr: weight 1.
+constexpr int kCombineVecs = 2;
+constexpr int kBatch = 4;
 template <typename Te, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
     combine_rows_kernel(const Te* __restrict__ rows, int64_t ldr,
                         const int32_t* __restrict__ row_of, const float* __restrict__ alpha,
                         const Te* residual, int64_t ldres, int64_t T, int d, int k_max,
                         int cap_rows, Te* out, int64_t ldo, int segments) {
+  using S = Share<Te, VEC, kCombineVecs>;
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31;
@@ -291,103 +297,95 @@ __global__ void __launch_bounds__(kThreads)
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
        u < units; u += step) {
     const int64_t t = u / segments;
-    const Span<VEC> s{d, static_cast<int>(u - t * segments) * kSpan, lane};
-    float res[VE];
-    if (residual != nullptr) s.load(residual + t * ldres, res);
+    const int c0 = static_cast<int>(u - t * segments) * S::kSpan;
+    S res;
+    if (residual != nullptr) res.load(residual + t * ldres, c0, d);
     int row, slot;
+    float my_a = 1.f;
+    if (alpha != nullptr && lane < k_max) my_a = alpha[t * k_max + lane];
     const int n = used_slots(row_of, t, k_max, cap_rows, lane, row, slot);
-    float a = 1.f;
-    if (alpha != nullptr && lane < n) a = alpha[t * k_max + slot];
-    float acc[VE];
+    my_a = __shfl_sync(0xffffffffu, my_a, slot);
+    float acc[S::kElems];
 #pragma unroll
-    for (int i = 0; i < VE; ++i) acc[i] = 0.f;
+    for (int i = 0; i < S::kElems; ++i) acc[i] = 0.f;
     for (int j0 = 0; j0 < n; j0 += kBatch) {
-      float f[kBatch][VE];
+      S y[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int r = __shfl_sync(0xffffffffu, row, (j0 + b) & 31);
-        if (j0 + b < n) s.load(rows + r * ldr, f[b]);
+        if (j0 + b < n) y[b].load(rows + r * ldr, c0, d);
       }
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const float aj = __shfl_sync(0xffffffffu, a, (j0 + b) & 31);
+        const float a = __shfl_sync(0xffffffffu, my_a, (j0 + b) & 31);
         if (j0 + b < n)
 #pragma unroll
-          for (int i = 0; i < VE; ++i) acc[i] = __fmaf_rn(aj, f[b][i], acc[i]);
+          for (int i = 0; i < kCombineVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < S::kEach; ++e)
+              acc[i * S::kEach + e] = __fmaf_rn(a, y[b].at(i, e), acc[i * S::kEach + e]);
       }
     }
-    if (residual != nullptr)
 #pragma unroll
-      for (int i = 0; i < VE; ++i) acc[i] += res[i];
-    s.store(out + t * ldo, acc);
+    for (int i = 0; i < kCombineVecs; ++i) {
+      if (residual != nullptr)
+#pragma unroll
+        for (int e = 0; e < S::kEach; ++e) acc[i * S::kEach + e] += res.at(i, e);
+      S::store(out + t * ldo, c0, d, i, acc + i * S::kEach);
+    }
   }
 }
 
-// A warp per token and up to four of its used slots: Dout[t] is read by the warps of
-// a token one right after another, from HBM once.
+// A warp for a pair, its whole rows under way (up to 1024 columns of bf16 at a time);
+// the warps of a token run next to one another and read its gradient from L1 or L2.
+constexpr int kGradVecs = 4;
 template <typename Te, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
     combine_backward_kernel(const Te* __restrict__ d_out, int64_t ldd, const Te* rows, int64_t ldr,
                             const int32_t* __restrict__ row_of, const float* __restrict__ alpha,
                             int64_t T, int d, int k_max, int cap_rows, Te* d_rows, int64_t lddr,
-                            float* __restrict__ d_alpha, int batches) {
+                            float* __restrict__ d_alpha) {
+  using S = Share<Te, VEC, kGradVecs>;
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31;
-  const int64_t units = T * batches;
+  const int64_t pairs = T * k_max;
   const int64_t step = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-       u < units; u += step) {
-    const int64_t t = u / batches;
-    const int j0 = static_cast<int>(u - t * batches) * kBatch;
-    int row, slot;
-    const int n = used_slots(row_of, t, k_max, cap_rows, lane, row, slot);
-    if (j0 == 0 && d_alpha != nullptr && lane < k_max) {
-      const int r = row_of[t * k_max + lane];
-      if (r < 0 || r >= cap_rows) d_alpha[t * k_max + lane] = 0.f;
+       u < pairs; u += step) {
+    const int r = row_of[u];
+    if (r < 0 || r >= cap_rows) {
+      if (lane == 0 && d_alpha != nullptr) d_alpha[u] = 0.f;
+      continue;
     }
-    if (j0 >= n) continue;
-    const Te* y[kBatch];
-    Te* dy[kBatch];
-    float a[kBatch], dot[kBatch];
-    const float my_a = lane < n ? alpha[t * k_max + slot] : 0.f;
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const int64_t r = __shfl_sync(0xffffffffu, row, (j0 + b) & 31);
-      a[b] = __shfl_sync(0xffffffffu, my_a, (j0 + b) & 31);
-      y[b] = rows + r * ldr;
-      dy[b] = d_rows + r * lddr;
-      dot[b] = 0.f;
-    }
-    const Te* go = d_out + t * ldd;
-    for (int c0 = 0; c0 < d; c0 += kSpan) {
-      const Span<VEC> s{d, c0, lane};
-      float g[VE], f[kBatch][VE];
-      s.load(go, g);
+    const Te* go = d_out + u / k_max * ldd;
+    const Te* y = rows + r * ldr;
+    Te* dy = d_rows + r * lddr;
+    const float a = alpha[u];
+    float dot = 0.f;
+    for (int c0 = 0; c0 < d; c0 += S::kSpan) {
+      S g, f;
+      g.load(go, c0, d);
+      if (d_alpha != nullptr) f.load(y, c0, d);
       if (d_alpha != nullptr)
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b)
-          if (j0 + b < n) s.load(y[b], f[b]);
+        for (int i = 0; i < kGradVecs; ++i)
+          if (S::col(c0, i) < d)
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        if (j0 + b >= n) continue;
-        float o[VE];
+            for (int e = 0; e < S::kEach; ++e) dot = __fmaf_rn(g.at(i, e), f.at(i, e), dot);
+      if (d_rows != nullptr)
 #pragma unroll
-        for (int i = 0; i < VE; ++i) o[i] = a[b] * g[i];
-        if (d_rows != nullptr) s.store(dy[b], o);
-        if (d_alpha != nullptr)
+        for (int i = 0; i < kGradVecs; ++i) {
+          float o[S::kEach];
 #pragma unroll
-          for (int i = 0; i < VE; ++i) dot[b] = __fmaf_rn(g[i], f[b][i], dot[b]);
-      }
+          for (int e = 0; e < S::kEach; ++e) o[e] = a * g.at(i, e);
+          S::store(dy, c0, d, i, o);
+        }
     }
     if (d_alpha == nullptr) continue;
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot[b] += __shfl_xor_sync(0xffffffffu, dot[b], o);
-      const int sl = __shfl_sync(0xffffffffu, slot, (j0 + b) & 31);
-      if (lane == 0 && j0 + b < n) d_alpha[t * k_max + sl] = dot[b];
-    }
+    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if (lane == 0) d_alpha[u] = dot;
   }
 }
 
@@ -411,6 +409,7 @@ cudaError_t launch_rows(const ExpertRowsArgs& p, const void* x, int64_t ldx, voi
 
 template <typename Te, bool VEC>
 cudaError_t launch_combine_rows(const ExpertRowsArgs& p, int sms, cudaStream_t s) {
+  constexpr int kSpan = Share<Te, VEC, kCombineVecs>::kSpan;
   const int segments = (p.d + kSpan - 1) / kSpan;
   return launch_pdl(combine_rows_kernel<Te, VEC>, dim3(warps_grid(p.T * segments, sms)),
                     dim3(kThreads), 0, s, static_cast<const Te*>(p.rows), p.ldr, p.row_of, p.alpha,
@@ -420,11 +419,10 @@ cudaError_t launch_combine_rows(const ExpertRowsArgs& p, int sms, cudaStream_t s
 
 template <typename Te, bool VEC>
 cudaError_t launch_combine_backward(const ExpertRowsArgs& p, int sms, cudaStream_t s) {
-  const int batches = (p.k_max + kBatch - 1) / kBatch;
-  return launch_pdl(combine_backward_kernel<Te, VEC>, dim3(warps_grid(p.T * batches, sms)),
+  return launch_pdl(combine_backward_kernel<Te, VEC>, dim3(warps_grid(p.T * p.k_max, sms)),
                     dim3(kThreads), 0, s, static_cast<const Te*>(p.x), p.ldx,
                     static_cast<const Te*>(p.rows), p.ldr, p.row_of, p.alpha, p.T, p.d, p.k_max,
-                    p.cap_rows, static_cast<Te*>(p.out), p.ldo, p.d_alpha, batches);
+                    p.cap_rows, static_cast<Te*>(p.out), p.ldo, p.d_alpha);
 }
 
 // pairs of a warp and CTAs of the plan
@@ -483,7 +481,7 @@ cudaError_t launch_expert_rows(int dtype, const ExpertRowsArgs& p, int sms, cuda
 cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backward, int sms,
                                   cudaStream_t s) {
   const int es = dtype == 0 ? 4 : 2;
-  const bool vec = p.d % VE == 0 && on16(p.x, p.ldx, es) && on16(p.rows, p.ldr, es) &&
+  const bool vec = p.d % 8 == 0 && on16(p.x, p.ldx, es) && on16(p.rows, p.ldr, es) &&
                    on16(p.out, p.ldo, es);
   if (backward) {
     if (dtype == 0)

@@ -45,6 +45,11 @@ constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kStaging = 32 * 128;  // of an epilogue warp
 constexpr int kJobs = 4;            // tiles that are known ahead
+// Stages whose products the tensor cores add by themselves in a loss tile.  They cut
+// sums instead of rounding them, always downwards in magnitude: over the 2048 of a row
+// that put 2.4e-5 on logits of 20.  Sums of 256 are added in registers instead, to the
+// nearest: 8 times as many reads of TMEM, which the MMAs hide.
+constexpr int kLossChunk = 4;
 constexpr int kSmemBytes = kStages * kStageBytes + kEpiWarps * kStaging + 512 + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 constexpr uint64_t kWaitNs = 2000000000ull;
@@ -436,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------- MMAs ----------------
     int stage = 0;
     uint32_t phase = 0;
+    uint32_t acc_n = 0;
     bool ok = true, issued_any = false;
     for (uint32_t n = 0; ok; ++n) {
       int j;
@@ -449,35 +455,40 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
       // 16 along the reduction: 32 bytes of a row, or 16 rows of 128 bytes
       const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
-      const int ab = n & 1;
-      if (!mbar_wait(&acc_empty[ab], ((n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
-        ok = false;
-        break;
-      }
-      tc_fence_after();
-      const uint32_t d = tmem_base + static_cast<uint32_t>(ab * kTile);
-      for (int kb = t.kb0; kb < t.kb1; ++kb) {
-        if (!mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
+      int kb = t.kb0;
+      do {  // (once for a tile without a reduction)
+        const int ab = acc_n & 1, first = kb;
+        const int last = LOSS ? min(t.kb1, kb + kLossChunk) : t.kb1;
+        if (!mbar_wait(&acc_empty[ab], ((acc_n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
           break;
         }
+        ++acc_n;
         tc_fence_after();
-        const uint32_t a = smem_addr(sa + stage * kOperand), b = smem_addr(sb + stage * kOperand);
-        const uint64_t da = a_mn ? desc_mn(a) : desc_sw128(a);
-        const uint64_t db = b_mn ? desc_mn(b) : desc_sw128(b);
+        const uint32_t d = tmem_base + static_cast<uint32_t>(ab * kTile);
+        for (; kb < last; ++kb) {
+          if (!mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a = smem_addr(sa + stage * kOperand), b = smem_addr(sb + stage * kOperand);
+          const uint64_t da = a_mn ? desc_mn(a) : desc_sw128(a);
+          const uint64_t db = b_mn ? desc_mn(b) : desc_sw128(b);
 #pragma unroll
-        for (int u = 0; u < BK / 16; ++u)
-          mma_bf16_pair(d, da + u * a_step, db + u * b_step, idesc,
-                        (kb > t.kb0 || u > 0) ? 1u : 0u);
-        issued_any = true;
-        mma_commit_pair(smem_addr(&empty[stage]));
-        if (++stage == kStages) {
-          stage = 0;
-          phase ^= 1u;
+          for (int u = 0; u < BK / 16; ++u)
+            mma_bf16_pair(d, da + u * a_step, db + u * b_step, idesc,
+                          (kb > first || u > 0) ? 1u : 0u);
+          issued_any = true;
+          mma_commit_pair(smem_addr(&empty[stage]));
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
         }
-      }
-      if (!ok) break;
-      mma_commit_pair(smem_addr(&acc_full[ab]));
+        if (!ok) break;
+        mma_commit_pair(smem_addr(&acc_full[ab]));
+      } while (kb < t.kb1);
     }
     if (!ok) give_up(true);
     if (*abort_flag && issued_any) {
@@ -506,6 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_proxy_async_smem();
       __syncwarp();
     };
+    uint32_t acc_n = 0;
     for (uint32_t n = 0;; ++n) {
       int j = -1, ok = 1;
       if (lane == 0) ok = next_job(n, j) ? 1 : 0;
@@ -517,7 +529,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (j < 0) break;
       const Tile t = decode(p, counts, live, LOSS, j);
-      const int ab = n & 1;
       const int row = t.row0 + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
       const int warp_row = row - lane;
       const int col0 = t.col0 + half * 128;
@@ -530,19 +541,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           lse_c = p.row_lse[row] * kLog2e;
         }
       }
-      if (lane == 0) ok = mbar_wait(&acc_full[ab], (n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) {
+      uint32_t tm = 0, release = 0;
+      auto acc_ready = [&] {  // the next accumulator is complete
+        const int ab = acc_n & 1;
+        if (lane == 0)
+          ok = mbar_wait(&acc_full[ab], (acc_n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        ++acc_n;
+        tc_fence_after();
+        tm = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+             static_cast<uint32_t>(ab * kTile + half * 128);
+        release = map_to_rank(smem_addr(&acc_empty[ab]), 0);
+        return ok != 0;
+      };
+      if (!acc_ready()) {
         if (lane == 0) give_up(true);
         break;
       }
-      tc_fence_after();
-      const uint32_t tm = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
-                          static_cast<uint32_t>(ab * kTile + half * 128);
       auto hand_back = [&] {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_rank(smem_addr(&acc_empty[ab]), 0));
+        if (lane == 0) mbar_arrive_cluster_relaxed(release);
       };
       float z[32];
       auto load = [&](int c) {  // 32 columns from 32 c
@@ -554,23 +573,42 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (c == 3) hand_back();
       };
       if (LOSS) {
-        Stats st{-INFINITY, 0.f};
-#pragma unroll 1
+        float sum[4][32];
+#pragma unroll
         for (int c = 0; c < 4; ++c) {
           load(c);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sum[c][i] = z[i];
+        }
+        for (int kb = t.kb0 + kLossChunk; kb < t.kb1; kb += kLossChunk) {
+          if (!acc_ready()) break;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            load(c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum[c][i] += z[i];
+          }
+        }
+        if (!ok) {
+          if (lane == 0) give_up(true);
+          break;
+        }
+        Stats st{-INFINITY, 0.f};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
           const int v = col0 + 32 * c;
           if (v + 32 > p.vocab)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (v + i >= p.vocab) z[i] = -INFINITY;
+              if (v + i >= p.vocab) sum[c][i] = -INFINITY;
           const uint32_t at = static_cast<uint32_t>(target - v);
           if (at < 32u) {
-            float zt = z[0];
+            float zt = sum[c][0];
 #pragma unroll
-            for (int i = 1; i < 32; ++i) zt = at == static_cast<uint32_t>(i) ? z[i] : zt;
+            for (int i = 1; i < 32; ++i) zt = at == static_cast<uint32_t>(i) ? sum[c][i] : zt;
             p.z_target[row] = zt;
           }
-          if (v < p.vocab) add_chunk(st, z);
+          if (v < p.vocab) add_chunk(st, sum[c]);
         }
         p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
       } else if (t.kind == kGrad) {

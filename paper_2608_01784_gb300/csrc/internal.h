@@ -287,7 +287,8 @@ cudaError_t launch_sample(int dtype, const SampleArgs& p, int num_sms, cudaStrea
 // ---- norms around a block (block_norm.cu) -------------------------------------
 struct BlockNormArgs {
   int64_t rows;
-  int d, tpr;  // tpr: threads that share a row (set by the launcher)
+  int d;
+  int tpr, depth;  // set by the launcher: threads that share a row, rows of the ring
   float scale, eps;
   const void* h;
   int64_t ldh;
@@ -316,6 +317,7 @@ struct BlockNormArgs {
   float* partial;  // [3][block_norm_parts][d]: sums of the weights' gradients
 };
 int block_norm_max_width();
+// sums of a weight's gradient before they are added up, at most
 int64_t block_norm_parts(int64_t rows, int d, int sms);
 cudaError_t launch_block_norm(int dtype, const BlockNormArgs& p, bool backward, int sms,
                               cudaStream_t s);
