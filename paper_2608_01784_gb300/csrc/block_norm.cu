@@ -702,8 +702,8 @@ cudaError_t launch_norm(BlockNormArgs p, int sms, cudaStream_t s, int64_t* grid)
   if constexpr (BACK) kernel = norm_backward_kernel<Te, VEC, N, TPR, TGATE>;
   else kernel = norm_kernel<Te, VEC, N, TPR, TGATE>;
   if (smem > 32 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(
-        kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(kernel, kRingBytes, done);
     if (e != cudaSuccess) return e;
   }
   *grid = norm_grid(p.rows, p.tpr, per_sm, sms);

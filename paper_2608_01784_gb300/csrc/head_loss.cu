@@ -803,8 +803,8 @@ template <bool LOSS>
 cudaError_t launch_tiles(const Maps& maps, const HeadTiles& p, int64_t jobs, int sms,
                          cudaStream_t stream) {
   auto kernel = head_tiles_kernel<LOSS>;
-  cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(kernel, kSmemBytes, done);
   if (e != cudaSuccess) return e;
   const int64_t pairs = jobs < sms / 2 ? jobs : sms / 2;
   cudaLaunchConfig_t cfg = {};

@@ -8,9 +8,25 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace rx {
+
+// Lets a kernel have `bytes` of dynamic shared memory, asking the runtime once for each
+// device (`done`, a bit a device): the call takes longer than the checks of a launch.
+template <typename K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = uint64_t{1} << (dev & 63);
+  if (e != cudaSuccess || (done.load(std::memory_order_relaxed) & bit)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           static_cast<int>(bytes));
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 struct AllocArgs {
   int k_min, k_base, k_max, delta_role, delta_cur;

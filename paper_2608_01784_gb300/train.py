@@ -15,38 +15,46 @@ from .fp8 import _DTYPES, _matrix, _new, _status_word, _want
 
 def _here(device):
     """A launch goes to the current device; tensors of another one are refused."""
-    _want(device.index == torch.cuda.current_device(),
-          "the tensors are on another device than the current one")
+    if device.index != B.current_device():
+        raise ValueError("the tensors are on another device than the current one")
 
 
 def _like(t: torch.Tensor, x: torch.Tensor, what: str) -> int:
     """The row stride of t, which has x's shape, type and device."""
-    rows, cols, ld = _matrix(t, what, (x.dtype,))
-    _want((rows, cols) == tuple(x.shape) and t.device == x.device, f"{what}: shape or device")
-    return ld
+    if t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
+        raise ValueError(f"{what}: shape, type or device")
+    return x.shape[1] if t.is_contiguous() else _matrix(t, what, _DTYPES)[2]
+
+
+def _rows(t: torch.Tensor, rows: int, dtype, device, what: str):
+    if not (t.dtype is dtype and t.shape == (rows,) and t.is_contiguous() and t.device == device):
+        raise ValueError(f"{what}: {rows} contiguous values of {dtype}")
 
 
 def _vector(t: torch.Tensor | None, d: int, x: torch.Tensor, what: str):
-    _want(t is None or (t.dtype == x.dtype and t.device == x.device and tuple(t.shape) == (d,)
-                        and (d == 1 or t.stride(0) == 1)),
-          f"{what}: {d} contiguous values of the stream's type on its device")
+    if t is not None and not (t.dtype is x.dtype and t.shape == (d,) and t.is_contiguous()
+                              and t.device == x.device):
+        raise ValueError(f"{what}: {d} contiguous values of the stream's type on its device")
 
 
 def _norm_inputs(h, y, w_after, w_before, gate):
     """Checks them; (rows, d, ldh, ldy, ldg)."""
     rows, d, ldh = _matrix(h, "h", _DTYPES)
-    _want(d > 0, "h: at least one column")
+    if d < 1:
+        raise ValueError("h: at least one column")
     _here(h.device)
-    ldy = _like(y, h, "y") if y is not None else 0
+    if y is not None:
+        ldy = _like(y, h, "y")
+    elif w_after is not None or gate is not None:
+        raise ValueError("w_after and gate need y")
+    else:
+        ldy = 0
     _vector(w_after, d, h, "w_after")
     _vector(w_before, d, h, "w_before")
-    _want(y is not None or (w_after is None and gate is None), "w_after and gate need y")
-    ldg = 0
     if gate is not None and gate.dim() == 2:
-        ldg = _like(gate, h, "gate")
-    else:
-        _vector(gate, d, h, "gate")
-    return rows, d, ldh, ldy, ldg
+        return rows, d, ldh, ldy, _like(gate, h, "gate")
+    _vector(gate, d, h, "gate")
+    return rows, d, ldh, ldy, 0
 
 
 def block_norm(h: torch.Tensor, y: torch.Tensor | None = None, *,
@@ -58,13 +66,16 @@ def block_norm(h: torch.Tensor, y: torch.Tensor | None = None, *,
     y is not normalised, without y the stream is h itself, without w_before the
     second value is None.  `out` and `norm` may be h or y."""
     rows, d, ldh, ldy, ldg = _norm_inputs(h, y, w_after, w_before, gate)
-    _want(norm is None or w_before is not None, "norm needs w_before")
+    ldo = ldn = d
     if out is None:
         out = _new((rows, d), h.dtype, h.device, stream)
-    if norm is None and w_before is not None:
+    else:
+        ldo = _like(out, h, "out")
+    if norm is not None:
+        _want(w_before is not None, "norm needs w_before")
+        ldn = _like(norm, h, "norm")
+    elif w_before is not None:
         norm = _new((rows, d), h.dtype, h.device, stream)
-    ldo = _like(out, h, "out")
-    ldn = _like(norm, h, "norm") if norm is not None else 0
     B.reflex_block_norm(_DTYPES[h.dtype], h, ldh, y, ldy, w_after, gate, ldg, w_before, scale, eps,
                         rows, d, out, ldo, norm, ldn, stream)
     return out, norm
@@ -88,40 +99,59 @@ def block_norm_backward(h: torch.Tensor, y: torch.Tensor | None, d_out: torch.Te
 
     def new(like, *shape):
         return None if like is None else _new(shape, h.dtype, h.device, stream)
-    d_h = new(h, rows, d) if d_h is None else d_h
-    d_y = new(y, rows, d) if d_y is None else d_y
-    ld_d_h = _like(d_h, h, "d_h")
-    ld_d_y = _like(d_y, h, "d_y") if d_y is not None else 0
+    ld_d_h = _like(d_h, h, "d_h") if d_h is not None else d
+    ld_d_y = _like(d_y, h, "d_y") if d_y is not None else d
     got = dict(w_after=new(w_after, d), w_before=new(w_before, d),
-               gate=new(gate, rows, d) if ldg else new(gate, d), h=d_h, y=d_y)
+               gate=new(gate, rows, d) if ldg else new(gate, d),
+               h=new(h, rows, d) if d_h is None else d_h,
+               y=new(y, rows, d) if d_y is None else d_y)
     ws_bytes = B.reflex_block_norm_workspace_size(rows, d)
     _want(ws_bytes > 0, "unsupported width")
     ws = _new(ws_bytes, torch.uint8, h.device, stream)
     B.reflex_block_norm_backward(_DTYPES[h.dtype], h, ldh, y, ldy, w_after, gate, ldg, w_before,
-                                 scale, eps, rows, d, d_out, ld_d_out, d_norm, ld_d_norm, d_h,
-                                 ld_d_h, d_y, ld_d_y, got["gate"], d, got["w_after"],
-                                 got["w_before"], ws, ws_bytes, stream)
+                                 scale, eps, rows, d, d_out, ld_d_out, d_norm, ld_d_norm,
+                                 got["h"], ld_d_h, got["y"], ld_d_y, got["gate"], d,
+                                 got["w_after"], got["w_before"], ws, ws_bytes, stream)
     return got
 
 
 class ExpertPlan:
     """Where the pairs of a routing lie in expert order (reflex_expert_plan): row_of
     int32 [T, k_max], counts [E], offsets [E + 1], all on the device; the pairs' rows
-    are 0 .. offsets[E] - 1 of at most cap_rows."""
+    are 0 .. offsets[E] - 1 of at most cap_rows.  One allocation holds them all; the
+    tensors are views of it."""
 
     def __init__(self, T: int, E: int, k_max: int, cap_rows: int, device, stream=None):
-        def new(*shape):
-            return _new(shape, torch.int32, device, stream)
         self.T, self.E, self.k_max, self.cap_rows = T, E, k_max, cap_rows
-        self.row_of, self.counts, self.offsets = new(T, k_max), new(E), new(E + 1)
-        self.error = new(1)
         self.ws_bytes = B.reflex_expert_plan_workspace_size(T, E, k_max)
-        _want(self.ws_bytes > 0, "unsupported shape: E up to 1024, k_max up to 32")
-        self.ws = _new(self.ws_bytes, torch.uint8, device, stream)
+        if self.ws_bytes == 0:
+            raise ValueError("unsupported shape: E up to 1024, k_max up to 32")
+        # the workspace, then row_of, counts, offsets and the error word
+        self._at = at = self.ws_bytes // 4
+        self._words = _new(at + T * k_max + 2 * E + 2, torch.int32, device, stream)
+        self.device = device
+        self.ws = base = self._words.data_ptr()
+        self.row_of_ptr = base + 4 * at
+        self.counts_ptr = self.row_of_ptr + 4 * T * k_max
+        self.offsets_ptr = self.counts_ptr + 4 * E
+        self.error_ptr = self.offsets_ptr + 4 * (E + 1)
+
+    @property
+    def row_of(self) -> torch.Tensor:
+        return self._words.as_strided((self.T, self.k_max), (self.k_max, 1), self._at)
+
+    @property
+    def counts(self) -> torch.Tensor:
+        return self._words.as_strided((self.E,), (1,), self._at + self.T * self.k_max)
+
+    @property
+    def offsets(self) -> torch.Tensor:
+        return self._words.as_strided((self.E + 1,), (1,),
+                                      self._at + self.T * self.k_max + self.E)
 
     def status(self, stream=None) -> int:
         """What the last plan found wrong with its routing (waits)."""
-        return B.reflex_read_status(self.error, stream)
+        return B.reflex_read_status(self.error_ptr, stream)
 
 
 def expert_plan(ids: torch.Tensor, *, E: int, k: torch.Tensor | None = None,
@@ -130,59 +160,57 @@ def expert_plan(ids: torch.Tensor, *, E: int, k: torch.Tensor | None = None,
     """reflex_expert_plan of ids int32 [T, k_max]: slots j < k[t] are used, or, without
     k, those with ids >= 0.  `plan` (of the same T, E, k_max and cap_rows) is filled
     again instead of a new one; `perm` int32 [T * k_max] receives row -> t * k_max + j."""
-    _want(ids.is_cuda and ids.dim() == 2 and ids.dtype == torch.int32 and ids.is_contiguous(),
-          "ids: a contiguous CUDA matrix of torch.int32")
-    _here(ids.device)
+    if not (ids.is_cuda and ids.dim() == 2 and ids.dtype is torch.int32 and ids.is_contiguous()):
+        raise ValueError("ids: a contiguous CUDA matrix of torch.int32")
+    dev = ids.device
+    _here(dev)
     T, k_max = ids.shape
     for t, n, what in ((k, T, "k"), (perm, T * k_max, "perm")):
-        _want(t is None or (t.dtype == torch.int32 and tuple(t.shape) == (n,)
-                            and t.is_contiguous() and t.device == ids.device),
-              f"{what}: {n} contiguous values of torch.int32 on the device of ids")
+        if t is not None:
+            _rows(t, n, torch.int32, dev, what)
     if plan is None:
-        plan = ExpertPlan(T, E, k_max, T * k_max if cap_rows is None else cap_rows, ids.device,
-                          stream)
-    _want((plan.T, plan.E, plan.k_max) == (T, E, k_max) and plan.row_of.device == ids.device
-          and cap_rows in (None, plan.cap_rows), "plan: made for another shape or device")
-    B.reflex_expert_plan(ids, k, T, E, k_max, plan.cap_rows, plan.row_of, plan.counts,
-                         plan.offsets, perm, plan.error, plan.ws, plan.ws_bytes, stream)
+        plan = ExpertPlan(T, E, k_max, T * k_max if cap_rows is None else cap_rows, dev, stream)
+    else:
+        _want((plan.T, plan.E, plan.k_max) == (T, E, k_max) and plan.device == dev
+              and cap_rows in (None, plan.cap_rows), "plan: made for another shape or device")
+    B.reflex_expert_plan(ids, k, T, E, k_max, plan.cap_rows, plan.row_of_ptr, plan.counts_ptr,
+                         plan.offsets_ptr, perm, plan.error_ptr, plan.ws, plan.ws_bytes, stream)
     return plan
 
 
 def _pair_rows(rows: torch.Tensor, plan: ExpertPlan, what: str):
     """(d, row stride) of the pairs' rows of a plan."""
     n, d, ld = _matrix(rows, what, _DTYPES)
-    _want(n >= plan.cap_rows and rows.device == plan.row_of.device,
-          f"{what}: fewer rows than the plan's cap_rows, or another device")
-    _want(d > 0, f"{what}: at least one column")
-    _here(rows.device)
+    if n < plan.cap_rows or d < 1 or rows.device != plan.device:
+        raise ValueError(f"{what}: fewer rows than the plan's cap_rows, no columns, or another "
+                         "device")
+    _here(plan.device)
     return d, ld
 
 
 def _tokens(x: torch.Tensor, plan: ExpertPlan, d: int, dtype, what: str) -> int:
     rows, cols, ld = _matrix(x, what, (dtype,))
-    _want((rows, cols) == (plan.T, d) and x.device == plan.row_of.device,
-          f"{what}: a row for each of the plan's tokens, of the rows' width and device")
+    if (rows, cols) != (plan.T, d) or x.device != plan.device:
+        raise ValueError(f"{what}: a row for each of the plan's tokens, of the rows' width and "
+                         "device")
     return ld
 
 
 def _weights(alpha: torch.Tensor, plan: ExpertPlan, what: str):
-    _want(alpha.dtype == torch.float32 and tuple(alpha.shape) == (plan.T, plan.k_max)
-          and alpha.is_contiguous() and alpha.device == plan.row_of.device,
-          f"{what}: a contiguous tensor of torch.float32 of the plan's [T, k_max]")
+    if not (alpha.dtype is torch.float32 and alpha.shape == (plan.T, plan.k_max)
+            and alpha.is_contiguous() and alpha.device == plan.device):
+        raise ValueError(f"{what}: a contiguous tensor of torch.float32 of the plan's [T, k_max]")
 
 
 def expert_rows(x: torch.Tensor, plan: ExpertPlan, *, rows: torch.Tensor | None = None,
                 stream=None) -> torch.Tensor:
     """reflex_expert_rows: x [T, d] (fp32 or bf16) laid out by expert, [cap_rows, d].
     `rows` behind the last pair are left as they are; of a new tensor they are not set."""
-    _, d, ldx = _matrix(x, "x", _DTYPES)
-    _want(d > 0, "x: at least one column")
     if rows is None:
-        rows = _new((plan.cap_rows, d), x.dtype, x.device, stream)
-    dr, ldr = _pair_rows(rows, plan, "rows")
-    _want(dr == d, "rows: another width than x")
-    _tokens(x, plan, d, rows.dtype, "x")
-    B.reflex_expert_rows(_DTYPES[x.dtype], x, ldx, plan.row_of, plan.T, d, plan.k_max,
+        rows = _new((plan.cap_rows, x.shape[-1]), x.dtype, x.device, stream)
+    d, ldr = _pair_rows(rows, plan, "rows")
+    ldx = _tokens(x, plan, d, rows.dtype, "x")
+    B.reflex_expert_rows(_DTYPES[x.dtype], x, ldx, plan.row_of_ptr, plan.T, d, plan.k_max,
                          plan.cap_rows, rows, ldr, stream)
     return rows
 
@@ -193,7 +221,7 @@ def _sum(rows, alpha, plan, residual, out, stream):
     if out is None:
         out = _new((plan.T, d), rows.dtype, rows.device, stream)
     ldo = _tokens(out, plan, d, rows.dtype, "out")
-    B.reflex_expert_combine(_DTYPES[rows.dtype], rows, ldr, alpha, plan.row_of, residual, ldres,
+    B.reflex_expert_combine(_DTYPES[rows.dtype], rows, ldr, alpha, plan.row_of_ptr, residual, ldres,
                             plan.T, d, plan.k_max, plan.cap_rows, out, ldo, stream)
     return out
 
@@ -229,7 +257,7 @@ def expert_combine_backward(d_out: torch.Tensor, rows: torch.Tensor, alpha: torc
     _want(dd == d and d_rows.dtype == rows.dtype, "d_rows: another width or type than rows")
     _weights(d_alpha, plan, "d_alpha")
     B.reflex_expert_combine_backward(_DTYPES[rows.dtype], d_out, ldd, rows, ldr, alpha,
-                                     plan.row_of, plan.T, d, plan.k_max, plan.cap_rows, d_rows,
+                                     plan.row_of_ptr, plan.T, d, plan.k_max, plan.cap_rows, d_rows,
                                      lddr, d_alpha, stream)
     return d_rows, d_alpha
 
@@ -241,21 +269,20 @@ def _head(hidden, weight, targets, status):
     """Checks them; (rows, vocab, k, ld_hidden, ldw)."""
     rows, k, ld_hidden = _matrix(hidden, "hidden", _BF16)
     vocab, kw, ldw = _matrix(weight, "weight", _BF16)
-    _want(k > 0 and vocab > 0 and kw == k, "hidden and weight disagree on their columns")
+    if k < 1 or vocab < 1 or kw != k:
+        raise ValueError("hidden and weight disagree on their columns, or have none")
     if vocab == 1:
         ldw = -(-k // 8) * 8
-    _want(ldw % 8 == 0 and weight.data_ptr() % 16 == 0,
-          "weight: rows start on 16-byte boundaries")
-    _want(hidden.device == weight.device, "tensors on several devices")
-    _here(hidden.device)
-    _rows(targets, rows, torch.int32, hidden.device, "targets")
-    _status_word(status, hidden.device)
+    if ldw % 8 or weight.data_ptr() % 16:
+        raise ValueError("weight: rows start on 16-byte boundaries")
+    dev = hidden.device
+    if dev != weight.device:
+        raise ValueError("tensors on several devices")
+    _here(dev)
+    _rows(targets, rows, torch.int32, dev, "targets")
+    if status is not None:
+        _status_word(status, dev)
     return rows, vocab, k, ld_hidden, ldw
-
-
-def _rows(t: torch.Tensor, rows: int, dtype, device, what: str):
-    _want(t.dtype == dtype and tuple(t.shape) == (rows,) and t.is_contiguous()
-          and t.device == device, f"{what}: {rows} contiguous values of {dtype}")
 
 
 def head_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
@@ -265,15 +292,18 @@ def head_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
     targets int32 [rows], zeros where a target is negative.  hidden [rows, k] and weight
     [vocab, k] are bf16; the logits are not kept."""
     rows, vocab, k, ld_hidden, ldw = _head(hidden, weight, targets, status)
+    dev = hidden.device
     if loss is None:
-        loss = _new(rows, torch.float32, hidden.device, stream)
+        loss = _new(rows, torch.float32, dev, stream)
+    else:
+        _rows(loss, rows, torch.float32, dev, "loss")
     if lse is None:
-        lse = _new(rows, torch.float32, hidden.device, stream)
-    _rows(loss, rows, torch.float32, hidden.device, "loss")
-    _rows(lse, rows, torch.float32, hidden.device, "lse")
+        lse = _new(rows, torch.float32, dev, stream)
+    else:
+        _rows(lse, rows, torch.float32, dev, "lse")
     ws_bytes = B.reflex_head_loss_workspace_size(rows, vocab, k)
     _want(ws_bytes > 0, "unsupported sizes")
-    ws = _new(ws_bytes, torch.uint8, hidden.device, stream)
+    ws = _new(ws_bytes, torch.uint8, dev, stream)
     B.reflex_head_loss(hidden, ld_hidden, weight, ldw, targets, rows, vocab, k, loss, lse, status,
                        ws, ws_bytes, stream)
     return loss, lse
