@@ -678,8 +678,8 @@ int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_
  *             supported), 256-B aligned.
  * Any sizes up to 2^24 rows, 2^24 columns of the vocabulary and k = 2^20 (above:
  * REFLEX_EUNSUPPORTED).  A row's results have the same bits on every run, whatever
- * the other rows are.  Logits are finite; a row with one that is not has a loss that is
- * not, and no influence on others.
+ * the other rows are; up to 64 rows are summed in another order than more.  A row with
+ * a logit that is not finite has no influence on others.
  */
 size_t reflex_head_loss_workspace_size(int32_t rows, int32_t vocab, int32_t k);
 int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,

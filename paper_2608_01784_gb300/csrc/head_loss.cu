@@ -103,6 +103,16 @@ __global__ void __launch_bounds__(kRowsThreads)
   const int64_t per = (p.rows + gridDim.x - 1) / gridDim.x;
   const int64_t lo = min(p.rows, blockIdx.x * per), hi = min(p.rows, lo + per);
   int before = 0, total = 0, wrong = 0;
+  // a CTA's only row is on its way while it counts those in front
+  constexpr int kAhead = 2;  // vectors of a thread
+  const bool ahead = per == 1 && vec && p.k <= kAhead * kRowsThreads * 8;
+  uint4 row[kAhead];
+  if (ahead && lo < hi && p.targets[lo] >= 0)
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int c = (i * kRowsThreads + tid) * 8;
+      if (c < p.k) row[i] = *reinterpret_cast<const uint4*>(p.hidden + lo * p.ld_hidden + c);
+    }
 #pragma unroll 4
   for (int64_t r = tid; r < p.rows; r += kRowsThreads) {
     const int t = p.targets[r];
@@ -175,12 +185,22 @@ __global__ void __launch_bounds__(kRowsThreads)
       }
     }
     __syncthreads();
+    if (ahead) {
+      if (s_at[0] >= 0)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int c = (i * kRowsThreads + tid) * 8;
+          if (c < p.k)
+            *reinterpret_cast<uint4*>(p.packed + s_at[0] * p.ld_packed + c) = row[i];
+        }
+      break;
+    }
     const int n = static_cast<int>(min(static_cast<int64_t>(kRowsThreads), hi - r0));
     for (int i = w; i < n; i += kRowsThreads / 32)
       if (s_at[i] >= 0) copy_row(s_at[i], p.hidden + (r0 + i) * p.ld_hidden);
   }
   // rows of zeros up to whole tiles
-  const int64_t most = (total + kTile - 1) / kTile * kTile;
+  const int64_t most = static_cast<int64_t>(total + p.tile - 1) / p.tile * p.tile;
   for (int64_t i = total + static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + w; i < most;
        i += static_cast<int64_t>(gridDim.x) * (kRowsThreads / 32)) {
     copy_row(i, nullptr);
@@ -731,6 +751,319 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// ---- few rows -------------------------------------------------------------------
+// Up to NT (32 or 64) rows: W is what costs, so its rows are the tiles, up to 128 at a
+// time by single CTAs (M = 128, N = NT; as many as give every CTA the same number of
+// tiles), and stream through a ring of nine or ten stages at HBM's rate.  A thread has one row of W and NT logits.  Loss: it keeps a maximum and a
+// sum for each of its columns over all of its tiles; the threads' are joined when the
+// tiles are done, the CTAs' by the last of them, both in a fixed order.  Gradient: G
+// of the whole vocabulary, 64 bytes of a row by a warp.
+// 32 x 65536 x 2048: FIGURES
+constexpr int kFewThreads = 192;  // TMA, MMA and four epilogue warps
+template <int NT>
+struct Few {
+  static constexpr int kWBytes = kHalf * 128;
+  static constexpr int kStageBytes = kWBytes + NT * 128;
+  static constexpr int kStages = NT == 32 ? 10 : 9;
+  static constexpr int kMisc = 512 + 3 * NT * 4;
+  static constexpr int kSmem = kStages * kStageBytes + kMisc + 1024;
+  static constexpr int kTmem = 2 * NT;
+  static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
+  static_assert(kHalf * NT * 8 <= kStages * kStageBytes, "the threads' sums go into the ring");
+};
+
+template <int NT, bool GRAD>
+__global__ void __launch_bounds__(kFewThreads, 1)
+    head_few_kernel(const __grid_constant__ CUtensorMap map_w,
+                    const __grid_constant__ CUtensorMap map_h, const HeadTiles p, int tile_rows,
+                    __nv_bfloat16* g_out, int64_t ld_g, float* loss, float* lse) {
+  using F = Few<NT>;
+  constexpr int kRing = F::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kRing * F::kStageBytes);
+  uint64_t* full = bars;
+  uint64_t* empty = full + kRing;
+  uint64_t* acc_full = empty + kRing;
+  uint64_t* acc_empty = acc_full + 2;
+  uint64_t* drain = acc_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* s_last = reinterpret_cast<int*>(tmem_slot + 2);
+  static_assert((2 * kRing + 5) * 8 + 12 <= 512, "barriers");
+  int* s_target = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(bars) + 512);
+  float* s_lse = reinterpret_cast<float*>(s_target + NT);
+  float* s_grad = s_lse + NT;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ntiles = (p.vocab + tile_rows - 1) / tile_rows;
+  const uint32_t w_bytes = tile_rows * 128;
+  const int nk = (p.k + BK - 1) / BK;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kRing; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], 4);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_map(&map_w);
+    prefetch_map(&map_h);
+  }
+  __syncwarp();
+  auto load_w = [&](int t, int kb, int s) {
+    tma_load_2d(smem_addr(smem + s * F::kStageBytes), &map_w, kb * BK, t * tile_rows,
+                smem_addr(&full[s]));
+  };
+  // The ring's first weights while the rows are still being packed: the kernel in front
+  // (head_rows_kernel) waited for all before it when it let this one start, and writes
+  // none of W.
+  int early = 0;
+  if (warp == 0 && lane == 0) {
+    early = min(nk, kRing);  // (of the first tile)
+    for (int s = 0; s < early; ++s) {
+      mbar_expect_tx_only(smem_addr(&full[s]), w_bytes);
+      load_w(blockIdx.x, s, s);
+    }
+  }
+  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), F::kTmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+  for (int i = threadIdx.x; i < NT; i += kFewThreads) {
+    s_target[i] = p.target[i];  // (rows up to whole tiles have one)
+    if (GRAD) {
+      s_lse[i] = p.row_lse[i] * kLog2e;
+      s_grad[i] = p.row_grad[i];
+    }
+  }
+  __syncthreads();
+  auto give_up = [&] {
+    if (!*abort_flag) set_err(p.err, kErrTimeout);
+    *abort_flag = 1;
+  };
+
+  if (warp == 0 && lane == 0) {
+    // ---------------- TMA loads ----------------
+    int stage = 0;
+    uint32_t phase = 0, issued_mask = 0, issued_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+      for (int kb = 0; kb < nk; ++kb) {
+        if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
+          ok = false;
+          break;
+        }
+        const bool ahead = early > 0;
+        mbar_expect_tx(smem_addr(&full[stage]), NT * 128 + (ahead ? 0u : w_bytes));
+        if (ahead) --early;
+        else load_w(t, kb, stage);
+        tma_load_2d(smem_addr(smem + stage * F::kStageBytes + F::kWBytes), &map_h, kb * BK, 0,
+                    smem_addr(&full[stage]));
+        issued_mask |= 1u << stage;
+        issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+        if (++stage == kRing) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    if (!ok) give_up();
+    if (*abort_flag) {
+      for (int i = 0; i < early; ++i) {  // the arrivals that are missing
+        mbar_arrive1(smem_addr(&full[stage + i]));
+        mbar_wait(&full[stage + i], 0, nullptr, kDrainNs);
+      }
+      for (int s = 0; s < kRing; ++s)
+        if (issued_mask & (1u << s))
+          mbar_wait(&full[s], (issued_phase >> s) & 1u, nullptr, kDrainNs);
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---------------- MMAs ----------------
+    constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) |
+                               (static_cast<uint32_t>(NT >> 3) << 17) |
+                               (static_cast<uint32_t>(kHalf >> 4) << 24);
+    int stage = 0;
+    uint32_t phase = 0, acc_n = 0;
+    bool ok = true, issued_any = false;
+    for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+      for (int kb = 0; kb < nk && ok;) {
+        const int ab = acc_n & 1, first = kb;
+        const int last = GRAD ? nk : min(nk, kb + kLossChunk);
+        if (!mbar_wait(&acc_empty[ab], ((acc_n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
+          ok = false;
+          break;
+        }
+        ++acc_n;
+        tc_fence_after();
+        const uint32_t d = tmem_base + static_cast<uint32_t>(ab * NT);
+        for (; kb < last; ++kb) {
+          if (!mbar_wait(&full[stage], phase, abort_flag, kWaitNs)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a = smem_addr(smem + stage * F::kStageBytes);
+          const uint64_t da = desc_sw128(a), db = desc_sw128(a + F::kWBytes);
+#pragma unroll
+          for (int u = 0; u < BK / 16; ++u) {
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "setp.ne.b32 p, %4, 0;\n\t"
+                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+                "l"(da + 2 * u), "l"(db + 2 * u), "r"(idesc),
+                "r"(kb > first || u > 0 ? 1u : 0u)
+                : "memory");
+          }
+          issued_any = true;
+          mma_commit(smem_addr(&empty[stage]));
+          if (++stage == kRing) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok) mma_commit(smem_addr(&acc_full[ab]));
+      }
+    }
+    if (!ok) give_up();
+    if (*abort_flag && issued_any) {
+      mma_commit(smem_addr(drain));
+      mbar_wait(drain, 0, nullptr, kDrainNs);
+    }
+  } else if (warp >= 2) {
+    // ---------------- epilogue: a row of W each ----------------
+    const int quarter = warp & 3, row = quarter * 32 + lane;
+    float m[GRAD ? 1 : NT], sum[GRAD ? 1 : NT];
+    if (!GRAD)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        m[j] = -INFINITY;
+        sum[j] = 0.f;
+      }
+    uint32_t acc_n = 0;
+    int ok = 1;
+    for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+      float z[NT];
+      for (int kb = 0; kb < nk; kb += GRAD ? nk : kLossChunk) {
+        const int ab = acc_n & 1;
+        if (lane == 0)
+          ok = mbar_wait(&acc_full[ab], (acc_n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        ++acc_n;
+        tc_fence_after();
+        const uint32_t tm = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                            static_cast<uint32_t>(ab * NT);
+#pragma unroll
+        for (int c = 0; c < NT / 32; ++c) {
+          uint32_t r[32];
+          tmem_ld32(tm + 32 * c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            z[32 * c + i] = (kb > 0 ? z[32 * c + i] : 0.f) + __uint_as_float(r[i]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(smem_addr(&acc_empty[ab]));
+      }
+      if (!ok) {
+        if (lane == 0) give_up();
+        break;
+      }
+      const int v = t * tile_rows + row;
+      const bool mine = row < tile_rows && v < p.vocab;  // (else it is not W's)
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          float x = exp2_fast(__fmaf_rn(z[j], kLog2e, -s_lse[j]));
+          x = s_target[j] == v ? x - 1.f : x;
+          if (mine) g_out[j * ld_g + v] = __float2bfloat16_rn(s_grad[j] * x);
+        }
+      } else if (mine) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if (s_target[j] == v) p.z_target[j] = z[j];
+          // the larger one is the new maximum
+          const float d = z[j] - m[j], e = exp2_fast(-fabsf(d) * kLog2e);
+          sum[j] = d > 0.f ? __fmaf_rn(sum[j], e, 1.f) : sum[j] + e;
+          m[j] = fmaxf(m[j], z[j]);
+        }
+      }
+    }
+    if (GRAD && blockIdx.x == 0)  // zeros up to whole tiles of the products that take G
+      for (int v = p.vocab + row; v < (p.vocab + kTile - 1) / kTile * kTile; v += kHalf)
+        for (int j = 0; j < NT; ++j) g_out[j * ld_g + v] = __float2bfloat16_rn(0.f);
+    if constexpr (!GRAD) {
+      // (all MMAs have read the ring: the last accumulator came after them)
+      float2* part = reinterpret_cast<float2*>(smem);  // [NT][128]
+      if (ok)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[j * kHalf + (row ^ j)] = make_float2(m[j], sum[j]);
+    }
+  }
+  __syncthreads();
+  if constexpr (!GRAD) {
+    auto merge = [](float2 a, float2 b) {
+      const float mm = fmaxf(a.x, b.x), ref = safe_max(mm);
+      return make_float2(mm, a.y * exp2_fast((a.x - ref) * kLog2e) +
+                                 b.y * exp2_fast((b.x - ref) * kLog2e));
+    };
+    if (!*abort_flag) {
+      // 128 threads' sums of a column by 128 / NT threads, then by lanes
+      const float2* part = reinterpret_cast<const float2*>(smem);
+      constexpr int kShare = 128 / NT;
+      if (threadIdx.x < 128) {
+        const int j = threadIdx.x / kShare, g = threadIdx.x % kShare;
+        float2 st = make_float2(-INFINITY, 0.f);
+        for (int i = 0; i < NT; ++i) st = merge(st, part[j * kHalf + ((g * NT + i) ^ j)]);
+#pragma unroll
+        for (int o = kShare / 2; o > 0; o >>= 1)
+          st = merge(st, make_float2(__shfl_down_sync(0xffffffffu, st.x, o),
+                                     __shfl_down_sync(0xffffffffu, st.y, o)));
+        if (g == 0) p.stats[blockIdx.x * NT + j] = st;
+      }
+    }
+    // the last CTA joins them all
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *s_last = atomicAdd(p.queue, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (*s_last && threadIdx.x < 128) {
+      __threadfence();
+      constexpr int kShare = 128 / NT;
+      const int live = min(max(*p.live, 0), p.rows);
+      const int j = threadIdx.x / kShare, g = threadIdx.x % kShare;
+      float2 st = make_float2(-INFINITY, 0.f);
+#pragma unroll 8
+      for (unsigned c = g; c < gridDim.x; c += kShare) st = merge(st, __ldcg(p.stats + c * NT + j));
+#pragma unroll
+      for (int o = kShare / 2; o > 0; o >>= 1)
+        st = merge(st, make_float2(__shfl_down_sync(0xffffffffu, st.x, o),
+                                   __shfl_down_sync(0xffffffffu, st.y, o)));
+      if (g == 0 && j < live) {
+        const float ln = logf(st.y), mm = safe_max(st.x);
+        const int r = p.row[j];
+        lse[r] = mm + ln;
+        loss[r] = (mm - __ldcg(p.z_target + j)) + ln;
+      }
+    }
+  }
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem_base, F::kTmem);
+  }
+}
+
 // ---- ends ---------------------------------------------------------------------
 // The maxima and sums of a row's slices to its lse and loss: 32 rows x 32 groups of
 // slices a CTA.
@@ -846,18 +1179,42 @@ cudaError_t launch_tiles(const Maps& maps, const HeadTiles& p, int64_t jobs, int
   return cudaLaunchKernelEx(&cfg, kernel, maps, p);
 }
 
+template <int NT, bool GRAD>
+cudaError_t launch_few(const HeadProblem& h, const HeadTiles& p, void* g, int64_t ld_g,
+                       float* loss, float* lse, int sms, cudaStream_t stream) {
+  // rows of a tile: what the CTAs' rounds of 128 leave shared out evenly
+  const int rounds = (p.vocab + sms * kHalf - 1) / (sms * kHalf);
+  const int tile_rows = (p.vocab + sms * rounds - 1) / (sms * rounds);
+  CUtensorMap map_w, map_h;
+  if (!box_map(&map_w, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, tile_rows) ||
+      !box_map(&map_h, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, NT))
+    return cudaErrorInvalidValue;
+  auto kernel = head_few_kernel<NT, GRAD>;
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(kernel, Few<NT>::kSmem, done);
+  if (e != cudaSuccess) return e;
+  const int tiles = (p.vocab + tile_rows - 1) / tile_rows;
+  return launch_pdl(kernel, dim3(tiles < sms ? tiles : sms), dim3(kFewThreads), Few<NT>::kSmem,
+                    stream, map_w, map_h, p, tile_rows, static_cast<__nv_bfloat16*>(g), ld_g,
+                    loss, lse);
+}
+
 }  // namespace
 
 cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream) {
   const bool vec = p.k % 8 == 0 && reinterpret_cast<uintptr_t>(p.hidden) % 16 == 0 &&
                    p.ld_hidden % 8 == 0;
-  const int64_t ctas = p.rows < 2 * sms ? p.rows : 2 * sms;
+  // (with rows of zeros to write, a few CTAs more than rows)
+  const int64_t ctas = p.rows > 2 * sms ? 2 * sms : p.rows > 32 ? p.rows : 32;
   return launch_pdl(head_rows_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kRowsThreads), 0,
                     stream, p, vec);
 }
 
 cudaError_t launch_head_loss(const HeadProblem& h, HeadTiles p, float* loss, float* lse, int sms,
                              cudaStream_t stream) {
+  if (head_few_rows(p.rows, 1))
+    return p.rows <= 32 ? launch_few<32, false>(h, p, nullptr, 0, loss, lse, sms, stream)
+                        : launch_few<64, false>(h, p, nullptr, 0, loss, lse, sms, stream);
   Maps maps;
   if (!box_map(&maps.h_rows, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, kHalf) ||
       !box_map(&maps.w_rows, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, kHalf))
@@ -916,6 +1273,12 @@ cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const H
     p.parts = q.sums != nullptr ? (blocks + q.part_blocks - 1) / q.part_blocks : 0;
     p.hidden_first = q.sums != nullptr && p.part_blocks * BK >= p.rows;
     p.queue = queue + i;
+    if (i == 0 && head_few_rows(p.rows, pieces)) {
+      // (64 rows: a whole stage of the products that take G)
+      const cudaError_t e = launch_few<64, true>(h, p, g_next, ld_g, nullptr, nullptr, sms, stream);
+      if (e != cudaSuccess) return e;
+      continue;
+    }
     const int64_t jobs = mt * next + mt * p.kt * p.parts + (p.dw != nullptr ? now * p.kt : 0);
     if (jobs == 0) continue;
     const cudaError_t e = launch_tiles<false>(maps, p, jobs, sms, stream);

@@ -364,6 +364,7 @@ cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backw
 
 // ---- loss of a vocabulary head (head_loss.cu) --------------------------------------
 constexpr int kHeadTile = 256;  // rows and columns of a tile of any of its products
+constexpr int kHeadFewRows = 64;  // as many rows or fewer go past W, not W past them
 constexpr int kHeadGroup = 32;  // tiles of rows that stay in L2 while the weights pass by
 
 // The rows with a target in [0, vocab) to the front, zeros behind them up to whole
@@ -371,6 +372,7 @@ constexpr int kHeadGroup = 32;  // tiles of rows that stay in L2 while the weigh
 struct HeadRows {
   int64_t rows;
   int vocab, k;
+  int tile;  // rows of a whole tile
   const int32_t* targets;
   const __nv_bfloat16* hidden;
   int64_t ld_hidden;
@@ -391,6 +393,8 @@ struct HeadRows {
   uint32_t* err;  // nullable
 };
 cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream);
+// Whether W goes past the rows, for a vocabulary in `pieces`.
+inline bool head_few_rows(int64_t rows, int pieces) { return rows <= kHeadFewRows && pieces == 1; }
 
 struct HeadProblem {
   PFN_cuTensorMapEncodeTiled_v12000 encode;

@@ -87,7 +87,7 @@ struct HeadLayout {
   size_t row_lse, row_grad, place, g, sums;                  // backward
   size_t total;
   int64_t rows_up, ld_packed, ld_sums;
-  int n_queue, piece_tiles, part_blocks, parts;
+  int n_queue, piece_tiles, pieces, part_blocks, parts;
 };
 struct Carve {
   size_t at = 0;
@@ -102,14 +102,15 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t k, bool backward) {
   L.rows_up = tiles(rows) * kHeadTile;
   L.ld_packed = (k + 7) / 8 * 8;
   L.ld_sums = (k + 31) / 32 * 32;
-  L.n_queue = 1;
+  L.n_queue = L.pieces = 1;
   const int64_t vt = tiles(vocab);
   if (backward) {
     // pieces of G of some 128 MB: what is written for the next products is mostly still
     // in L2 when they read it
     const int64_t most = std::max<int64_t>(1, (int64_t{128} << 20) / (L.rows_up * kHeadTile * 2));
     L.piece_tiles = static_cast<int>(std::min(most, vt));
-    L.n_queue = static_cast<int>(tiles(vocab) / L.piece_tiles) + 2;
+    L.pieces = static_cast<int>((vt + L.piece_tiles - 1) / L.piece_tiles);
+    L.n_queue = L.pieces + 1;
     // parts of Dh: enough tiles for all pairs of SMs, so that none is long for the launch
     const int64_t mt = tiles(rows), kt = tiles(k), blocks = L.piece_tiles * (kHeadTile / 64);
     const int64_t want = std::min<int64_t>((100 + mt * kt - 1) / std::max<int64_t>(1, mt * kt), 64);
@@ -158,6 +159,8 @@ rx::HeadRows head_rows(const HeadLayout& L, void* ws, const void* hidden, int64_
   r.queue = at<uint32_t>(ws, L.queue);
   r.n_queue = L.n_queue;
   r.err = reinterpret_cast<uint32_t*>(dev_status);
+  // (the products of a few rows take 64 at a time)
+  r.tile = rx::head_few_rows(rows, L.pieces) ? rx::kHeadFewRows : kHeadTile;
   return r;
 }
 rx::HeadTiles head_tiles(const HeadLayout& L, const rx::HeadRows& r) {

@@ -89,7 +89,8 @@ def run(h, w, t, grad, **kw):
 
 SHAPES = [(1, 1, 1), (1, 2, 1), (2, 5, 8), (3, 300, 17), (32, 1000, 64), (33, 257, 65),
           (128, 256, 128), (129, 511, 256), (255, 1025, 250), (256, 2048, 512), (257, 4099, 130),
-          (600, 3001, 320), (1000, 700, 2048), (5, 20000, 96), (2000, 1, 40), (31, 1500, 5000)]
+          (600, 3001, 320), (1000, 700, 2048), (5, 20000, 96), (2000, 1, 40), (31, 1500, 5000),
+          (64, 20000, 130), (65, 20000, 130), (50, 70001, 96), (1, 128, 1100), (17, 385, 700)]
 
 
 @pytest.mark.parametrize("rows,vocab,k", SHAPES)
@@ -205,15 +206,22 @@ def test_the_same_bits():
     few = slice(1111, 1300)
     loss, lse = api.head_loss(h[few], w, t[few].contiguous())
     assert torch.equal(loss, a[0][few]) and torch.equal(lse, a[1][few])
+    # up to 64 rows in an order of their own
+    few = slice(1111, 1170)
+    a, b = (run(h[few], w, t[few].contiguous(), grad[few].contiguous()) for _ in range(2))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    loss, lse = api.head_loss(h[1120:1163], w, t[1120:1163].contiguous())
+    assert torch.equal(loss, a[0][9:52]) and torch.equal(lse, a[1][9:52])
 
 
-def test_a_row_that_is_not_finite_stays_by_itself():
-    h, w, t, grad = make(9, 500, 900, 64)
+@pytest.mark.parametrize("rows", [40, 500])
+def test_a_row_that_is_not_finite_stays_by_itself(rows):
+    h, w, t, grad = make(9, rows, 900, 64)
     loss, lse = api.head_loss(h, w, t)
-    h[17, 3], h[300, 5] = float("nan"), float("inf")
+    h[17, 3], h[30, 5] = float("nan"), float("inf")
     a, b = api.head_loss(h, w, t)
-    keep = torch.ones(500, dtype=torch.bool, device="cuda")
-    keep[17] = keep[300] = False
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[17] = keep[30] = False
     assert torch.equal(a[keep], loss[keep]) and torch.equal(b[keep], lse[keep])
     assert not a[~keep].isfinite().any()
 
@@ -276,8 +284,9 @@ def test_differences():
         assert abs(terms.sum().item() - slope) <= 2.0 ** -7 * terms.abs().sum().item() + 1e-6
 
 
-def test_streams_and_graphs():
-    h, w, t, grad = make(11, 500, 3000, 256, 0.6)
+@pytest.mark.parametrize("rows", [60, 500])
+def test_streams_and_graphs(rows):
+    h, w, t, grad = make(11, rows, 3000, 256, 0.6)
     want = run(h, w, t, grad)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
