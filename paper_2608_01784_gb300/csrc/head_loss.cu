@@ -666,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           load(c);
-          if (col0 + 32 * c >= p.ld_sums) continue;
+          if (col0 + 32 * c >= p.ld_sums || warp_row >= live) continue;
           box_free();
 #pragma unroll
           for (int q = 0; q < 8; ++q)

@@ -5,7 +5,9 @@ next forward:
     the residual, layer by layer -> output head in 8 bits -> sampled tokens and
     their confidences -> commits, history and active blocks (reflex_update_state)
 
-The tokens stay independent of one another between the layers, as in MoEStack.
+The tokens stay independent of one another between the layers, as in MoEStack; a
+layer may have norms in front of and behind its experts, with a gate and a scale on
+the way back into the stream (block_norm).
 Everything runs in libreflex.so's kernels on the current stream; a forward
 allocates nothing and waits for nothing, so it can be captured in a CUDA graph.
 
@@ -20,10 +22,13 @@ from . import api
 
 
 def quantize_layer(w_router: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor,
-                   stream=None) -> dict:
+                   stream=None, norms: dict | None = None) -> dict:
     """A layer of DenoiserFp8: the router [E, d] stays in bf16, the experts go to
-    8 bits (quantize_experts)."""
-    return dict(w_router=w_router, **api.quantize_experts(w_gate_up, w_down, stream))
+    8 bits (quantize_experts).  norms: w_before [d] bf16, by which the layer's normalised
+    input is multiplied, and what block_norm takes for its output: w_after, gate (both
+    [d]), scale."""
+    layer = dict(w_router=w_router, **api.quantize_experts(w_gate_up, w_down, stream))
+    return layer if norms is None else dict(layer, norms=norms)
 
 
 def _a_header_a_layer(op, layers: int) -> list:
@@ -43,17 +48,40 @@ def _check(t: torch.Tensor, shape: tuple, what: str, device=None):
         raise ValueError(f"{what}: a contiguous CUDA tensor {shape} of torch.bfloat16")
 
 
+def _norms(layers: list, d: int, final_norm) -> list | None:
+    """The layers' norms, checked; None where there are none."""
+    norms = [w["norms"] for w in layers if w.get("norms") is not None]
+    if len(norms) not in (0, len(layers)) or (final_norm is not None and not norms):
+        raise ValueError("norms: in every layer or in none")
+    dev = layers[0]["w_router"].device
+    for n in norms:
+        if not set(n) <= {"w_before", "w_after", "gate", "scale"}:
+            raise ValueError("norms: w_before, w_after, gate and scale")
+        _check(n["w_before"], (d,), "w_before", dev)
+        for name in ("w_after", "gate"):
+            if n.get(name) is not None:
+                _check(n[name], (d,), name, dev)
+    if final_norm is not None:
+        _check(final_norm, (d,), "final_norm", dev)
+    return norms or None
+
+
 class DenoiserFp8:
     """Layers (quantize_layer) of one shape, without a shared expert, and an
     output head (codes, scales: quantize_fp8 of [vocab, d] in 128 x 128 blocks),
     with buffers for `max_tokens` tokens.  The router's workspace is that of a whole
     bf16 layer (2.4 GB at 32768 tokens, d = 2048, 64 experts of 1024, 12 slots), of
-    which a forward uses the scores and the record alone."""
+    which a forward uses the scores and the record alone.  With norms (in every layer or
+    in none), the stream is multiplied by its norm and final_norm [d] in front of the
+    head, if that is given."""
 
     def __init__(self, layers: list, head: tuple, *, d: int, E: int, inter: int, k_max: int,
-                 max_tokens: int, flags: int = B.REFLEX_FLAG_RENORM_TOPK):
+                 max_tokens: int, flags: int = B.REFLEX_FLAG_RENORM_TOPK,
+                 final_norm: torch.Tensor | None = None, eps: float = 1e-6):
         if not layers:
             raise ValueError("a denoiser needs at least one layer")
+        self.norms = _norms(layers, d, final_norm)
+        self.final_norm, self.eps = final_norm, eps
         self.layers, self.flags, self.max_tokens = layers, flags, max_tokens
         # the router, its counts and its record; of the experts it runs nothing
         self.router = api.MoELayer(layers[0], dtype="bf16", d=d, E=E, inter=inter, shared_inter=0,
@@ -72,7 +100,7 @@ class DenoiserFp8:
             raise ValueError("the head takes another width than the layers give")
         dev = head[0].device
         self._h = [torch.empty((max_tokens, d), dtype=torch.bfloat16, device=dev)
-                   for _ in range(2)]
+                   for _ in range(2 if self.norms is None else 3)]
         ld = -(-self.head.N // 8) * 8
         self._logits = torch.empty((max_tokens, ld), dtype=torch.bfloat16,
                                    device=dev)[:, :self.head.N]
@@ -91,8 +119,13 @@ class DenoiserFp8:
         _check(hidden, (T, self.experts.d), "hidden", self.k.device)
         k, route = self.k[:T], self.flags | B.REFLEX_STAGE_ROUTE
         h = hidden
+        if self.norms is not None:
+            stream, x, y = (t[:T] for t in self._h)
+            api.block_norm(hidden, w_before=self.norms[0]["w_before"], eps=self.eps, out=stream,
+                           norm=x)
+            h = x
         for i, w in enumerate(self.layers):
-            out = self._h[i & 1][:T]
+            out = self._h[i & 1][:T] if self.norms is None else y
             self.router.w = self.experts.w = w
             self.router.ws, self.experts.ws = self._ws[i]
             if i == 0:  # counts and the first router in one call
@@ -101,8 +134,18 @@ class DenoiserFp8:
             else:
                 self.router.forward(h, k, out, route)
             ids, alpha = self.router.routing()
-            self.experts.forward(h, ids, alpha, k, out, residual=True)
-            h = out
+            self.experts.forward(h, ids, alpha, k, out, residual=self.norms is None)
+            if self.norms is None:
+                h = out
+                continue
+            # back into the stream, and from there to the next layer or the head
+            last = i + 1 == len(self.layers)
+            after = self.final_norm if last else self.norms[i + 1]["w_before"]
+            api.block_norm(stream, y, w_after=self.norms[i].get("w_after"),
+                           gate=self.norms[i].get("gate"), scale=self.norms[i].get("scale", 1.0),
+                           w_before=after, eps=self.eps, out=stream,
+                           norm=None if after is None else x)
+            h = stream if after is None else x
         return self.head.forward(h, self._logits[:T])
 
     def forward(self, state: dict, params: B.reflex_alloc_params, hidden: torch.Tensor,
