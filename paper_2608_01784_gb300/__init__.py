@@ -3,9 +3,9 @@
 C ABI: include/reflex.h, implemented in csrc/ and built into
 _build/libreflex.so by `python -m paper_2608_01784_gb300.build`.
 `_binding` mirrors the C entry points one to one; `api` adds device-buffer
-conveniences (with `fp8` for the 8-bit products); `denoise` runs one denoising
-forward in 8 bits, counts to sampled tokens; `workloads` draws the seeded
-synthetic inputs.  There is no
+conveniences (with `fp8` for the 8-bit products and `train` for the calls that have
+gradients); `denoise` runs one denoising forward in 8 bits, counts to sampled
+tokens; `workloads` draws the seeded synthetic inputs.  There is no
 CPU fallback: loading fails loudly when the library is missing.
 """
 from ._binding import (  # noqa: F401

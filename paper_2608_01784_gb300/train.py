@@ -19,6 +19,13 @@ def _here(device):
         raise ValueError("the tensors are on another device than the current one")
 
 
+def _new_like(t: torch.Tensor, stream) -> torch.Tensor:
+    """An empty contiguous tensor like t, as _new has it (0.4 us less where t allows)."""
+    if stream is None and t.is_contiguous():
+        return torch.empty_like(t)
+    return _new(tuple(t.shape), t.dtype, t.device, stream)
+
+
 def _like(t: torch.Tensor, x: torch.Tensor, what: str) -> int:
     """The row stride of t, which has x's shape, type and device."""
     if t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
@@ -68,14 +75,14 @@ def block_norm(h: torch.Tensor, y: torch.Tensor | None = None, *,
     rows, d, ldh, ldy, ldg = _norm_inputs(h, y, w_after, w_before, gate)
     ldo = ldn = d
     if out is None:
-        out = _new((rows, d), h.dtype, h.device, stream)
+        out = _new_like(h, stream)
     else:
         ldo = _like(out, h, "out")
     if norm is not None:
         _want(w_before is not None, "norm needs w_before")
         ldn = _like(norm, h, "norm")
     elif w_before is not None:
-        norm = _new((rows, d), h.dtype, h.device, stream)
+        norm = _new_like(h, stream)
     B.reflex_block_norm(_DTYPES[h.dtype], h, ldh, y, ldy, w_after, gate, ldg, w_before, scale, eps,
                         rows, d, out, ldo, norm, ldn, stream)
     return out, norm
@@ -97,14 +104,12 @@ def block_norm_backward(h: torch.Tensor, y: torch.Tensor | None, d_out: torch.Te
     ld_d_out = _like(d_out, h, "d_out") if d_out is not None else 0
     ld_d_norm = _like(d_norm, h, "d_norm") if d_norm is not None else 0
 
-    def new(like, *shape):
-        return None if like is None else _new(shape, h.dtype, h.device, stream)
+    def new(like):
+        return None if like is None else _new_like(like, stream)
     ld_d_h = _like(d_h, h, "d_h") if d_h is not None else d
     ld_d_y = _like(d_y, h, "d_y") if d_y is not None else d
-    got = dict(w_after=new(w_after, d), w_before=new(w_before, d),
-               gate=new(gate, rows, d) if ldg else new(gate, d),
-               h=new(h, rows, d) if d_h is None else d_h,
-               y=new(y, rows, d) if d_y is None else d_y)
+    got = dict(w_after=new(w_after), w_before=new(w_before), gate=new(gate),
+               h=new(h) if d_h is None else d_h, y=new(y) if d_y is None else d_y)
     ws_bytes = B.reflex_block_norm_workspace_size(rows, d)
     _want(ws_bytes > 0, "unsupported width")
     ws = _new(ws_bytes, torch.uint8, h.device, stream)
@@ -218,9 +223,12 @@ def expert_rows(x: torch.Tensor, plan: ExpertPlan, *, rows: torch.Tensor | None 
 def _sum(rows, alpha, plan, residual, out, stream):
     d, ldr = _pair_rows(rows, plan, "rows")
     ldres = _tokens(residual, plan, d, rows.dtype, "residual") if residual is not None else 0
+    ldo = d
     if out is None:
-        out = _new((plan.T, d), rows.dtype, rows.device, stream)
-    ldo = _tokens(out, plan, d, rows.dtype, "out")
+        out = (_new_like(residual, stream) if residual is not None else
+               _new((plan.T, d), rows.dtype, rows.device, stream))
+    else:
+        ldo = _tokens(out, plan, d, rows.dtype, "out")
     B.reflex_expert_combine(_DTYPES[rows.dtype], rows, ldr, alpha, plan.row_of_ptr, residual, ldres,
                             plan.T, d, plan.k_max, plan.cap_rows, out, ldo, stream)
     return out
@@ -249,13 +257,16 @@ def expert_combine_backward(d_out: torch.Tensor, rows: torch.Tensor, alpha: torc
     d, ldr = _pair_rows(rows, plan, "rows")
     ldd = _tokens(d_out, plan, d, rows.dtype, "d_out")
     _weights(alpha, plan, "alpha")
+    if d_alpha is None:
+        d_alpha = _new_like(alpha, stream)
+    else:
+        _weights(d_alpha, plan, "d_alpha")
+    lddr = d
     if d_rows is None:
         d_rows = _new((plan.cap_rows, d), rows.dtype, rows.device, stream)
-    if d_alpha is None:
-        d_alpha = _new((plan.T, plan.k_max), torch.float32, rows.device, stream)
-    dd, lddr = _pair_rows(d_rows, plan, "d_rows")
-    _want(dd == d and d_rows.dtype == rows.dtype, "d_rows: another width or type than rows")
-    _weights(d_alpha, plan, "d_alpha")
+    else:
+        dd, lddr = _pair_rows(d_rows, plan, "d_rows")
+        _want(dd == d and d_rows.dtype == rows.dtype, "d_rows: another width or type than rows")
     B.reflex_expert_combine_backward(_DTYPES[rows.dtype], d_out, ldd, rows, ldr, alpha,
                                      plan.row_of_ptr, plan.T, d, plan.k_max, plan.cap_rows, d_rows,
                                      lddr, d_alpha, stream)

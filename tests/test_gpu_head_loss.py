@@ -113,7 +113,8 @@ def test_gradient(rows, vocab, k):
         check_grad(h, w, t, grad, dh, dw)
 
 
-@pytest.mark.parametrize("rows,vocab,k", [(8192, 9001, 136), (4100, 35000, 72), (20000, 5000, 64)])
+@pytest.mark.parametrize("rows,vocab,k", [(8192, 9001, 136), (4100, 35000, 72), (20000, 5000, 64),
+                                          (3, 263000, 16)])
 def test_several_pieces(rows, vocab, k):
     h, w, t, grad = make(rows, rows, vocab, k, 0.9)
     loss, lse, dh, dw = run(h, w, t, grad)
