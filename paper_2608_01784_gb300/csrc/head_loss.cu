@@ -410,14 +410,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Tile t = decode(p, counts, live, LOSS, j);
       const int ra = t.row0 + static_cast<int>(rank) * kHalf;
       const int rb = t.col0 + static_cast<int>(rank) * kHalf;
-      bool fetched = false;
+      // The next tile's number takes a microsecond (the MMAs of two stages and a half):
+      // asked for eight stages before the end of a longer tile (8192 x 16384 x 2048: 350 ->
+      // 344 us), not earlier, so that a long tile does not hold back one that is waiting.
+      const int ask = t.kb1 - t.kb0 > 8 ? t.kb1 - 8 : max(t.kb0, t.kb1 - 1);
       auto fetch = [&] {
-        if (leader) {
-          const uint32_t q = atomicAdd(p.queue, 1u) + static_cast<uint32_t>(npairs);
-          next = q < static_cast<uint32_t>(njobs) ? static_cast<int>(q) : -1;
-        }
-        fetched = true;
+        if (!leader) return;
+        const uint32_t q = atomicAdd(p.queue, 1u) + static_cast<uint32_t>(npairs);
+        next = q < static_cast<uint32_t>(njobs) ? static_cast<int>(q) : -1;
       };
+      if (t.kb0 >= t.kb1) fetch();
       for (int kb = t.kb0; kb < t.kb1; ++kb) {
         if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
@@ -447,9 +449,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           stage = 0;
           phase ^= 1u;
         }
-        if (kb + 1 == t.kb1) fetch();
+        if (kb == ask) fetch();
       }
-      if (!fetched) fetch();
     }
     if (!ok) give_up(true);
     if (*abort_flag && leader) {
