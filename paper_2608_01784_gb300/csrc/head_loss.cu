@@ -227,12 +227,12 @@ struct Maps {
   CUtensorMap dh_out;   // [splits x rows] fp32 sums, 32 x 32
 };
 
-struct Tile {
-  int kind;
+struct __align__(16) Tile {
+  int kind;      // -1: the end
   int row0;      // rows of the tile: packed rows, weight: rows of the piece
   int col0;      // columns: vocabulary (grad: in the piece) or hidden columns
-  int kb0, kb1;  // stages of the reduction
   int part;      // hidden: which part of the piece
+  int kb0, kb1;  // stages of the reduction
 };
 
 // How many tiles of each kind the launch has, for `live` rows.
@@ -328,8 +328,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain = job_empty + kJobs;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* s_job = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [kJobs]
-  static_assert((2 * kStages + 4 + 2 * kJobs + 1) * 8 + 8 + kJobs * 4 <= 512, "barriers");
+  // [kJobs] tiles, decoded by the leader's producer
+  Tile* s_job = reinterpret_cast<Tile*>(reinterpret_cast<uint8_t*>(bars) + 256);
+  static_assert((2 * kStages + 4 + 2 * kJobs + 1) * 8 + 8 <= 256 && sizeof(Tile) == 32 &&
+                    kJobs * sizeof(Tile) <= 256, "barriers and tiles");
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -369,14 +371,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   const Counts counts = count_tiles(p, live, LOSS);
   const int njobs = counts.all();
 
-  // The number of the n-th tile of this pair; -1 after the last one.  Arrives for the
-  // calling thread; false on a timeout.
-  auto next_job = [&](uint32_t n, int& j) {
+  // The n-th tile of this pair; false on a timeout.
+  auto next_job = [&](uint32_t n, Tile& t) {
     const int slot = n % kJobs;
     if (!mbar_wait_cluster(&job_full[slot], (n / kJobs) & 1u, abort_flag, kWaitNs)) return false;
-    j = s_job[slot];
-    mbar_arrive_cluster(map_to_rank(smem_addr(&job_empty[slot]), 0));
+    const int4 a = reinterpret_cast<const int4*>(&s_job[slot])[0];
+    const int2 b = reinterpret_cast<const int2*>(&s_job[slot])[2];
+    t = Tile{a.x, a.y, a.z, a.w, b.x, b.y};
     return true;
+  };
+  // The calling thread has used it.  Relaxed: a release would wait until the thread's
+  // stores of the last tile's results have reached L2.
+  auto job_read = [&](uint32_t n) {
+    mbar_arrive_cluster_relaxed(map_to_rank(smem_addr(&job_empty[n % kJobs]), 0));
   };
   auto give_up = [&](bool timeout) {
     if (timeout && !*abort_flag) set_err(p.err, kErrTimeout);
@@ -390,24 +397,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     int next = pair < njobs ? pair : -1;  // leader
     for (uint32_t n = 0; ok; ++n) {
-      int j = next;
+      Tile t{-1};
       if (leader) {
+        if (next >= 0) t = decode(p, counts, live, LOSS, next);
         const int slot = n % kJobs;
         if (!mbar_wait_cluster(&job_empty[slot], ((n / kJobs) & 1u) ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
           break;
         }
-        s_job[slot] = j;
-        const uint32_t there = map_to_rank(smem_addr(const_cast<int*>(&s_job[slot])), 1);
-        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(there), "r"(j) : "memory");
-        mbar_arrive_cluster(map_to_rank(smem_addr(&job_full[slot]), 0));
-        mbar_arrive_cluster(map_to_rank(smem_addr(&job_full[slot]), 1));
-      } else if (!next_job(n, j)) {
-        ok = false;
-        break;
+        for (uint32_t c = 0; c < 2; ++c) {
+          const uint32_t there = map_to_rank(smem_addr(&s_job[slot]), c);
+          asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(there),
+                       "r"(t.kind), "r"(t.row0), "r"(t.col0), "r"(t.part)
+                       : "memory");
+          asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(there + 16), "r"(t.kb0),
+                       "r"(t.kb1)
+                       : "memory");
+          mbar_arrive_cluster(map_to_rank(smem_addr(&job_full[slot]), c));
+        }
+      } else {
+        if (!next_job(n, t)) {
+          ok = false;
+          break;
+        }
+        if (t.kind >= 0) job_read(n);
       }
-      if (j < 0) break;
-      const Tile t = decode(p, counts, live, LOSS, j);
+      if (t.kind < 0) break;
       const int ra = t.row0 + static_cast<int>(rank) * kHalf;
       const int rb = t.col0 + static_cast<int>(rank) * kHalf;
       // The next tile's number takes a microsecond (the MMAs of two stages and a half):
@@ -466,13 +481,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t acc_n = 0;
     bool ok = true, issued_any = false;
     for (uint32_t n = 0; ok; ++n) {
-      int j;
-      if (!next_job(n, j)) {
+      Tile t;
+      if (!next_job(n, t)) {
         ok = false;
         break;
       }
-      if (j < 0) break;
-      const Tile t = decode(p, counts, live, LOSS, j);
+      if (t.kind < 0) break;
+      job_read(n);
       const bool a_mn = !LOSS && t.kind == kWeight, b_mn = !LOSS && t.kind >= kHidden;
       const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
       // 16 along the reduction: 32 bytes of a row, or 16 rows of 128 bytes
@@ -541,16 +556,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     uint32_t acc_n = 0;
     for (uint32_t n = 0;; ++n) {
-      int j = -1, ok = 1;
-      if (lane == 0) ok = next_job(n, j) ? 1 : 0;
+      Tile t{-1};
+      int ok = 1;
+      if (lane == 0) ok = next_job(n, t) ? 1 : 0;
       ok = __shfl_sync(0xffffffffu, ok, 0);
-      j = __shfl_sync(0xffffffffu, j, 0);
+      t.kind = __shfl_sync(0xffffffffu, t.kind, 0);
+      t.row0 = __shfl_sync(0xffffffffu, t.row0, 0);
+      t.col0 = __shfl_sync(0xffffffffu, t.col0, 0);
+      t.part = __shfl_sync(0xffffffffu, t.part, 0);
+      t.kb0 = __shfl_sync(0xffffffffu, t.kb0, 0);
+      t.kb1 = __shfl_sync(0xffffffffu, t.kb1, 0);
       if (!ok) {
         if (lane == 0) give_up(true);
         break;
       }
-      if (j < 0) break;
-      const Tile t = decode(p, counts, live, LOSS, j);
+      if (t.kind < 0) break;
+      if (lane == 0) job_read(n);
       const int row = t.row0 + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
       const int warp_row = row - lane;
       const int col0 = t.col0 + half * 128;
@@ -623,14 +644,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (v + i >= p.vocab) sum[c][i] = -INFINITY;
-          const uint32_t at = static_cast<uint32_t>(target - v);
+          if (v < p.vocab) add_chunk(st, sum[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {  // (the target is on its way from L2 until here)
+          const uint32_t at = static_cast<uint32_t>(target - (col0 + 32 * c));
           if (at < 32u) {
             float zt = sum[c][0];
 #pragma unroll
             for (int i = 1; i < 32; ++i) zt = at == static_cast<uint32_t>(i) ? sum[c][i] : zt;
             p.z_target[row] = zt;
           }
-          if (v < p.vocab) add_chunk(st, sum[c]);
         }
         p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
       } else if (t.kind == kGrad) {
