@@ -353,6 +353,8 @@ def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torc
         d_hidden, ld_dh = _gradient(d_hidden, rows, k, dev, stream, "d_hidden")
         dt_h = _DTYPES[d_hidden.dtype]
     if need_weight:
+        if d_weight is not None and d_weight.data_ptr() == weight.data_ptr():
+            raise ValueError("d_weight: the weights are still read while it is written")
         d_weight, ld_dw = _gradient(d_weight, vocab, k, dev, stream, "d_weight")
         dt_w = _DTYPES[d_weight.dtype]
     ws_bytes = B.reflex_head_loss_backward_workspace_size(rows, vocab, k)

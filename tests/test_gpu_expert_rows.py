@@ -220,6 +220,19 @@ def test_strides_and_alignment(dtype, d, ld, shift):
         assert bool((wide == 7.0).all())
 
 
+def test_one_gradient_alone():
+    """Either output of the gradient of the way back by itself (C entry point)."""
+    ids, alpha = routing(8, 70, 8, 5)
+    plan = api.expert_plan(ids, E=8)
+    y, g = draw(1, BF16, plan.cap_rows, 96), draw(2, BF16, 70, 96)
+    both = api.expert_combine_backward(g, y, alpha, plan, d_rows=torch.zeros_like(y))
+    d_rows, d_alpha = torch.zeros_like(y), torch.full_like(alpha, 7.0)
+    args = (B.REFLEX_DTYPE_BF16, g, 96, y, 96, alpha, plan.row_of, 70, 96, 5, plan.cap_rows)
+    B.reflex_expert_combine_backward(*args, d_rows, 96, None)
+    B.reflex_expert_combine_backward(*args, None, 0, d_alpha)
+    assert torch.equal(d_rows, both[0]) and torch.equal(d_alpha, both[1])
+
+
 def test_large_row_offsets():
     """Rows behind 2^31 elements."""
     T, d, k_max = 40000, 8192, 8

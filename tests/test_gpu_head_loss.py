@@ -169,12 +169,21 @@ def test_gradients_at_odd_addresses():
     assert float(dh[0]) == float(dw[0]) == 7.0
 
 
-def test_no_row_counts():
-    h, w, t, grad = make(5, 300, 600, 64)
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_no_row_counts(rows):
+    h, w, t, grad = make(5, rows, 600, 64)
     t.fill_(-1)
     loss, lse, dh, dw = run(h, w, t, grad)
     for x in (loss, lse, dh, dw):
         assert not x.any()
+
+
+@pytest.mark.parametrize("rows", [40, 300])
+def test_the_rows_gradient_in_place(rows):
+    h, w, t, grad = make(13, rows, 500, 64, 0.8)
+    want = run(h, w, t, grad)[2:]
+    got = run(h, w, t, grad, d_hidden=h)[2:]
+    assert got[0] is h and torch.equal(h, want[0]) and torch.equal(got[1], want[1])
 
 
 def test_no_rows():
@@ -334,6 +343,7 @@ def test_refusals(monkeypatch):
              lambda: api.head_loss_backward(h, w, t, lse, grad.double()),
              lambda: api.head_loss_backward(h, w, t, lse, grad, d_hidden=h[:5]),
              lambda: api.head_loss_backward(h, w, t, lse, grad, d_weight=w.half()),
+             lambda: api.head_loss_backward(h, w, t, lse, grad, d_weight=w),
              lambda: api.head_loss_backward(h, w, t, lse, grad, need_hidden=False,
                                             need_weight=False),
              lambda: api.head_loss_backward(h, w, t, lse, grad, need_weight=False,
