@@ -114,7 +114,8 @@ def test_gradient(rows, vocab, k):
 
 
 @pytest.mark.parametrize("rows,vocab,k", [(8192, 9001, 136), (4100, 35000, 72), (20000, 5000, 64),
-                                          (3, 263000, 16)])
+                                          (3, 263000, 16), (8192, 33000, 40),
+                                          (20000, 14000, 64), (3, 1050000, 16)])
 def test_several_pieces(rows, vocab, k):
     h, w, t, grad = make(rows, rows, vocab, k, 0.9)
     loss, lse, dh, dw = run(h, w, t, grad)
