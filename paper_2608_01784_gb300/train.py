@@ -1,9 +1,9 @@
 """Torch-facing convenience over the entry points around the experts that have
-gradients: norms around a block, tokens to experts and back, the loss of a head.  A gradient is a call of
-its own (no autograd graph is kept), takes the forward call's inputs again and
-allocates only what it returns and a workspace, so each can be captured in a CUDA
-graph.  With a `stream`, new outputs belong to it: to use them on another, wait for
-it, as torch's own rules have it.
+gradients: norms around a block, tokens to experts and back, the loss of a head.  A
+gradient is a call of its own (no autograd graph is kept), takes the forward call's
+inputs again and allocates only what it returns and a workspace, so each can be
+captured in a CUDA graph.  With a `stream`, new outputs belong to it: to use them on
+another, wait for it, as torch's own rules have it.
 """
 from __future__ import annotations
 
