@@ -187,15 +187,20 @@ __global__ void __launch_bounds__(kPlanThreads)
 // ---- copies and sums ---------------------------------------------------------
 constexpr int kThreads = 256;
 
-// A lane's share of `kVecs` turns over a row, as stored: 16-byte vectors one warp apart,
-// or, where rows or columns do not allow it, elements.
-template <typename Te, bool VEC, int kVecs>
+// A lane's share of several turns over a row, as stored: units of UB bytes one warp
+// apart, 16-byte vectors, or, where rows or columns do not allow it, words or elements
+// (and then eight elements in more units, as a unit is all that a load brings).
+// Words matter to bf16 rows of an even width: 65536 tokens of 150, one slot, combine
+// 44 us by elements and 30 by words, 16384 of 1004, four slots, 71 and 44, and their
+// gradients 83 and 63.
+template <typename Te, int UB, int kVecs16>
 struct Share {
-  static constexpr int kEach = VEC ? 16 / static_cast<int>(sizeof(Te)) : 1;
+  static constexpr int kEach = UB / static_cast<int>(sizeof(Te));
+  static constexpr int kVecs = UB == 16 ? kVecs16 : 8 / kEach;
   static constexpr int kSpan = 32 * kEach * kVecs;  // columns of a warp
   static constexpr int kElems = kEach * kVecs;
   // (as words: elements of two bytes by themselves would take a register each)
-  using Unit = std::conditional_t<VEC, uint4, Te>;
+  using Unit = std::conditional_t<UB == 16, uint4, std::conditional_t<UB == 4, uint32_t, Te>>;
   Unit u[kVecs];
   static __device__ __forceinline__ int col(int c0, int i) {
     return c0 + (i * 32 + static_cast<int>(threadIdx.x & 31)) * kEach;
@@ -207,19 +212,25 @@ struct Share {
   }
   // (elements past the row are not set)
   __device__ __forceinline__ float at(int i, int e) const {
-    if constexpr (!VEC) {
+    uint32_t w;
+    if constexpr (UB == 2) {
       return to_f32(u[i]);
+    } else if constexpr (UB == 4) {
+      w = u[i];
     } else {
-      const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
-      if constexpr (sizeof(Te) == 4) return __uint_as_float(w[e]);
-      return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+      const uint32_t q[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+      w = q[sizeof(Te) == 4 ? e : e >> 1];
     }
+    if constexpr (sizeof(Te) == 4) return __uint_as_float(w);
+    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
   }
   // unit i, kEach floats
   static __device__ __forceinline__ void store(Te* row, int c0, int d, int i, const float* f) {
     if (col(c0, i) >= d) return;
     Te* to = row + col(c0, i);
-    if constexpr (!VEC) *to = from_f32<Te>(f[0]);
+    if constexpr (kEach == 1) *to = from_f32<Te>(f[0]);
+    else if constexpr (kEach == 2)
+      *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(f[0], f[1]);
     else if constexpr (sizeof(Te) == 2) store8(to, f);
     else *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
   }
@@ -278,17 +289,17 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// A warp for a token and kCombineVecs turns of its columns, four pair rows under way
+// A warp for a token and a few turns of its columns, four pair rows under way
 // together.  alpha == nullptr: weight 1.
 constexpr int kCombineVecs = 2;
 constexpr int kBatch = 4;
-template <typename Te, bool VEC>
+template <typename Te, int UB>
 __global__ void __launch_bounds__(kThreads, 3)
     combine_rows_kernel(const Te* __restrict__ rows, int64_t ldr,
                         const int32_t* __restrict__ row_of, const float* __restrict__ alpha,
                         const Te* residual, int64_t ldres, int64_t T, int d, int k_max,
                         int cap_rows, Te* out, int64_t ldo, int segments) {
-  using S = Share<Te, VEC, kCombineVecs>;
+  using S = Share<Te, UB, kCombineVecs>;
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31;
@@ -320,14 +331,14 @@ __global__ void __launch_bounds__(kThreads, 3)
         const float a = __shfl_sync(0xffffffffu, my_a, (j0 + b) & 31);
         if (j0 + b < n)
 #pragma unroll
-          for (int i = 0; i < kCombineVecs; ++i)
+          for (int i = 0; i < S::kVecs; ++i)
 #pragma unroll
             for (int e = 0; e < S::kEach; ++e)
               acc[i * S::kEach + e] = __fmaf_rn(a, y[b].at(i, e), acc[i * S::kEach + e]);
       }
     }
 #pragma unroll
-    for (int i = 0; i < kCombineVecs; ++i) {
+    for (int i = 0; i < S::kVecs; ++i) {
       if (residual != nullptr)
 #pragma unroll
         for (int e = 0; e < S::kEach; ++e) acc[i * S::kEach + e] += res.at(i, e);
@@ -339,13 +350,13 @@ __global__ void __launch_bounds__(kThreads, 3)
 // A warp for a pair, its whole rows under way (up to 1024 columns of bf16 at a time);
 // the warps of a token run next to one another and read its gradient from L1 or L2.
 constexpr int kGradVecs = 4;
-template <typename Te, bool VEC>
+template <typename Te, int UB>
 __global__ void __launch_bounds__(kThreads, 4)
     combine_backward_kernel(const Te* __restrict__ d_out, int64_t ldd, const Te* rows, int64_t ldr,
                             const int32_t* __restrict__ row_of, const float* __restrict__ alpha,
                             int64_t T, int d, int k_max, int cap_rows, Te* d_rows, int64_t lddr,
                             float* __restrict__ d_alpha) {
-  using S = Share<Te, VEC, kGradVecs>;
+  using S = Share<Te, UB, kGradVecs>;
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31;
@@ -369,13 +380,13 @@ __global__ void __launch_bounds__(kThreads, 4)
       if (d_alpha != nullptr) f.load(y, c0, d);
       if (d_alpha != nullptr)
 #pragma unroll
-        for (int i = 0; i < kGradVecs; ++i)
+        for (int i = 0; i < S::kVecs; ++i)
           if (S::col(c0, i) < d)
 #pragma unroll
             for (int e = 0; e < S::kEach; ++e) dot = __fmaf_rn(g.at(i, e), f.at(i, e), dot);
       if (d_rows != nullptr)
 #pragma unroll
-        for (int i = 0; i < kGradVecs; ++i) {
+        for (int i = 0; i < S::kVecs; ++i) {
           float o[S::kEach];
 #pragma unroll
           for (int e = 0; e < S::kEach; ++e) o[e] = a * g.at(i, e);
@@ -389,8 +400,8 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 }
 
-bool on16(const void* p, int64_t ld, int es) {
-  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0);
+bool on(int bytes, const void* p, int64_t ld, int es) {
+  return p == nullptr || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * es % bytes == 0);
 }
 unsigned warps_grid(int64_t warps, int sms) {
   const int64_t need = (warps + kThreads / 32 - 1) / (kThreads / 32);
@@ -407,19 +418,19 @@ cudaError_t launch_rows(const ExpertRowsArgs& p, const void* x, int64_t ldx, voi
                     static_cast<V*>(rows), ldr, segments);
 }
 
-template <typename Te, bool VEC>
+template <typename Te, int UB>
 cudaError_t launch_combine_rows(const ExpertRowsArgs& p, int sms, cudaStream_t s) {
-  constexpr int kSpan = Share<Te, VEC, kCombineVecs>::kSpan;
+  constexpr int kSpan = Share<Te, UB, kCombineVecs>::kSpan;
   const int segments = (p.d + kSpan - 1) / kSpan;
-  return launch_pdl(combine_rows_kernel<Te, VEC>, dim3(warps_grid(p.T * segments, sms)),
+  return launch_pdl(combine_rows_kernel<Te, UB>, dim3(warps_grid(p.T * segments, sms)),
                     dim3(kThreads), 0, s, static_cast<const Te*>(p.rows), p.ldr, p.row_of, p.alpha,
                     static_cast<const Te*>(p.x), p.ldx, p.T, p.d, p.k_max, p.cap_rows,
                     static_cast<Te*>(p.out), p.ldo, segments);
 }
 
-template <typename Te, bool VEC>
+template <typename Te, int UB>
 cudaError_t launch_combine_backward(const ExpertRowsArgs& p, int sms, cudaStream_t s) {
-  return launch_pdl(combine_backward_kernel<Te, VEC>, dim3(warps_grid(p.T * p.k_max, sms)),
+  return launch_pdl(combine_backward_kernel<Te, UB>, dim3(warps_grid(p.T * p.k_max, sms)),
                     dim3(kThreads), 0, s, static_cast<const Te*>(p.x), p.ldx,
                     static_cast<const Te*>(p.rows), p.ldr, p.row_of, p.alpha, p.T, p.d, p.k_max,
                     p.cap_rows, static_cast<Te*>(p.out), p.ldo, p.d_alpha);
@@ -471,30 +482,35 @@ cudaError_t launch_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, 
 
 cudaError_t launch_expert_rows(int dtype, const ExpertRowsArgs& p, int sms, cudaStream_t s) {
   const int es = dtype == 0 ? 4 : 2;
-  if (p.d * es % 16 == 0 && on16(p.x, p.ldx, es) && on16(p.out, p.ldo, es))
+  auto rows_on = [&](int bytes) {
+    return p.d * es % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.out, p.ldo, es);
+  };
+  if (rows_on(16))
     return launch_rows<uint4>(p, p.x, p.ldx * es / 16, p.out, p.ldo * es / 16, p.d * es / 16, sms,
                               s);
-  if (dtype == 0) return launch_rows<uint32_t>(p, p.x, p.ldx, p.out, p.ldo, p.d, sms, s);
+  if (rows_on(4))
+    return launch_rows<uint32_t>(p, p.x, p.ldx * es / 4, p.out, p.ldo * es / 4, p.d * es / 4, sms,
+                                 s);
   return launch_rows<unsigned short>(p, p.x, p.ldx, p.out, p.ldo, p.d, sms, s);
 }
 
 cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backward, int sms,
                                   cudaStream_t s) {
   const int es = dtype == 0 ? 4 : 2;
-  const bool vec = p.d % 8 == 0 && on16(p.x, p.ldx, es) && on16(p.rows, p.ldr, es) &&
-                   on16(p.out, p.ldo, es);
-  if (backward) {
-    if (dtype == 0)
-      return vec ? launch_combine_backward<float, true>(p, sms, s)
-                 : launch_combine_backward<float, false>(p, sms, s);
-    return vec ? launch_combine_backward<__nv_bfloat16, true>(p, sms, s)
-               : launch_combine_backward<__nv_bfloat16, false>(p, sms, s);
-  }
+  auto rows_on = [&](int bytes) {
+    return p.d * es % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.rows, p.ldr, es) &&
+           on(bytes, p.out, p.ldo, es);
+  };
+  auto go = [&](auto combine, auto gradient) {
+    return backward ? gradient(p, sms, s) : combine(p, sms, s);
+  };
+  using Bf = __nv_bfloat16;
   if (dtype == 0)
-    return vec ? launch_combine_rows<float, true>(p, sms, s)
-               : launch_combine_rows<float, false>(p, sms, s);
-  return vec ? launch_combine_rows<__nv_bfloat16, true>(p, sms, s)
-             : launch_combine_rows<__nv_bfloat16, false>(p, sms, s);
+    return rows_on(16) ? go(launch_combine_rows<float, 16>, launch_combine_backward<float, 16>)
+                       : go(launch_combine_rows<float, 4>, launch_combine_backward<float, 4>);
+  return rows_on(16)  ? go(launch_combine_rows<Bf, 16>, launch_combine_backward<Bf, 16>)
+         : rows_on(4) ? go(launch_combine_rows<Bf, 4>, launch_combine_backward<Bf, 4>)
+                      : go(launch_combine_rows<Bf, 2>, launch_combine_backward<Bf, 2>);
 }
 
 }  // namespace rx

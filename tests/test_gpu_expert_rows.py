@@ -130,7 +130,8 @@ def test_plans(T, E, k_max, gaps):
 @pytest.mark.parametrize("T,d,E,k_max,gaps", [
     (1, 1, 1, 1, False), (3, 7, 2, 2, False), (40, 8, 64, 12, False), (33, 64, 8, 32, True),
     (257, 100, 60, 4, True), (100, 255, 8, 12, False), (64, 257, 64, 5, True),
-    (31, 2048, 64, 12, False), (700, 1001, 256, 8, False), (12, 8192, 8, 12, True)])
+    (31, 2048, 64, 12, False), (700, 1001, 256, 8, False), (12, 8192, 8, 12, True),
+    (90, 1030, 16, 6, True)])
 def test_shapes(T, d, E, k_max, gaps, dtype):
     ids, alpha = routing(T * 3 + d, T, E, k_max, gaps)
     check_all(api.expert_plan(ids, E=E), alpha, d, dtype)
