@@ -19,8 +19,9 @@
 // one tail; pairs take tiles from a queue, the long ones first.  Every tile is summed
 // by one pair in one order, wherever it runs: results do not depend on timing.
 //
-// G is rounded to bf16 (2^-9 of each term, as the products take them); z, the sums of
-// exponentials and all accumulators are fp32.  exp(z - m) is taken as 2^(z c - m c), c =
+// G is rounded to bf16 (by up to 2^-8 of each term, as the products take them: 999 x 50001
+// x 2048, gradients in bf16 off by 2.37e-3 of their norm, their own rounding alone by
+// 1.66e-3); z, the sums of exponentials and all accumulators are fp32.  exp(z - m) is taken as 2^(z c - m c), c =
 // log2 e, with the rounding error of m c, the same for all terms, put back at the end.
 //
 // Bound: the tensor cores, in a loop of seconds under the card's power cap (1.37 kW).
@@ -53,12 +54,13 @@ constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kStaging = 32 * 128;  // of an epilogue warp
 constexpr int kJobs = 4;            // tiles that are known ahead
-// Stages whose products the tensor cores add by themselves in a loss tile.  They cut
+// Stages whose products the tensor cores add by themselves in a tile of logits.  They cut
 // sums instead of rounding them, always downwards in magnitude: over the 2048 of a row
-// that put 2.4e-5 on logits of 20.  Sums of 512 are added in registers instead, to the
-// nearest (error of a loss 2.2e-7 of it, of 256 1.1e-7; 8192 x 16384 x 2048: 329 us, of 256
-// 360).
-constexpr int kLossChunk = 8;
+// that put 2.4e-5 on logits of 20, over 8192 1.4e-3 on logits of 40.  Sums of 512 are added
+// in registers instead, to the nearest (error of a loss 2.2e-7 of it, of 256 1.1e-7; 8192 x
+// 16384 x 2048: 329 us, of 256 360).  The same in both directions: the gradient takes z
+// against the lse that the loss made of it, and of a sure row nothing must be left.
+constexpr int kLogitChunk = 8;
 constexpr int kSmemBytes = kStages * kStageBytes + kEpiWarps * kStaging + 512 + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 constexpr uint64_t kWaitNs = 2000000000ull;
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int kb = t.kb0;
       do {  // (once for a tile without a reduction)
         const int ab = acc_n & 1, first = kb;
-        const int last = LOSS ? min(t.kb1, kb + kLossChunk) : t.kb1;
+        const int last = LOSS || t.kind == kGrad ? min(t.kb1, kb + kLogitChunk) : t.kb1;
         if (!mbar_wait(&acc_empty[ab], ((acc_n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
           break;
@@ -623,15 +625,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(r[i]);
         if (c == 3) hand_back();
       };
-      if (LOSS) {
-        float sum[4][32];
+      // logits: a row of 128 columns, in parts of kLogitChunk stages
+      float sum[4][32];
+      if (LOSS || t.kind == kGrad) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           load(c);
 #pragma unroll
           for (int i = 0; i < 32; ++i) sum[c][i] = z[i];
         }
-        for (int kb = t.kb0 + kLossChunk; kb < t.kb1; kb += kLossChunk) {
+        for (int kb = t.kb0 + kLogitChunk; kb < t.kb1; kb += kLogitChunk) {
           if (!acc_ready()) break;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -644,6 +647,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) give_up(true);
           break;
         }
+      }
+      if (LOSS) {
         Stats st{-INFINITY, 0.f};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -666,27 +671,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
       } else if (t.kind == kGrad) {
-#pragma unroll 1
+#pragma unroll
         for (int c = 0; c < 4; ++c) {
-          load(c);
+          float (&g)[32] = sum[c];
           const int v = col0 + 32 * c;  // in the piece
           const uint32_t at = static_cast<uint32_t>(target - v);
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            float g = exp2_fast(__fmaf_rn(z[i], kLog2e, -lse_c));
-            g = at == static_cast<uint32_t>(i) ? g - 1.f : g;
-            z[i] = c_row * g;
+            float x = exp2_fast(__fmaf_rn(g[i], kLog2e, -lse_c));
+            x = at == static_cast<uint32_t>(i) ? x - 1.f : x;
+            g[i] = c_row * x;
           }
           if (p.v_next + v + 32 > p.vocab)  // zeros behind the last column
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (p.v_next + v + i >= p.vocab) z[i] = 0.f;
+              if (p.v_next + v + i >= p.vocab) g[i] = 0.f;
           if ((c & 1) == 0) box_free();
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            put((c & 1) * 4 + q, pack_bf16(z[8 * q], z[8 * q + 1]),
-                pack_bf16(z[8 * q + 2], z[8 * q + 3]), pack_bf16(z[8 * q + 4], z[8 * q + 5]),
-                pack_bf16(z[8 * q + 6], z[8 * q + 7]));
+            put((c & 1) * 4 + q, pack_bf16(g[8 * q], g[8 * q + 1]),
+                pack_bf16(g[8 * q + 2], g[8 * q + 3]), pack_bf16(g[8 * q + 4], g[8 * q + 5]),
+                pack_bf16(g[8 * q + 6], g[8 * q + 7]));
           if (c & 1) {
             box_filled();
             if (lane == 0) {
@@ -931,7 +936,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
       for (int kb = 0; kb < nk && ok;) {
         const int ab = acc_n & 1, first = kb;
-        const int last = GRAD ? nk : min(nk, kb + kLossChunk);
+        const int last = min(nk, kb + kLogitChunk);
         if (!mbar_wait(&acc_empty[ab], ((acc_n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
           break;
@@ -986,7 +991,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     int ok = 1;
     for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
       float z[NT];
-      for (int kb = 0; kb < nk; kb += GRAD ? nk : kLossChunk) {
+      for (int kb = 0; kb < nk; kb += kLogitChunk) {
         const int ab = acc_n & 1;
         if (lane == 0)
           ok = mbar_wait(&acc_full[ab], (acc_n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
