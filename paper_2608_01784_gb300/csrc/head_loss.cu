@@ -19,10 +19,11 @@
 // one tail; pairs take tiles from a queue, the long ones first.  Every tile is summed
 // by one pair in one order, wherever it runs: results do not depend on timing.
 //
-// G is rounded to bf16 (by up to 2^-8 of each term, as the products take them: 999 x 50001
-// x 2048, gradients in bf16 off by 2.37e-3 of their norm, their own rounding alone by
-// 1.66e-3); z, the sums of exponentials and all accumulators are fp32.  exp(z - m) is taken as 2^(z c - m c), c =
-// log2 e, with the rounding error of m c, the same for all terms, put back at the end.
+// G is rounded to bf16 (by up to 2^-8 of each term, as the products take them: 999 x
+// 50001 x 2048, gradients in bf16 off by 2.37e-3 of their norm, their own rounding alone
+// by 1.66e-3); z, the sums of exponentials and all accumulators are fp32.  exp(z - m) is
+// taken as 2^(z c - m c), c = log2 e, with the rounding error of m c, the same for all
+// terms, put back at the end.
 //
 // Bound: the tensor cores, in a loop of seconds under the card's power cap (1.37 kW).
 // 8192 rows x 16384 x 2048: the loss 329 us, 1.67 PFLOP/s (cuBLAS's product alone 307 at
@@ -1221,9 +1222,7 @@ cudaError_t launch_tiles(const Maps& maps, const HeadTiles& p, int64_t jobs, int
 template <int NT, bool GRAD>
 cudaError_t launch_few(const HeadProblem& h, const HeadTiles& p, void* g, int64_t ld_g,
                        float* loss, float* lse, int sms, cudaStream_t stream) {
-  // rows of a tile: what the CTAs' rounds of 128 leave shared out evenly
-  const int rounds = (p.vocab + sms * kHalf - 1) / (sms * kHalf);
-  const int tile_rows = (p.vocab + sms * rounds - 1) / (sms * rounds);
+  const int tile_rows = head_few_tile_rows(p.vocab, sms);
   CUtensorMap map_w, map_h;
   if (!box_map(&map_w, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, tile_rows) ||
       !box_map(&map_h, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, NT))
@@ -1232,8 +1231,7 @@ cudaError_t launch_few(const HeadProblem& h, const HeadTiles& p, void* g, int64_
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_smem(kernel, Few<NT>::kSmem, done);
   if (e != cudaSuccess) return e;
-  const int tiles = (p.vocab + tile_rows - 1) / tile_rows;
-  return launch_pdl(kernel, dim3(tiles < sms ? tiles : sms), dim3(kFewThreads), Few<NT>::kSmem,
+  return launch_pdl(kernel, dim3(head_few_ctas(p.vocab, sms)), dim3(kFewThreads), Few<NT>::kSmem,
                     stream, map_w, map_h, p, tile_rows, static_cast<__nv_bfloat16*>(g), ld_g,
                     loss, lse);
 }
@@ -1252,8 +1250,9 @@ cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream) {
 cudaError_t launch_head_loss(const HeadProblem& h, HeadTiles p, float* loss, float* lse, int sms,
                              cudaStream_t stream) {
   if (head_few_rows(p.rows, 1))
-    return p.rows <= 32 ? launch_few<32, false>(h, p, nullptr, 0, loss, lse, sms, stream)
-                        : launch_few<64, false>(h, p, nullptr, 0, loss, lse, sms, stream);
+    return head_few_columns(p.rows) == 32
+               ? launch_few<32, false>(h, p, nullptr, 0, loss, lse, sms, stream)
+               : launch_few<64, false>(h, p, nullptr, 0, loss, lse, sms, stream);
   Maps maps;
   if (!box_map(&maps.h_rows, h.encode, h.packed, false, p.rows_up, p.k, h.ld_packed, BK, kHalf) ||
       !box_map(&maps.w_rows, h.encode, h.w, false, p.vocab, p.k, h.ldw, BK, kHalf))

@@ -395,6 +395,17 @@ struct HeadRows {
 cudaError_t launch_head_rows(const HeadRows& p, int sms, cudaStream_t stream);
 // Whether W goes past the rows, for a vocabulary in `pieces`.
 inline bool head_few_rows(int64_t rows, int pieces) { return rows <= kHeadFewRows && pieces == 1; }
+// Then: columns of a tile, rows of W in one (what the CTAs' rounds of 128 leave shared out
+// evenly), and the CTAs, each of which leaves a maximum and a sum for every column.
+inline int head_few_columns(int64_t rows) { return rows <= 32 ? 32 : kHeadFewRows; }
+inline int head_few_tile_rows(int vocab, int sms) {
+  const int rounds = (vocab + sms * (kHeadTile / 2) - 1) / (sms * (kHeadTile / 2));
+  return (vocab + sms * rounds - 1) / (sms * rounds);
+}
+inline int head_few_ctas(int vocab, int sms) {
+  const int rows = head_few_tile_rows(vocab, sms), tiles = (vocab + rows - 1) / rows;
+  return tiles < sms ? tiles : sms;
+}
 
 struct HeadProblem {
   PFN_cuTensorMapEncodeTiled_v12000 encode;
@@ -412,7 +423,9 @@ struct HeadTiles {
   const float* row_lse;
   const float* row_grad;
   float* z_target;  // [rows_up]
-  float2* stats;    // [2 * tiles of the vocabulary][rows_up]: maximum, sum
+  // maximum and sum: [2 * tiles of the vocabulary][rows_up]; of few rows [head_few_ctas]
+  // [head_few_columns]
+  float2* stats;
   int64_t ld_stats;
   uint32_t* queue;
   uint32_t* err;

@@ -126,7 +126,11 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t k, bool backward) {
   L.packed = take(L.rows_up * L.ld_packed * 2);
   if (!backward) {
     L.z_target = take(L.rows_up * 4);
-    L.stats = take(2 * vt * L.rows_up * sizeof(float2));
+    const int64_t stats = rx::head_few_rows(rows, L.pieces)
+                              ? int64_t{rx::head_few_ctas(static_cast<int>(vocab), rx::device_sms())} *
+                                    rx::head_few_columns(rows)
+                              : 2 * vt * L.rows_up;
+    L.stats = take(stats * sizeof(float2));
   } else {
     L.row_lse = take(L.rows_up * 4);
     L.row_grad = take(L.rows_up * 4);
