@@ -22,8 +22,8 @@
 // G is rounded to bf16 (by up to 2^-8 of each term, as the products take them: 999 x
 // 50001 x 2048, gradients in bf16 off by 2.37e-3 of their norm, their own rounding alone
 // by 1.66e-3); z, the sums of exponentials and all accumulators are fp32.  exp(z - m) is
-// taken as 2^(z c - m c), c = log2 e, with the rounding error of m c, the same for all
-// terms, put back at the end.
+// taken as 2^((z - m) c), c = log2 e: the difference is exact where it matters, however
+// large z and m are (z c - m c is off by the rounding of m c, 0.4 at m = 1e7).
 //
 // Bound: the tensor cores, in a loop of seconds under the card's power cap (1.37 kW).
 // 8192 rows x 16384 x 2048: the loss 329 us, 1.67 PFLOP/s (cuBLAS's product alone 307 at
@@ -67,7 +67,6 @@ static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint64_t kDrainNs = 1000000000ull;
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLn2 = 0.693147180559945309f;
 
 // kind::f16, bf16 operands, fp32 accumulator, M = N = 256; bits 15 and 16: A, B MN-major.
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) |
@@ -89,6 +88,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// (a - m) log2 e and (b - m) log2 e, two at a time.
+__device__ __forceinline__ float2 exponents(float a, float b, float m) {
+  float2 e;
+  asm("{\n\t.reg .b64 v, n, c;\n\t"
+      "mov.b64 v, {%2, %3};\n\t"
+      "mov.b64 n, {%4, %4};\n\t"
+      "mov.b64 c, {%5, %5};\n\t"
+      "add.rn.f32x2 v, v, n;\n\t"
+      "mul.rn.f32x2 v, v, c;\n\t"
+      "mov.b64 {%0, %1}, v;\n\t}"
+      : "=f"(e.x), "=f"(e.y)
+      : "f"(a), "f"(b), "f"(-m), "f"(kLog2e));
+  return e;
 }
 
 // A staged box added to global memory in fp32.
@@ -310,13 +324,15 @@ __device__ __forceinline__ void add_chunk(Stats& st, const float (&z)[32]) {
   for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], top[i + 4]);
   const float m = fmaxf(st.m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
   const float ref = safe_max(m);
-  const float mc = ref * kLog2e;
-  const float lost = __fmaf_rn(ref, kLog2e, -mc);  // exponents are too large by this
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) sum[i & 3] += exp2_fast(__fmaf_rn(z[i], kLog2e, -mc));
+  for (int i = 0; i < 32; i += 2) {
+    const float2 e = exponents(z[i], z[i + 1], ref);
+    sum[i & 3] += exp2_fast(e.x);
+    sum[(i + 1) & 3] += exp2_fast(e.y);
+  }
   const float chunk = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  st.s = __fmaf_rn(st.s, exp2_fast((st.m - ref) * kLog2e), __fmaf_rn(-lost * kLn2, chunk, chunk));
+  st.s = __fmaf_rn(st.s, exp2_fast((st.m - ref) * kLog2e), chunk);
   st.m = m;
 }
 
@@ -587,12 +603,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int warp_row = row - lane;
       const int col0 = t.col0 + half * 128;
       int target = -1;
-      float c_row = 0.f, lse_c = 0.f;
+      float c_row = 0.f, lse = 0.f;
       if (LOSS || t.kind == kGrad) {
         target = p.target[row] - (LOSS ? 0 : p.v_next);  // (rows up to whole tiles have one)
         if (!LOSS) {
           c_row = p.row_grad[row];
-          lse_c = p.row_lse[row] * kLog2e;
+          lse = p.row_lse[row];
         }
       }
       uint32_t tm = 0, release = 0;
@@ -678,10 +694,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int v = col0 + 32 * c;  // in the piece
           const uint32_t at = static_cast<uint32_t>(target - v);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float x = exp2_fast(__fmaf_rn(g[i], kLog2e, -lse_c));
-            x = at == static_cast<uint32_t>(i) ? x - 1.f : x;
-            g[i] = c_row * x;
+          for (int i = 0; i < 32; i += 2) {
+            const float2 e = exponents(g[i], g[i + 1], lse);
+            const float x[2] = {exp2_fast(e.x), exp2_fast(e.y)};
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+              g[i + b] = c_row * (at == static_cast<uint32_t>(i + b) ? x[b] - 1.f : x[b]);
           }
           if (p.v_next + v + 32 > p.vocab)  // zeros behind the last column
 #pragma unroll
@@ -881,7 +899,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   for (int i = threadIdx.x; i < NT; i += kFewThreads) {
     s_target[i] = p.target[i];  // (rows up to whole tiles have one)
     if (GRAD) {
-      s_lse[i] = p.row_lse[i] * kLog2e;
+      s_lse[i] = p.row_lse[i];
       s_grad[i] = p.row_grad[i];
     }
   }
@@ -1024,7 +1042,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       if constexpr (GRAD) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          float x = exp2_fast(__fmaf_rn(z[j], kLog2e, -s_lse[j]));
+          float x = exp2_fast((z[j] - s_lse[j]) * kLog2e);
           x = s_target[j] == v ? x - 1.f : x;
           if (mine) g_out[j * ld_g + v] = __float2bfloat16_rn(s_grad[j] * x);
         }
