@@ -66,6 +66,7 @@ constexpr int kSmemBytes = kStages * kStageBytes + kEpiWarps * kStaging + 512 + 
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one CTA");
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint64_t kDrainNs = 1000000000ull;
+constexpr float kLargest = 3.402823466e+38f;  // of fp32
 constexpr float kLog2e = 1.44269504088896341f;
 
 // kind::f16, bf16 operands, fp32 accumulator, M = N = 256; bits 15 and 16: A, B MN-major.
@@ -1003,7 +1004,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     if (!GRAD)
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        m[j] = -INFINITY;
+        m[j] = -kLargest;
         sum[j] = 0.f;
       }
     uint32_t acc_n = 0;
@@ -1050,7 +1051,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           if (s_target[j] == v) p.z_target[j] = z[j];
-          // the larger one is the new maximum
+          // the larger one is the new maximum, which is finite for z = -inf too (exp 0)
           const float d = z[j] - m[j], e = exp2_fast(-fabsf(d) * kLog2e);
           sum[j] = d > 0.f ? __fmaf_rn(sum[j], e, 1.f) : sum[j] + e;
           m[j] = fmaxf(m[j], z[j]);
