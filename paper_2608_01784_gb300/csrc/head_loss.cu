@@ -814,8 +814,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 // time by single CTAs (M = 128, N = NT; as many as give every CTA the same number of
 // tiles), and stream through a ring of nine or ten stages at HBM's rate.  A thread has one row of W and NT logits.  Loss: it keeps a maximum and a
 // sum for each of its columns over all of its tiles; the threads' are joined when the
-// tiles are done, the CTAs' by the last of them, both in a fixed order.  Gradient: G
-// of the whole vocabulary, 64 bytes of a row by a warp.
+// tiles are done, the CTAs' by the last of them, both in an order that depends neither on
+// NT nor on the column: four groups of them, each from front to back, then the first two,
+// the last two and both.  Gradient: G of the whole vocabulary, 64 bytes of a row by a
+// warp.
 // 32 x 65536 x 2048 with the packing of the rows: 54 us, W's bytes take 40; by pairs on 256
 // rows 69 (as long as 256 of them take).
 constexpr int kFewThreads = 192;  // TMA, MMA and four epilogue warps
@@ -1073,21 +1075,31 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   if constexpr (!GRAD) {
     auto merge = [](float2 a, float2 b) {
       const float mm = fmaxf(a.x, b.x), ref = safe_max(mm);
-      return make_float2(mm, a.y * exp2_fast((a.x - ref) * kLog2e) +
-                                 b.y * exp2_fast((b.x - ref) * kLog2e));
+      return make_float2(mm, __fmaf_rn(a.y, exp2_fast((a.x - ref) * kLog2e),
+                                       __fmul_rn(b.y, exp2_fast((b.x - ref) * kLog2e))));
+    };
+    // four groups by kShare lanes
+    constexpr int kShare = 128 / NT;
+    auto join = [&](auto of_group) {
+      const int g = static_cast<int>(threadIdx.x) % kShare * (4 / kShare);
+      float2 st = of_group(g);
+      if (kShare == 2) st = merge(st, of_group(g + 1));
+#pragma unroll
+      for (int o = 1; o < kShare; o *= 2)
+        st = merge(st, make_float2(__shfl_down_sync(0xffffffffu, st.x, o),
+                                   __shfl_down_sync(0xffffffffu, st.y, o)));
+      return st;
     };
     if (!*abort_flag) {
-      // 128 threads' sums of a column by 128 / NT threads, then by lanes
+      // 128 threads' sums of a column by 128 / NT threads
       const float2* part = reinterpret_cast<const float2*>(smem);
-      constexpr int kShare = 128 / NT;
       if (threadIdx.x < 128) {
         const int j = threadIdx.x / kShare, g = threadIdx.x % kShare;
-        float2 st = make_float2(-INFINITY, 0.f);
-        for (int i = 0; i < NT; ++i) st = merge(st, part[j * kHalf + ((g * NT + i) ^ j)]);
-#pragma unroll
-        for (int o = kShare / 2; o > 0; o >>= 1)
-          st = merge(st, make_float2(__shfl_down_sync(0xffffffffu, st.x, o),
-                                     __shfl_down_sync(0xffffffffu, st.y, o)));
+        const float2 st = join([&](int group) {
+          float2 a = make_float2(-INFINITY, 0.f);
+          for (int i = 0; i < 32; ++i) a = merge(a, part[j * kHalf + ((group * 32 + i) ^ j)]);
+          return a;
+        });
         if (g == 0) p.stats[blockIdx.x * NT + j] = st;
       }
     }
@@ -1098,16 +1110,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     __syncthreads();
     if (*s_last && threadIdx.x < 128) {
       __threadfence();
-      constexpr int kShare = 128 / NT;
       const int live = min(max(*p.live, 0), p.rows);
       const int j = threadIdx.x / kShare, g = threadIdx.x % kShare;
-      float2 st = make_float2(-INFINITY, 0.f);
+      const float2 st = join([&](int group) {
+        float2 a = make_float2(-INFINITY, 0.f);
 #pragma unroll 8
-      for (unsigned c = g; c < gridDim.x; c += kShare) st = merge(st, __ldcg(p.stats + c * NT + j));
-#pragma unroll
-      for (int o = kShare / 2; o > 0; o >>= 1)
-        st = merge(st, make_float2(__shfl_down_sync(0xffffffffu, st.x, o),
-                                   __shfl_down_sync(0xffffffffu, st.y, o)));
+        for (unsigned c = group; c < gridDim.x; c += 4) a = merge(a, __ldcg(p.stats + c * NT + j));
+        return a;
+      });
       if (g == 0 && j < live) {
         const float ln = logf(st.y), mm = safe_max(st.x);
         const int r = p.row[j];
