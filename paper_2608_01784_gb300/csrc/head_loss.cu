@@ -604,10 +604,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int warp_row = row - lane;
       const int col0 = t.col0 + half * 128;
       int target = -1;
+      bool counted = false;  // else its weight is 0, even against weights that are infinite
       float c_row = 0.f, lse = 0.f;
       if (LOSS || t.kind == kGrad) {
-        target = p.target[row] - (LOSS ? 0 : p.v_next);  // (rows up to whole tiles have one)
+        target = p.target[row];  // (rows up to whole tiles have one)
         if (!LOSS) {
+          counted = target >= 0;
+          target -= p.v_next;
           c_row = p.row_grad[row];
           lse = p.row_lse[row];
         }
@@ -702,10 +705,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int b = 0; b < 2; ++b)
               g[i + b] = c_row * (at == static_cast<uint32_t>(i + b) ? x[b] - 1.f : x[b]);
           }
-          if (p.v_next + v + 32 > p.vocab)  // zeros behind the last column
+          const int left = counted ? p.vocab - (p.v_next + v) : 0;
+          if (left < 32)  // zeros behind the last column
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (p.v_next + v + i >= p.vocab) g[i] = 0.f;
+              if (i >= left) g[i] = 0.f;
           if ((c & 1) == 0) box_free();
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -1047,7 +1051,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         for (int j = 0; j < NT; ++j) {
           float x = exp2_fast((z[j] - s_lse[j]) * kLog2e);
           x = s_target[j] == v ? x - 1.f : x;
-          if (mine) g_out[j * ld_g + v] = __float2bfloat16_rn(s_grad[j] * x);
+          x = s_target[j] < 0 ? 0.f : s_grad[j] * x;  // (W may be infinite)
+          if (mine) g_out[j * ld_g + v] = __float2bfloat16_rn(x);
         }
       } else if (mine) {
 #pragma unroll
