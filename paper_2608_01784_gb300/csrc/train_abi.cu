@@ -108,7 +108,8 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t k, bool backward) {
     // pieces of G of up to 512 MB, two of them: 8192 rows x 131072 x 2048 11.11 ms in pieces of
     // 128 MB, 10.95 of 256, 10.85 of 512 (fewer launches, each with a tail; pieces that fit
     // the L2, 32 and 64 MB, take longer)
-    const int64_t most = std::max<int64_t>(1, (int64_t{512} << 20) / (L.rows_up * kHeadTile * 2));
+    const int64_t column = std::max<int64_t>(1, L.rows_up) * kHeadTile * 2;  // of tiles: bytes
+    const int64_t most = std::max<int64_t>(1, (int64_t{512} << 20) / column);
     L.piece_tiles = static_cast<int>(std::min(most, vt));
     L.pieces = static_cast<int>((vt + L.piece_tiles - 1) / L.piece_tiles);
     L.n_queue = L.pieces + 1;
