@@ -38,6 +38,20 @@ bool matrix_ok(const Matrix& m, int64_t cols, size_t es) {
   return m.p != nullptr && aligned(m.p, es) && m.ld >= cols;
 }
 
+// Whether two matrices share bytes. Rows of one pitch may lie between one another (halves
+// of wider rows); ranges of different pitches that cross count as shared.
+bool overlap(const Matrix& a, size_t es_a, const Matrix& b, size_t es_b, int64_t rows,
+             int64_t cols) {
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+  const uint64_t pitch_a = a.ld * es_a, pitch_b = b.ld * es_b;
+  const uint64_t row_a = cols * es_a, row_b = cols * es_b;
+  if (pa + (rows - 1) * pitch_a + row_a <= pb || pb + (rows - 1) * pitch_b + row_b <= pa)
+    return false;
+  if (pitch_a != pitch_b) return true;
+  const uint64_t off = pb >= pa ? (pb - pa) % pitch_a : (pitch_a - (pa - pb) % pitch_a) % pitch_a;
+  return off < row_a || off + row_b > pitch_a;
+}
+
 bool norm_ok(int32_t dtype, const Matrix& h, const Matrix& y, const void* w_after,
              const Matrix& gate, const void* w_before, float scale, float eps, int64_t rows,
              int32_t d) {
@@ -463,6 +477,8 @@ int reflex_head_loss_backward(const void* hidden, int64_t ld_hidden, const void*
   const HeadLayout L = head_layout(rows, vocab, k, true);
   if (workspace == nullptr || ws_bytes < L.total || !aligned(workspace, kAlign))
     return REFLEX_EWORKSPACE;
+  // (the weights are still read while their gradient is written)
+  if (d_w != nullptr && overlap({w, ldw}, 2, {d_w, ld_d_w}, es_w, vocab, k)) return REFLEX_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (rows == 0) {
     if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));

@@ -331,6 +331,19 @@ def _gradient(out, rows: int, cols: int, device, stream, what: str):
     return out, ld
 
 
+def _overlap(a: torch.Tensor, lda: int, b: torch.Tensor, ldb: int) -> bool:
+    """Whether two matrices of one shape share bytes (as reflex_head_loss_backward has it:
+    rows of one stride may lie between one another, ranges of different ones that cross
+    count as shared)."""
+    rows, cols = a.shape
+    (pa, pitch, wa), (pb, other, wb) = ((t.data_ptr(), ld * t.element_size(), cols * t.element_size())
+                                        for t, ld in ((a, lda), (b, ldb)))
+    if pa + (rows - 1) * pitch + wa <= pb or pb + (rows - 1) * other + wb <= pa:
+        return False
+    off = (pb - pa) % pitch
+    return pitch != other or off < wa or off + wb > pitch
+
+
 def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
                        lse: torch.Tensor, grad: torch.Tensor, *,
                        d_hidden: torch.Tensor | None = None,
@@ -339,7 +352,8 @@ def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torc
                        stream=None):
     """reflex_head_loss_backward: the gradients (of hidden, of weight) from grad fp32
     [rows], that of each row's loss, and head_loss's lse.  They come in bf16, or in the
-    type of `d_hidden` and `d_weight` (fp32 or bf16); the one that is not needed is None."""
+    type of `d_hidden` and `d_weight` (fp32 or bf16); the one that is not needed is None.
+    `d_hidden` may be hidden; `d_weight` shares no bytes with weight."""
     rows, vocab, k, ld_hidden, ldw = _head(hidden, weight, targets, status)
     dev = hidden.device
     _rows(lse, rows, torch.float32, dev, "lse")
@@ -353,9 +367,10 @@ def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torc
         d_hidden, ld_dh = _gradient(d_hidden, rows, k, dev, stream, "d_hidden")
         dt_h = _DTYPES[d_hidden.dtype]
     if need_weight:
-        if d_weight is not None and d_weight.data_ptr() == weight.data_ptr():
-            raise ValueError("d_weight: the weights are still read while it is written")
+        given = d_weight is not None
         d_weight, ld_dw = _gradient(d_weight, vocab, k, dev, stream, "d_weight")
+        _want(not given or not _overlap(weight, ldw, d_weight, ld_dw),
+              "d_weight: the weights are still read while it is written")
         dt_w = _DTYPES[d_weight.dtype]
     ws_bytes = B.reflex_head_loss_backward_workspace_size(rows, vocab, k)
     _want(ws_bytes > 0, "unsupported sizes")
