@@ -493,7 +493,9 @@ __global__ void __launch_bounds__(cta_threads(TPR), 512 / cta_threads(TPR))
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) sum_a[i] = sum_b[i] = f2(0.f);
   for (int64_t t = at.first; t - at.in_warp < p.rows; t += at.step) {
-    if (TPR == 0 && t >= p.rows) s.d = 0;
+    // a row of zeros behind the last one stays out of the sums: with eps = 0 its r is infinite
+    const bool live = TPR != 0 || t < p.rows;
+    if (!live) s.d = 0;
     in.wait();
     Raw<Te, N> y_raw, g;
     F2 y[N / 2];  // y r(y)
@@ -510,7 +512,7 @@ __global__ void __launch_bounds__(cta_threads(TPR), 512 / cta_threads(TPR))
         for (int i = 0; i < N / 2; ++i) q2 = fma(y[i], y[i], q2);
         float q[1] = {total(q2)};
         at.sum(q);
-        ry = rsqrtf(__fmaf_rn(q[0], inv_d, p.eps));
+        ry = live ? rsqrtf(__fmaf_rn(q[0], inv_d, p.eps)) : 0.f;
         const F2 r = f2(ry);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) y[i] = mul(y[i], r);
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(cta_threads(TPR), 512 / cta_threads(TPR))
       }
       float q[2] = {total(qo), total(qv)};
       at.sum(q);
-      const float ro1 = rsqrtf(__fmaf_rn(q[0], inv_d, p.eps));
+      const float ro1 = live ? rsqrtf(__fmaf_rn(q[0], inv_d, p.eps)) : 0.f;
       const F2 ro = f2(ro1), m = f2(-(q[1] * inv_d * ro1 * ro1));
       Raw<Te, N> d_out;
       if (p.d_out) in.read(2, s, d_out);
