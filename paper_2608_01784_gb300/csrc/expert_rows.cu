@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kPlanWarps = 16;
 constexpr int kPlanThreads = 32 * kPlanWarps;
+constexpr int kPlanExperts = 1024;  // at most
 constexpr int kPlanPairs = 2 * kPlanThreads;  // pairs of a CTA, at least
 
 // The expert of pair i, -1 for an unused or refused slot.
@@ -80,7 +81,7 @@ __global__ void __launch_bounds__(kPlanThreads)
   }
 }
 
-// Exclusive scan over E <= 1024 values in shared memory, two to a thread; returns the sum.
+// Exclusive scan over E <= kPlanExperts values in shared memory, two to a thread; returns the sum.
 __device__ int scan_experts(int32_t* v, int E, int32_t* s_warp) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int i = 2 * threadIdx.x;
@@ -463,11 +464,11 @@ cudaError_t launch_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, 
   const size_t place_smem = count_smem + 2 * static_cast<size_t>(E) * 4;
   cudaError_t e;
   if (place_smem > 48 * 1024) {
-    e = cudaFuncSetAttribute(plan_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(count_smem));
+    // as much as any plan needs, so that no call lowers what another is about to launch with
+    static std::atomic<uint64_t> count_done{0}, place_done{0};
+    e = allow_smem(plan_count_kernel, size_t{kPlanWarps} * kPlanExperts * 4, count_done);
     if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(place_smem));
+      e = allow_smem(plan_place_kernel, size_t{kPlanWarps + 2} * kPlanExperts * 4, place_done);
     if (e != cudaSuccess) return e;
   }
   if (nblk > 1) {
