@@ -57,6 +57,8 @@ def _norms(layers: list, d: int, final_norm) -> list | None:
     for n in norms:
         if not set(n) <= {"w_before", "w_after", "gate", "scale"}:
             raise ValueError("norms: w_before, w_after, gate and scale")
+        if n.get("w_before") is None:
+            raise ValueError("norms: w_before is needed")
         _check(n["w_before"], (d,), "w_before", dev)
         for name in ("w_after", "gate"):
             if n.get(name) is not None:
