@@ -408,10 +408,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     t = Tile{a.x, a.y, a.z, a.w, b.x, b.y};
     return true;
   };
-  // The calling thread has used it.  Relaxed: a release would wait until the thread's
-  // stores of the last tile's results have reached L2.
-  auto job_read = [&](uint32_t n) {
-    mbar_arrive_cluster_relaxed(map_to_rank(smem_addr(&job_empty[n % kJobs]), 0));
+  // The calling thread has read it (not the end, behind which no slot is written).  Relaxed:
+  // a release would wait until the thread's stores of the last tile's results have reached
+  // L2, and its fence alone takes the MMAs 3 %.  The slot is written again only behind this
+  // arrival, which depends on words of both of next_job's loads (kb0 <= kb1 in every
+  // tile), so that neither load can be under way still.
+  auto job_read = [&](uint32_t n, const Tile& t) {
+    if (t.kind >= 0 && t.kb0 <= t.kb1)
+      mbar_arrive_cluster_relaxed(map_to_rank(smem_addr(&job_empty[n % kJobs]), 0));
   };
   auto give_up = [&](bool timeout) {
     if (timeout && !*abort_flag) set_err(p.err, kErrTimeout);
@@ -448,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = false;
           break;
         }
-        if (t.kind >= 0) job_read(n);
+        job_read(n, t);
       }
       if (t.kind < 0) break;
       const int ra = t.row0 + static_cast<int>(rank) * kHalf;
@@ -515,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       if (t.kind < 0) break;
-      job_read(n);
+      job_read(n, t);
       const bool a_mn = !LOSS && t.kind == kWeight, b_mn = !LOSS && t.kind >= kHidden;
       const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
       // 16 along the reduction: 32 bytes of a row, or 16 rows of 128 bytes
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       if (t.kind < 0) break;
-      if (lane == 0) job_read(n);
+      if (lane == 0) job_read(n, t);
       const int row = t.row0 + static_cast<int>(rank) * kHalf + quarter * 32 + lane;
       const int warp_row = row - lane;
       const int col0 = t.col0 + half * 128;
