@@ -631,7 +631,8 @@ int reflex_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, int32_t 
  * reflex_expert_rows — tokens to their experts: rows[row_of[t, j]] = x[t].
  *   x         [T, d] (ldx); rows [cap_rows, d] (ldr).  Rows without a pair are
  *             left as they are.  row_of outside [0, cap_rows) is an unused slot.
- * Its gradient is reflex_expert_combine with alpha == NULL and no residual.
+ * Its gradient is reflex_expert_combine with alpha == NULL and no residual.  In these
+ * calls d is at most 2^30 (above: REFLEX_EUNSUPPORTED).
  */
 int reflex_expert_rows(int32_t dtype, const void* x, int64_t ldx, const int32_t* row_of,
                        int64_t T, int32_t d, int32_t k_max, int64_t cap_rows, void* rows,

@@ -483,23 +483,25 @@ cudaError_t launch_expert_plan(const int32_t* ids, const int32_t* k, int64_t T, 
 
 cudaError_t launch_expert_rows(int dtype, const ExpertRowsArgs& p, int sms, cudaStream_t s) {
   const int es = dtype == 0 ? 4 : 2;
+  const int64_t row = int64_t{p.d} * es;  // bytes
   auto rows_on = [&](int bytes) {
-    return p.d * es % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.out, p.ldo, es);
+    return row % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.out, p.ldo, es);
   };
   if (rows_on(16))
-    return launch_rows<uint4>(p, p.x, p.ldx * es / 16, p.out, p.ldo * es / 16, p.d * es / 16, sms,
-                              s);
+    return launch_rows<uint4>(p, p.x, p.ldx * es / 16, p.out, p.ldo * es / 16,
+                              static_cast<int>(row / 16), sms, s);
   if (rows_on(4))
-    return launch_rows<uint32_t>(p, p.x, p.ldx * es / 4, p.out, p.ldo * es / 4, p.d * es / 4, sms,
-                                 s);
+    return launch_rows<uint32_t>(p, p.x, p.ldx * es / 4, p.out, p.ldo * es / 4,
+                                 static_cast<int>(row / 4), sms, s);
   return launch_rows<unsigned short>(p, p.x, p.ldx, p.out, p.ldo, p.d, sms, s);
 }
 
 cudaError_t launch_expert_combine(int dtype, const ExpertRowsArgs& p, bool backward, int sms,
                                   cudaStream_t s) {
   const int es = dtype == 0 ? 4 : 2;
+  const int64_t row = int64_t{p.d} * es;  // bytes
   auto rows_on = [&](int bytes) {
-    return p.d * es % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.rows, p.ldr, es) &&
+    return row % bytes == 0 && on(bytes, p.x, p.ldx, es) && on(bytes, p.rows, p.ldr, es) &&
            on(bytes, p.out, p.ldo, es);
   };
   auto go = [&](auto combine, auto gradient) {

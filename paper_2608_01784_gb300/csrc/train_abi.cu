@@ -71,6 +71,7 @@ bool plan_ok(int64_t T, int32_t E, int32_t k_max) {
   return T >= 0 && E >= 1 && E <= 1024 && k_max >= 1 && k_max <= 32 &&
          T <= (int64_t{1} << 30) / k_max;
 }
+constexpr int32_t kRowMost = 1 << 30;  // columns of a row: what lies a few steps on fits 31 bits
 bool rows_ok(int32_t dtype, int64_t T, int32_t d, int32_t k_max, int64_t cap_rows) {
   return dtype_ok(dtype) && d >= 1 && plan_ok(T, 1, k_max) && cap_rows >= 0 &&
          cap_rows <= INT32_MAX;
@@ -334,6 +335,7 @@ int reflex_expert_rows(int32_t dtype, const void* x, int64_t ldx, const int32_t*
                        int64_t ldr, void* stream) {
   if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
   if (T == 0 || cap_rows == 0) return REFLEX_OK;
+  if (d > kRowMost) return REFLEX_EUNSUPPORTED;
   const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
   if (!matrix_ok({x, ldx}, d, es) || !matrix_ok({rows, ldr}, d, es) || row_of == nullptr ||
       !aligned(row_of, 4))
@@ -358,6 +360,7 @@ int reflex_expert_combine(int32_t dtype, const void* rows, int64_t ldr, const fl
                           void* stream) {
   if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
   if (T == 0) return REFLEX_OK;
+  if (d > kRowMost) return REFLEX_EUNSUPPORTED;
   const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
   if (!matrix_ok({out, ldo}, d, es) || (cap_rows > 0 && !matrix_ok({rows, ldr}, d, es)) ||
       (residual != nullptr && !matrix_ok({residual, ldres}, d, es)) || row_of == nullptr ||
@@ -388,6 +391,7 @@ int reflex_expert_combine_backward(int32_t dtype, const void* d_out, int64_t ld_
                                    float* d_alpha, void* stream) {
   if (!rows_ok(dtype, T, d, k_max, cap_rows)) return REFLEX_EINVAL;
   if (T == 0) return REFLEX_OK;
+  if (d > kRowMost) return REFLEX_EUNSUPPORTED;
   const size_t es = dtype == REFLEX_DTYPE_F32 ? 4 : 2;
   if (!matrix_ok({d_out, ld_d_out}, d, es) || alpha == nullptr || row_of == nullptr ||
       (d_rows == nullptr && d_alpha == nullptr) || !aligned(row_of, 4) || !aligned(alpha, 4) ||
