@@ -13,6 +13,9 @@ from . import _binding as B
 from .fp8 import _DTYPES, _matrix, _new, _status_word, _want
 
 
+_MOST = 2 ** 31 - 1  # of a size that the library takes in 32 bits
+
+
 def _here(device):
     """A launch goes to the current device; tensors of another one are refused."""
     if device.index != B.current_device():
@@ -47,8 +50,8 @@ def _vector(t: torch.Tensor | None, d: int, x: torch.Tensor, what: str):
 def _norm_inputs(h, y, w_after, w_before, gate):
     """Checks them; (rows, d, ldh, ldy, ldg)."""
     rows, d, ldh = _matrix(h, "h", _DTYPES)
-    if d < 1:
-        raise ValueError("h: at least one column")
+    if not 1 <= d <= _MOST:
+        raise ValueError("h: no columns, or an unsupported width")
     _here(h.device)
     if y is not None:
         ldy = _like(y, h, "y")
@@ -128,7 +131,8 @@ class ExpertPlan:
 
     def __init__(self, T: int, E: int, k_max: int, cap_rows: int, device, stream=None):
         self.T, self.E, self.k_max, self.cap_rows = T, E, k_max, cap_rows
-        self.ws_bytes = B.reflex_expert_plan_workspace_size(T, E, k_max)
+        fits = E <= _MOST and k_max <= _MOST
+        self.ws_bytes = B.reflex_expert_plan_workspace_size(T, E, k_max) if fits else 0
         if self.ws_bytes == 0:
             raise ValueError("unsupported shape: E up to 1024, k_max up to 32")
         # the workspace, then row_of, counts, offsets and the error word
@@ -186,9 +190,9 @@ def expert_plan(ids: torch.Tensor, *, E: int, k: torch.Tensor | None = None,
 def _pair_rows(rows: torch.Tensor, plan: ExpertPlan, what: str):
     """(d, row stride) of the pairs' rows of a plan."""
     n, d, ld = _matrix(rows, what, _DTYPES)
-    if n < plan.cap_rows or d < 1 or rows.device != plan.device:
-        raise ValueError(f"{what}: fewer rows than the plan's cap_rows, no columns, or another "
-                         "device")
+    if n < plan.cap_rows or not 1 <= d <= _MOST or rows.device != plan.device:
+        raise ValueError(f"{what}: fewer rows than the plan's cap_rows, no columns or too many, or "
+                         "another device")
     _here(plan.device)
     return d, ld
 
@@ -282,6 +286,7 @@ def _head(hidden, weight, targets, status):
     vocab, kw, ldw = _matrix(weight, "weight", _BF16)
     if k < 1 or vocab < 1 or kw != k:
         raise ValueError("hidden and weight disagree on their columns, or have none")
+    _want(max(rows, vocab, k) <= _MOST, "unsupported sizes")
     if vocab == 1:
         ldw = -(-k // 8) * 8
     if ldw % 8 or weight.data_ptr() % 16:
