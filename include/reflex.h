@@ -691,10 +691,11 @@ int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64
 /*
  * reflex_head_loss_backward — its gradients from grad[r], the gradient of loss[r] (that
  * of a mean is 1 / rows, of a weighted loss the weight), and the forward call's lse:
- *   G[r, v] = grad[r] (exp(z[r, v] - lse[r]) - [v == targets[r]]),  in bf16
+ *   G[r, v] = grad[r] (exp(z[r, v] - lse[r]) - [v == targets[r]])
  *   d_hidden = G w  [rows, k], zeros in rows left out;  d_w = G^T hidden  [vocab, k]
- * with sums in fp32.  The logits are computed again, a piece of the vocabulary at a
- * time.
+ * with sums in fp32, of terms of which G is rounded to bf16, but for those of the targets
+ * (in d_w those of a token's first four rows), which are taken in fp32.  The logits are
+ * computed again, a piece of the vocabulary at a time.
  *   lse, grad [rows] fp32, of rows with a target.
  *   d_hidden, d_w  fp32 or bf16 by their dtype argument, any strides; either may be
  *             NULL (not wanted).  Rows of d_w on 16-byte boundaries are stored fastest.

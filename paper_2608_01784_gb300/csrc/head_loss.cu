@@ -9,7 +9,7 @@
 // two accumulators of 256 columns in all of TMEM), fed by TMA through a ring of six
 // stages of 64 along the reduction:
 //   loss    z tile -> each thread has a row of 128 columns in fp32, of which it leaves
-//           the maximum, the sum of exponentials and, where it has it, the target's z;
+//           the maximum and the sum of exponentials;
 //   grad    z tile -> G in bf16, a piece of the vocabulary at a time (MN-major operands
 //           of the next two, straight from row-major memory);
 //   hidden  G W of a part of the piece, added in fp32 where the last piece left off;
@@ -19,11 +19,17 @@
 // one tail; pairs take tiles from a queue, the long ones first.  Every tile is summed
 // by one pair in one order, wherever it runs: results do not depend on timing.
 //
-// G is rounded to bf16 (by up to 2^-8 of each term, as the products take them: 999 x
-// 50001 x 2048, gradients in bf16 off by 2.37e-3 of their norm, their own rounding alone
-// by 1.66e-3); z, the sums of exponentials and all accumulators are fp32.  exp(z - m) is
-// taken as 2^((z - m) c), c = log2 e: the difference is exact where it matters, however
-// large z and m are (z c - m c is off by the rounding of m c, 0.4 at m = 1e7).
+// A row's logit of its target is the one that its loss and its largest term of G depend
+// on most, so it is added up in fp32 by itself (head_rows_kernel) and stands in its tile
+// instead of the tensor cores' sum.  G is rounded to bf16, by up to 2^-8 of each term, as
+// the products take it; what that takes from the target's term is added in fp32 where the
+// gradients are put together (to the weights of a token for its first four rows, behind
+// which roundings average out).  999 x 50001 x 2048: gradients in bf16 are off by 1.66e-3
+// of their norm, as much as their own rounding, and were by 2.37e-3 without; a few rows,
+// or rows of one weight, by up to 4e-3.  z, the sums of exponentials and all accumulators
+// are fp32.  exp(z - m) is taken as 2^((z - m) c), c = log2 e: the difference is exact
+// where it matters, however large z and m are (z c - m c is off by the rounding of m c,
+// 0.4 at m = 1e7).
 //
 // Bound: the tensor cores, in a loop of seconds under the card's power cap (1.37 kW).
 // 8192 rows x 16384 x 2048: the loss 329 us, 1.67 PFLOP/s (cuBLAS's product alone 307 at
@@ -54,6 +60,7 @@ constexpr int kStageBytes = 2 * kOperand;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kStaging = 32 * 128;  // of an epilogue warp
+constexpr int kOwn = 4;  // rows of a token whose term its weights' gradient has in fp32
 constexpr int kJobs = 4;            // tiles that are known ahead
 // Stages whose products the tensor cores add by themselves in a tile of logits.  They cut
 // sums instead of rounding them, always downwards in magnitude: over the 2048 of a row
@@ -106,6 +113,12 @@ __device__ __forceinline__ float2 exponents(float a, float b, float m) {
   return e;
 }
 
+// What rounding takes from a term of G (0 where that would not be a number).
+__device__ __forceinline__ float lost_in_bf16(float x) {
+  const float g = __bfloat162float(__float2bfloat16_rn(x));
+  return fabsf(g) < INFINITY ? x - g : 0.f;
+}
+
 // A staged box added to global memory in fp32.
 __device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
   asm volatile(
@@ -116,13 +129,41 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src,
 
 // ---- rows that count ----------------------------------------------------------
 constexpr int kRowsThreads = 256;
+constexpr int kRowsAhead = 2;  // vectors of a thread that are on their way early
+
+// Eight products of bf16, added in their order.
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s = __fmaf_rn(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+    s = __fmaf_rn(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+  }
+  return s;
+}
+// The vector of a row from column c on, zeros behind its end.
+__device__ __forceinline__ uint4 vector_at(const __nv_bfloat16* row, int c, int k, bool vec) {
+  if (vec && c + 8 <= k) return *reinterpret_cast<const uint4*>(row + c);
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto* at = reinterpret_cast<const uint16_t*>(row) + c + 2 * i;
+    const uint32_t lo = c + 2 * i < k ? at[0] : 0u, hi = c + 2 * i + 1 < k ? at[1] : 0u;
+    v[i] = lo | hi << 16;
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 
 // Each CTA counts the rows in front of its own by itself (the targets of a batch are
-// few bytes), so that packing them takes one launch.
+// few bytes), so that packing them takes one launch.  A row's logit of its target, which
+// its loss and its largest term of G come from, is added up here, in fp32 and to the
+// nearest: by eights of columns, a lane's one after another, then the lanes'.
 __global__ void __launch_bounds__(kRowsThreads)
     head_rows_kernel(const HeadRows p, bool vec) {
   __shared__ int s_count[3][kRowsThreads / 32];
   __shared__ int s_at[kRowsThreads];
+  __shared__ float s_dot[kRowsAhead * kRowsThreads];
   grid_dep_wait();
   grid_dep_launch();
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -130,14 +171,16 @@ __global__ void __launch_bounds__(kRowsThreads)
   const int64_t lo = min(p.rows, blockIdx.x * per), hi = min(p.rows, lo + per);
   int before = 0, total = 0, wrong = 0;
   // a CTA's only row is on its way while it counts those in front
-  constexpr int kAhead = 2;  // vectors of a thread
-  const bool ahead = per == 1 && vec && p.k <= kAhead * kRowsThreads * 8;
-  uint4 row[kAhead];
-  if (ahead && lo < hi && p.targets[lo] >= 0)
+  const bool ahead = per == 1 && vec && p.k <= kRowsAhead * kRowsThreads * 8;
+  uint4 row[kRowsAhead], row_w[kRowsAhead];
+  const int target_lo = ahead && lo < hi ? p.targets[lo] : -1;
+  if (target_lo >= 0 && target_lo < p.vocab)
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
+    for (int i = 0; i < kRowsAhead; ++i) {
       const int c = (i * kRowsThreads + tid) * 8;
-      if (c < p.k) row[i] = *reinterpret_cast<const uint4*>(p.hidden + lo * p.ld_hidden + c);
+      if (c >= p.k) continue;
+      row[i] = *reinterpret_cast<const uint4*>(p.hidden + lo * p.ld_hidden + c);
+      row_w[i] = *reinterpret_cast<const uint4*>(p.w + target_lo * p.ldw + c);
     }
 #pragma unroll 4
   for (int64_t r = tid; r < p.rows; r += kRowsThreads) {
@@ -172,15 +215,27 @@ __global__ void __launch_bounds__(kRowsThreads)
     }
     for (int i = tid; i < p.n_queue; i += kRowsThreads) p.queue[i] = 0u;
   }
-  auto copy_row = [&](int64_t at, const __nv_bfloat16* from) {  // a warp; zeros from nullptr
+  // a warp: a row, and its share of the target's logit; zeros from nullptr
+  auto copy_row = [&](int64_t at, const __nv_bfloat16* from, const __nv_bfloat16* w) {
     __nv_bfloat16* to = p.packed + at * p.ld_packed;
-    if (vec) {
-      for (int c = lane * 8; c < p.k; c += 256)
-        *reinterpret_cast<uint4*>(to + c) =
-            from ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0u, 0u, 0u, 0u);
-    } else {
-      for (int c = lane; c < p.k; c += 32) to[c] = from ? from[c] : __float2bfloat16_rn(0.f);
+    float dot = 0.f;
+#pragma unroll 2
+    for (int c = lane * 8; c < p.k; c += 256) {
+      uint4 h = make_uint4(0u, 0u, 0u, 0u);
+      if (from != nullptr) {
+        h = vector_at(from, c, p.k, vec);
+        dot = __fadd_rn(dot, dot8(h, vector_at(w, c, p.k, true)));
+      }
+      *reinterpret_cast<uint4*>(to + c) = h;  // (rows hold whole vectors)
     }
+    return dot;
+  };
+  auto target_done = [&](int64_t at, int64_t r, float dot) {  // a warp
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if (lane != 0) return;
+    if (p.z_target != nullptr) p.z_target[at] = dot;
+    if (p.target_term != nullptr) p.target_term[at] = p.grad[r] * expm1f(dot - p.lse[r]);
   };
   for (int64_t r0 = lo; r0 < hi; r0 += kRowsThreads) {
     const int64_t r = r0 + tid;
@@ -212,25 +267,37 @@ __global__ void __launch_bounds__(kRowsThreads)
     }
     __syncthreads();
     if (ahead) {
-      if (s_at[0] >= 0)
+      const int64_t to = s_at[0];
+      if (to < 0) break;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int c = (i * kRowsThreads + tid) * 8;
-          if (c < p.k)
-            *reinterpret_cast<uint4*>(p.packed + s_at[0] * p.ld_packed + c) = row[i];
-        }
+      for (int i = 0; i < kRowsAhead; ++i) {
+        const int c = (i * kRowsThreads + tid) * 8;
+        if (c < p.k) *reinterpret_cast<uint4*>(p.packed + to * p.ld_packed + c) = row[i];
+        s_dot[i * kRowsThreads + tid] = c < p.k ? dot8(row[i], row_w[i]) : 0.f;
+      }
+      __syncthreads();
+      if (w == 0) {
+        float dot = 0.f;
+        for (int c = lane; c * 8 < p.k; c += 32) dot = __fadd_rn(dot, s_dot[c]);
+        target_done(to, r0, dot);
+      }
       break;
     }
     const int n = static_cast<int>(min(static_cast<int64_t>(kRowsThreads), hi - r0));
     for (int i = w; i < n; i += kRowsThreads / 32)
-      if (s_at[i] >= 0) copy_row(s_at[i], p.hidden + (r0 + i) * p.ld_hidden);
+      if (s_at[i] >= 0)
+        target_done(s_at[i], r0 + i,
+                    copy_row(s_at[i], p.hidden + (r0 + i) * p.ld_hidden,
+                             p.w + p.targets[r0 + i] * p.ldw));
   }
   // rows of zeros up to whole tiles
   const int64_t most = static_cast<int64_t>(total + p.tile - 1) / p.tile * p.tile;
   for (int64_t i = total + static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + w; i < most;
        i += static_cast<int64_t>(gridDim.x) * (kRowsThreads / 32)) {
-    copy_row(i, nullptr);
+    copy_row(i, nullptr, nullptr);
     if (lane == 0) {
+      if (p.z_target != nullptr) p.z_target[i] = 0.f;
+      if (p.target_term != nullptr) p.target_term[i] = 0.f;
       p.target[i] = -1;
       if (p.grad != nullptr) p.row_grad[i] = 0.f;
       if (p.lse != nullptr) p.row_lse[i] = 0.f;
@@ -609,14 +676,45 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int col0 = t.col0 + half * 128;
       int target = -1;
       bool counted = false;  // else its weight is 0, even against weights that are infinite
-      float c_row = 0.f, lse = 0.f;
+      float c_row = 0.f, lse = 0.f, of_target = 0.f;  // its logit, or its term of G
       if (LOSS || t.kind == kGrad) {
         target = p.target[row];  // (rows up to whole tiles have one)
+        of_target = LOSS ? p.z_target[row] : p.target_term[row];
         if (!LOSS) {
           counted = target >= 0;
           target -= p.v_next;
           c_row = p.row_grad[row];
           lse = p.row_lse[row];
+        }
+      }
+      // weight: rows whose target is this thread's, in their order, while the products run
+      int own[kOwn], n_own = 0;
+      if (!LOSS && t.kind == kWeight) {
+        constexpr int kAhead = 8;
+        const int v = p.v0 + row, v_warp = v - lane;
+        uint32_t open = 0xffffffffu;  // lanes that have fewer than kOwn
+        for (int r0 = 0; r0 < live && open != 0u; r0 += 32 * kAhead) {
+          int at[kAhead];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + 32 * u + lane;
+            at[u] = r < live ? p.target[r] : -1;
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            if (r0 + 32 * u >= live) break;
+            const uint32_t to = static_cast<uint32_t>(at[u] - v_warp);
+            uint32_t in = __ballot_sync(0xffffffffu, to < 32u && (open >> (to & 31u) & 1u));
+            for (; in != 0u; in &= in - 1u) {
+              const int j = __ffs(in) - 1;
+              if (__shfl_sync(0xffffffffu, at[u], j) != v || n_own == kOwn) continue;
+#pragma unroll
+              for (int q = 0; q < kOwn; ++q)
+                if (q == n_own) own[q] = r0 + 32 * u + j;
+              ++n_own;
+            }
+          }
+          open = __ballot_sync(0xffffffffu, n_own < kOwn);
         }
       }
       uint32_t tm = 0, release = 0;
@@ -651,8 +749,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (c == 3) hand_back();
       };
       // logits: a row of 128 columns, in parts of kLogitChunk stages
-      float sum[4][32];
       if (LOSS || t.kind == kGrad) {
+        float sum[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           load(c);
@@ -672,59 +770,56 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) give_up(true);
           break;
         }
-      }
-      if (LOSS) {
-        Stats st{-INFINITY, 0.f};
+        if (LOSS) {
+          Stats st{-INFINITY, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int v = col0 + 32 * c;
-          if (v + 32 > p.vocab)
+          for (int c = 0; c < 4; ++c) {
+            const int v = col0 + 32 * c;
+            const uint32_t at = static_cast<uint32_t>(target - v);
+            if (at < 32u)
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (v + i >= p.vocab) sum[c][i] = -INFINITY;
-          if (v < p.vocab) add_chunk(st, sum[c]);
-        }
+              for (int i = 0; i < 32; ++i)
+                sum[c][i] = at == static_cast<uint32_t>(i) ? of_target : sum[c][i];
+            if (v + 32 > p.vocab)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {  // (the target is on its way from L2 until here)
-          const uint32_t at = static_cast<uint32_t>(target - (col0 + 32 * c));
-          if (at < 32u) {
-            float zt = sum[c][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) zt = at == static_cast<uint32_t>(i) ? sum[c][i] : zt;
-            p.z_target[row] = zt;
+              for (int i = 0; i < 32; ++i)
+                if (v + i >= p.vocab) sum[c][i] = -INFINITY;
+            if (v < p.vocab) add_chunk(st, sum[c]);
           }
-        }
-        p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
-      } else if (t.kind == kGrad) {
+          p.stats[static_cast<int64_t>(col0 / 128) * p.ld_stats + row] = make_float2(st.m, st.s);
+        } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float (&g)[32] = sum[c];
-          const int v = col0 + 32 * c;  // in the piece
-          const uint32_t at = static_cast<uint32_t>(target - v);
+          for (int c = 0; c < 4; ++c) {
+            float (&g)[32] = sum[c];
+            const int v = col0 + 32 * c;  // in the piece
+            const uint32_t at = static_cast<uint32_t>(target - v);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float2 e = exponents(g[i], g[i + 1], lse);
-            const float x[2] = {exp2_fast(e.x), exp2_fast(e.y)};
+            for (int i = 0; i < 32; i += 2) {
+              const float2 e = exponents(g[i], g[i + 1], lse);
+              g[i] = c_row * exp2_fast(e.x);
+              g[i + 1] = c_row * exp2_fast(e.y);
+            }
+            const int left = counted ? p.vocab - (p.v_next + v) : 0;
+            if (left < 32)  // zeros behind the last column
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-              g[i + b] = c_row * (at == static_cast<uint32_t>(i + b) ? x[b] - 1.f : x[b]);
-          }
-          const int left = counted ? p.vocab - (p.v_next + v) : 0;
-          if (left < 32)  // zeros behind the last column
+              for (int i = 0; i < 32; ++i)
+                if (i >= left) g[i] = 0.f;
+            if (at < 32u)
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i >= left) g[i] = 0.f;
-          if ((c & 1) == 0) box_free();
+              for (int i = 0; i < 32; ++i)
+                g[i] = at == static_cast<uint32_t>(i) ? of_target : g[i];
+            if ((c & 1) == 0) box_free();
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            put((c & 1) * 4 + q, pack_bf16(g[8 * q], g[8 * q + 1]),
-                pack_bf16(g[8 * q + 2], g[8 * q + 3]), pack_bf16(g[8 * q + 4], g[8 * q + 5]),
-                pack_bf16(g[8 * q + 6], g[8 * q + 7]));
-          if (c & 1) {
-            box_filled();
-            if (lane == 0) {
-              tma_store_2d(&maps.g_out, stg_s, v - 32, warp_row);
-              bulk_commit();
+            for (int q = 0; q < 4; ++q)
+              put((c & 1) * 4 + q, pack_bf16(g[8 * q], g[8 * q + 1]),
+                  pack_bf16(g[8 * q + 2], g[8 * q + 3]), pack_bf16(g[8 * q + 4], g[8 * q + 5]),
+                  pack_bf16(g[8 * q + 6], g[8 * q + 7]));
+            if (c & 1) {
+              box_filled();
+              if (lane == 0) {
+                tma_store_2d(&maps.g_out, stg_s, v - 32, warp_row);
+                bulk_commit();
+              }
             }
           }
         }
@@ -781,6 +876,25 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) z[i] = 0.f;
           const int col = col0 + 32 * c;
+#pragma unroll
+          for (int q = 0; q < kOwn; ++q)
+            if (q < n_own) {
+              const float rest = lost_in_bf16(p.target_term[own[q]]);
+              const __nv_bfloat16* from = p.packed + own[q] * p.ld_packed + col;
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                if (col + 8 * x < p.k) {
+                  const uint4 h = *reinterpret_cast<const uint4*>(from + 8 * x);
+                  const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    float& lo = z[8 * x + 2 * i];
+                    float& hi = z[8 * x + 2 * i + 1];
+                    lo = __fmaf_rn(rest, __uint_as_float(w[i] << 16), lo);
+                    hi = __fmaf_rn(rest, __uint_as_float(w[i] & 0xffff0000u), hi);
+                  }
+                }
+            }
           if (p.dw_f32) {
             box_free();
 #pragma unroll
@@ -820,8 +934,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---- few rows -------------------------------------------------------------------
 // Up to NT (32 or 64) rows: W is what costs, so its rows are the tiles, up to 128 at a
 // time by single CTAs (M = 128, N = NT; as many as give every CTA the same number of
-// tiles), and stream through a ring of nine or ten stages at HBM's rate.  A thread has one row of W and NT logits.  Loss: it keeps a maximum and a
-// sum for each of its columns over all of its tiles; the threads' are joined when the
+// tiles), and stream through a ring of nine or ten stages at HBM's rate.  A thread has one
+// row of W and NT logits.  Loss: it keeps a maximum and a sum for each of its columns over
+// all of its tiles; the threads' are joined when the
 // tiles are done, the CTAs' by the last of them, both in an order that depends neither on
 // NT nor on the column: four groups of them, each from front to back, then the first two,
 // the last two and both.  Gradient: G of the whole vocabulary, 64 bytes of a row by a
@@ -834,7 +949,7 @@ struct Few {
   static constexpr int kWBytes = kHalf * 128;
   static constexpr int kStageBytes = kWBytes + NT * 128;
   static constexpr int kStages = NT == 32 ? 10 : 9;
-  static constexpr int kMisc = 512 + 3 * NT * 4;
+  static constexpr int kMisc = 512 + 4 * NT * 4;
   static constexpr int kSmem = kStages * kStageBytes + kMisc + 1024;
   static constexpr int kTmem = 2 * NT;
   static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
@@ -862,7 +977,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   int* s_last = reinterpret_cast<int*>(tmem_slot + 2);
   static_assert((2 * kRing + 5) * 8 + 12 <= 512, "barriers");
   int* s_target = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(bars) + 512);
-  float* s_lse = reinterpret_cast<float*>(s_target + NT);
+  float* s_of_target = reinterpret_cast<float*>(s_target + NT);
+  float* s_lse = s_of_target + NT;
   float* s_grad = s_lse + NT;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -909,6 +1025,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   grid_dep_launch();
   for (int i = threadIdx.x; i < NT; i += kFewThreads) {
     s_target[i] = p.target[i];  // (rows up to whole tiles have one)
+    s_of_target[i] = GRAD ? p.target_term[i] : p.z_target[i];
     if (GRAD) {
       s_lse[i] = p.row_lse[i];
       s_grad[i] = p.row_grad[i];
@@ -1053,15 +1170,15 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       if constexpr (GRAD) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          float x = exp2_fast((z[j] - s_lse[j]) * kLog2e);
-          x = s_target[j] == v ? x - 1.f : x;
-          x = s_target[j] < 0 ? 0.f : s_grad[j] * x;  // (W may be infinite)
+          float x = s_grad[j] * exp2_fast((z[j] - s_lse[j]) * kLog2e);
+          if (s_target[j] == v) x = s_of_target[j];
+          if (s_target[j] < 0) x = 0.f;  // (W may be infinite)
           if (mine) g_out[j * ld_g + v] = __float2bfloat16_rn(x);
         }
       } else if (mine) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          if (s_target[j] == v) p.z_target[j] = z[j];
+          if (s_target[j] == v) z[j] = s_of_target[j];
           // the larger one is the new maximum, which is finite for z = -inf too (exp 0)
           const float d = z[j] - m[j], e = exp2_fast(-fabsf(d) * kLog2e);
           sum[j] = d > 0.f ? __fmaf_rn(sum[j], e, 1.f) : sum[j] + e;
@@ -1175,12 +1292,15 @@ __global__ void __launch_bounds__(1024)
   loss[r] = (m - z_target[i]) + ln;  // (m is often the target's own logit)
 }
 
-// Dh of the rows that count, the sums of its parts in their order; zeros elsewhere.  A
-// thread has four columns of a row (ld_sums is a multiple of 32, so they are there).
+// Dh of the rows that count, the sums of its parts in their order and what rounding took
+// from the target's term; zeros elsewhere.  A thread has four columns of a row (ld_sums
+// is a multiple of 32, so they are there).
 template <typename Te>
 __global__ void __launch_bounds__(256)
     head_hidden_kernel(const float* __restrict__ sums, int64_t ld_sums, int64_t part_stride,
-                       int parts, const int* __restrict__ place, int64_t rows, int k,
+                       int parts, const int* __restrict__ place, const int* __restrict__ target,
+                       const float* __restrict__ target_term,
+                       const __nv_bfloat16* __restrict__ w, int64_t ldw, int64_t rows, int k,
                        Te* __restrict__ out, int64_t ldo, bool vec) {
   grid_dep_wait();
   grid_dep_launch();
@@ -1201,6 +1321,13 @@ __global__ void __launch_bounds__(256)
         f[1] += v.y;
         f[2] += v.z;
         f[3] += v.w;
+      }
+      const float rest = lost_in_bf16(target_term[at]);
+      const __nv_bfloat16* row = w + target[at] * ldw + c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = c + e < k ? to_f32(row[e]) : 0.f;
+        if (fabsf(x) < INFINITY) f[e] = __fmaf_rn(rest, x, f[e]);
       }
     }
     Te* to = out + r * ldo + c;
@@ -1302,7 +1429,7 @@ cudaError_t launch_head_loss(const HeadProblem& h, HeadTiles p, float* loss, flo
   if (e != cudaSuccess) return e;
   return launch_pdl(head_loss_kernel, dim3(static_cast<unsigned>((p.rows + 31) / 32)), dim3(1024),
                     0, stream, static_cast<const float2*>(p.stats), p.ld_stats, 2 * p.vt_next,
-                    p.live, p.row, static_cast<const float*>(p.z_target), loss, lse);
+                    p.live, p.row, p.z_target, loss, lse);
 }
 
 cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const HeadPieces& q,
@@ -1363,6 +1490,7 @@ cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const H
   if (q.sums == nullptr) return cudaSuccess;
   const int64_t ctas = std::min<int64_t>((rows * ((p.k + 3) / 4) + 255) / 256, int64_t{sms} * 16);
   const int es_h = d_hidden_f32 ? 4 : 2;
+  const auto* w = static_cast<const __nv_bfloat16*>(h.w);
   const bool vec = p.k % 4 == 0 && ld_d_hidden % 4 == 0 &&
                    reinterpret_cast<uintptr_t>(d_hidden) % (4 * es_h) == 0;
   // parts of the first piece; a shorter last piece adds to fewer of them
@@ -1372,10 +1500,12 @@ cudaError_t launch_head_loss_backward(const HeadProblem& h, HeadTiles p, const H
   if (d_hidden_f32)
     return launch_pdl(head_hidden_kernel<float>, dim3(static_cast<unsigned>(ctas)), dim3(256), 0,
                       stream, static_cast<const float*>(q.sums), p.ld_sums, stride, parts, place,
-                      rows, p.k, static_cast<float*>(d_hidden), ld_d_hidden, vec);
+                      p.target, p.target_term, w, h.ldw, rows, p.k,
+                      static_cast<float*>(d_hidden), ld_d_hidden, vec);
   return launch_pdl(head_hidden_kernel<__nv_bfloat16>, dim3(static_cast<unsigned>(ctas)),
                     dim3(256), 0, stream, static_cast<const float*>(q.sums), p.ld_sums, stride,
-                    parts, place, rows, p.k, static_cast<__nv_bfloat16*>(d_hidden), ld_d_hidden, vec);
+                    parts, place, p.target, p.target_term, w, h.ldw, rows, p.k,
+                    static_cast<__nv_bfloat16*>(d_hidden), ld_d_hidden, vec);
 }
 
 }  // namespace rx

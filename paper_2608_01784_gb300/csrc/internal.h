@@ -368,7 +368,8 @@ constexpr int kHeadFewRows = 64;  // as many rows or fewer go past W, not W past
 constexpr int kHeadGroup = 32;  // tiles of rows that stay in L2 while the weights pass by
 
 // The rows with a target in [0, vocab) to the front, zeros behind them up to whole
-// tiles; what the other kernels read of each.  Clears the queue and sets the error word.
+// tiles; what the other kernels read of each, its target's logit among it.  Clears the
+// queue and sets the error word.
 struct HeadRows {
   int64_t rows;
   int vocab, k;
@@ -384,6 +385,10 @@ struct HeadRows {
   int* target;  // [rows up to whole tiles], like the next two
   float* row_lse;
   float* row_grad;
+  const __nv_bfloat16* w;
+  int64_t ldw;
+  float* z_target;     // forward
+  float* target_term;  // backward
   int* place;  // [rows] nullable: row -> packed row or -1
   int* live;
   uint32_t* queue;
@@ -418,11 +423,14 @@ struct HeadTiles {
   int rows, vocab, k;
   int rows_up;  // rows up to whole tiles
   const int* live;
+  const __nv_bfloat16* packed;
+  int64_t ld_packed;
   const int* row;
   const int* target;
   const float* row_lse;
   const float* row_grad;
-  float* z_target;  // [rows_up]
+  const float* z_target;     // [rows_up] the target's logit
+  const float* target_term;  // [rows_up] G's term of the row's target, in fp32
   // maximum and sum: [2 * tiles of the vocabulary][rows_up]; of few rows [head_few_ctas]
   // [head_few_columns]
   float2* stats;

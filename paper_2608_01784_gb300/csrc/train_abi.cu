@@ -99,7 +99,7 @@ bool head_ok(const void* hidden, int64_t ld_hidden, const void* w, int64_t ldw,
 // What both directions keep of the rows that count.
 struct HeadLayout {
   size_t live, queue, row, target, packed, z_target, stats;  // forward
-  size_t row_lse, row_grad, place, g, sums;                  // backward
+  size_t row_lse, row_grad, target_term, place, g, sums;     // backward
   size_t total;
   int64_t rows_up, ld_packed, ld_sums;
   int n_queue, piece_tiles, pieces, part_blocks, parts;
@@ -150,6 +150,7 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t k, bool backward) {
   } else {
     L.row_lse = take(L.rows_up * 4);
     L.row_grad = take(L.rows_up * 4);
+    L.target_term = take(L.rows_up * 4);
     L.place = take(rows * 4);
     const int buffers = L.piece_tiles < vt ? 2 : 1;
     L.g = take(buffers * L.rows_up * L.piece_tiles * kHeadTile * 2);
@@ -163,9 +164,11 @@ T* at(void* ws, size_t offset) {
   return reinterpret_cast<T*>(static_cast<uint8_t*>(ws) + offset);
 }
 rx::HeadRows head_rows(const HeadLayout& L, void* ws, const void* hidden, int64_t ld_hidden,
-                       const int32_t* targets, int32_t rows, int32_t vocab, int32_t k,
-                       int32_t* dev_status) {
+                       const void* w, int64_t ldw, const int32_t* targets, int32_t rows,
+                       int32_t vocab, int32_t k, int32_t* dev_status) {
   rx::HeadRows r{};
+  r.w = static_cast<const __nv_bfloat16*>(w);
+  r.ldw = ldw;
   r.rows = rows;
   r.vocab = vocab;
   r.k = k;
@@ -191,6 +194,8 @@ rx::HeadTiles head_tiles(const HeadLayout& L, const rx::HeadRows& r) {
   t.k = r.k;
   t.rows_up = static_cast<int>(L.rows_up);
   t.live = r.live;
+  t.packed = r.packed;
+  t.ld_packed = r.ld_packed;
   t.row = r.row;
   t.target = r.target;
   t.queue = r.queue;
@@ -444,12 +449,13 @@ int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64
   if (encode == nullptr) return REFLEX_ECUDA;
   const int sms = rx::device_sms();
   rx::HeadRows r =
-      head_rows(L, workspace, hidden, ld_hidden, targets, rows, vocab, k, dev_status);
+      head_rows(L, workspace, hidden, ld_hidden, w, ldw, targets, rows, vocab, k, dev_status);
+  r.z_target = at<float>(workspace, L.z_target);
   r.loss_out = loss;
   r.lse_out = lse;
   RX_CUDA(rx::launch_head_rows(r, sms, s));
   rx::HeadTiles t = head_tiles(L, r);
-  t.z_target = at<float>(workspace, L.z_target);
+  t.z_target = r.z_target;
   t.stats = at<float2>(workspace, L.stats);
   t.ld_stats = L.rows_up;
   RX_CUDA(rx::launch_head_loss({encode, r.packed, L.ld_packed, w, ldw}, t, loss, lse, sms, s));
@@ -494,16 +500,18 @@ int reflex_head_loss_backward(const void* hidden, int64_t ld_hidden, const void*
   if (encode == nullptr) return REFLEX_ECUDA;
   const int sms = rx::device_sms();
   rx::HeadRows r =
-      head_rows(L, workspace, hidden, ld_hidden, targets, rows, vocab, k, dev_status);
+      head_rows(L, workspace, hidden, ld_hidden, w, ldw, targets, rows, vocab, k, dev_status);
   r.lse = lse;
   r.grad = grad;
   r.row_lse = at<float>(workspace, L.row_lse);
   r.row_grad = at<float>(workspace, L.row_grad);
+  r.target_term = at<float>(workspace, L.target_term);
   r.place = at<int>(workspace, L.place);
   RX_CUDA(rx::launch_head_rows(r, sms, s));
   rx::HeadTiles t = head_tiles(L, r);
   t.row_lse = r.row_lse;
   t.row_grad = r.row_grad;
+  t.target_term = r.target_term;
   t.dw = d_w;
   t.ld_dw = ld_d_w;
   t.dw_f32 = d_w_dtype == REFLEX_DTYPE_F32;
