@@ -941,8 +941,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 // NT nor on the column: four groups of them, each from front to back, then the first two,
 // the last two and both.  Gradient: G of the whole vocabulary, 64 bytes of a row by a
 // warp.
-// 32 x 65536 x 2048 with the packing of the rows: 54 us, W's bytes take 40; by pairs on 256
+// 32 x 65536 x 2048 with the packing of the rows: 57 us, W's bytes take 40; by pairs on 256
 // rows 69 (as long as 256 of them take).
+// Sums of 256 in the tensor cores, where larger calls have 512: with a row or two nothing
+// averages out what they cut (losses off by up to 2.8e-6 of themselves at K = 4096, and by
+// half of that here), and W's bytes hide most of it with eight accumulators to go round
+// (32 x 65536 x 2048: 55.2 -> 56.7 us; of 128 61.7).
+constexpr int kFewChunk = 4;
 constexpr int kFewThreads = 192;  // TMA, MMA and four epilogue warps
 template <int NT>
 struct Few {
@@ -951,7 +956,9 @@ struct Few {
   static constexpr int kStages = NT == 32 ? 10 : 9;
   static constexpr int kMisc = 512 + 4 * NT * 4;
   static constexpr int kSmem = kStages * kStageBytes + kMisc + 1024;
-  static constexpr int kTmem = 2 * NT;
+  static constexpr int kAcc = 8;  // accumulators
+  static constexpr int kTmem = kAcc * NT;
+  static_assert(kTmem <= 512, "columns of TMEM");
   static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
   static_assert(kHalf * NT * 8 <= kStages * kStageBytes, "the threads' sums go into the ring");
 };
@@ -970,12 +977,12 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint64_t* full = bars;
   uint64_t* empty = full + kRing;
   uint64_t* acc_full = empty + kRing;
-  uint64_t* acc_empty = acc_full + 2;
-  uint64_t* drain = acc_empty + 2;
+  uint64_t* acc_empty = acc_full + F::kAcc;
+  uint64_t* drain = acc_empty + F::kAcc;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_last = reinterpret_cast<int*>(tmem_slot + 2);
-  static_assert((2 * kRing + 5) * 8 + 12 <= 512, "barriers");
+  static_assert((2 * kRing + 2 * F::kAcc + 1) * 8 + 12 <= 512, "barriers");
   int* s_target = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(bars) + 512);
   float* s_of_target = reinterpret_cast<float*>(s_target + NT);
   float* s_lse = s_of_target + NT;
@@ -990,7 +997,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < F::kAcc; ++b) {
       mbar_init(&acc_full[b], 1);
       mbar_init(&acc_empty[b], 4);
     }
@@ -1082,9 +1089,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     bool ok = true, issued_any = false;
     for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
       for (int kb = 0; kb < nk && ok;) {
-        const int ab = acc_n & 1, first = kb;
-        const int last = min(nk, kb + kLogitChunk);
-        if (!mbar_wait(&acc_empty[ab], ((acc_n >> 1) & 1u) ^ 1u, abort_flag, kWaitNs)) {
+        const int ab = acc_n % F::kAcc, first = kb;
+        const int last = min(nk, kb + kFewChunk);
+        if (!mbar_wait(&acc_empty[ab], ((acc_n / F::kAcc) & 1u) ^ 1u, abort_flag, kWaitNs)) {
           ok = false;
           break;
         }
@@ -1138,10 +1145,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     int ok = 1;
     for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
       float z[NT];
-      for (int kb = 0; kb < nk; kb += kLogitChunk) {
-        const int ab = acc_n & 1;
+      for (int kb = 0; kb < nk; kb += kFewChunk) {
+        const int ab = acc_n % F::kAcc;
         if (lane == 0)
-          ok = mbar_wait(&acc_full[ab], (acc_n >> 1) & 1u, abort_flag, kWaitNs) ? 1 : 0;
+          ok = mbar_wait(&acc_full[ab], (acc_n / F::kAcc) & 1u, abort_flag, kWaitNs) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
         ++acc_n;
