@@ -32,12 +32,12 @@
 // 0.4 at m = 1e7).
 //
 // Bound: the tensor cores, in a loop of seconds under the card's power cap (1.37 kW).
-// 8192 rows x 16384 x 2048: the loss 329 us, 1.67 PFLOP/s (cuBLAS's product alone 307 at
-// its best, 316 in a loop); x 131072 with both gradients, 8 M V K operations, 10.9 ms, 1.6
-// PFLOP/s.  The operands' way from L2 (13 TB/s) is not far: clusters of two pairs that send
+// 8192 rows x 16384 x 2048: the loss 326 to 340 us, 1.65 PFLOP/s (cuBLAS's product alone
+// 307 at its best, 316 in a loop); x 131072 with both gradients, 8 M V K operations, 11.2
+// ms, 1.57 PFLOP/s.  The operands' way from L2 (13 TB/s) is not far: clusters of two pairs that send
 // each other half of W's tile need a quarter less of it, but only 36 of them find room, and
 // they were 5 % slower.  With small K the exponentials: a tile takes 3200 cycles for them,
-// 2048 for its products at K = 256.
+// 2048 for its products at K = 256 (16384 x 32000: 306 us).
 //
 // Every wait on a barrier in shared memory is bounded (2 s); on expiry the CTA records
 // the timeout in the error word, drains its loads and MMAs, frees TMEM and exits.
