@@ -699,8 +699,9 @@ int reflex_head_loss(const void* hidden, int64_t ld_hidden, const void* w, int64
  *   lse, grad [rows] fp32, of rows with a target.
  *   d_hidden, d_w  fp32 or bf16 by their dtype argument, any strides; either may be
  *             NULL (not wanted).  Rows of d_w on 16-byte boundaries are stored fastest.
- *             d_hidden may be hidden; d_w overlaps nothing (REFLEX_EINVAL where it shares
- *             bytes with w, or crosses it with rows of another stride).
+ *             d_hidden may be hidden; else they overlap nothing (REFLEX_EINVAL where one
+ *             shares bytes with w or with the other, or crosses it with rows of another
+ *             stride).
  *   workspace >= reflex_head_loss_backward_workspace_size(...) bytes (for these very
  *             sizes), 256-B aligned.
  * The rest as in reflex_head_loss; the same bits on every run.

@@ -40,12 +40,12 @@ bool matrix_ok(const Matrix& m, int64_t cols, size_t es) {
 
 // Whether two matrices share bytes. Rows of one pitch may lie between one another (halves
 // of wider rows); ranges of different pitches that cross count as shared.
-bool overlap(const Matrix& a, size_t es_a, const Matrix& b, size_t es_b, int64_t rows,
-             int64_t cols) {
+bool overlap(const Matrix& a, int64_t rows_a, size_t es_a, const Matrix& b, int64_t rows_b,
+             size_t es_b, int64_t cols) {
   const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
   const uint64_t pitch_a = a.ld * es_a, pitch_b = b.ld * es_b;
   const uint64_t row_a = cols * es_a, row_b = cols * es_b;
-  if (pa + (rows - 1) * pitch_a + row_a <= pb || pb + (rows - 1) * pitch_b + row_b <= pa)
+  if (pa + (rows_a - 1) * pitch_a + row_a <= pb || pb + (rows_b - 1) * pitch_b + row_b <= pa)
     return false;
   if (pitch_a != pitch_b) return true;
   const uint64_t off = pb >= pa ? (pb - pa) % pitch_a : (pitch_a - (pa - pb) % pitch_a) % pitch_a;
@@ -487,8 +487,12 @@ int reflex_head_loss_backward(const void* hidden, int64_t ld_hidden, const void*
   const HeadLayout L = head_layout(rows, vocab, k, true);
   if (workspace == nullptr || ws_bytes < L.total || !aligned(workspace, kAlign))
     return REFLEX_EWORKSPACE;
-  // (the weights are still read while their gradient is written)
-  if (d_w != nullptr && overlap({w, ldw}, 2, {d_w, ld_d_w}, es_w, vocab, k)) return REFLEX_EINVAL;
+  // (the weights are still read while either gradient is written)
+  const Matrix weights{w, ldw}, dw{d_w, ld_d_w}, dh{rows > 0 ? d_hidden : nullptr, ld_d_hidden};
+  if ((d_w != nullptr && overlap(weights, vocab, 2, dw, vocab, es_w, k)) ||
+      (dh.p != nullptr && overlap(weights, vocab, 2, dh, rows, es_h, k)) ||
+      (d_w != nullptr && dh.p != nullptr && overlap(dw, vocab, es_w, dh, rows, es_h, k)))
+    return REFLEX_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (rows == 0) {
     if (dev_status != nullptr) RX_CUDA(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s));

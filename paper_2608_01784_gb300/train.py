@@ -337,13 +337,15 @@ def _gradient(out, rows: int, cols: int, device, stream, what: str):
 
 
 def _overlap(a: torch.Tensor, lda: int, b: torch.Tensor, ldb: int) -> bool:
-    """Whether two matrices of one shape share bytes (as reflex_head_loss_backward has it:
+    """Whether two matrices of one width share bytes (as reflex_head_loss_backward has it:
     rows of one stride may lie between one another, ranges of different ones that cross
     count as shared)."""
-    rows, cols = a.shape
+    (rows, cols), rows_b = a.shape, b.shape[0]
+    if rows == 0 or rows_b == 0:
+        return False
     (pa, pitch, wa), (pb, other, wb) = ((t.data_ptr(), ld * t.element_size(), cols * t.element_size())
                                         for t, ld in ((a, lda), (b, ldb)))
-    if pa + (rows - 1) * pitch + wa <= pb or pb + (rows - 1) * other + wb <= pa:
+    if pa + (rows - 1) * pitch + wa <= pb or pb + (rows_b - 1) * other + wb <= pa:
         return False
     off = (pb - pa) % pitch
     return pitch != other or off < wa or off + wb > pitch
@@ -358,7 +360,7 @@ def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torc
     """reflex_head_loss_backward: the gradients (of hidden, of weight) from grad fp32
     [rows], that of each row's loss, and head_loss's lse.  They come in bf16, or in the
     type of `d_hidden` and `d_weight` (fp32 or bf16); the one that is not needed is None.
-    `d_hidden` may be hidden; `d_weight` shares no bytes with weight."""
+    `d_hidden` may be hidden; neither shares bytes with weight or with the other."""
     rows, vocab, k, ld_hidden, ldw = _head(hidden, weight, targets, status)
     dev = hidden.device
     _rows(lse, rows, torch.float32, dev, "lse")
@@ -369,13 +371,18 @@ def head_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torc
     ld_dh = ld_dw = k
     dt_h = dt_w = B.REFLEX_DTYPE_BF16
     if need_hidden:
+        given_h = d_hidden is not None
         d_hidden, ld_dh = _gradient(d_hidden, rows, k, dev, stream, "d_hidden")
+        _want(not given_h or not _overlap(weight, ldw, d_hidden, ld_dh),
+              "d_hidden: the weights are still read while it is written")
         dt_h = _DTYPES[d_hidden.dtype]
     if need_weight:
         given = d_weight is not None
         d_weight, ld_dw = _gradient(d_weight, vocab, k, dev, stream, "d_weight")
         _want(not given or not _overlap(weight, ldw, d_weight, ld_dw),
               "d_weight: the weights are still read while it is written")
+        _want(not (given and need_hidden) or not _overlap(d_weight, ld_dw, d_hidden, ld_dh),
+              "d_hidden and d_weight overlap")
         dt_w = _DTYPES[d_weight.dtype]
     ws_bytes = B.reflex_head_loss_backward_workspace_size(rows, vocab, k)
     _want(ws_bytes > 0, "unsupported sizes")

@@ -38,3 +38,15 @@ def test_beside_the_weights(up, across):
     dh, got = api.head_loss_backward(h, w, t, lse, grad, d_weight=dw)
     assert got is dw and torch.equal(w, kept)
     check_grad(h, w, t, grad, dh, dw)
+
+
+def test_gradients_of_the_rows_refused(monkeypatch):
+    def enqueued(*args, **kw):
+        raise AssertionError("the call went on")
+    h, w, t, grad, dw = both(VOCAB, 0)
+    lse = torch.zeros(ROWS, device="cuda")
+    monkeypatch.setattr(B, "reflex_head_loss_backward", enqueued)
+    for kw in (dict(d_hidden=w[:ROWS]), dict(d_hidden=w[VOCAB - ROWS:], need_weight=False),
+               dict(d_hidden=dw[7:7 + ROWS], d_weight=dw)):
+        with pytest.raises(ValueError):
+            api.head_loss_backward(h, w, t, lse, grad, **kw)

@@ -38,6 +38,14 @@ def test_refused(B, changes):
     assert refused(B, **changes) == B.REFLEX_EINVAL
 
 
+@pytest.mark.parametrize("changes", [
+    dict(d_hidden=P), dict(d_hidden=END - 2), dict(d_hidden=P - 2 * (3 * K + K) + 2),
+    dict(d_hidden=P + 8, d_hidden_dtype=0, d_w=None), dict(d_hidden=(1 << 28) + 2 * LD, d_w=1 << 28),
+    dict(d_hidden=(1 << 28) - 2 * 3 * K, d_w=1 << 28)])
+def test_gradients_of_the_rows_refused(B, changes):
+    assert refused(B, **{**dict(d_w=1 << 29), **changes}) == B.REFLEX_EINVAL
+
+
 def test_matrices_in_one_buffer():
     """Halves of wider rows and neighbours share nothing."""
     from paper_2608_01784_gb300.train import _overlap
